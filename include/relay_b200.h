@@ -145,6 +145,20 @@ typedef struct {
     int32_t sh, sw;   /* stride, >= 1 */
 } relay_pool2d_attrs_t;
 
+/* How a gated linear recurrence makes its coefficients of the gate tensor f and the value tensor u:
+ *   GIVEN    a = f,           b = u             (the program made the coefficients itself)
+ *   SIGMOID  a = sigmoid(f),  b = u
+ *   MIX      a = sigmoid(f),  b = (1 - a) u     (the state is a running mean of the values) */
+typedef enum { RELAY_GATE_GIVEN = 0, RELAY_GATE_SIGMOID = 1, RELAY_GATE_MIX = 2 } relay_gate_t;
+
+/* Newton-Schulz orthogonalisation: `steps` products with a I + b A + c A A, A the Gram matrix of the shorter side. */
+typedef struct {
+    int32_t steps;    /* 1..16 */
+    float a, b, c;    /* finite */
+    float eps;        /* added to the norm, >= 0; positive if a matrix may be all zero */
+    float scale;      /* the result is multiplied by it (finite) */
+} relay_orthogonalize_attrs_t;
+
 /* ---------------------------------------------------------------------------------------------
  * Type relations, host only (no GPU needed).  Each fills `out` (dtype, rank, shape, layout;
  * data = NULL) with the result type the operator's relation gives for the argument types,
@@ -378,6 +392,76 @@ relay_status_t relay_max_pool2d_grad(const relay_tensor_t *idx, const relay_tens
  * parameters.  A parameter may not overlap any other parameter or gradient.  n_params = 0 is a no-op. */
 relay_status_t relay_sgd_update(const relay_tensor_t *const *params, const relay_tensor_t *const *grads, int32_t n_params,
                                 float lr, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Recurrent language models: a sequence layer whose steps need no contraction, the scoring of given tokens at the end of the
+ * program, and the orthogonalised update of a weight matrix.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Gated linear recurrence over a sequence (the recursive program of relay_lstm_cell_seq with elementwise steps, so that the
+ * time axis can be cut and joined):
+ *   h_t = a_t (.) h_{t-1} + b_t,   a_t and b_t of f_t and u_t as `gate` says (relay_gate_t),   h_{-1} = h0
+ *   f,u:(T,B,D) t in {f32, bf16};  or u = NULL and f:(T,B,2D), whose last axis holds the blocks [ f | u ] (one dense result)
+ *   h0:(B,D) f32 or NULL (zero);  lengths:(B) i32 or NULL (all T)
+ *   -> h_all:(T,B,D) of type t or f32;  h_final:(B,D) f32 or NULL.   The state is kept in f32.
+ * lengths: sequence b ends before step lengths[b] (values outside [0,T] count as 0 and T): h_all is zero from there on,
+ * h_final is the state after its last step, and what f and u hold there is not used.  T = 1 is the step of a decoder.
+ * B = 0 or D = 0 is a no-op; T = 0 gives h_final = h0.  No workspace.
+ * Long sequences are summed in spans that are joined afterwards: with GIVEN coefficients whose products over a span
+ * overflow, a state can become infinite or NaN where a step-by-step sum would not. */
+relay_status_t relay_infer_gated_recurrence(const relay_tensor_t *f, const relay_tensor_t *u, relay_tensor_t *h_all, relay_tensor_t *h_final);
+relay_status_t relay_gated_recurrence(const relay_tensor_t *f, const relay_tensor_t *u, const relay_tensor_t *h0, const relay_tensor_t *lengths,
+                                      int32_t gate, const relay_tensor_t *h_all, const relay_tensor_t *h_final, void *stream);
+
+/* Gradient group of the recurrence (Section 4.2), given the saved h_all and the partials dh_all:(T,B,D) of h_all's type and
+ * dh_final:(B,D) f32 or NULL (zero):
+ *   g_t = dh_all[t] + G_{t+1};  G_t = a_t g_t;  G_T = dh_final;   dh0 = G_0
+ *   GIVEN:   df = g h_{t-1}                       du = g
+ *   SIGMOID: df = g h_{t-1} a (1-a)               du = g
+ *   MIX:     df = g (h_{t-1} - u) a (1-a)         du = g (1-a)
+ *   df, du: types and shapes of f and u (df:(T,B,2D) with du = NULL where u is NULL);  dh0:(B,D) f32 or NULL.
+ * Steps behind a sequence's end get zero partials; what f, u, h_all and dh_all hold there is not used. */
+relay_status_t relay_gated_recurrence_grad(const relay_tensor_t *f, const relay_tensor_t *u, const relay_tensor_t *h0,
+                                           const relay_tensor_t *lengths, int32_t gate, const relay_tensor_t *h_all,
+                                           const relay_tensor_t *dh_all, const relay_tensor_t *dh_final, const relay_tensor_t *df,
+                                           const relay_tensor_t *du, const relay_tensor_t *dh0, void *stream);
+
+/* Log-probabilities of given tokens under softmax(scores / temperature), the distributions' entropies, and the most probable
+ * tokens.  Where relay_softmax_xent weighs every class, here one integer names the class, so a row costs V scores and no targets.
+ *   lse[i] = log sum_j exp(z[i,j]),  z = scores / temperature;   logp[i] = z[i,tokens[i]] - lse[i]
+ *   entropy[i] = - sum_j p[i,j] log p[i,j]
+ *   top_ids[i,:], top_logp[i,:]: the K tokens of the largest scores, largest first, equal scores by the lower id
+ *   scores:(..,V) f32 or bf16, rank 1..6, the leading axes are the rows;  tokens:(..) i32 or i64;  temperature > 0
+ *   -> logp, entropy, lse:(..) f32;  top_logp:(..,K) f32, top_ids:(..,K) i32, 1 <= K <= min(V, RELAY_MAX_TOP).
+ * tokens and logp may be NULL together, top_logp and top_ids too, entropy and lse each (not all outputs at once).
+ * Arithmetic in f32.  A token outside [0,V) names no class: its logp is 0.  Scores of -inf are classes that cannot occur; a
+ * row of nothing else has lse = -inf, logp = -inf, entropy 0.  A row with a NaN or +inf has NaN results; among the ids NaN
+ * counts as larger than +inf.  Rows = 0 is a no-op; V = 0 is RELAY_ERR_SHAPE; V < 2^31. */
+#define RELAY_MAX_TOP 64
+relay_status_t relay_token_logprob(const relay_tensor_t *scores, const relay_tensor_t *tokens, float temperature, const relay_tensor_t *logp,
+                                   const relay_tensor_t *entropy, const relay_tensor_t *lse, const relay_tensor_t *top_logp,
+                                   const relay_tensor_t *top_ids, void *stream);
+
+/* Gradient group of the log-probabilities, given the forward call's lse (and entropy, where dentropy is given):
+ *   dscores[i,j] = ( dlogp[i] (1[j = tokens[i]] - p[i,j]) - dentropy[i] p[i,j] (log p[i,j] + entropy[i]) ) / temperature
+ *   dlogp:(..) f32;  dentropy:(..) f32 or NULL, entropy:(..) f32 with it;  dscores: type and shape of scores.
+ * A row whose token names no class has no dlogp term; a row with lse = -inf gets zeros. */
+relay_status_t relay_token_logprob_grad(const relay_tensor_t *scores, const relay_tensor_t *tokens, float temperature,
+                                        const relay_tensor_t *lse, const relay_tensor_t *entropy, const relay_tensor_t *dlogp,
+                                        const relay_tensor_t *dentropy, const relay_tensor_t *dscores, void *stream);
+
+/* Orthogonalised update of weight matrices (what relay_sgd_update then applies): x is divided by its Frobenius norm and driven
+ * towards the nearest matrix with singular values near one by products,
+ *   X <- x / (|x|_F + eps);   `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X   (A = X^T X and X <- a X + X (b A + c A A)
+ *   where M > N);   y = scale X
+ *   x:(..,M,N) f32 or bf16, rank 2..6, each leading index a matrix of its own -> y: the same shape, bf16.
+ * The products' operands are 16-bit floats with 10 fraction bits, sums are f32: against 64 bits the result is off by about
+ * 1e-3 of its norm before y's own rounding, more in directions whose singular values are below 1e-3 of the largest (there the
+ * first products' roundings grow by a^steps).  `ws` must hold relay_workspace_bytes_orthogonalize() bytes.  An empty tensor is a
+ * no-op. */
+size_t relay_workspace_bytes_orthogonalize(const relay_tensor_t *x);
+relay_status_t relay_orthogonalize(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *attrs, const relay_tensor_t *y, void *ws,
+                                   size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Status helpers.

@@ -21,6 +21,7 @@ MAX_RANK = 6
 F32, BF16, I32, I64, BOOL = 0, 1, 2, 3, 4
 ROWMAJOR, NCHW, NHWC, OIHW = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_TANH, ACT_SIGMOID = 0, 1, 2, 3
+GATE_GIVEN, GATE_SIGMOID, GATE_MIX = 0, 1, 2
 RED_NONE, RED_SUM, RED_MAX, RED_MEAN, RED_ARGMAX = 0, 1, 2, 3, 4
 
 STATUS_NAMES = ["OK", "ERR_NULL", "ERR_RANK", "ERR_SHAPE", "ERR_DTYPE", "ERR_LAYOUT", "ERR_ALIGN", "ERR_ATTR",
@@ -59,6 +60,11 @@ class OutSpec(ctypes.Structure):
 class Conv2dAttrs(ctypes.Structure):
     _fields_ = [("stride", ctypes.c_int32), ("pad", ctypes.c_int32), ("dilation", ctypes.c_int32),
                 ("groups", ctypes.c_int32)]
+
+
+class OrthogonalizeAttrs(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float),
+                ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -390,6 +396,49 @@ def relay_max_pool2d_grad(idx, dy, kh, kw, sh, sw, dx):
 def relay_sgd_update(params, grads, lr: float):
     pd, gd = [desc(p) for p in params], [desc(g) for g in grads]
     _check(lib().relay_sgd_update(_desc_array(pd), _desc_array(gd), len(pd), ctypes.c_float(lr), _stream()))
+
+
+# ---- recurrent language models ---------------------------------------------------------------------------
+def relay_infer_gated_recurrence(f: TensorDesc, u: Optional[TensorDesc] = None):
+    h_all, h_final = TensorDesc(), TensorDesc()
+    _check(lib().relay_infer_gated_recurrence(_ref(f), _ref(u), ctypes.byref(h_all), ctypes.byref(h_final)))
+    return h_all, h_final
+
+
+def relay_gated_recurrence(f, u, h0, lengths, gate, h_all, h_final):
+    """u = None: f holds the column blocks [ f | u ].  h0, lengths and h_final may be None."""
+    _check(lib().relay_gated_recurrence(_ref(desc(f)), _ref(desc(u)), _ref(desc(h0)), _ref(desc(lengths)), int(gate), _ref(desc(h_all)),
+                                        _ref(desc(h_final)), _stream()))
+
+
+def relay_gated_recurrence_grad(f, u, h0, lengths, gate, h_all, dh_all, dh_final, df, du, dh0):
+    """u = None goes with du = None: df holds the column blocks [ df | du ].  h0, lengths, dh_final and dh0 may be None."""
+    _check(lib().relay_gated_recurrence_grad(_ref(desc(f)), _ref(desc(u)), _ref(desc(h0)), _ref(desc(lengths)), int(gate), _ref(desc(h_all)),
+                                             _ref(desc(dh_all)), _ref(desc(dh_final)), _ref(desc(df)), _ref(desc(du)), _ref(desc(dh0)),
+                                             _stream()))
+
+
+def relay_token_logprob(scores, tokens, temperature, logp, entropy, lse, top_logp=None, top_ids=None):
+    """tokens and logp, top_logp and top_ids go in pairs; each pair, entropy and lse may be None."""
+    _check(lib().relay_token_logprob(_ref(desc(scores)), _ref(desc(tokens)), ctypes.c_float(temperature), _ref(desc(logp)), _ref(desc(entropy)),
+                                     _ref(desc(lse)), _ref(desc(top_logp)), _ref(desc(top_ids)), _stream()))
+
+
+def relay_token_logprob_grad(scores, tokens, temperature, lse, entropy, dlogp, dentropy, dscores):
+    """entropy and dentropy may be None together."""
+    _check(lib().relay_token_logprob_grad(_ref(desc(scores)), _ref(desc(tokens)), ctypes.c_float(temperature), _ref(desc(lse)),
+                                          _ref(desc(entropy)), _ref(desc(dlogp)), _ref(desc(dentropy)), _ref(desc(dscores)), _stream()))
+
+
+def relay_workspace_bytes_orthogonalize(x) -> int:
+    return int(lib().relay_workspace_bytes_orthogonalize(_ref(desc(x))))
+
+
+def relay_orthogonalize(x, steps, coefficients, eps, scale, y, ws=None):
+    """coefficients = (a, b, c) of X <- a X + (b A + c A A) X."""
+    wp, wb = _ws(ws)
+    at = OrthogonalizeAttrs(int(steps), *[float(v) for v in coefficients], float(eps), float(scale))
+    _check(lib().relay_orthogonalize(_ref(desc(x)), ctypes.byref(at), _ref(desc(y)), wp, wb, _stream()))
 
 
 # ---- status helpers -----------------------------------------------------------------------------------
