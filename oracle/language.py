@@ -73,8 +73,9 @@ def token_logprob(scores, tokens, temperature, top=0):
             out["lse"][i] = out["entropy"][i] = np.nan
         else:
             m = z.max()
-            out["lse"][i] = m + np.log(np.exp(z - m).sum())
-            lp = z - out["lse"][i]
+            log_s = np.log(np.exp(z - m).sum())
+            out["lse"][i] = m + log_s
+            lp = (z - m) - log_s                          # not z - lse: at |m| = 3e38 even fp64 has no room for log_s beside m
             live = ~np.isneginf(lp)
             out["entropy"][i] = -np.sum(np.exp(lp[live]) * lp[live])
         if tokens is not None and 0 <= tokens[i] < V:
