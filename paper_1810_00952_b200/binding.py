@@ -87,7 +87,8 @@ def lib() -> ctypes.CDLL:
         L.relay_launch_count.restype = ctypes.c_int64
         for name in ("relay_workspace_bytes_dense_act", "relay_workspace_bytes_dense_act_grad",
                      "relay_workspace_bytes_conv2d_act", "relay_workspace_bytes_conv2d_act_grad",
-                     "relay_workspace_bytes_reduce", "relay_workspace_bytes_lstm", "relay_workspace_bytes_lstm_grad"):
+                     "relay_workspace_bytes_reduce", "relay_workspace_bytes_lstm", "relay_workspace_bytes_lstm_grad",
+                     "relay_workspace_bytes_orthogonalize"):
             getattr(L, name).restype = ctypes.c_size_t
         _lib = L
     return _lib

@@ -20,6 +20,7 @@
 #include "ewise_kernels.cuh"
 #include "gemm.h"
 #include "gemm_tc_common.cuh"
+#include "orthogonalize.h"
 #include "tc_common.cuh"
 
 namespace relay {
@@ -252,6 +253,21 @@ relay_status_t make_tmap_2d_bf16(CUtensorMap *m, const void *base, uint64_t inne
                                  uint32_t box_inner, uint32_t box_outer)
 {
     return make_tmap_2d(m, false, base, inner, outer, row_stride, box_inner, box_outer, true);
+}
+
+relay_status_t make_tmap_3d_f16(CUtensorMap *m, const void *base, uint64_t inner, uint64_t outer, uint64_t batch, uint64_t row_stride,
+                                uint64_t batch_stride, uint32_t box_inner, uint32_t box_outer)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return fail(RELAY_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    cuuint64_t dims[3] = {inner, outer, batch};
+    cuuint64_t strides[2] = {row_stride * 2, batch_stride * 2};
+    cuuint32_t box[3] = {box_inner, box_outer, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(RELAY_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return RELAY_OK;
 }
 
 bool gemm_tc_eligible(const GemmDesc &g)
