@@ -5,8 +5,13 @@
 
 #include "common.h"
 #include "ewise_kernels.cuh"
+#include "tc_common.cuh"
 
 namespace relay {
+
+relay_status_t make_tmap_2d(CUtensorMap *m, bool f32, const void *base, uint64_t inner, uint64_t outer, uint64_t row_stride,
+                            uint32_t box_inner, uint32_t box_outer, bool swizzle128);
+
 namespace {
 
 constexpr int kThreads = 128;
@@ -23,12 +28,15 @@ struct Args {
     void *df, *du;                 // addressed like f and u
     float *dh0;                    // [C] or null
     long long T, C, D;             // C = batch * D channels
+    int *err;
 };
 
 // ---- vectors of V consecutive channels -----------------------------------------------------------------
 template <typename T, int V> struct RawOf { using type = T; };
 template <> struct RawOf<__nv_bfloat16, 2> { using type = uint32_t; };
+template <> struct RawOf<__nv_bfloat16, 4> { using type = uint2; };
 template <> struct RawOf<float, 2> { using type = uint2; };
+template <> struct RawOf<float, 4> { using type = uint4; };
 template <typename T, int V> using Raw = typename RawOf<T, V>::type;
 
 // Each value is touched once: past L1.
@@ -55,11 +63,19 @@ __device__ __forceinline__ void store_raw<__nv_bfloat16>(void *p, const __nv_bfl
     if (relay_in_bounds(p, 2)) __stcs((unsigned short *)p, __bfloat16_as_ushort(r));
 }
 __device__ __forceinline__ void to_f32(uint32_t r, float (&x)[2]) { x[0] = __uint_as_float(r << 16); x[1] = __uint_as_float(r & 0xffff0000u); }
+__device__ __forceinline__ void to_f32(uint2 r, float (&x)[4])
+{
+    x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
+    x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
+}
+__device__ __forceinline__ void to_f32(uint4 r, float (&x)[4]) { unpack(r, x); }
 __device__ __forceinline__ void to_f32(uint2 r, float (&x)[2]) { x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); }
 __device__ __forceinline__ void to_f32(__nv_bfloat16 r, float (&x)[1]) { x[0] = __bfloat162float(r); }
 __device__ __forceinline__ void to_f32(float r, float (&x)[1]) { x[0] = r; }
 __device__ __forceinline__ void from_f32(const float (&x)[2], uint32_t &r) { r = pack2(x[0], x[1]); }
 __device__ __forceinline__ void from_f32(const float (&x)[2], uint2 &r) { r = make_uint2(__float_as_uint(x[0]), __float_as_uint(x[1])); }
+__device__ __forceinline__ void from_f32(const float (&x)[4], uint2 &r) { r = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3])); }
+__device__ __forceinline__ void from_f32(const float (&x)[4], uint4 &r) { r = pack(x); }
 __device__ __forceinline__ void from_f32(const float (&x)[1], __nv_bfloat16 &r) { r = __float2bfloat16_rn(x[0]); }
 __device__ __forceinline__ void from_f32(const float (&x)[1], float &r) { r = x[0]; }
 
@@ -89,6 +105,85 @@ __device__ __forceinline__ void store_state(float *p, long long c, const float (
     if (p != nullptr) store<float, V>(p, c, x);
 }
 
+// ---- arithmetic on V channels: fp32 in pairs (one instruction for two), fp64 one by one ------------------------------------
+__device__ __forceinline__ unsigned long long pair(float lo, float hi)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(unsigned long long r, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r)); }
+template <int V>
+__device__ __forceinline__ void mul(const float (&a)[V], const float (&b)[V], float (&r)[V])
+{
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            unsigned long long q;
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(pair(a[i], a[i + 1])), "l"(pair(b[i], b[i + 1])));
+            unpair(q, r[i], r[i + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = a[i] * b[i];
+    }
+}
+template <int V>
+__device__ __forceinline__ void add(const float (&a)[V], const float (&b)[V], float (&r)[V])
+{
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            unsigned long long q;
+            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(pair(a[i], a[i + 1])), "l"(pair(b[i], b[i + 1])));
+            unpair(q, r[i], r[i + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = a[i] + b[i];
+    }
+}
+// a b + c
+template <int V>
+__device__ __forceinline__ void muladd(const float (&a)[V], const float (&b)[V], const float (&c)[V], float (&r)[V])
+{
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+            unsigned long long q;
+            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(q) : "l"(pair(a[i], a[i + 1])), "l"(pair(b[i], b[i + 1])), "l"(pair(c[i], c[i + 1])));
+            unpair(q, r[i], r[i + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = fmaf(a[i], b[i], c[i]);
+    }
+}
+template <int V>
+__device__ __forceinline__ void mul(const double (&a)[V], const double (&b)[V], double (&r)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = a[i] * b[i];
+}
+template <int V>
+__device__ __forceinline__ void add(const double (&a)[V], const double (&b)[V], double (&r)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = a[i] + b[i];
+}
+template <int V>
+__device__ __forceinline__ void muladd(const double (&a)[V], const double (&b)[V], const double (&c)[V], double (&r)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = a[i] * b[i] + c[i];
+}
+template <int V>
+__device__ __forceinline__ void fill(float x, float (&r)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = x;
+}
+
 // ---- coefficients ------------------------------------------------------------------------------------
 // a = sigmoid(f) and 1 - a.  Of the two the smaller is e / (1 + e) with e = exp(-|f|), so it keeps its relative precision
 // however far the gate is open or shut; the larger is one minus it, rounded once.  A long sum weighs its terms by powers of
@@ -111,56 +206,108 @@ __device__ __forceinline__ float exp_fine(float x)
     p = fmaf(p, z, 1.0f);
     return x < -87.0f ? 0.0f : __int_as_float(__float_as_int(p) + ((int)n << 23));
 }
-template <bool FINE>
-__device__ __forceinline__ void sigmoid_pair(float f, float &a, float &one_less)
+template <bool FINE, int V>
+__device__ __forceinline__ void sigmoid_pair(const float (&f)[V], float (&a)[V], float (&one_less)[V])
 {
-    float small;
-    if (FINE) {
-        const float e = exp_fine(-fabsf(f)), d = 1.0f + e, r = __fdividef(1.0f, d);
-        small = e * fmaf(r, fmaf(-d, r, 1.0f), r);         // one Newton step on the reciprocal
+    if constexpr (FINE) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float e = exp_fine(-fabsf(f[i])), d = 1.0f + e, r = __fdividef(1.0f, d);
+            const float small = e * fmaf(r, fmaf(-d, r, 1.0f), r);    // one Newton step on the reciprocal
+            const float large = 1.0f - small;
+            a[i] = f[i] >= 0.0f ? large : small;
+            one_less[i] = f[i] >= 0.0f ? small : large;
+            if (f[i] != f[i]) a[i] = one_less[i] = f[i];
+        }
     } else {
-        const float e = __expf(-fabsf(f));
-        small = __fdividef(e, 1.0f + e);
+        // 1 - a = 1 / (1 + exp(f)), and a from it: what a loses where it is itself small is lost on a state that it all but
+        // erases.  An infinite exponential gives exactly 0.
+        float y[V], c[V];
+        fill(1.44269504f, c);
+        mul(f, c, y);
+#pragma unroll
+        for (int i = 0; i < V; ++i) asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(y[i]));
+        fill(1.0f, c);
+        add(y, c, y);
+#pragma unroll
+        for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(one_less[i]) : "f"(y[i]));
+        float m[V];
+        fill(-1.0f, m);
+        muladd(one_less, m, c, a);
     }
-    const float large = 1.0f - small;
-    a = f >= 0.0f ? large : small;
-    one_less = f >= 0.0f ? small : large;
-    if (f != f) a = one_less = f;
 }
 // A step's coefficient and the type F that states are carried in: fp32; beside fp32 gates fp64, rounded where a state is stored,
 // so that a result which is the difference of two states' terms is as good as its inputs (the arithmetic is far from being the
 // bound).  There an open gate (f >= 0) is held as -(1 - a), its sign saying so: a in fp32, near one, has no bits left for 1 - a,
 // and over a long span of like gates that error would add up.
-template <typename T, int GATE> struct Coefficient {
+template <typename T, int GATE, int V> struct Coefficient {
     static constexpr bool FINE = sizeof(T) == 4, SIGNED = FINE && GATE != RELAY_GATE_GIVEN;
     using F = std::conditional_t<FINE, double, float>;
     static __device__ __forceinline__ float keep() { return SIGNED ? -0.0f : 1.0f; }                     // a = 1
-    static __device__ __forceinline__ F value(float k) { return SIGNED && __float_as_int(k) < 0 ? F(1) + F(k) : F(k); }
-    static __device__ __forceinline__ void of(float f, float u, float &k, float &b)
+    static __device__ __forceinline__ void value(const float (&k)[V], F (&a)[V])
     {
-        if (GATE == RELAY_GATE_GIVEN) {
-            k = f;
-            b = u;
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = SIGNED && __float_as_int(k[i]) < 0 ? F(1) + F(k[i]) : F(k[i]);
+    }
+    static __device__ __forceinline__ void of(const float (&f)[V], float (&k)[V])
+    {
+        float s[V];
+        if constexpr (GATE == RELAY_GATE_GIVEN) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) k[i] = f[i];
         } else {
-            float a, s;
-            sigmoid_pair<FINE>(f, a, s);
-            b = GATE == RELAY_GATE_MIX ? s * u : u;
-            k = SIGNED && f >= 0.0f ? -s : a;
+            sigmoid_pair<FINE>(f, k, s);
+            if (SIGNED) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) k[i] = f[i] >= 0.0f ? -s[i] : k[i];
+            }
         }
+    }
+    static __device__ __forceinline__ void of(const float (&f)[V], const float (&u)[V], float (&k)[V], float (&b)[V])
+    {
+        if constexpr (GATE == RELAY_GATE_MIX) {
+            float s[V];
+            sigmoid_pair<FINE>(f, k, s);
+            mul(s, u, b);
+            if (SIGNED) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) k[i] = f[i] >= 0.0f ? -s[i] : k[i];
+            }
+        } else {
+            of(f, k);
+#pragma unroll
+            for (int i = 0; i < V; ++i) b[i] = u[i];
+        }
+    }
+    // h <- a h + b
+    static __device__ __forceinline__ void step(const float (&k)[V], const float (&b)[V], F (&h)[V])
+    {
+        F a[V], x[V];
+        value(k, a);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = F(b[i]);
+        muladd(a, h, x, h);
     }
 };
 // partials of one step: g = dh_t + G_{t+1}
-template <int GATE, bool FINE>
-__device__ __forceinline__ void partials(float f, float u, float before, float g, float &df, float &du)
+template <int GATE, bool FINE, int V>
+__device__ __forceinline__ void partials(const float (&f)[V], const float (&u)[V], const float (&before)[V], const float (&g)[V], float (&df)[V], float (&du)[V])
 {
-    if (GATE == RELAY_GATE_GIVEN) {
-        df = g * before;
-        du = g;
+    if constexpr (GATE == RELAY_GATE_GIVEN) {
+        mul(g, before, df);
+#pragma unroll
+        for (int i = 0; i < V; ++i) du[i] = g[i];
     } else {
-        float a, s;
+        float a[V], s[V], d[V], gs[V];
         sigmoid_pair<FINE>(f, a, s);
-        df = (GATE == RELAY_GATE_MIX ? g * (before - u) : g * before) * (a * s);
-        du = GATE == RELAY_GATE_MIX ? g * s : g;
+        mul(g, s, gs);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            d[i] = GATE == RELAY_GATE_MIX ? before[i] - u[i] : before[i];
+            du[i] = GATE == RELAY_GATE_MIX ? gs[i] : g[i];
+        }
+        mul(gs, a, gs);
+        mul(gs, d, df);
     }
 }
 
@@ -189,11 +336,35 @@ __device__ __forceinline__ void store_final(float *p, long long c, const F (&sta
     store_state(p, c, x);
 }
 
+// One step backwards: partials of f and u, and G <- a (dh + G); a step behind the end has none and leaves G.
+template <typename K, int GATE, int V>
+__device__ __forceinline__ void backward_step(const float (&f)[V], const float (&u)[V], const float (&dh)[V], const float (&before)[V], bool on,
+                                              typename K::F (&G)[V], float (&df)[V], float (&du)[V])
+{
+    using F = typename K::F;
+    F g[V], a[V];
+    float k[V], g32[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] = F(dh[i]);
+    add(g, G, g);
+#pragma unroll
+    for (int i = 0; i < V; ++i) g32[i] = (float)g[i];
+    K::of(f, k);
+    K::value(k, a);
+    partials<GATE, K::FINE>(f, u, before, g32, df, du);
+    if (on) {
+        mul(a, g, G);
+    } else {
+        fill(0.0f, df);
+        fill(0.0f, du);
+    }
+}
+
 // ---- one thread per V channels, step by step ------------------------------------------------------------
 template <typename T, typename TH, int GATE, int V>
 __global__ void __launch_bounds__(kThreads) recurrence_steps_kernel(const Args p)
 {
-    using K = Coefficient<T, GATE>;
+    using K = Coefficient<T, GATE, V>;
     using F = typename K::F;
     const long long c = ((long long)blockIdx.x * kThreads + threadIdx.x) * V;
     pdl_wait();
@@ -206,14 +377,11 @@ __global__ void __launch_bounds__(kThreads) recurrence_steps_kernel(const Args p
         float f[V], u[V], out[V];
         load<T, V>(p.f, t * p.ld + at, f);
         load<T, V>(p.u, t * p.ld + at, u);
+        float k[V], x[V];
+        K::of(f, u, k, x);
+        if (t < end) K::step(k, x, h);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float k, x;
-            K::of(f[i], u[i], k, x);
-            const F next = K::value(k) * h[i] + F(x);
-            if (t < end) h[i] = next;
-            out[i] = t < end ? (float)next : 0.0f;
-        }
+        for (int i = 0; i < V; ++i) out[i] = t < end ? (float)h[i] : 0.0f;
         store<TH, V>(p.h, t * p.C + c, out);
     }
     store_final(p.h_final, c, h);
@@ -222,7 +390,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_steps_kernel(const Args p
 template <typename T, typename TH, int GATE, int V>
 __global__ void __launch_bounds__(kThreads) recurrence_grad_steps_kernel(const Args p)
 {
-    using K = Coefficient<T, GATE>;
+    using K = Coefficient<T, GATE, V>;
     using F = typename K::F;
     const long long c = ((long long)blockIdx.x * kThreads + threadIdx.x) * V;
     pdl_wait();
@@ -238,15 +406,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_grad_steps_kernel(const A
         load<TH, V>(p.dh, t * p.C + c, dh);
         if (t > 0) load<TH, V>(p.h, (t - 1) * p.C + c, before);
         else load_state(p.h0, c, before);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const F g = F(dh[i]) + G[i];
-            float k, x;
-            K::of(f[i], u[i], k, x);
-            partials<GATE, K::FINE>(f[i], u[i], before[i], (float)g, df[i], du[i]);
-            if (t < end) G[i] = K::value(k) * g;
-            else df[i] = du[i] = 0.0f;
-        }
+        backward_step<K, GATE, V>(f, u, dh, before, t < end, G, df, du);
         store<T, V>(p.df, t * p.ld + at, df);
         store<T, V>(p.du, t * p.ld + at, du);
     }
@@ -258,7 +418,7 @@ __global__ void __launch_bounds__(kThreads) recurrence_grad_steps_kernel(const A
 // warp TS consecutive steps of them, a block kWarps such spans one after the other, a cluster of S blocks S such blocks; a
 // cluster walks the sequence in slabs of S * kWarps * TS steps.  Per slab every thread reads its steps once into registers,
 // composes them, the block's spans are joined through shared memory, the blocks' through their neighbours' shared memory (each
-// block writes its map to all of the cluster, one cluster barrier), and the steps are then run again from registers with the
+// block sends its map to all of the cluster), and the steps are then run again from registers with the
 // right state.  Every value is read from memory once.  The next slab's values are requested before the barriers.
 // The gradient is the same recursion backwards in time: G_t = a_t G_{t+1} + a_t dh_t.
 constexpr int kWarps = 8;
@@ -268,11 +428,8 @@ template <typename F, int V>
 __device__ __forceinline__ Map<F, V> then(const Map<F, V> &first, const Map<F, V> &second)
 {
     Map<F, V> r;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        r.a[i] = first.a[i] * second.a[i];
-        r.h[i] = second.a[i] * first.h[i] + second.h[i];
-    }
+    mul(first.a, second.a, r.a);
+    muladd(second.a, first.h, second.h, r.h);
     return r;
 }
 template <typename F, int V>
@@ -283,247 +440,791 @@ __device__ __forceinline__ Map<F, V> identity()
     for (int i = 0; i < V; ++i) { r.a[i] = F(1); r.h[i] = F(0); }
     return r;
 }
-// the state behind a map: an overflowed product must not turn a zero state into NaN
-template <typename F, int V>
+// The state behind a map.  SAFE, for coefficients that may exceed one: an overflowed product must not turn a zero state into NaN.
+template <bool SAFE, typename F, int V>
 __device__ __forceinline__ void apply(const Map<F, V> &m, F (&h)[V])
 {
+    F r[V];
+    muladd(m.a, h, m.h, r);
 #pragma unroll
-    for (int i = 0; i < V; ++i) h[i] = h[i] == F(0) ? m.h[i] : m.a[i] * h[i] + m.h[i];
+    for (int i = 0; i < V; ++i) h[i] = SAFE && h[i] == F(0) ? m.h[i] : r[i];
 }
 
 template <typename F, int V>
 struct Joints {
-    Map<F, V> span[kWarps][32];        // this block's spans
-    Map<F, V> block[2][8][32];         // the cluster's blocks, alternating between slabs
+    Map<F, V> span[kWarps][32];        // this block's spans, then what lies ahead of each
+    struct { F h[V]; } state[32];      // before this block
+    Map<F, V> block[2][8][32];         // the cluster's blocks, sent by each; alternating between slabs
+    uint64_t arrived[2];               // all of block[.] is here
+    int gave_up;
+    __device__ __forceinline__ void init()
+    {
+        if (threadIdx.x == 0) {
+            tc::mbar_init(&arrived[0], 1);
+            tc::mbar_init(&arrived[1], 1);
+            gave_up = 0;
+            tc::fence_barrier_init();
+        }
+        tc::cluster_sync();            // every block of the cluster runs, its barriers set up, before anything is sent to it
+    }
 };
-__device__ __forceinline__ uint32_t cluster_address(const void *p, uint32_t rank)
-{
-    uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-    return r;
-}
+// one-way: the data and the byte count that completes the receiver's barrier travel together.  (A cluster barrier per slab
+// would make every block wait for its own stores to global memory.)
 template <typename F, int V>
-__device__ __forceinline__ void store_cluster(uint32_t at, const Map<F, V> &m)
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map<F, V> &m)
 {
-    static_assert(sizeof(m) % 8 == 0, "pairs of words");
     const uint2 *w = reinterpret_cast<const uint2 *>(&m);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(m) / 8); ++i)
-        asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(at + 8 * i), "r"(w[i].x), "r"(w[i].y) : "memory");
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.u32 [%0], {%1, %2}, [%3];" ::"r"(to + 8 * i), "r"(w[i].x), "r"(w[i].y), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void cluster_barrier()
+__device__ __forceinline__ bool try_wait_cluster(uint64_t *bar, uint32_t parity)
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred P;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 P, [%1], %2;\n\tselp.u32 %0, 1, 0, P;\n\t}\n"
+                 : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded: a warp that gives up records it, and this block's later waits end at once (its results are then not to be used).
+__device__ __forceinline__ void wait_arrived(uint64_t *bar, uint32_t parity, int *gave_up, int *err)
+{
+    if (try_wait_cluster(bar, parity)) return;
+    const long long began = clock64();
+    while (!try_wait_cluster(bar, parity)) {
+        if (*(volatile int *)gave_up) return;
+        if (clock64() - began > tc::kWaitLimitCycles) {
+            *(volatile int *)gave_up = 1;
+            atomicCAS(err, 0, tc::ERR_WAIT_EXCHANGE);
+            return;
+        }
+    }
 }
 
-// Joins the maps of all threads of a lane's channels over the slab.  `state` is the state before the slab on entry, the state
-// behind it on return; the result is the state before this thread's own span.
-template <typename F, int V>
-__device__ __forceinline__ void join_slab(Joints<F, V> &j, const Map<F, V> &mine, int warp, int lane, uint32_t rank, int S, int slab,
+// Joins the maps of all threads of a lane's channels over the slab.  Warp 0 does it for the block (eight warps doing it each for
+// themselves would execute more instructions than the steps do); its `state` is the state before the slab on entry, behind it on
+// return.  The result is the state before this thread's own span.
+template <bool SAFE, typename F, int V>
+__device__ __forceinline__ void join_slab(Joints<F, V> &j, const Map<F, V> &mine, int warp, int lane, uint32_t rank, int S, int slab, int *err,
                                           F (&state)[V], F (&before)[V])
 {
     j.span[warp][lane] = mine;
     __syncthreads();
-    Map<F, V> ahead = identity<F, V>(), all = identity<F, V>();
+    if (warp == 0) {
+        Map<F, V> m[kWarps], all = mine;                  // all loads in flight together
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w == warp) ahead = all;
-        all = then(all, j.span[w][lane]);
-    }
-    // warp r tells block r of the cluster
-    if (warp < S) store_cluster(cluster_address(&j.block[slab & 1][rank][lane], (uint32_t)warp), all);
-    cluster_barrier();
-#pragma unroll 1
-    for (int r = 0; r < S; ++r) {
-        if (r == (int)rank) {
+        for (int w = 1; w < kWarps; ++w) m[w] = j.span[w][lane];
+        j.span[0][lane] = identity<F, V>();
 #pragma unroll
-            for (int i = 0; i < V; ++i) before[i] = state[i];
+        for (int w = 1; w < kWarps; ++w) {
+            j.span[w][lane] = all;
+            all = then(all, m[w]);
         }
-        apply(j.block[slab & 1][r][lane], state);
+        if (S == 1) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) j.state[lane].h[i] = state[i];
+            apply<SAFE>(all, state);
+        } else {
+            const int buf = slab & 1;
+            // arming may come after a neighbour's first bytes: the phase ends when both are complete
+            if (lane == 0) tc::mbar_expect_tx(&j.arrived[buf], (uint32_t)(S * 32 * sizeof(mine)));
+            const uint32_t to = tc::smem_u32(&j.block[buf][rank][lane]), bar = tc::smem_u32(&j.arrived[buf]);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < S) send(tc::mapa(to, (uint32_t)r), tc::mapa(bar, (uint32_t)r), all);
+            // A neighbour sends for slab i + 2 only when it has this block's message for slab i + 1, which this warp sends after it
+            // has read slab i's: two buffers are enough.
+            wait_arrived(&j.arrived[buf], (slab >> 1) & 1, &j.gave_up, err);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < S) m[r] = j.block[buf][r][lane];
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < S) {
+                    if (r == (int)rank) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) j.state[lane].h[i] = state[i];
+                    }
+                    apply<SAFE>(m[r], state);
+                }
+        }
     }
-    apply(ahead, before);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) before[i] = j.state[lane].h[i];
+    apply<SAFE>(j.span[warp][lane], before);
 }
+
+// The place of a thread: warp-uniform rows, and 32-bit byte offsets of its channels within a row, so that an access needs no
+// 64-bit arithmetic of its own.  Lanes behind the last channel repeat it and store nothing.
+template <typename T, typename TH, int V>
+struct Place {
+    int warp, lane;
+    uint32_t rank;
+    bool live;
+    long long c, end;
+    uint32_t at_f, at_h;               // in rows of f / u and of h / dh
+    __device__ __forceinline__ Place(const Args &p, int S)
+    {
+        warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0); lane = threadIdx.x & 31;
+        rank = blockIdx.x % S;
+        const long long wanted = ((long long)(blockIdx.x / S) * 32 + lane) * V;
+        live = wanted < p.C;
+        c = live ? wanted : p.C - V;
+        const long long b = c / p.D;
+        at_f = (uint32_t)((b * p.bs + (c - b * p.D)) * sizeof(T));
+        at_h = (uint32_t)(c * sizeof(TH));
+        end = end_of(p, b);
+    }
+};
+template <typename R>
+__device__ __forceinline__ R load_at(const char *row, uint32_t off) { return load_raw<R>(row + off); }
+// how many of the TS steps from t0 on lie before `end`
+template <int TS> __device__ __forceinline__ int steps_before(long long t0, long long end)
+{
+    return t0 >= end ? 0 : end - t0 < TS ? (int)(end - t0) : TS;
+}
+
 template <typename T, typename TH, int GATE, int V, int TS>
 __global__ void __launch_bounds__(32 * kWarps, 2) recurrence_spans_kernel(const Args p, int S)
 {
-    using K = Coefficient<T, GATE>;
+    using K = Coefficient<T, GATE, V>;
     using F = typename K::F;
+    using R = Raw<T, V>;
     __shared__ __align__(16) Joints<F, V> joints;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = blockIdx.x % S;
-    const long long c = ((long long)(blockIdx.x / S) * 32 + lane) * V;
-    const bool live = c < p.C;
-    cluster_barrier();                 // every block of the cluster runs before its shared memory is written
+    joints.init();
     pdl_wait();
-    const long long b = live ? c / p.D : 0, at = b * p.bs + (c - b * p.D), end = live ? end_of(p, b) : 0;
+    const Place<T, TH, V> me(p, S);
     F state[V];
-    load_initial(p.h0, c, live, state);
+    load_initial(p.h0, me.c, true, state);
     const long long slab_steps = (long long)S * kWarps * TS;
     const int slabs = (int)((p.T + slab_steps - 1) / slab_steps);
-    long long t0 = ((long long)rank * kWarps + warp) * TS;
+    const long long ldf = p.ld * (long long)sizeof(T), ldh = p.C * (long long)sizeof(TH);
+    long long t0 = ((long long)me.rank * kWarps + me.warp) * TS;
 
-    Raw<T, V> rf[TS], ru[TS];
+    R rf[TS], ru[TS];
     auto request = [&](long long first) {
-        const T *f = (const T *)p.f + first * p.ld + at, *u = (const T *)p.u + first * p.ld + at;
+        const char *f = (const char *)p.f + first * ldf, *u = (const char *)p.u + first * ldf;
+        if (first + TS <= p.T) {
 #pragma unroll
-        for (int s = 0; s < TS; ++s) {
-            rf[s] = Raw<T, V>{}; ru[s] = Raw<T, V>{};
-            if (live && first + s < p.T) { rf[s] = load_raw<Raw<T, V>>(f + s * p.ld); ru[s] = load_raw<Raw<T, V>>(u + s * p.ld); }
+            for (int s = 0; s < TS; ++s) { rf[s] = load_at<R>(f + s * ldf, me.at_f); ru[s] = load_at<R>(u + s * ldf, me.at_f); }
+        } else {
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                rf[s] = R{}; ru[s] = R{};
+                if (first + s < p.T) { rf[s] = load_at<R>(f + s * ldf, me.at_f); ru[s] = load_at<R>(u + s * ldf, me.at_f); }
+            }
         }
     };
     request(t0);
     for (int slab = 0; slab < slabs; ++slab, t0 += slab_steps) {
+        const int n = steps_before<TS>(t0, me.end);
+        const bool full = __all_sync(0xffffffffu, n == TS);
         float a[TS][V], x[TS][V];
         Map<F, V> mine = identity<F, V>();
 #pragma unroll
         for (int s = 0; s < TS; ++s) {
             float f[V], u[V];
             to_f32(rf[s], f); to_f32(ru[s], u);
+            K::of(f, u, a[s], x[s]);
+        }
+        if (!full) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                K::of(f[i], u[i], a[s][i], x[s][i]);
-                if (t0 + s >= end) { a[s][i] = K::keep(); x[s][i] = 0.0f; }
-                const F v = K::value(a[s][i]);
-                mine.a[i] *= v;
-                mine.h[i] = v * mine.h[i] + F(x[s][i]);
-            }
+            for (int s = 0; s < TS; ++s)
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (s >= n) { a[s][i] = K::keep(); x[s][i] = 0.0f; }
         }
         if (slab + 1 < slabs) request(t0 + slab_steps);
-        F h[V];
-        join_slab(joints, mine, warp, lane, rank, S, slab, state, h);
-        TH *out = (TH *)p.h + t0 * p.C + c;
 #pragma unroll
         for (int s = 0; s < TS; ++s) {
-            float o[V];
+            F v[V], b[V];
+            K::value(a[s], v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                h[i] = K::value(a[s][i]) * h[i] + F(x[s][i]);
-                o[i] = t0 + s < end ? (float)h[i] : 0.0f;
+            for (int i = 0; i < V; ++i) b[i] = F(x[s][i]);
+            mul(mine.a, v, mine.a);
+            muladd(v, mine.h, b, mine.h);
+        }
+        F h[V];
+        join_slab<GATE == RELAY_GATE_GIVEN>(joints, mine, me.warp, me.lane, me.rank, S, slab, p.err, state, h);
+        char *out = (char *)p.h + t0 * ldh;
+        if (full) {
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                float o[V];
+                K::step(a[s], x[s], h);
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = (float)h[i];
+                if (me.live) store<TH, V>(out + s * ldh + me.at_h, 0, o);
             }
-            if (live && t0 + s < p.T) store<TH, V>(out, (long long)s * p.C, o);
+        } else {
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                float o[V];
+                K::step(a[s], x[s], h);
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = s < n ? (float)h[i] : 0.0f;
+                if (me.live && t0 + s < p.T) store<TH, V>(out + s * ldh + me.at_h, 0, o);
+            }
         }
     }
-    if (live && rank == 0 && warp == 0) store_final(p.h_final, c, state);
-    cluster_barrier();                 // no block leaves while another may still write to its shared memory
+    if (me.live && me.rank == 0 && me.warp == 0) store_final(p.h_final, me.c, state);
+    tc::cluster_sync();                // no block leaves while another may still write to its shared memory
 }
 
 template <typename T, typename TH, int GATE, int V, int TS>
 __global__ void __launch_bounds__(32 * kWarps, 2) recurrence_grad_spans_kernel(const Args p, int S)
 {
-    using K = Coefficient<T, GATE>;
+    using K = Coefficient<T, GATE, V>;
     using F = typename K::F;
+    using R = Raw<T, V>;
+    using RH = Raw<TH, V>;
     __shared__ __align__(16) Joints<F, V> joints;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = blockIdx.x % S;
-    const long long c = ((long long)(blockIdx.x / S) * 32 + lane) * V;
-    const bool live = c < p.C;
-    cluster_barrier();                 // every block of the cluster runs before its shared memory is written
+    joints.init();
     pdl_wait();
-    const long long b = live ? c / p.D : 0, at = b * p.bs + (c - b * p.D), end = live ? end_of(p, b) : 0;
+    const Place<T, TH, V> me(p, S);
     F state[V];
-    load_initial(p.dh_final, c, live, state);
+    load_initial(p.dh_final, me.c, true, state);
     const long long slab_steps = (long long)S * kWarps * TS;
     const int slabs = (int)((p.T + slab_steps - 1) / slab_steps);
-    long long t0 = p.T - 1 - ((long long)rank * kWarps + warp) * TS;      // this thread's steps are t0, t0 - 1, ..
+    const long long ldf = p.ld * (long long)sizeof(T), ldh = p.C * (long long)sizeof(TH);
+    long long t0 = p.T - 1 - ((long long)me.rank * kWarps + me.warp) * TS;      // this thread's steps are t0, t0 - 1, ..
 
-    Raw<T, V> nf[TS], nu[TS];
-    Raw<TH, V> nd[TS], nh[TS];
+    R nf[TS], nu[TS];
+    RH nd[TS], nh[TS];
     auto request = [&](long long first) {
+        const char *f = (const char *)p.f + first * ldf, *u = (const char *)p.u + first * ldf;
+        const char *d = (const char *)p.dh + first * ldh, *h = (const char *)p.h + (first - 1) * ldh;
+        if (first >= TS) {             // h is wanted for the step before each
 #pragma unroll
-        for (int s = 0; s < TS; ++s) {
-            const long long t = first - s;
-            nf[s] = Raw<T, V>{}; nu[s] = Raw<T, V>{}; nd[s] = Raw<TH, V>{}; nh[s] = Raw<TH, V>{};
-            if (live && t >= 0) {
-                nf[s] = load_raw<Raw<T, V>>((const T *)p.f + t * p.ld + at);
-                nu[s] = load_raw<Raw<T, V>>((const T *)p.u + t * p.ld + at);
-                nd[s] = load_raw<Raw<TH, V>>((const TH *)p.dh + t * p.C + c);
-                if (t > 0) nh[s] = load_raw<Raw<TH, V>>((const TH *)p.h + (t - 1) * p.C + c);
+            for (int s = 0; s < TS; ++s) {
+                nf[s] = load_at<R>(f - s * ldf, me.at_f); nu[s] = load_at<R>(u - s * ldf, me.at_f);
+                nd[s] = load_at<RH>(d - s * ldh, me.at_h); nh[s] = load_at<RH>(h - s * ldh, me.at_h);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                nf[s] = R{}; nu[s] = R{}; nd[s] = RH{}; nh[s] = RH{};
+                if (first - s >= 0) {
+                    nf[s] = load_at<R>(f - s * ldf, me.at_f); nu[s] = load_at<R>(u - s * ldf, me.at_f);
+                    nd[s] = load_at<RH>(d - s * ldh, me.at_h);
+                    if (first - s > 0) nh[s] = load_at<RH>(h - s * ldh, me.at_h);
+                }
             }
         }
     };
     request(t0);
     for (int slab = 0; slab < slabs; ++slab, t0 -= slab_steps) {
-        Raw<T, V> rf[TS], ru[TS];
-        Raw<TH, V> rd[TS], rh[TS];
+        R rf[TS], ru[TS];
+        RH rd[TS], rh[TS];
+#pragma unroll
+        for (int s = 0; s < TS; ++s) { rf[s] = nf[s]; ru[s] = nu[s]; rd[s] = nd[s]; rh[s] = nh[s]; }
+        const bool full = __all_sync(0xffffffffu, t0 < me.end && t0 >= TS);     // every step exists, and none is the first
         Map<F, V> mine = identity<F, V>();
 #pragma unroll
         for (int s = 0; s < TS; ++s) {
-            rf[s] = nf[s]; ru[s] = nu[s]; rd[s] = nd[s]; rh[s] = nh[s];
             float f[V], dh[V];
             to_f32(rf[s], f); to_f32(rd[s], dh);
+            float k[V];
+            F v[V], d[V];
+            K::of(f, k);
+            K::value(k, v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float k, unused;
-                K::of(f[i], 0.0f, k, unused);
-                if (t0 - s < end && t0 - s >= 0) {
-                    const F v = K::value(k);
-                    mine.a[i] *= v;
-                    mine.h[i] = v * (mine.h[i] + F(dh[i]));
-                }
+            for (int i = 0; i < V; ++i) d[i] = F(dh[i]);
+            if (full || (t0 - s < me.end && t0 - s >= 0)) {
+                mul(mine.a, v, mine.a);
+                add(mine.h, d, mine.h);
+                mul(mine.h, v, mine.h);
             }
         }
         if (slab + 1 < slabs) request(t0 - slab_steps);
         F G[V];
-        join_slab(joints, mine, warp, lane, rank, S, slab, state, G);
+        join_slab<GATE == RELAY_GATE_GIVEN>(joints, mine, me.warp, me.lane, me.rank, S, slab, p.err, state, G);
+        char *df_row = (char *)p.df + t0 * ldf, *du_row = (char *)p.du + t0 * ldf;
 #pragma unroll
         for (int s = 0; s < TS; ++s) {
             const long long t = t0 - s;
             float f[V], u[V], dh[V], before[V], df[V], du[V];
             to_f32(rf[s], f); to_f32(ru[s], u); to_f32(rd[s], dh); to_f32(rh[s], before);
-            if (live && t == 0) load_state(p.h0, c, before);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const F g = F(dh[i]) + G[i];
-                float k, unused;
-                K::of(f[i], u[i], k, unused);
-                partials<GATE, K::FINE>(f[i], u[i], before[i], (float)g, df[i], du[i]);
-                if (t < end) G[i] = K::value(k) * g;
-                else df[i] = du[i] = 0.0f;
-            }
-            if (live && t >= 0) {
-                store<T, V>(p.df, t * p.ld + at, df);
-                store<T, V>(p.du, t * p.ld + at, du);
+            if (!full && t == 0) load_state(p.h0, me.c, before);
+            backward_step<K, GATE, V>(f, u, dh, before, full || t < me.end, G, df, du);
+            if (me.live && (full || t >= 0)) {
+                store<T, V>(df_row - s * ldf + me.at_f, 0, df);
+                store<T, V>(du_row - s * ldf + me.at_f, 0, du);
             }
         }
     }
-    if (live && rank == 0 && warp == 0) store_final(p.dh0, c, state);
-    cluster_barrier();
+    if (me.live && me.rank == 0 && me.warp == 0) store_final(p.dh0, me.c, state);
+    tc::cluster_sync();
+}
+
+// ---- the same with tiles fetched ahead and the joining left to a warp of its own --------------------------------
+// The cluster's blocks run in step, so per slab each waits for the slowest of its loads and for an exchange of about a
+// microsecond.  Where rows are whole 16-byte pieces these waits are taken off the path:
+//   - a block's part of a slab (kWarps * TS steps x 64 channels of each operand) is a 2-D tile, asked for by TMA up to a ring's
+//     length ahead;
+//   - a ninth warp joins: it takes the spans' maps, tells the cluster, collects its blocks' maps and hands the state back, while
+//     the other warps already compose the next slab and only then run the current one;
+//   - a cluster stays for several tiles of channels, whose slabs follow each other without a gap.
+constexpr int kTile = 64;              // channels
+constexpr int kStages = 3;             // 3 x 32 KB and 17 KB: two blocks fit an SM's 228 KB
+constexpr int tile_blocks(int item) { return item == 2 ? 2 : 1; }        // per SM; fp64 states need the registers of two
+constexpr int kTileThreads = 32 * (kWarps + 1);
+
+struct TilePlan {
+    int S;                             // blocks per cluster
+    int per_row;                       // tiles per batch element
+    long long tiles;
+    int slabs;                         // of a sequence
+};
+
+// Walks a cluster's slabs, tile after tile.  A tile: batch element b, channels d0 .. of its D.
+template <typename T>
+struct Cursor {
+    long long tile;
+    int slab;
+    bool live;                         // this lane's channels exist
+    int x_f, x_h;                      // first column of the tile in rows of f / u and of h / dh
+    long long c, end;
+    uint32_t at_f;                     // this lane's byte offset in a row of df / du
+    __device__ __forceinline__ void place(const Args &p, const TilePlan &q, int lane)
+    {
+        const long long b = tile / q.per_row, d0 = (tile - b * q.per_row) * kTile, d = d0 + 2 * lane;
+        live = d < p.D;
+        x_f = (int)(b * p.bs + d0); x_h = (int)(b * p.D + d0);
+        c = b * p.D + (live ? d : p.D - 2);
+        at_f = (uint32_t)((b * p.bs + d) * sizeof(T));
+        end = end_of(p, b);
+    }
+    __device__ __forceinline__ void start(const Args &p, const TilePlan &q, int lane)
+    {
+        tile = blockIdx.x / q.S;
+        slab = 0;
+        if (tile < q.tiles) place(p, q, lane);
+    }
+    __device__ __forceinline__ bool more(const TilePlan &q) const { return tile < q.tiles; }
+    __device__ __forceinline__ void next(const Args &p, const TilePlan &q, int lane)
+    {
+        if (++slab == q.slabs) {
+            slab = 0;
+            tile += gridDim.x / q.S;
+            if (tile < q.tiles) place(p, q, lane);
+        }
+    }
+};
+// counts through a ring of N barriers
+template <int N> struct Turn {
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() { if (++at == N) { at = 0; phase ^= 1; } }
+};
+
+template <typename F, int V>
+struct Exchange {                      // everything but the ring twice, alternating between slabs
+    Map<F, V> span[2][kWarps][32];     // this block's spans, then what lies ahead of each
+    struct { F h[V]; } state[2][32];   // before this block
+    Map<F, V> block[2][8][32];         // the cluster's blocks, sent by each
+    uint64_t full[kStages];            // a tile is here
+    uint64_t handed[2], arrived[2], ready[2];      // all spans are here; all of block[.]; state and span are what a warp needs
+    int gave_up;
+    __device__ __forceinline__ void init()
+    {
+        if (threadIdx.x == 0) {
+            for (int s = 0; s < kStages; ++s) tc::mbar_init(&full[s], 1);
+            for (int b = 0; b < 2; ++b) { tc::mbar_init(&handed[b], kWarps); tc::mbar_init(&arrived[b], 1); tc::mbar_init(&ready[b], 1); }
+            gave_up = 0;
+            tc::fence_barrier_init();
+        }
+        tc::cluster_sync();            // every block of the cluster runs, its barriers set up, before anything is sent to it
+    }
+    __device__ __forceinline__ void wait(uint64_t *bar, uint32_t parity, int *err, int code) { (void)tc::mbar_wait(bar, parity, &gave_up, err, code); }
+    // a working warp's side
+    __device__ __forceinline__ void hand(Turn<2> &turn, int warp, int lane, const Map<F, V> &m)
+    {
+        span[turn.at][warp][lane] = m;
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&handed[turn.at]);
+        turn.next();
+    }
+    template <bool SAFE>
+    __device__ __forceinline__ void take(Turn<2> &turn, int warp, int lane, int *err, F (&h)[V])
+    {
+        wait(&ready[turn.at], turn.phase, err, tc::ERR_WAIT_STEP);
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = state[turn.at][lane].h[i];
+        apply<SAFE>(span[turn.at][warp][lane], h);
+        turn.next();
+    }
+};
+
+// The joining warp over all slabs.  `initial` and `final` are the states before a sequence's first slab and behind its last
+// (null: zero, not wanted).  request(cursor, stage) asks for a slab's tiles; a tile may be overwritten once its slab has been
+// composed (LAG 0) or run (LAG 2: the map of the slab two later has been handed in).
+template <bool SAFE, int LAG, typename T, typename F, int V, typename Request>
+__device__ __forceinline__ void join_slabs(Exchange<F, V> &x, const Args &p, const TilePlan &q, int lane, const float *initial, float *final, Request request)
+{
+    const uint32_t rank = blockIdx.x % q.S;
+    Cursor<T> ahead, here;
+    ahead.start(p, q, lane);
+    here = ahead;
+    Turn<kStages> ring;
+    int asked = 0, done = 0;
+    auto ask = [&] {
+        if (!ahead.more(q)) return;
+        if (lane == 0) request(ahead, ring.at);
+        ring.next();
+        ahead.next(p, q, lane);
+        ++asked;
+    };
+    for (int s = 0; s < kStages; ++s) ask();
+    F state[V];
+    Turn<2> turn;
+    for (; here.more(q); here.next(p, q, lane), turn.next(), ++done) {
+        const int buf = turn.at;
+        if (here.slab == 0) load_initial(initial, here.c, true, state);
+        // arming may come after a neighbour's first bytes: the phase ends when both are complete
+        if (q.S > 1 && lane == 0) tc::mbar_expect_tx(&x.arrived[buf], (uint32_t)(q.S * 32 * sizeof(Map<F, V>)));
+        x.wait(&x.handed[buf], turn.phase, p.err, tc::ERR_WAIT_STEP);
+        Map<F, V> m[kWarps];                                          // all loads in flight together
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) m[w] = x.span[buf][w][lane];
+        if (done >= LAG) ask();
+        Map<F, V> all = m[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) all = then(all, m[w]);
+        if (q.S > 1) {
+            const uint32_t to = tc::smem_u32(&x.block[buf][rank][lane]), bar = tc::smem_u32(&x.arrived[buf]);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < q.S) send(tc::mapa(to, (uint32_t)r), tc::mapa(bar, (uint32_t)r), all);
+        }
+        Map<F, V> before = identity<F, V>();                          // while the exchange is under way
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            x.span[buf][w][lane] = before;
+            before = then(before, m[w]);
+        }
+        if (q.S > 1) {
+            // A neighbour sends for slab i + 2 only when it has this block's message for slab i + 1, which this warp sends after
+            // it has read slab i's: two buffers are enough.
+            wait_arrived(&x.arrived[buf], turn.phase, &x.gave_up, p.err);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < q.S) m[r] = x.block[buf][r][lane];
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < q.S) {
+                    if (r == (int)rank) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) x.state[buf][lane].h[i] = state[i];
+                    }
+                    apply<SAFE>(m[r], state);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) x.state[buf][lane].h[i] = state[i];
+            apply<SAFE>(all, state);
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&x.ready[buf]);
+        if (here.slab + 1 == q.slabs && here.live && rank == 0) store_final(final, here.c, state);
+    }
+    // a block that gave up still lets the tiles land that it asked for
+    if (*(volatile int *)&x.gave_up && lane == 0)
+        for (int s = max(0, asked - kStages); s < asked; ++s)
+            for (int i = 0; i < 1000000 && !tc::mbar_try_wait(&x.full[s % kStages], (s / kStages) & 1); ++i) {}
+    __syncwarp();
+}
+
+template <typename T, typename TH, int GATE, int TS>
+__global__ void __launch_bounds__(kTileThreads, tile_blocks(sizeof(T)))
+recurrence_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_constant__ CUtensorMap tm_u, const Args p, const TilePlan q)
+{
+    constexpr int V = 2, ROWS = kWarps * TS, TILE = ROWS * kTile * (int)sizeof(T);
+    constexpr bool SAFE = GATE == RELAY_GATE_GIVEN;
+    using K = Coefficient<T, GATE, V>;
+    using F = typename K::F;
+    using R = Raw<T, V>;
+    extern __shared__ __align__(128) uint8_t tiles[];                // [kStages][f, u][ROWS][kTile]
+    __shared__ __align__(16) Exchange<F, V> ex;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % q.S;
+    const long long slab_steps = (long long)q.S * ROWS;
+    ex.init();
+    pdl_wait();
+    if (warp == kWarps) {
+        join_slabs<SAFE, 0, T>(ex, p, q, lane, p.h0, p.h_final, [&](const Cursor<T> &at, int stage) {
+            const int row = (int)(at.slab * slab_steps) + rank * ROWS;
+            uint8_t *to = tiles + stage * 2 * TILE;
+            tc::mbar_expect_tx(&ex.full[stage], 2 * TILE);
+            tc::tma_load_2d(to, &tm_f, &ex.full[stage], at.x_f, row);
+            tc::tma_load_2d(to + TILE, &tm_u, &ex.full[stage], at.x_f, row);
+        });
+    } else {
+        const long long ldh = p.C * (long long)sizeof(TH);
+        const int first = (rank * kWarps + warp) * TS;
+        Cursor<T> composing, running;
+        composing.start(p, q, lane);
+        running = composing;
+        Turn<kStages> ring;
+        Turn<2> handing, taking;
+        auto compose = [&](float (&a)[TS][V], float (&x)[TS][V]) {
+            if (!composing.more(q)) return;
+            ex.wait(&ex.full[ring.at], ring.phase, p.err, tc::ERR_WAIT_FULL);
+            const R *f = reinterpret_cast<const R *>(tiles + ring.at * 2 * TILE) + warp * TS * (kTile / V) + lane;
+            const R *u = f + TILE / (int)sizeof(R);
+            ring.next();
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                float fv[V], uv[V];
+                to_f32(f[s * (kTile / V)], fv); to_f32(u[s * (kTile / V)], uv);
+                K::of(fv, uv, a[s], x[s]);
+            }
+            const int n = steps_before<TS>(first + composing.slab * slab_steps, composing.end);
+            if (!__all_sync(0xffffffffu, n == TS)) {
+#pragma unroll
+                for (int s = 0; s < TS; ++s)
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (s >= n) { a[s][i] = K::keep(); x[s][i] = 0.0f; }
+            }
+            Map<F, V> mine = identity<F, V>();
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                F v[V], b[V];
+                K::value(a[s], v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) b[i] = F(x[s][i]);
+                mul(mine.a, v, mine.a);
+                muladd(v, mine.h, b, mine.h);
+            }
+            ex.hand(handing, warp, lane, mine);
+            composing.next(p, q, lane);
+        };
+        auto run = [&](const float (&a)[TS][V], const float (&x)[TS][V]) {
+            if (!running.more(q)) return;
+            F h[V];
+            ex.template take<SAFE>(taking, warp, lane, p.err, h);
+            const long long t0 = first + running.slab * slab_steps;
+            const int n = steps_before<TS>(t0, running.end);
+            char *out = (char *)p.h + t0 * ldh + running.c * (long long)sizeof(TH);
+            if (__all_sync(0xffffffffu, n == TS)) {
+#pragma unroll
+                for (int s = 0; s < TS; ++s) {
+                    float o[V];
+                    K::step(a[s], x[s], h);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[i] = (float)h[i];
+                    if (running.live) store<TH, V>(out, 0, o);
+                    out += ldh;
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < TS; ++s) {
+                    float o[V];
+                    K::step(a[s], x[s], h);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[i] = s < n ? (float)h[i] : 0.0f;
+                    if (running.live && t0 + s < p.T) store<TH, V>(out, 0, o);
+                    out += ldh;
+                }
+            }
+            running.next(p, q, lane);
+        };
+        float a0[TS][V], x0[TS][V], a1[TS][V], x1[TS][V];
+        compose(a0, x0);
+        while (running.more(q)) {
+            compose(a1, x1);
+            run(a0, x0);
+            compose(a0, x0);
+            run(a1, x1);
+        }
+    }
+    tc::cluster_sync();                // no block leaves while another may still send to it
+}
+
+template <typename T, typename TH, int GATE, int TS>
+__global__ void __launch_bounds__(kTileThreads, tile_blocks(sizeof(T)))
+recurrence_grad_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_d,
+                             const __grid_constant__ CUtensorMap tm_h, const Args p, const TilePlan q)
+{
+    constexpr int V = 2, ROWS = kWarps * TS, TILE = ROWS * kTile * (int)sizeof(T), TILE_H = ROWS * kTile * (int)sizeof(TH), STAGE = 2 * (TILE + TILE_H);
+    constexpr bool SAFE = GATE == RELAY_GATE_GIVEN;
+    using K = Coefficient<T, GATE, V>;
+    using F = typename K::F;
+    using R = Raw<T, V>;
+    using RH = Raw<TH, V>;
+    extern __shared__ __align__(128) uint8_t tiles[];                // [kStages][f, u, dh, h one step earlier][ROWS][kTile]
+    __shared__ __align__(16) Exchange<F, V> ex;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % q.S;
+    const long long slab_steps = (long long)q.S * ROWS;
+    ex.init();
+    pdl_wait();
+    if (warp == kWarps) {
+        join_slabs<SAFE, 2, T>(ex, p, q, lane, p.dh_final, p.dh0, [&](const Cursor<T> &at, int stage) {
+            uint8_t *to = tiles + stage * STAGE;
+            const int row = (int)(p.T - (at.slab * slab_steps + (long long)(rank + 1) * ROWS));     // rows in front of the first read as zero
+            tc::mbar_expect_tx(&ex.full[stage], STAGE);
+            tc::tma_load_2d(to, &tm_f, &ex.full[stage], at.x_f, row);
+            tc::tma_load_2d(to + TILE, &tm_u, &ex.full[stage], at.x_f, row);
+            tc::tma_load_2d(to + 2 * TILE, &tm_d, &ex.full[stage], at.x_h, row);
+            tc::tma_load_2d(to + 2 * TILE + TILE_H, &tm_h, &ex.full[stage], at.x_h, row - 1);
+        });
+    } else {
+        const long long ldf = p.ld * (long long)sizeof(T);
+        const long long first = p.T - 1 - (long long)(rank * kWarps + warp) * TS;             // the steps of slab i are this - i slab_steps and before
+        const int last = (ROWS - 1 - warp * TS) * (kTile / V) + lane;                         // the first of them in the tile
+        Cursor<T> composing, running;
+        composing.start(p, q, lane);
+        running = composing;
+        Turn<kStages> ring, ring_run;
+        Turn<2> handing, taking;
+        auto compose = [&] {
+            if (!composing.more(q)) return;
+            ex.wait(&ex.full[ring.at], ring.phase, p.err, tc::ERR_WAIT_FULL);
+            const long long t0 = first - composing.slab * slab_steps;
+            const bool all_on = __all_sync(0xffffffffu, t0 < composing.end && t0 >= TS);
+            const R *f = reinterpret_cast<const R *>(tiles + ring.at * STAGE) + last;
+            const RH *d = reinterpret_cast<const RH *>(tiles + ring.at * STAGE + 2 * TILE) + last;
+            ring.next();
+            Map<F, V> mine = identity<F, V>();
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                float fv[V], dh[V], k[V];
+                F v[V], dv[V];
+                to_f32(f[-s * (kTile / V)], fv); to_f32(d[-s * (kTile / V)], dh);
+                K::of(fv, k);
+                K::value(k, v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) dv[i] = F(dh[i]);
+                if (all_on || (t0 - s < composing.end && t0 - s >= 0)) {
+                    mul(mine.a, v, mine.a);
+                    add(mine.h, dv, mine.h);
+                    mul(mine.h, v, mine.h);
+                }
+            }
+            ex.hand(handing, warp, lane, mine);
+            composing.next(p, q, lane);
+        };
+        compose();
+        while (running.more(q)) {
+            compose();
+            F G[V];
+            ex.template take<SAFE>(taking, warp, lane, p.err, G);
+            const long long t0 = first - running.slab * slab_steps;
+            const bool all_on = __all_sync(0xffffffffu, t0 < running.end && t0 >= TS);        // and none is the first step
+            const uint8_t *at = tiles + ring_run.at * STAGE;
+            ring_run.next();
+            const R *f = reinterpret_cast<const R *>(at) + last, *u = reinterpret_cast<const R *>(at + TILE) + last;
+            const RH *d = reinterpret_cast<const RH *>(at + 2 * TILE) + last, *hb = reinterpret_cast<const RH *>(at + 2 * TILE + TILE_H) + last;
+            char *df_at = (char *)p.df + t0 * ldf + running.at_f, *du_at = (char *)p.du + t0 * ldf + running.at_f;
+#pragma unroll
+            for (int s = 0; s < TS; ++s) {
+                const long long t = t0 - s;
+                float fv[V], uv[V], dh[V], before[V], df[V], du[V];
+                to_f32(f[-s * (kTile / V)], fv); to_f32(u[-s * (kTile / V)], uv);
+                to_f32(d[-s * (kTile / V)], dh); to_f32(hb[-s * (kTile / V)], before);
+                if (!all_on && t == 0) load_state(p.h0, running.c, before);
+                backward_step<K, GATE, V>(fv, uv, dh, before, all_on || t < running.end, G, df, du);
+                if (running.live && (all_on || t >= 0)) {
+                    store<T, V>(df_at, 0, df);
+                    store<T, V>(du_at, 0, du);
+                }
+                df_at -= ldf; du_at -= ldf;
+            }
+            running.next(p, q, lane);
+        }
+    }
+    tc::cluster_sync();
+}
+
+template <typename T, typename TH, int GATE>
+bool tiles_fit(const Args &p)
+{
+    const long long piece = 16 / (long long)sizeof(T);
+    return p.T > 2 * kWarps && p.D % piece == 0 && p.bs % piece == 0 && p.ld < (1ll << 31) && p.C < (1ll << 31) && p.T < (1ll << 30);
+}
+template <typename T, typename TH, int GATE>
+relay_status_t launch_tiles(const Args &p, bool grad, cudaStream_t st)
+{
+    constexpr int TS = 8, TSG = sizeof(T) + sizeof(TH) == 4 ? 8 : 4;
+    int dev = 0, sms = 148;
+    RELAY_CUDA(cudaGetDevice(&dev));
+    RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const int rows = kWarps * (grad ? TSG : TS), resident = tile_blocks(sizeof(T)) * sms;
+    TilePlan q;
+    q.per_row = (int)((p.D + kTile - 1) / kTile);
+    q.tiles = (p.C / p.D) * q.per_row;
+    // as many blocks per tile as find room at once and have something to do; no more clusters than find room
+    q.S = (int)std::max<long long>(1, std::min<long long>({8, resident / q.tiles, (p.T + rows - 1) / rows}));
+    q.slabs = (int)((p.T + (long long)q.S * rows - 1) / ((long long)q.S * rows));
+    const size_t smem = (size_t)kStages * rows * kTile * 2 * (sizeof(T) + (grad ? sizeof(TH) : 0));
+    const dim3 grid((unsigned)(std::min<long long>(q.tiles, resident / q.S) * q.S)), block(kTileThreads), cluster((unsigned)q.S);
+    const bool t32 = sizeof(T) == 4, h32 = sizeof(TH) == 4;
+    CUtensorMap f, u, d, h;
+    const uint64_t ld = (uint64_t)p.ld;
+    // packed: the map of u starts D columns into the rows, the last D columns of f's belong to nobody's u
+    RELAY_TRY(make_tmap_2d(&f, t32, p.f, ld, p.T, ld, kTile, rows, false));
+    RELAY_TRY(make_tmap_2d(&u, t32, p.u, ld - (p.bs == 2 * p.D ? p.D : 0), p.T, ld, kTile, rows, false));
+    if (!grad) {
+        RELAY_CUDA(cudaFuncSetAttribute(recurrence_tiles_kernel<T, TH, GATE, TS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        RELAY_CUDA(launch_pdl_cluster(recurrence_tiles_kernel<T, TH, GATE, TS>, grid, block, cluster, smem, st, f, u, p, q));
+    } else {
+        RELAY_TRY(make_tmap_2d(&d, h32, p.dh, p.C, p.T, p.C, kTile, rows, false));
+        RELAY_TRY(make_tmap_2d(&h, h32, p.h, p.C, p.T, p.C, kTile, rows, false));
+        RELAY_CUDA(cudaFuncSetAttribute(recurrence_grad_tiles_kernel<T, TH, GATE, TSG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        RELAY_CUDA(launch_pdl_cluster(recurrence_grad_tiles_kernel<T, TH, GATE, TSG>, grid, block, cluster, smem, st, f, u, d, h, p, q));
+    }
+    return check_launch("gated_recurrence");
 }
 
 // Sequences of up to kSteps steps run step by step.  Longer ones: the smallest cluster that gives every SM a block.
 constexpr long long kSteps = 32;
 
-template <typename T, typename TH, int GATE, int V>
+// W channels a thread in the spans kernels, at most two in the step-by-step ones (more threads where there are few steps)
+template <typename T, typename TH, int GATE, int W>
 relay_status_t launch(const Args &p, bool grad, cudaStream_t st)
 {
-    if (p.T > kSteps) {
-        constexpr int TS = sizeof(T) == 2 ? 16 : 8, TSG = sizeof(T) + sizeof(TH) == 4 ? 8 : 4;
+    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
+    const bool narrow = p.ld * (long long)sizeof(T) < (1ll << 32) && p.C * (long long)sizeof(TH) < (1ll << 32);   // a row's offsets fit 32 bits
+    if (p.T > kSteps && narrow) {
+        constexpr int TS = (sizeof(T) == 2 ? 32 : 16) / (W == 1 ? 2 : W), TSG = (sizeof(T) + sizeof(TH) == 4 ? 16 : 8) / (W == 1 ? 2 : W);
         int dev = 0, sms = 148;
         RELAY_CUDA(cudaGetDevice(&dev));
         RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-        const long long tiles = (p.C + 32 * V - 1) / (32 * V), steps = kWarps * (grad ? TSG : TS);
+        const long long tiles = (p.C + 32 * W - 1) / (32 * W), steps = kWarps * (grad ? TSG : TS);
         int S = 1;
         while (S < 8 && tiles * S < sms && p.T > S * steps) S *= 2;
         if (tiles * S > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "gated_recurrence: %lld channels", p.C);
         const dim3 grid((unsigned)(tiles * S)), block(32 * kWarps), cluster((unsigned)S);
-        if (grad) RELAY_CUDA(launch_pdl_cluster(recurrence_grad_spans_kernel<T, TH, GATE, V, TSG>, grid, block, cluster, 0, st, p, S));
-        else RELAY_CUDA(launch_pdl_cluster(recurrence_spans_kernel<T, TH, GATE, V, TS>, grid, block, cluster, 0, st, p, S));
+        if (grad) RELAY_CUDA(launch_pdl_cluster(recurrence_grad_spans_kernel<T, TH, GATE, W, TSG>, grid, block, cluster, 0, st, p, S));
+        else RELAY_CUDA(launch_pdl_cluster(recurrence_spans_kernel<T, TH, GATE, W, TS>, grid, block, cluster, 0, st, p, S));
         return check_launch("gated_recurrence");
     }
-    const dim3 grid((unsigned)((p.C / V + kThreads - 1) / kThreads));
+    constexpr int V = W == 1 ? 1 : 2;
+    const long long blocks = (p.C / V + kThreads - 1) / kThreads;
+    if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "gated_recurrence: %lld channels", p.C);
+    const dim3 grid((unsigned)blocks);
     if (grad) RELAY_CUDA(launch_pdl(recurrence_grad_steps_kernel<T, TH, GATE, V>, grid, dim3(kThreads), 0, st, p));
     else RELAY_CUDA(launch_pdl(recurrence_steps_kernel<T, TH, GATE, V>, grid, dim3(kThreads), 0, st, p));
     return check_launch("gated_recurrence");
 }
+template <typename T, typename TH, int GATE>
+relay_status_t launch_gate(const Args &p, bool grad, cudaStream_t st)
+{
+    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
+    if (p.T > kSteps && tiles_fit<T, TH, GATE>(p)) return launch_tiles<T, TH, GATE>(p, grad, st);
+    // several channels a thread where every row starts at a multiple of them, so that they are one aligned access
+    const long long rows = p.D | p.ld | p.bs;
+    return rows % 2 == 0 ? launch<T, TH, GATE, 2>(p, grad, st) : launch<T, TH, GATE, 1>(p, grad, st);
+}
 template <typename T, typename TH>
 relay_status_t launch_typed(const Args &p, int32_t gate, bool grad, cudaStream_t st)
 {
-    // two channels a thread where every row starts at an even element, so that the pair is one aligned access
-    const bool pair = p.D % 2 == 0 && p.ld % 2 == 0 && p.bs % 2 == 0;
     switch (gate) {
-    case RELAY_GATE_GIVEN: return pair ? launch<T, TH, RELAY_GATE_GIVEN, 2>(p, grad, st) : launch<T, TH, RELAY_GATE_GIVEN, 1>(p, grad, st);
-    case RELAY_GATE_SIGMOID: return pair ? launch<T, TH, RELAY_GATE_SIGMOID, 2>(p, grad, st) : launch<T, TH, RELAY_GATE_SIGMOID, 1>(p, grad, st);
-    default: return pair ? launch<T, TH, RELAY_GATE_MIX, 2>(p, grad, st) : launch<T, TH, RELAY_GATE_MIX, 1>(p, grad, st);
+    case RELAY_GATE_GIVEN: return launch_gate<T, TH, RELAY_GATE_GIVEN>(p, grad, st);
+    case RELAY_GATE_SIGMOID: return launch_gate<T, TH, RELAY_GATE_SIGMOID>(p, grad, st);
+    default: return launch_gate<T, TH, RELAY_GATE_MIX>(p, grad, st);
     }
 }
 relay_status_t launch_any(const Args &p, int32_t t, int32_t th, int32_t gate, bool grad, cudaStream_t st)
@@ -597,7 +1298,8 @@ Args make_args(const relay_tensor_t *f, const relay_tensor_t *u, const relay_ten
     p.ld = s.B * p.bs;
     p.h0 = h0 ? (const float *)h0->data : nullptr;
     p.lengths = lengths ? (const int *)lengths->data : nullptr;
-    if (!s.packed && !lengths) p.D = p.C;          // nothing depends on the batch element: one row of channels
+    p.err = device_error_word();
+    if (!s.packed && !lengths) p.D = p.bs = p.C;   // nothing depends on the batch element: one row of channels
     return p;
 }
 
