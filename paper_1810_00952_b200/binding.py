@@ -106,16 +106,13 @@ def desc(t: Optional[torch.Tensor], layout: int = ROWMAJOR) -> Optional[TensorDe
         return None
     if not t.is_contiguous():
         raise ValueError("tensors crossing the C-ABI must be contiguous")
-    if t.dtype not in _TORCH2RELAY:
+    dtype = _TORCH2RELAY.get(t.dtype)
+    if dtype is None:
         raise ValueError(f"dtype {t.dtype} has no Relay base type here")
-    d = TensorDesc()
-    d.data = t.data_ptr() if t.numel() else (t.data_ptr() or None)
-    d.dtype = _TORCH2RELAY[t.dtype]
-    d.rank = t.dim()
-    for i, s in enumerate(t.shape):
-        d.shape[i] = s
-    d.layout = layout
-    return d
+    shape = tuple(t.shape)
+    if len(shape) > MAX_RANK:
+        raise IndexError(f"rank {len(shape)}: a descriptor has room for {MAX_RANK} extents")
+    return TensorDesc(t.data_ptr() or None, dtype, len(shape), shape, layout, 0)
 
 
 def desc_of_type(dtype: int, shape: Sequence[int], layout: int = ROWMAJOR, data: int = 0) -> TensorDesc:
@@ -138,6 +135,9 @@ def _shape(d: TensorDesc):
 
 
 def _stream() -> ctypes.c_void_p:
+    """The current stream of the current device; the raw handle costs a tenth of building a torch.cuda.Stream per call."""
+    if torch.cuda.is_initialized():
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 

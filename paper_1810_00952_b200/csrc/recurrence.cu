@@ -289,28 +289,6 @@ template <typename T, int GATE, int V> struct Coefficient {
         muladd(a, h, x, h);
     }
 };
-// partials of one step: g = dh_t + G_{t+1}
-template <int GATE, bool FINE, int V>
-__device__ __forceinline__ void partials(const float (&f)[V], const float (&u)[V], const float (&before)[V], const float (&g)[V], float (&df)[V], float (&du)[V])
-{
-    if constexpr (GATE == RELAY_GATE_GIVEN) {
-        mul(g, before, df);
-#pragma unroll
-        for (int i = 0; i < V; ++i) du[i] = g[i];
-    } else {
-        float a[V], s[V], d[V], gs[V];
-        sigmoid_pair<FINE>(f, a, s);
-        mul(g, s, gs);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            d[i] = GATE == RELAY_GATE_MIX ? before[i] - u[i] : before[i];
-            du[i] = GATE == RELAY_GATE_MIX ? gs[i] : g[i];
-        }
-        mul(gs, a, gs);
-        mul(gs, d, df);
-    }
-}
-
 __device__ __forceinline__ long long end_of(const Args &p, long long b)
 {
     if (p.lengths == nullptr) return p.T;
@@ -336,22 +314,42 @@ __device__ __forceinline__ void store_final(float *p, long long c, const F (&sta
     store_state(p, c, x);
 }
 
-// One step backwards: partials of f and u, and G <- a (dh + G); a step behind the end has none and leaves G.
+// One step backwards: with g = dh + G, partials of f and u, and G <- a g; a step behind the end has none and leaves G.
 template <typename K, int GATE, int V>
 __device__ __forceinline__ void backward_step(const float (&f)[V], const float (&u)[V], const float (&dh)[V], const float (&before)[V], bool on,
                                               typename K::F (&G)[V], float (&df)[V], float (&du)[V])
 {
     using F = typename K::F;
     F g[V], a[V];
-    float k[V], g32[V];
+    float g32[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) g[i] = F(dh[i]);
     add(g, G, g);
 #pragma unroll
     for (int i = 0; i < V; ++i) g32[i] = (float)g[i];
-    K::of(f, k);
-    K::value(k, a);
-    partials<GATE, K::FINE>(f, u, before, g32, df, du);
+    if constexpr (GATE == RELAY_GATE_GIVEN) {
+        mul(g32, before, df);
+#pragma unroll
+        for (int i = 0; i < V; ++i) { du[i] = g32[i]; a[i] = F(f[i]); }
+    } else {
+        float open[V], s[V], gs[V];
+        sigmoid_pair<K::FINE>(f, open, s);
+        mul(g32, s, gs);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            du[i] = GATE == RELAY_GATE_MIX ? gs[i] : g32[i];
+            a[i] = K::FINE && f[i] >= 0.0f ? F(1) - F(s[i]) : F(open[i]);
+        }
+        mul(gs, open, gs);
+        if constexpr (GATE == RELAY_GATE_MIX) {
+            float d[V], m[V];
+            fill(-1.0f, m);
+            muladd(u, m, before, d);
+            mul(gs, d, df);
+        } else {
+            mul(gs, before, df);
+        }
+    }
     if (on) {
         mul(a, g, G);
     } else {
