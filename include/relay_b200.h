@@ -436,7 +436,7 @@ relay_status_t relay_gated_recurrence_grad(const relay_tensor_t *f, const relay_
  * tokens and logp may be NULL together, top_logp and top_ids too, entropy and lse each (not all outputs at once).
  * Arithmetic in f32.  A token outside [0,V) names no class: its logp is 0.  Scores of -inf are classes that cannot occur; a
  * row of nothing else has lse = -inf, logp = -inf, entropy 0.  A row with a NaN or +inf has NaN results; among the ids NaN
- * counts as larger than +inf.  Rows = 0 is a no-op; V = 0 is RELAY_ERR_SHAPE; V < 2^31. */
+ * counts as larger than +inf.  Rows = 0 is a no-op; V = 0 is RELAY_ERR_SHAPE; V < 2^31 - 64. */
 #define RELAY_MAX_TOP 64
 relay_status_t relay_token_logprob(const relay_tensor_t *scores, const relay_tensor_t *tokens, float temperature, const relay_tensor_t *logp,
                                    const relay_tensor_t *entropy, const relay_tensor_t *lse, const relay_tensor_t *top_logp,
