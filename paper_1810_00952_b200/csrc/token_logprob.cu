@@ -66,20 +66,20 @@ __device__ __forceinline__ float exp2_(float x)
 // a finite difference even where a score or the maximum is infinite: its exponential is 0 and its product with that too
 __device__ __forceinline__ float below(float z, float m) { return fmaxf(z - m, -1.0e30f); }
 
-__device__ __forceinline__ Sums join(const Sums &a, const Sums &b, const Scale &k)
+// the sums of a warp's lanes together, in every lane; written out with intrinsics, so that every kernel rounds alike
+__device__ __forceinline__ Sums join_lanes(Sums a, const Scale &k)
 {
-    Sums r;
-    r.m = max_nan(a.m, b.m);
-    const float da = below(a.m, r.m), db = below(b.m, r.m);
-    const float ea = exp2_(da * k.log2e), eb = exp2_(db * k.log2e);
-    // written out, so that every kernel rounds alike
-    r.s = fmaf(a.s, ea, __fmul_rn(b.s, eb));
-    r.w = fmaf(ea, fmaf(da, a.s, a.w), __fmul_rn(eb, fmaf(db, b.s, b.w)));
-    return r;
-}
-__device__ __forceinline__ Sums shfl_xor(const Sums &a, int d)
-{
-    return Sums{__shfl_xor_sync(0xffffffffu, a.m, d), __shfl_xor_sync(0xffffffffu, a.s, d), __shfl_xor_sync(0xffffffffu, a.w, d)};
+    float m = a.m;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
+    const float d = below(a.m, m), f = exp2_(d * k.log2e);
+    float s = __fmul_rn(f, a.s), w = __fmul_rn(f, fmaf(d, a.s, a.w));
+#pragma unroll
+    for (int d2 = 16; d2 > 0; d2 >>= 1) {
+        s = __fadd_rn(s, __shfl_xor_sync(0xffffffffu, s, d2));
+        w = __fadd_rn(w, __shfl_xor_sync(0xffffffffu, w, d2));
+    }
+    return Sums{m, s, w};
 }
 
 // what a row's sums say
@@ -191,55 +191,68 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigne
     return r;
 }
 
-// One thread's running sums, in pairs; m is raised (and the sums scaled down) only when a vector holds something larger, some
-// ln(vectors) times a row.
+// One thread's running sums, in pairs, N vectors at a time: the maximum over all of them is looked at first, and only where it is
+// larger than the one so far are the sums scaled down (some ln(row / N) times a row).
 // Differences from -inf: the scores are raised to the lowest finite value first, so that 0 times the distance is 0; only where the
 // maximum itself is that low (masks of the lowest value and nothing else) are the elements looked at one by one.
 struct Running {
     float m = -INFINITY;
     unsigned long long s = 0, w = 0;                       // two partial sums each
-    float best = -INFINITY;                                // largest element so far, and the first vector that holds it
-    int best_at = -1;
-    template <typename T>
-    __device__ __forceinline__ void take(const uint4 &q, int j, const Scale &k, const T *type)
+    int best_at = -1;                                      // the first vector that holds the largest element, m unless NaN are about
+    template <typename T, int N>
+    __device__ __forceinline__ float take(const uint4 (&q)[N], int j, int stride, const Scale &k, const T *type)      // their largest
     {
         constexpr int E = Vec<T>::E;
-        const float top = largest(q, type);
-        if (!(top <= m)) {                                 // larger, or NaN
-            const float d = below(m, top), f = exp2_(d * k.log2e);
+        float top[N], most;
+#pragma unroll
+        for (int n = 0; n < N; ++n) top[n] = largest(q[n], type);
+        most = top[0];
+#pragma unroll
+        for (int n = 1; n < N; ++n) most = max_nan(most, top[n]);
+        if (best_at < 0) best_at = j;
+        if (!(most <= m)) {                                // larger, or NaN
+            const float d = below(m, most), f = exp2_(d * k.log2e);
             float s0, s1, w0, w1;
             unpair(s, s0, s1); unpair(w, w0, w1);
             w = pair(f * fmaf(d, s0, w0), f * fmaf(d, s1, w1));
             s = pair(f * s0, f * s1);
-            m = max_nan(m, top);
+            m = max_nan(m, most);
+#pragma unroll
+            for (int n = N - 1; n >= 0; --n)
+                if (top[n] == most) best_at = j + n * stride;
         }
-        if (top > best || best_at < 0) { best = top; best_at = j; }
-        float x[E];
         if (m < -1.0e36f) {
-            if (m == -INFINITY) return;                    // nothing but -inf so far
-            unpack(q, x);
-            float s0, s1, w0, w1;
-            unpair(s, s0, s1); unpair(w, w0, w1);
-            for (int i = 0; i < E; ++i)
-                if (x[i] != -INFINITY) {
-                    const float d = x[i] - m, e = exp2_(d * k.log2e);
-                    s0 += e;
-                    w0 = fmaf(e, d, w0);
-                }
-            s = pair(s0, s1); w = pair(w0, w1);
-            return;
+            if (m == -INFINITY) return most;               // nothing but -inf so far
+            for (int n = 0; n < N; ++n) {
+                float x[E], s0, s1, w0, w1;
+                unpack(q[n], x);
+                unpair(s, s0, s1); unpair(w, w0, w1);
+                for (int i = 0; i < E; ++i)
+                    if (x[i] != -INFINITY) {
+                        const float d = x[i] - m, e = exp2_(d * k.log2e);
+                        s0 += e;
+                        w0 = fmaf(e, d, w0);
+                    }
+                s = pair(s0, s1); w = pair(w0, w1);
+            }
+            return most;
         }
-        finite_elements(q, x);
         const unsigned long long nm = pair(-m, -m), c = pair(k.log2e, k.log2e);
 #pragma unroll
-        for (int i = 0; i < E; i += 2) {
-            const unsigned long long d = add2(pair(x[i], x[i + 1]), nm);
-            float t0, t1;
-            unpair(mul2(d, c), t0, t1);
-            const unsigned long long e = pair(exp2_(t0), exp2_(t1));
-            s = add2(s, e);
-            w = fma2(e, d, w);
+        for (int n = 0; n < N; ++n) {
+            float x[E];
+            finite_elements(q[n], x);
+#pragma unroll
+            for (int i = 0; i < E; i += 2) {
+                const unsigned long long d = add2(pair(x[i], x[i + 1]), nm);
+                float t0, t1;
+                unpair(mul2(d, c), t0, t1);
+                const unsigned long long e = pair(exp2_(t0), exp2_(t1));
+                s = add2(s, e);
+                w = fma2(e, d, w);
+            }
         }
+        return most;
     }
     __device__ __forceinline__ Sums sums() const
     {
@@ -249,16 +262,24 @@ struct Running {
     }
 };
 // Vector j of a row: its elements j E .. j E + E - 1 (-inf behind the row's end), wherever the row starts in memory, so that a
-// row's result does not depend on its place.  `skew`: how many elements before the row's first the nearest 16-byte boundary lies;
-// then two aligned pieces are read and shifted (the second is the next thread's first, and in L1).
-template <typename T>
+// row's result does not depend on its place.  EVEN: V is a multiple of E, every vector of every row is one aligned piece.
+// Otherwise `skew` is how many elements before the row's first the nearest 16-byte boundary lies, and two aligned pieces are read
+// and shifted (the second is the next thread's first, and in L1).
+template <typename T, bool EVEN>
 struct RowVectors {
     const T *aligned;                  // the row's start, rounded down
     int skew, V, safe;                 // vectors below `safe` can be read as whole pieces
     __device__ __forceinline__ RowVectors(const T *z, long long rows, long long row, int V_) : V(V_)
     {
         constexpr int E = Vec<T>::E;
-        const long long at = row * V, left = rows * V - at;        // elements from the row's start to the tensor's end
+        const long long at = row * V;
+        if (EVEN) {
+            aligned = z + at;
+            skew = 0;
+            safe = V / E;
+            return;
+        }
+        const long long left = rows * V - at;              // elements from the row's start to the tensor's end
         skew = (int)(at % E);
         aligned = z + (at - skew);
         // piece j + 1 ends (j + 2) E - skew elements behind the row's start
@@ -266,149 +287,53 @@ struct RowVectors {
         safe = (int)min((long long)(V / E), max(inside, 0ll));
     }
     __device__ __forceinline__ int count() const { return (int)(((long long)V + Vec<T>::E - 1) / Vec<T>::E); }
+    // N vectors j, j + stride, .. below `safe`: all loads before the first use
+    template <int N>
+    __device__ __forceinline__ void whole(int j, int stride, uint4 (&q)[N]) const
+    {
+        const uint4 *at = (const uint4 *)aligned + j;
+        if (EVEN) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) q[n] = ld_stream(at + n * stride);
+            return;
+        }
+        uint4 hi[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            q[n] = hi[n] = uint4{};
+            if (relay_in_bounds(at + n * stride, skew ? 32 : 16)) { q[n] = __ldg(at + n * stride); hi[n] = __ldg(at + n * stride + (skew != 0)); }
+        }
+        const int bytes = skew * (int)sizeof(T);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            uint32_t w[8] = {q[n].x, q[n].y, q[n].z, q[n].w, hi[n].x, hi[n].y, hi[n].z, hi[n].w};
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = bytes & 8 ? w[i + 2] : w[i];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = bytes & 4 ? w[i + 1] : w[i];
+            if (sizeof(T) == 2) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (bytes & 2) * 8);
+            }
+            q[n] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
     __device__ __forceinline__ uint4 operator[](int j) const
     {
         constexpr int E = Vec<T>::E;
-        const T *at = aligned + (long long)j * E;
-        if (j < safe) {
-            if (skew == 0) return ld_stream(at);
-            uint4 lo{}, hi{};
-            if (relay_in_bounds(at, 32)) { lo = __ldg((const uint4 *)at); hi = __ldg((const uint4 *)at + 1); }
-            uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            const int bytes = skew * (int)sizeof(T);
-            if (bytes & 8) {
-#pragma unroll
-                for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-            }
-            if (bytes & 4) {
-#pragma unroll
-                for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-            }
-            if (bytes & 2) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-            }
-            return make_uint4(w[0], w[1], w[2], w[3]);
+        uint4 q[1];
+        if (EVEN || j < safe) {
+            whole(j, 0, q);
+            return q[0];
         }
         float x[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = (long long)j * E + i < V ? load_score(at + skew + i) : -INFINITY;
+        for (int i = 0; i < E; ++i) x[i] = (long long)j * E + i < V ? load_score(aligned + (long long)j * E + skew + i) : -INFINITY;
         return pack(x);
     }
 };
 
-// ---- forward: a cluster of S blocks per row ------------------------------------------------------------------------------
-// Each block sums a contiguous part of the row's vectors; the blocks' sums meet in block 0's shared memory.
-// Alternatives: a thread remembers its largest element; of the largest of G groups of threads the K-th is a bound that the row's
-// K-th largest element cannot be below, so only the groups whose largest reaches it are looked through again (their vectors come
-// from L2) and what reaches it is listed; the position of a listed element is the number of larger ones.
-constexpr int kList = 512;             // listed elements: K of them by the bound, and as many as happen to share their groups
-constexpr int kWarpsPerBlock = kThreads / 32;
-
-struct Lists {
-    unsigned long long group[kThreads];
-    unsigned long long list[kList];
-    unsigned long long chosen[RELAY_MAX_TOP];
-    unsigned long long merged[8 * RELAY_MAX_TOP];          // block 0: the chosen of all blocks
-    int count;
-};
-
-// the K largest of n <= kList different keys in `from`, largest first (0 where there are fewer)
-__device__ __forceinline__ void rank_keys(const unsigned long long *from, int n, int K, unsigned long long *to)
-{
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const unsigned long long mine = from[i];
-        int larger = 0;
-        for (int o = 0; o < n; ++o) larger += from[o] > mine;
-        if (larger < K) to[larger] = mine;
-    }
-}
-
-// the K largest keys of vectors [v0, v1) of a row into l.chosen; `best_at` etc. of this thread; block-wide
-template <typename T>
-__device__ __forceinline__ void choose(Lists &l, const RowVectors<T> &r, int v0, int v1, int K, float best, int best_at, bool has_nan)
-{
-    constexpr int E = Vec<T>::E;
-    const int tid = threadIdx.x;
-    for (int i = tid; i < K; i += kThreads) l.chosen[i] = 0;
-    if (tid == 0) l.count = 0;
-    const int per = K <= 16 ? 4 : K <= 32 ? 2 : 1;         // threads per group: enough groups for K, few enough to compare
-    unsigned long long mine = 0;
-    if (best_at >= 0) {
-        float x[E];
-        unpack(r[best_at], x);
-#pragma unroll
-        for (int i = E - 1; i >= 0; --i) {
-            const int id = best_at * E + i;
-            if (x[i] == best && id < r.V) mine = key_of(x[i], id);
-        }
-    }
-    if (per > 1) mine = max(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
-    if (per > 2) mine = max(mine, __shfl_xor_sync(0xffffffffu, mine, 2));
-    if (tid % per == 0) l.group[tid / per] = mine;
-    __syncthreads();
-    bool searched = !has_nan;
-    if (searched) {
-        const int groups = kThreads / per;
-        bool is_bound = false;
-        if (tid < groups) {
-            const unsigned long long g = l.group[tid];
-            int larger = 0;
-            for (int o = 0; o < groups; ++o) larger += l.group[o] > g;
-            is_bound = larger == K - 1 && g != 0;
-            if (is_bound) l.list[0] = g;
-        }
-        // groups without elements share the key 0: the bound is then 0, everything is listed (fewer than K groups hold fewer
-        // than kList elements)
-        const unsigned long long bound = __syncthreads_or(is_bound) ? l.list[0] : 0;
-        __syncthreads();
-        if (mine != 0 && mine >= bound) {                  // one of the K groups: look through its vectors
-            for (int j = v0 + tid; j < v1; j += kThreads) {
-                float x[E];
-                unpack(r[j], x);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const int id = j * E + i;
-                    if (id >= r.V) continue;
-                    const unsigned long long key = key_of(x[i], id);
-                    if (key >= bound) {
-                        const int at = atomicAdd(&l.count, 1);
-                        if (at < kList) l.list[at] = key;
-                    }
-                }
-            }
-        }
-        __syncthreads();
-        searched = l.count <= kList;
-        if (searched) rank_keys(l.list, l.count, K, l.chosen);
-    }
-    if (!searched) {                                       // a NaN in the row, or a list that overflowed: one pass per alternative
-        unsigned long long last = ~0ull;
-        for (int k = 0; k < K; ++k) {
-            unsigned long long b = 0;
-            for (int j = v0 + tid; j < v1; j += kThreads) {
-                float x[E];
-                unpack(r[j], x);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const int id = j * E + i;
-                    if (id >= r.V) continue;
-                    const unsigned long long key = key_of(x[i], id);
-                    if (key < last && key > b) b = key;
-                }
-            }
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, d));
-            __syncthreads();
-            if ((tid & 31) == 0) l.group[tid >> 5] = b;
-            __syncthreads();
-            last = 0;
-            for (int i = 0; i < kWarpsPerBlock; ++i) last = max(last, l.group[i]);
-            if (tid == 0) l.chosen[k] = last;
-        }
-    }
-    __syncthreads();
-}
+// the score that a key was made of; 0 (the key of nothing) gives NaN, which nothing is below
 __device__ __forceinline__ float score_of(unsigned long long key)
 {
     const uint32_t b = (uint32_t)(key >> 32);
@@ -417,76 +342,242 @@ __device__ __forceinline__ float score_of(unsigned long long key)
 }
 __device__ __forceinline__ void store_remote(uint32_t at, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads) token_logprob_kernel(const Args p, int S)
+// ---- forward: a cluster of S blocks of NT threads per row --------------------------------------------------------------------
+// Each block sums a contiguous part of the row's vectors; the blocks' sums meet in block 0's shared memory.
+// Alternatives: a thread remembers the vector of its largest element.  With the threads in G groups, the K-th largest of the
+// groups' largest is a bound that the part's K-th largest element is not below.  Each thread also keeps the largest of every
+// eighth of its vectors; only the eighths that reach the bound (K and a few) can hold elements that do: they are looked through
+// again, shared out over the block (they come from L2), and what reaches the bound is listed; the position of a listed element is
+// the number of larger ones.
+constexpr int kList = 512;             // listed elements; expected -G ln(1 - K / G): 31 for K = 20, G = 32, 89 for K = 64, G = 128
+
+template <int NT>
+struct Lists {
+    unsigned long long largest[NT];    // per thread: a key not above its largest element's
+    unsigned long long list[kList];
+    unsigned long long chosen[RELAY_MAX_TOP];
+    unsigned long long merged[8 * RELAY_MAX_TOP];          // block 0: the chosen of all blocks
+    unsigned long long bound;
+    float eighth[8][NT];
+    short reached[8 * NT];             // thread * 8 + eighth
+    int count, eighths;
+};
+
+// the K largest of n <= kList different keys in `from`, largest first; calls put(position, key)
+template <int NT, typename Put>
+__device__ __forceinline__ void rank_keys(const unsigned long long *from, int n, int K, Put put)
 {
-    __shared__ Sums part[kWarpsPerBlock], blocks[8];
-    __shared__ Lists l;
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const unsigned long long mine = from[i];
+        int larger = 0;
+#pragma unroll 4
+        for (int o = 0; o < n; ++o) larger += from[o] > mine;
+        if (larger < K && mine != 0) put(larger, mine);
+    }
+}
+// Lists what can be among the K largest of vectors [v0, v1) of a row; l.largest is set, and a barrier has passed.  False: more
+// than fit the list.  `meanwhile` is run by the last warp while the others find the bound.
+template <int NT, typename T, bool EVEN, typename Meanwhile>
+__device__ __forceinline__ bool list_largest(Lists<NT> &l, const RowVectors<T, EVEN> &r, int v0, int v1, int K, unsigned long long mine, int per, int used, Meanwhile meanwhile)
+{
+    constexpr int E = Vec<T>::E;
+    const int tid = threadIdx.x, groups = K <= 20 ? 32 : 128;          // group: the threads of equal tid mod groups
+    if (tid == 0) l.count = l.eighths = 0;
+    bool is_bound = false;
+    if (tid < groups) {
+        unsigned long long g = l.largest[tid];
+        for (int i = groups; i < NT; i += groups) g = max(g, l.largest[tid + i]);
+        int larger = 0;
+        if (groups == 32) {
+#pragma unroll
+            for (int o = 0; o < 32; ++o) larger += __shfl_sync(0xffffffffu, g, o) > g;
+        } else {
+            for (int o = 0; o < NT; o += 4) {              // by groups, four at a time
+                if (o >= groups) break;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    unsigned long long other = l.largest[o + c];
+                    for (int i = groups; i < NT; i += groups) other = max(other, l.largest[o + c + i]);
+                    larger += other > g;
+                }
+            }
+        }
+        is_bound = larger == K - 1 && g != 0;
+        if (is_bound) l.bound = g;
+    }
+    if (tid >= NT - 32) meanwhile();
+    // groups without elements share the key 0: the bound is then 0 and everything is listed (fewer than K groups have fewer than K
+    // vectors among them)
+    const unsigned long long bound = __syncthreads_or(is_bound) ? l.bound : 0;
+    const float least = score_of(bound);
+    if (mine != 0 && mine >= bound)
+        for (int c = 0; c < used; ++c)
+            if (!(l.eighth[c][tid] < least)) l.reached[atomicAdd(&l.eighths, 1)] = (short)(tid * 8 + c);
+    __syncthreads();
+    const int items = l.eighths * per;
+    for (int it = tid; it < items; it += 4 * NT) {         // four vectors in flight
+        uint4 q[4];
+        int at[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int which = (it + u * NT) / per, i = it + u * NT - which * per;
+            at[u] = v1;
+            if (it + u * NT < items) at[u] = v0 + ((l.reached[which] & 7) * per + i) * NT + (l.reached[which] >> 3);
+            if (at[u] < v1) q[u] = r[at[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (at[u] >= v1 || largest(q[u], r.aligned) < least) continue;
+            float x[E];
+            unpack(q[u], x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const int id = at[u] * E + i;
+                const unsigned long long key = key_of(x[i], id);
+                if (key >= bound && id < r.V) {
+                    const int n = atomicAdd(&l.count, 1);
+                    if (n < kList) l.list[n] = key;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    return l.count <= kList;
+}
+// The same without a bound, one pass per alternative, into l.list in order: for a row with a NaN, or one whose list overflowed.
+template <int NT, typename T, bool EVEN>
+__device__ __forceinline__ void list_by_passes(Lists<NT> &l, const RowVectors<T, EVEN> &r, int v0, int v1, int K)
+{
+    constexpr int E = Vec<T>::E;
+    unsigned long long last = ~0ull;
+    for (int k = 0; k < K; ++k) {
+        unsigned long long b = 0;
+        for (int j = v0 + threadIdx.x; j < v1; j += NT) {
+            float x[E];
+            unpack(r[j], x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const int id = j * E + i;
+                const unsigned long long key = key_of(x[i], id);
+                if (id < r.V && key < last && key > b) b = key;
+            }
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, d));
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) l.largest[threadIdx.x >> 5] = b;
+        __syncthreads();
+        last = 0;
+        for (int i = 0; i < NT / 32; ++i) last = max(last, l.largest[i]);
+        if (threadIdx.x == 0) l.list[k] = last;
+    }
+    if (threadIdx.x == 0) l.count = K;
+    __syncthreads();
+}
+
+template <typename T, int NT, bool TOP, bool EVEN>
+__global__ void __launch_bounds__(NT, 1024 / NT) token_logprob_kernel(const Args p, int S)
+{
+    constexpr int E = Vec<T>::E, NW = NT / 32;
+    __shared__ Sums part[NW], blocks[8], total;
+    __shared__ Lists<TOP ? NT : 32> l;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = blockIdx.x % S;
     const T *z = (const T *)p.z;
     if (S > 1) tc::cluster_sync();                         // block 0 runs before anything is written to it
     pdl_wait();
     for (long long row = blockIdx.x / S; row < p.rows; row += gridDim.x / S) {
-        const RowVectors<T> r(z, p.rows, row, p.V);
+        const RowVectors<T, EVEN> r(z, p.rows, row, p.V);
         const int count = r.count(), each = (count + S - 1) / S, v0 = min(rank * each, count), v1 = min(v0 + each, count);
-        Running run;
-        int j = v0 + tid;
-        // four vectors in flight
-        for (; j + 3 * kThreads < v1; j += 4 * kThreads) {
-            uint4 q[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = r[j + i * kThreads];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) run.take(q[i], j + i * kThreads, p.k, z);
+        int token = -1;                                    // fetched now, used when the sums are there
+        float token_score = 0.0f;
+        if (tid == NT - 1 && rank == 0 && p.logp) {
+            token = token_of(p.tokens, p.tokens_i64, row, p.V);
+            if (token >= 0) token_score = load_score(z + row * p.V + token);
         }
-        for (; j < v1; j += kThreads) run.take(r[j], j, p.k, z);
-        Sums a = run.sums();
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) a = join(a, shfl_xor(a, d), p.k);
-        if (lane == 0) part[warp] = a;
-        __syncthreads();
-        a = part[0];
-#pragma unroll
-        for (int i = 1; i < kWarpsPerBlock; ++i) a = join(a, part[i], p.k);
-        if (TOP) choose(l, r, v0, v1, p.top, run.best, run.best_at, a.m != a.m);
-        if (S > 1) {
-            if (tid == 0) {
-                const uint32_t to = tc::mapa(tc::smem_u32(&blocks[rank]), 0);
-                store_remote(to, __float_as_uint(a.m)); store_remote(to + 4, __float_as_uint(a.s)); store_remote(to + 8, __float_as_uint(a.w));
+        Running run;
+        const int rounds = (v1 - v0 + NT - 1) / NT, per = max(4, (rounds + 31) / 32 * 4);      // vectors of an eighth: whole fours
+        float eighth = -INFINITY;
+        int used = 0, in = 0;
+        auto mark = [&](float most, int n) {
+            if constexpr (TOP) {
+                eighth = max_nan(eighth, most);
+                if ((in += n) == per) { l.eighth[used++][tid] = eighth; eighth = -INFINITY; in = 0; }
             }
-            if (TOP) {
+        };
+        int j = v0 + tid;
+        for (const int last = min(v1, r.safe); j + 3 * NT < last; j += 4 * NT) {             // four vectors in flight
+            uint4 q[4];
+            r.whole(j, NT, q);
+            mark(run.take(q, j, NT, p.k, z), 4);
+        }
+        for (; j < v1; j += NT) {
+            const uint4 q[1] = {r[j]};
+            mark(run.take(q, j, NT, p.k, z), 1);
+        }
+        if constexpr (TOP)
+            if (in > 0) l.eighth[used++][tid] = eighth;
+        const Sums mine = join_lanes(run.sums(), p.k);
+        if (lane == 0) part[warp] = mine;
+        // the vector's last id, not the element's: not above the largest element's key, and no second look at the vector
+        const unsigned long long key = run.best_at < 0 ? 0 : key_of(run.m, run.best_at * E + E - 1);
+        bool fits = false;
+        if constexpr (TOP) l.largest[tid] = key;
+        const bool has_nan = __syncthreads_or(run.m != run.m);
+        auto sum_up = [&] {                                // the last warp
+            const Sums a = join_lanes(lane < NW ? part[lane] : empty_sums(), p.k);
+            if (lane == 31) total = a;
+        };
+        if constexpr (TOP) {
+            if (!has_nan) fits = list_largest<NT>(l, r, v0, v1, p.top, key, per, used, sum_up);
+            if (!fits) {
+                if (has_nan && warp == NW - 1) sum_up();
+                list_by_passes<NT>(l, r, v0, v1, p.top);
+            }
+        } else {
+            if (warp == NW - 1) sum_up();
+            __syncwarp();
+        }
+        if (S > 1) {
+            if (tid == NT - 1) {
+                const uint32_t to = tc::mapa(tc::smem_u32(&blocks[rank]), 0);
+                store_remote(to, __float_as_uint(total.m)); store_remote(to + 4, __float_as_uint(total.s)); store_remote(to + 8, __float_as_uint(total.w));
+            }
+            if constexpr (TOP) {
+                for (int i = tid; i < p.top; i += NT) l.chosen[i] = 0;
+                __syncthreads();
+                rank_keys<NT>(l.list, l.count, p.top, [&](int at, unsigned long long k) { l.chosen[at] = k; });
+                __syncthreads();
                 const uint32_t to = tc::mapa(tc::smem_u32(&l.merged[rank * p.top]), 0);
-                for (int i = tid; i < p.top; i += kThreads) {
+                for (int i = tid; i < p.top; i += NT) {
                     store_remote(to + 8 * i, (uint32_t)l.chosen[i]); store_remote(to + 8 * i + 4, (uint32_t)(l.chosen[i] >> 32));
                 }
             }
             tc::cluster_sync();
             if (rank == 0) {
-                a = blocks[0];
-                for (int i = 1; i < S; ++i) a = join(a, blocks[i], p.k);
-                if (TOP) {
-                    __syncthreads();
-                    rank_keys(l.merged, S * p.top, p.top, l.chosen);
-                    __syncthreads();
+                if (warp == NW - 1) {
+                    const Sums a = join_lanes(lane < S ? blocks[lane] : empty_sums(), p.k);
+                    if (lane == 31) total = a;
                 }
+                __syncthreads();
             }
         }
         if (rank == 0) {
-            const Row sum(a, p.k);
-            if (tid == 0) {
+            if (tid == NT - 1) {
+                const Row sum(total, p.k);
                 if (p.lse) p.lse[row] = sum.lse;
                 if (p.entropy) p.entropy[row] = sum.entropy;
-                if (p.logp) {
-                    const int t = token_of(p.tokens, p.tokens_i64, row, p.V);
-                    p.logp[row] = t < 0 ? 0.0f : sum.logp(load_score(z + row * p.V + t), p.k);
-                }
+                if (p.logp) p.logp[row] = token < 0 ? 0.0f : sum.logp(token_score, p.k);
             }
-            if (TOP)
-                for (int i = tid; i < p.top; i += kThreads) {
-                    p.top_ids[row * p.top + i] = id_of(l.chosen[i]);
-                    p.top_logp[row * p.top + i] = sum.logp(score_of(l.chosen[i]), p.k);
-                }
+            if constexpr (TOP) {
+                auto put = [&](int at, unsigned long long k) {
+                    const Row sum(total, p.k);
+                    p.top_ids[row * p.top + at] = id_of(k);
+                    p.top_logp[row * p.top + at] = sum.logp(score_of(k), p.k);
+                };
+                if (S > 1) rank_keys<NT>(l.merged, S * p.top, p.top, put);
+                else rank_keys<NT>(l.list, l.count, p.top, put);
+            }
         }
         if (S > 1) tc::cluster_sync();                     // block 0 has read what the next row overwrites
         else __syncthreads();
@@ -640,20 +731,33 @@ relay_status_t check_temperature(float t)
     return RELAY_OK;
 }
 
+template <typename T, int NT>
+relay_status_t launch_blocks(const Args &p, int S, cudaStream_t st)
+{
+    const dim3 grid((unsigned)std::min<long long>(p.rows * S, 1 << 20)), block(NT), cluster((unsigned)S);
+    if (p.V % Vec<T>::E == 0) {
+        if (p.top) RELAY_CUDA(launch_pdl_cluster(token_logprob_kernel<T, NT, true, true>, grid, block, cluster, 0, st, p, S));
+        else RELAY_CUDA(launch_pdl_cluster(token_logprob_kernel<T, NT, false, true>, grid, block, cluster, 0, st, p, S));
+    } else {
+        if (p.top) RELAY_CUDA(launch_pdl_cluster(token_logprob_kernel<T, NT, true, false>, grid, block, cluster, 0, st, p, S));
+        else RELAY_CUDA(launch_pdl_cluster(token_logprob_kernel<T, NT, false, false>, grid, block, cluster, 0, st, p, S));
+    }
+    return check_launch("token_logprob");
+}
 template <typename T>
 relay_status_t launch_forward(const Args &p, cudaStream_t st)
 {
     int dev = 0, sms = 148;
     RELAY_CUDA(cudaGetDevice(&dev));
     RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    // few rows: several blocks each, as long as a block keeps a vector per thread
-    const long long vectors = (p.V + Vec<T>::E - 1) / Vec<T>::E;
+    // Rows enough for every SM: small blocks, eight to an SM, each with a row (at 8192 x 4000 a block spends most of its time on
+    // what follows the sums, and what counts is how many are at it).  Fewer rows: large blocks, and several per row as long as a
+    // thread keeps four vectors.
+    const long long vectors = ((long long)p.V + Vec<T>::E - 1) / Vec<T>::E;
+    if (p.rows >= 2 * sms) return launch_blocks<T, 128>(p, 1, st);
     int S = 1;
-    while (S < 8 && p.rows * S < sms && vectors > (long long)S * 2 * kThreads) S *= 2;
-    const dim3 grid((unsigned)std::min<long long>(p.rows * S, 1 << 20)), block(kThreads), cluster((unsigned)S);
-    if (p.top) RELAY_CUDA(launch_pdl_cluster(token_logprob_kernel<T, true>, grid, block, cluster, 0, st, p, S));
-    else RELAY_CUDA(launch_pdl_cluster(token_logprob_kernel<T, false>, grid, block, cluster, 0, st, p, S));
-    return check_launch("token_logprob");
+    while (S < 8 && p.rows * S < sms && vectors > (long long)S * 512) S *= 2;
+    return launch_blocks<T, 512>(p, S, st);
 }
 template <typename T>
 relay_status_t launch_gradient(const GradArgs &p, cudaStream_t st)
