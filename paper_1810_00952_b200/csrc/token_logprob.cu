@@ -287,21 +287,27 @@ struct RowVectors {
         safe = (int)min((long long)(V / E), max(inside, 0ll));
     }
     __device__ __forceinline__ int count() const { return (int)(((long long)V + Vec<T>::E - 1) / Vec<T>::E); }
-    // N vectors j, j + stride, .. below `safe`: all loads before the first use
+    // N vectors j, j + stride, .. as far as they lie below `last`, which is at most `safe`; -inf from there on.  All loads come before
+    // the first use.
     template <int N>
-    __device__ __forceinline__ void whole(int j, int stride, uint4 (&q)[N]) const
+    __device__ __forceinline__ void whole(int j, int stride, int last, uint4 (&q)[N]) const
     {
-        const uint4 *at = (const uint4 *)aligned + j;
+        const uint4 *at = (const uint4 *)aligned;
+        constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
         if (EVEN) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) q[n] = ld_stream(at + n * stride);
+            for (int n = 0; n < N; ++n) {
+                q[n] = make_uint4(none, none, none, none);
+                if (j + n * stride < last) q[n] = ld_stream(at + j + n * stride);
+            }
             return;
         }
         uint4 hi[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            q[n] = hi[n] = uint4{};
-            if (relay_in_bounds(at + n * stride, skew ? 32 : 16)) { q[n] = __ldg(at + n * stride); hi[n] = __ldg(at + n * stride + (skew != 0)); }
+            q[n] = hi[n] = make_uint4(none, none, none, none);
+            const uint4 *a = at + j + n * stride;
+            if (j + n * stride < last && relay_in_bounds(a, skew ? 32 : 16)) { q[n] = __ldg(a); hi[n] = __ldg(a + (skew != 0)); }
         }
         const int bytes = skew * (int)sizeof(T);
 #pragma unroll
@@ -323,7 +329,7 @@ struct RowVectors {
         constexpr int E = Vec<T>::E;
         uint4 q[1];
         if (EVEN || j < safe) {
-            whole(j, 0, q);
+            whole(j, 0, j + 1, q);
             return q[0];
         }
         float x[E];
@@ -505,13 +511,14 @@ __global__ void __launch_bounds__(NT, 1024 / NT) token_logprob_kernel(const Args
                 if ((in += n) == per) { l.eighth[used++][tid] = eighth; eighth = -INFINITY; in = 0; }
             }
         };
+        const int last = min(v1, r.safe);
         int j = v0 + tid;
-        for (const int last = min(v1, r.safe); j + 3 * NT < last; j += 4 * NT) {             // four vectors in flight
+        for (; j < last; j += 4 * NT) {                    // four vectors in flight
             uint4 q[4];
-            r.whole(j, NT, q);
-            mark(run.take(q, j, NT, p.k, z), 4);
+            r.whole(j, NT, last, q);
+            mark(run.take(q, j, NT, p.k, z), min(4, (last - j + NT - 1) / NT));
         }
-        for (; j < v1; j += NT) {
+        for (j = v0 + tid + (max(last - v0 - tid, 0) + NT - 1) / NT * NT; j < v1; j += NT) {       // one or two that are not whole
             const uint4 q[1] = {r[j]};
             mark(run.take(q, j, NT, p.k, z), 1);
         }
