@@ -28,6 +28,19 @@ struct Product {
     int *err;
 };
 
+// How the two-SM kernel cuts a product into units, made once for the products of equal shape.  n = 0: 256 x 256 units in order.
+struct UnitTable {
+    static constexpr int kMax = 640;
+    int n;
+    uint32_t e[kMax];                  // row block (256 rows) | first 128-column chunk << 8 | chunks << 17 | matrix << 20
+};
+void plan_units(const Product &p, int sms, UnitTable *table);
+
+// two-SM kernel (orthogonalize_pair.cu); boxes of its operands: 128 rows of A, 64 of B where the contraction index is contiguous,
+// else 64 x 64
+relay_status_t launch_product_pair(const Product &p, bool a_mn, bool b_mn, const CUtensorMap &a, const CUtensorMap &b, const UnitTable &units, int sms,
+                                   cudaStream_t st);
+
 }  // namespace orth
 
 // 3-D tensor map of `batch` fp16 matrices: `inner` contiguous elements per row, 128-byte swizzle, zero outside
