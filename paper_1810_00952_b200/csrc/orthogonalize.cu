@@ -38,7 +38,7 @@ constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + 256;
 
 // ---- norm and the 16-bit copy ----------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
-constexpr int kNormBlocks = 64;                        // partial sums per matrix
+constexpr int kNormMost = 256;                         // partial sums per matrix, at most
 
 template <typename T>
 __device__ __forceinline__ float element(const T *p)
@@ -47,18 +47,46 @@ __device__ __forceinline__ float element(const T *p)
     if constexpr (sizeof(T) == 2) return __bfloat162float(*p);
     else return *p;
 }
-
-// sums of squares in fp64: a square of any finite element fits, and the sum does not depend on the element's scale
+// eight consecutive elements; whole: they are 16-byte aligned
 template <typename T>
-__global__ void __launch_bounds__(kNormThreads) orth_norm_kernel(const T *__restrict__ x, long long size, double *__restrict__ partial)
+__device__ __forceinline__ void eight(const T *p, bool whole, int n, float (&x)[8])
+{
+    if (whole) {
+        if constexpr (sizeof(T) == 2) {
+            unpack(ld_stream(p), x);
+        } else {
+            float lo[4], hi[4];
+            unpack(ld_stream(p), lo);
+            unpack(ld_stream(p + 4), hi);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { x[i] = lo[i]; x[4 + i] = hi[i]; }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < n ? element(p + i) : 0.0f;
+    }
+}
+
+// The sum of squares in fp64: a square of any finite element fits, and the sum does not depend on the elements' scale.
+template <typename T>
+__global__ void __launch_bounds__(kNormThreads) orth_norm_kernel(const T *__restrict__ x, long long size, int even, double *__restrict__ partial)
 {
     __shared__ double warp_sum[kNormThreads / 32];
     pdl_wait();
     x += (long long)blockIdx.y * size;
     double s = 0.0;
-    for (long long i = (long long)blockIdx.x * kNormThreads + threadIdx.x; i < size; i += (long long)kNormBlocks * kNormThreads) {
-        const double v = element(x + i);
-        s = fma(v, v, s);
+    const long long groups = (size + 7) / 8, stride = (long long)gridDim.x * kNormThreads;
+    for (long long i = (long long)blockIdx.x * kNormThreads + threadIdx.x; i < groups; i += 4 * stride) {
+        float v[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const long long at = (i + u * stride) * 8, n = size - at;
+            eight(x + at, even && n >= 8, n < 0 ? 0 : n < 8 ? (int)n : 8, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) { const double d = v[u][c]; s = fma(d, d, s); }
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
@@ -66,21 +94,43 @@ __global__ void __launch_bounds__(kNormThreads) orth_norm_kernel(const T *__rest
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < kNormThreads / 32; ++i) s += warp_sum[i];
-        partial[blockIdx.y * kNormBlocks + blockIdx.x] = s;
+        partial[(long long)blockIdx.y * gridDim.x + blockIdx.x] = s;
     }
 }
 
+// out = fp16(x s / (|x| + eps)), rows padded to ld; a thread takes eight columns of a row at a time
 template <typename T>
-__global__ void __launch_bounds__(kNormThreads) orth_convert_kernel(const T *__restrict__ x, long long rows, long long cols, const double *__restrict__ partial,
+__global__ void __launch_bounds__(kNormThreads) orth_convert_kernel(const T *__restrict__ x, int rows, int cols, int even, const double *__restrict__ partial, int partials,
                                                                    float eps, float s, __half *__restrict__ out, long long ld)
 {
+    __shared__ double warp_sum[kNormThreads / 32];
     pdl_wait();
-    double sum = 0.0;
-    for (int i = 0; i < kNormBlocks; ++i) sum += partial[blockIdx.z * kNormBlocks + i];
+    const long long b = blockIdx.y;
+    double sum = threadIdx.x < partials ? partial[b * partials + threadIdx.x] : 0.0;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int i = 0; i < kNormThreads / 32; ++i) sum += warp_sum[i];
+    // in two factors, each of them within fp32's range where the whole may not be
     const double f = (double)s / (sqrt(sum) + (double)eps);
-    const long long c = (long long)blockIdx.x * kNormThreads + threadIdx.x;
-    for (long long r = blockIdx.y; r < rows; r += gridDim.y)
-        if (c < cols) out[((long long)blockIdx.z * rows + r) * ld + c] = __double2half(f * (double)element(x + ((long long)blockIdx.z * rows + r) * cols + c));
+    int e;
+    const float lo = (float)frexp(f, &e);
+    const float f1 = ldexpf(lo, e / 2), f2 = ldexpf(1.0f, e - e / 2);
+    const int per_row = (cols + 7) / 8;
+    const long long items = (long long)rows * per_row;
+    x += b * rows * cols;
+    out += b * rows * ld;
+    for (long long i = (long long)blockIdx.x * kNormThreads + threadIdx.x; i < items; i += (long long)gridDim.x * kNormThreads) {
+        const long long r = i / per_row;
+        const int c = (int)(i - r * per_row) * 8;
+        float v[8];
+        eight(x + r * cols + c, even, min(8, cols - c), v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = v[k] * f1 * f2;
+        *reinterpret_cast<uint4 *>(out + r * ld + c) = make_uint4(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]), pack_half2(v[4], v[5]), pack_half2(v[6], v[7]));
+    }
 }
 
 // ---- products ----------------------------------------------------------------------------------------------
@@ -384,7 +434,7 @@ Plan plan_of(const relay_tensor_t *x)
     p.x_bytes = align_up((size_t)(p.L * p.M * p.xld) * 2, 256);
     p.g_bytes = align_up((size_t)(p.L * p.m * p.gld) * 2, 256);
     p.v_bytes = align_up((size_t)(p.L * p.gld) * 4, 256);
-    p.total = align_up((size_t)p.L * kNormBlocks * sizeof(double), 256) + 2 * p.x_bytes + 2 * p.g_bytes + 2 * p.v_bytes;
+    p.total = align_up((size_t)p.L * kNormMost * sizeof(double), 256) + 2 * p.x_bytes + 2 * p.g_bytes + 2 * p.v_bytes;
     p.small = small_fits(p.m, p.n);
     if (p.small) p.total = 0;
     return p;
@@ -402,13 +452,16 @@ relay_status_t check_matrices(const relay_tensor_t *x)
 }
 
 template <typename T>
-relay_status_t prepare_x(const relay_tensor_t *x, const Plan &pl, double *partial, float eps, float s, __half *out, cudaStream_t st)
+relay_status_t prepare_x(const relay_tensor_t *x, const Plan &pl, double *partial, float eps, float s, int sms, __half *out, cudaStream_t st)
 {
-    RELAY_CUDA(launch_pdl(orth_norm_kernel<T>, dim3(kNormBlocks, (unsigned)pl.L), dim3(kNormThreads), 0, st, (const T *)x->data, (long long)(pl.M * pl.N), partial));
+    const long long size = pl.M * pl.N, each = kNormThreads * 8;
+    const int share = (int)std::max<int64_t>(1, 4 * sms / pl.L);             // blocks per matrix that fill the GPU
+    const int partials = (int)std::min<long long>({(size + each - 1) / each, share, kNormMost});
+    RELAY_CUDA(launch_pdl(orth_norm_kernel<T>, dim3((unsigned)partials, (unsigned)pl.L), dim3(kNormThreads), 0, st, (const T *)x->data, size, (int)(size % 8 == 0), partial));
     RELAY_TRY(check_launch("orthogonalize_norm"));
-    const dim3 grid((unsigned)((pl.N + kNormThreads - 1) / kNormThreads), (unsigned)std::min<int64_t>(pl.M, 4096), (unsigned)pl.L);
-    RELAY_CUDA(launch_pdl(orth_convert_kernel<T>, grid, dim3(kNormThreads), 0, st, (const T *)x->data, (long long)pl.M, (long long)pl.N, (const double *)partial, eps, s,
-                          out, (long long)pl.xld));
+    const dim3 grid((unsigned)std::min<long long>((pl.M * ((pl.N + 7) / 8) + kNormThreads - 1) / kNormThreads, 2 * share), (unsigned)pl.L);
+    RELAY_CUDA(launch_pdl(orth_convert_kernel<T>, grid, dim3(kNormThreads), 0, st, (const T *)x->data, (int)pl.M, (int)pl.N, (int)(pl.N % 8 == 0),
+                          (const double *)partial, partials, eps, s, out, (long long)pl.xld));
     return check_launch("orthogonalize_convert");
 }
 
@@ -464,7 +517,7 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
 
     char *w = (char *)ws;
     double *partial = (double *)w;
-    w += align_up((size_t)pl.L * kNormBlocks * sizeof(double), 256);
+    w += align_up((size_t)pl.L * kNormMost * sizeof(double), 256);
     __half *xa = (__half *)w, *xb = (__half *)(w + pl.x_bytes);
     __half *g = (__half *)(w + 2 * pl.x_bytes), *q = (__half *)(w + 2 * pl.x_bytes + pl.g_bytes);
     float *d = (float *)(w + 2 * pl.x_bytes + 2 * pl.g_bytes), *e = (float *)(w + 2 * pl.x_bytes + 2 * pl.g_bytes + pl.v_bytes);
@@ -473,8 +526,8 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
     BoundsReg reg;
     reg.add(x); reg.add(y); reg.add(ws, ws_bytes);
     RELAY_TRY(reg.commit(st));
-    if (x->dtype == RELAY_F32) RELAY_TRY(prepare_x<float>(x, pl, partial, at->eps, s, xa, st));
-    else RELAY_TRY(prepare_x<__nv_bfloat16>(x, pl, partial, at->eps, s, xa, st));
+    if (x->dtype == RELAY_F32) RELAY_TRY(prepare_x<float>(x, pl, partial, at->eps, s, sms, xa, st));
+    else RELAY_TRY(prepare_x<__nv_bfloat16>(x, pl, partial, at->eps, s, sms, xa, st));
 
     const bool tall = pl.M > pl.N;
     // boxes: 128 rows x 64 contiguous contraction elements, or 64 contraction rows x 64 contiguous rows/columns

@@ -46,5 +46,8 @@ relay_status_t launch_product_pair(const Product &p, bool a_mn, bool b_mn, const
 // 3-D tensor map of `batch` fp16 matrices: `inner` contiguous elements per row, 128-byte swizzle, zero outside
 relay_status_t make_tmap_3d_f16(CUtensorMap *m, const void *base, uint64_t inner, uint64_t outer, uint64_t batch, uint64_t row_stride,
                                 uint64_t batch_stride, uint32_t box_inner, uint32_t box_outer);
+// 3-D tensor map for stores of 32 x 32 blocks of 16-bit elements, 64-byte swizzle or none
+relay_status_t make_tmap_3d_block(CUtensorMap *m, bool bf16, const void *base, uint64_t inner, uint64_t outer, uint64_t batch, uint64_t row_stride,
+                                  uint64_t batch_stride, bool swizzle64);
 
 }  // namespace relay

@@ -24,7 +24,8 @@ constexpr int CHUNK_BYTES = 64 * BK * 2;                   // this block's 64 co
 constexpr int MN_BOX_BYTES = 64 * BK * 2;
 constexpr int RING_BYTES = 192 * 1024;
 constexpr int NUM_THREADS = 608, EPI_WARPS = 16, TMEM_COLS = 512;
-constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + 512;
+constexpr int STAGING_BYTES = EPI_WARPS * 2048;            // one 32 x 32 block of 16-bit results per epilogue warp
+constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + STAGING_BYTES + 512;
 
 __host__ __device__ constexpr int cls_stages(int c) { return c == 1 ? 8 : c == 2 ? 6 : 4; }
 __host__ __device__ constexpr int cls_stage_bytes(int c) { return A_BYTES + c * CHUNK_BYTES; }
@@ -64,14 +65,105 @@ __device__ __forceinline__ void tma_load_3d_pair(void *dst, const CUtensorMap *m
                  : "memory");
 }
 
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *m, const void *src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(src)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// this row's 32 columns of the addend (rows of the workspace are padded to whole 16-byte pieces)
+__device__ __forceinline__ void load_addend(const Product &p, int batch, int row, int c0, uint4 (&r)[4])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) r[q] = uint4{};
+    if (p.add == nullptr || row >= p.rows) return;
+    const uint4 *add = reinterpret_cast<const uint4 *>((const __half *)p.add + batch * p.add_bs + (long long)row * p.add_ld + c0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (c0 + 8 * q < p.cols) r[q] = __ldg(add + q);
+}
+// The epilogue of 32 rows x 32 columns by one warp: out = alpha acc + beta add, rounded once, staged in shared memory (64-byte
+// swizzle: 16-byte piece c of row r at piece c ^ ((r >> 1) & 3)) and stored by TMA, which leaves out what lies outside the matrix; the
+// mirrored copy is staged transposed.  of_row: this row's part of beta.
+__device__ __forceinline__ void finish_block(const Product &p, const CUtensorMap *tm_out, const CUtensorMap *tm_mirror, uint8_t *stage, const Tile &t, int lane,
+                                             int row, int c0, float of_row, float d_row, const uint4 (&add)[4], const uint32_t (&acc)[32])
+{
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = p.alpha * __uint_as_float(acc[j]);
+    if (p.add != nullptr) {
+        const float *col_v = p.col_v != nullptr ? p.col_v + t.batch * p.v_bs + c0 : nullptr;   // padded like the rows
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t w[4] = {add[q].x, add[q].y, add[q].z, add[q].w};
+            float beta[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) beta[i] = of_row;
+            if (col_v != nullptr && c0 + 8 * q < p.cols) {
+                const float4 lo = __ldg(reinterpret_cast<const float4 *>(col_v + 8 * q)), hi = __ldg(reinterpret_cast<const float4 *>(col_v + 8 * q + 4));
+                const float of_col[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) beta[i] = fmaf(p.gamma, of_col[i], beta[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+                v[8 * q + 2 * i] = fmaf(beta[2 * i], f.x, v[8 * q + 2 * i]);
+                v[8 * q + 2 * i + 1] = fmaf(beta[2 * i + 1], f.y, v[8 * q + 2 * i + 1]);
+            }
+        }
+    }
+    if (p.diag != nullptr && !t.mirror && row >= c0 && row < c0 + 32 && row < p.rows) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (row == c0 + j) {                           // `add` has a zero here: v is alpha times the sum
+                p.diag[t.batch * p.v_bs + row] = v[j] + p.q0 + d_row * (p.q1 + p.q2 * d_row);
+                v[j] = 0.0f;
+            }
+    }
+    uint32_t h[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) h[j] = p.out_bf16 ? pack2(v[2 * j], v[2 * j + 1]) : pack_half2(v[2 * j], v[2 * j + 1]);
+    if (tc::elect_one()) tc::tma_store_wait_read<0>();     // the previous store (same elected lane) has read the buffer
+    __syncwarp();
+    const int sw = (lane >> 1) & 3;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4 *>(stage + lane * 64 + ((q ^ sw) << 4)) = make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+    tc::fence_proxy_async();
+    __syncwarp();
+    if (tc::elect_one()) {                                 // the election is deterministic: always the same lane of the warp
+        tma_store_3d(tm_out, stage, c0, row - lane, t.batch);
+        tc::tma_store_commit();
+    }
+    if (!t.mirror) return;
+    // lanes hold consecutive rows of the same columns: a pair of lanes exchanges halves, the even one writes rows (r, r + 1) of
+    // column c, the odd one rows (r - 1, r) of column c + 1: 128 contiguous bytes per store
+    if (tc::elect_one()) tc::tma_store_wait_read<0>();
+    __syncwarp();
+    const bool odd = lane & 1;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, h[j], 1);
+        const uint32_t w = odd ? __byte_perm(other, h[j], 0x7632) : __byte_perm(h[j], other, 0x5410);
+        *reinterpret_cast<uint32_t *>(stage + (2 * j + (odd ? 1 : 0)) * 64 + (lane & ~1) * 2) = w;
+    }
+    tc::fence_proxy_async();
+    __syncwarp();
+    if (tc::elect_one()) {
+        tma_store_3d(tm_mirror, stage, row - lane, c0, t.batch);
+        tc::tma_store_commit();
+    }
+}
+
 template <bool A_MN, bool B_MN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
-orth_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const Product p,
-                 const __grid_constant__ UnitTable tb)
+orth_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_out,
+                 const __grid_constant__ CUtensorMap tm_mirror, const Product p, const __grid_constant__ UnitTable tb)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + RING_BYTES);
+    uint8_t *staging = smem + RING_BYTES;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + STAGING_BYTES);
     uint64_t *tmem_full = bars + BAR_TMEM, *tmem_empty = bars + BAR_TMEM + 2;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + BAR_TMEM + 4);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
@@ -211,36 +303,53 @@ orth_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     } else {
         const int quarter = warp & 3;                      // TMEM lanes [32 quarter, 32 quarter + 32)
         const int slot = (warp - 2) >> 2;                  // which quarter of an accumulator's 32-column groups this warp drains
+        uint8_t *my_stage = staging + (size_t)(warp - 2) * 2048;
+        const bool by_tma = !p.out_bf16 || p.out_ld % 8 == 0;
         uint32_t t_local = 0;
         bool ok_all = true;
         for (long long u = pair; u < n_units && ok_all; u += n_pairs) {
             const Unit w = unit_of(p, tb, u);
             const int items = w.width > BN ? 2 : 1;        // accumulators of this unit
+            const int row = w.m0 + (int)rank * 128 + quarter * 32 + lane;
+            const float d_row = p.row_v != nullptr && row < p.rows ? p.row_v[w.batch * p.v_bs + row] : 0.0f;
+            const float of_row = fmaf(p.gamma, d_row, p.beta);
             for (int item = 0; item < items; ++item, ++t_local) {
                 const int buf = t_local & 1;
                 const int n0 = w.n0 + item * BN, width = item == 0 ? min(w.width, BN) : w.width - BN;
+                const int per = width / 128;               // 32-column groups per warp: 2 for a 256-column accumulator, 1 for 128
+                uint4 add[4];                              // requested a group ahead: before the wait, and before the group at hand is finished
+                load_addend(p, w.batch, row, n0 + slot * per * 32, add);
                 int ok = 1;
                 if (lane == 0) ok = tc::mbar_wait(&tmem_full[buf], (t_local >> 1) & 1, abort_flag, p.err, tc::ERR_WAIT_TMEM_FULL) ? 1 : 0;
                 ok = __shfl_sync(0xffffffffu, ok, 0);
                 if (!ok) { ok_all = false; break; }
                 tc::tc_fence_after_sync();
-                const int row = w.m0 + (int)rank * 128 + quarter * 32 + lane;
                 const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * BN;
-                const int per = width / 128;               // 32-column groups per warp: 2 for a 256-column accumulator, 1 for 128
 #pragma unroll 1
                 for (int g = slot * per; g < slot * per + per; ++g) {
                     uint32_t acc[32];
                     tc::tmem_ld_32x32(taddr + g * 32, acc);
+                    uint4 next[4];
+                    if (g + 1 < slot * per + per) load_addend(p, w.batch, row, n0 + (g + 1) * 32, next);
                     tc::tmem_ld_wait();
                     const int c0 = n0 + g * 32;
                     // right of the diagonal's 256 x 256 block the mirrored place is not computed by anyone
-                    finish_columns(p, Tile{w.batch, w.m0, c0, p.symmetric && c0 >= w.m0 + 256}, lane, row, c0, acc);
+                    const Tile t{w.batch, w.m0, c0, p.symmetric && c0 >= w.m0 + 256};
+                    if (by_tma) {
+                        if (row - lane < p.rows && c0 < p.cols) finish_block(p, &tm_out, &tm_mirror, my_stage, t, lane, row, c0, of_row, d_row, add, acc);
+                    } else {
+                        finish_columns(p, t, lane, row, c0, acc);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) add[q] = next[q];
                 }
                 tc::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive_cluster(tc::mapa(tc::smem_u32(&tmem_empty[buf]), 0));
             }
         }
+        __syncwarp();
+        if (tc::elect_one()) tc::tma_store_wait_all<0>();
     }
 
     tc::tc_fence_before_sync();
@@ -326,10 +435,16 @@ relay_status_t launch_product_pair(const Product &q, bool a_mn, bool b_mn, const
     const Product p = in_tiles(q);
     const long long n = table.n > 0 ? table.n : (long long)p.units * p.batch;
     const dim3 grid((unsigned)(2 * std::min<long long>(n, sms / 2)));
+    CUtensorMap out, mirror;
+    out = mirror = ta;                                     // not used where rows of the result are not whole 16-byte pieces
+    if (p.out_ld % 8 == 0) {
+        RELAY_TRY(make_tmap_3d_block(&out, p.out_bf16 != 0, p.out, p.cols, p.rows, p.batch, p.out_ld, p.out_bs, true));
+        if (p.symmetric) RELAY_TRY(make_tmap_3d_block(&mirror, p.out_bf16 != 0, p.out, p.cols, p.rows, p.batch, p.out_ld, p.out_bs, false));
+    }
 #define LAUNCH(AMN, BMN)                                                                                                          \
     do {                                                                                                                          \
         RELAY_CUDA(cudaFuncSetAttribute(orth_pair_kernel<AMN, BMN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES)); \
-        RELAY_CUDA(launch_pdl(orth_pair_kernel<AMN, BMN>, grid, dim3(NUM_THREADS), SMEM_BYTES, st, ta, tb, p, table));             \
+        RELAY_CUDA(launch_pdl(orth_pair_kernel<AMN, BMN>, grid, dim3(NUM_THREADS), SMEM_BYTES, st, ta, tb, out, mirror, p, table));             \
     } while (0)
     if (a_mn && b_mn) LAUNCH(true, true);
     else if (b_mn) LAUNCH(false, true);
