@@ -22,15 +22,15 @@ constexpr int BK = 64, BN = 256;                           // BN: columns of one
 constexpr int A_BYTES = 128 * BK * 2;                      // this block's 128 rows of A: 16 KB
 constexpr int CHUNK_BYTES = 64 * BK * 2;                   // this block's 64 columns of one 128-column chunk: 8 KB
 constexpr int MN_BOX_BYTES = 64 * BK * 2;
-constexpr int RING_BYTES = 192 * 1024;
+constexpr int RING_BYTES = 144 * 1024;
 constexpr int NUM_THREADS = 608, EPI_WARPS = 16, TMEM_COLS = 512;
-constexpr int STAGING_BYTES = EPI_WARPS * 2048;            // one 32 x 32 block of 16-bit results per epilogue warp
+constexpr int STAGING_BYTES = EPI_WARPS * 4096;            // two 32 x 32 blocks of 16-bit results per epilogue warp
 constexpr size_t SMEM_BYTES = 1024 + (size_t)RING_BYTES + STAGING_BYTES + 512;
 
-__host__ __device__ constexpr int cls_stages(int c) { return c == 1 ? 8 : c == 2 ? 6 : 4; }
+__host__ __device__ constexpr int cls_stages(int c) { return c == 1 ? 6 : c == 2 ? 4 : 3; }
 __host__ __device__ constexpr int cls_stage_bytes(int c) { return A_BYTES + c * CHUNK_BYTES; }
-__host__ __device__ constexpr int cls_bar_base(int c) { return c == 1 ? 0 : c == 2 ? 16 : c == 3 ? 28 : 36; }   // full[], then empty[]
-constexpr int BAR_TMEM = 44;                               // tmem_full[2], tmem_empty[2]
+__host__ __device__ constexpr int cls_bar_base(int c) { return c == 1 ? 0 : c == 2 ? 12 : c == 3 ? 20 : 26; }   // full[], then empty[]
+constexpr int BAR_TMEM = 32;                               // tmem_full[2], tmem_empty[2]
 
 struct Unit { int batch, m0, n0, width; };
 __device__ __forceinline__ Unit unit_of(const Product &p, const UnitTable &tb, long long u)
@@ -84,7 +84,7 @@ __device__ __forceinline__ void load_addend(const Product &p, int batch, int row
 // The epilogue of 32 rows x 32 columns by one warp: out = alpha acc + beta add, rounded once, staged in shared memory (64-byte
 // swizzle: 16-byte piece c of row r at piece c ^ ((r >> 1) & 3)) and stored by TMA, which leaves out what lies outside the matrix; the
 // mirrored copy is staged transposed.  of_row: this row's part of beta.
-__device__ __forceinline__ void finish_block(const Product &p, const CUtensorMap *tm_out, const CUtensorMap *tm_mirror, uint8_t *stage, const Tile &t, int lane,
+__device__ __forceinline__ void finish_block(const Product &p, const CUtensorMap *tm_out, const CUtensorMap *tm_mirror, uint8_t *stages, int &turn, const Tile &t, int lane,
                                              int row, int c0, float of_row, float d_row, const uint4 (&add)[4], const uint32_t (&acc)[32])
 {
     float v[32];
@@ -123,8 +123,10 @@ __device__ __forceinline__ void finish_block(const Product &p, const CUtensorMap
     uint32_t h[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) h[j] = p.out_bf16 ? pack2(v[2 * j], v[2 * j + 1]) : pack_half2(v[2 * j], v[2 * j + 1]);
-    if (tc::elect_one()) tc::tma_store_wait_read<0>();     // the previous store (same elected lane) has read the buffer
+    // two buffers in turn: the store before the last (same elected lane) has read this one
+    if (tc::elect_one()) tc::tma_store_wait_read<1>();
     __syncwarp();
+    uint8_t *stage = stages + (turn++ & 1) * 2048;
     const int sw = (lane >> 1) & 3;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -138,8 +140,9 @@ __device__ __forceinline__ void finish_block(const Product &p, const CUtensorMap
     if (!t.mirror) return;
     // lanes hold consecutive rows of the same columns: a pair of lanes exchanges halves, the even one writes rows (r, r + 1) of
     // column c, the odd one rows (r - 1, r) of column c + 1: 128 contiguous bytes per store
-    if (tc::elect_one()) tc::tma_store_wait_read<0>();
+    if (tc::elect_one()) tc::tma_store_wait_read<1>();
     __syncwarp();
+    stage = stages + (turn++ & 1) * 2048;
     const bool odd = lane & 1;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -303,7 +306,8 @@ orth_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     } else {
         const int quarter = warp & 3;                      // TMEM lanes [32 quarter, 32 quarter + 32)
         const int slot = (warp - 2) >> 2;                  // which quarter of an accumulator's 32-column groups this warp drains
-        uint8_t *my_stage = staging + (size_t)(warp - 2) * 2048;
+        uint8_t *my_stage = staging + (size_t)(warp - 2) * 4096;
+        int turn = 0;
         const bool by_tma = !p.out_bf16 || p.out_ld % 8 == 0;
         uint32_t t_local = 0;
         bool ok_all = true;
@@ -336,7 +340,7 @@ orth_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     // right of the diagonal's 256 x 256 block the mirrored place is not computed by anyone
                     const Tile t{w.batch, w.m0, c0, p.symmetric && c0 >= w.m0 + 256};
                     if (by_tma) {
-                        if (row - lane < p.rows && c0 < p.cols) finish_block(p, &tm_out, &tm_mirror, my_stage, t, lane, row, c0, of_row, d_row, add, acc);
+                        if (row - lane < p.rows && c0 < p.cols) finish_block(p, &tm_out, &tm_mirror, my_stage, turn, t, lane, row, c0, of_row, d_row, add, acc);
                     } else {
                         finish_columns(p, t, lane, row, c0, acc);
                     }
