@@ -270,22 +270,6 @@ relay_status_t make_tmap_3d_f16(CUtensorMap *m, const void *base, uint64_t inner
     return RELAY_OK;
 }
 
-relay_status_t make_tmap_3d_block(CUtensorMap *m, bool bf16, const void *base, uint64_t inner, uint64_t outer, uint64_t batch, uint64_t row_stride,
-                                  uint64_t batch_stride, bool swizzle64)
-{
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return fail(RELAY_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-    cuuint64_t dims[3] = {inner, outer, batch};
-    cuuint64_t strides[2] = {row_stride * 2, batch_stride * 2};
-    cuuint32_t box[3] = {32, 32, 1};
-    cuuint32_t estr[3] = {1, 1, 1};
-    CUresult r = fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return fail(RELAY_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
-    return RELAY_OK;
-}
-
 bool gemm_tc_eligible(const GemmDesc &g)
 {
     if (g.in_dtype != RELAY_BF16) return false;

@@ -21,20 +21,13 @@
 
 #include "common.h"
 #include "ewise_kernels.cuh"
-#include "orthogonalize.cuh"
+#include "orthogonalize.h"
 
 namespace relay {
 
 namespace {
 
 using namespace orth;
-
-constexpr int BM = 128, BN = 128, BK = 64, STAGES = 6;
-constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
-constexpr int MN_BOX_BYTES = 64 * BK * 2;              // one TMA box of an operand whose row index is contiguous
-constexpr int NUM_THREADS = 192;                       // warp 0 TMA producer, warp 1 MMA issuer, warps 2-5 epilogue
-constexpr int TMEM_COLS = 256;                         // two accumulators
-constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + 256;
 
 // ---- norm and the 16-bit copy ----------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
@@ -46,6 +39,11 @@ __device__ __forceinline__ float element(const T *p)
     if (!relay_in_bounds(p, sizeof(T))) return 0.0f;
     if constexpr (sizeof(T) == 2) return __bfloat162float(*p);
     else return *p;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
+{
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&v);
 }
 // eight consecutive elements; whole: they are 16-byte aligned
 template <typename T>
@@ -98,14 +96,15 @@ __global__ void __launch_bounds__(kNormThreads) orth_norm_kernel(const T *__rest
     }
 }
 
-// out = fp16(x s / (|x| + eps)), rows padded to ld; a thread takes eight columns of a row at a time
+// out = fp16(x s / (|x| + eps)), rows padded to ld, and the matrix's counter set to zero; a thread takes eight columns of a row at a time
 template <typename T>
 __global__ void __launch_bounds__(kNormThreads) orth_convert_kernel(const T *__restrict__ x, int rows, int cols, int even, const double *__restrict__ partial, int partials,
-                                                                   float eps, float s, __half *__restrict__ out, long long ld)
+                                                                   float eps, float s, __half *__restrict__ out, long long ld, unsigned int *__restrict__ done)
 {
     __shared__ double warp_sum[kNormThreads / 32];
     pdl_wait();
     const long long b = blockIdx.y;
+    if (blockIdx.x == 0 && threadIdx.x == 0) done[b] = 0;  // what the products count in
     double sum = threadIdx.x < partials ? partial[b * partials + threadIdx.x] : 0.0;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -131,163 +130,6 @@ __global__ void __launch_bounds__(kNormThreads) orth_convert_kernel(const T *__r
         for (int k = 0; k < 8; ++k) v[k] = v[k] * f1 * f2;
         *reinterpret_cast<uint4 *>(out + r * ld + c) = make_uint4(pack_half2(v[0], v[1]), pack_half2(v[2], v[3]), pack_half2(v[4], v[5]), pack_half2(v[6], v[7]));
     }
-}
-
-// ---- products ----------------------------------------------------------------------------------------------
-__device__ __forceinline__ Tile tile_of(const Product &p, int unit)
-{
-    Tile t;
-    t.batch = unit / p.units;
-    int u = unit - t.batch * p.units;
-    if (p.symmetric) {                                 // u = j (j + 1) / 2 + i,  i <= j
-        int j = (int)((sqrtf(8.0f * (float)u + 1.0f) - 1.0f) * 0.5f);
-        while (j * (j + 1) / 2 > u) --j;
-        while ((j + 1) * (j + 2) / 2 <= u) ++j;
-        const int i = u - j * (j + 1) / 2;
-        t.m0 = i * BM; t.n0 = j * BN; t.mirror = i != j;
-    } else {
-        t.m0 = (u % p.tiles_m) * BM; t.n0 = (u / p.tiles_m) * BN; t.mirror = false;
-    }
-    return t;
-}
-
-template <bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(NUM_THREADS, 1)
-orth_product_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const Product p)
-{
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (size_t)STAGES * STAGE_BYTES);
-    uint64_t *full = bars, *empty = bars + STAGES, *tmem_full = bars + 2 * STAGES, *tmem_empty = bars + 2 * STAGES + 2;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * STAGES + 4);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-
-    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int n_units = p.units * p.batch;
-
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&full[s], 1); tc::mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { tc::mbar_init(&tmem_full[b], 1); tc::mbar_init(&tmem_empty[b], 4); }
-        *abort_flag = 0;
-        tc::fence_barrier_init();
-        tc::prefetch_tmap(&tm_a);
-        tc::prefetch_tmap(&tm_b);
-    }
-    if (warp == 1) {
-        tc::tmem_alloc(tmem_slot, TMEM_COLS);
-        tc::tmem_relinquish();
-    }
-    tc::tc_fence_before_sync();
-    __syncthreads();
-    tc::tc_fence_after_sync();
-    const uint32_t tmem_base = *tmem_slot;
-    pdl_wait();
-
-    if (warp == 0) {
-        int s = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int unit = blockIdx.x; unit < n_units && ok; unit += gridDim.x) {
-            const Tile t = tile_of(p, unit);
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
-                ok = __all_sync(0xffffffffu, tc::mbar_wait(&empty[s], phase ^ 1, abort_flag, p.err, tc::ERR_WAIT_EMPTY));
-                if (!ok) break;
-                uint8_t *sa = smem + (size_t)s * STAGE_BYTES, *sb = sa + A_BYTES;
-                const int k0 = kb * BK;
-                if (tc::elect_one()) {
-                    tc::mbar_expect_tx(&full[s], STAGE_BYTES);
-                    if (A_MN) {
-#pragma unroll
-                        for (int i = 0; i < BM / 64; ++i) tc::tma_load_3d(sa + i * MN_BOX_BYTES, &tm_a, &full[s], t.m0 + i * 64, k0, t.batch);
-                    } else {
-                        tc::tma_load_3d(sa, &tm_a, &full[s], k0, t.m0, t.batch);
-                    }
-                    if (B_MN) {
-#pragma unroll
-                        for (int i = 0; i < BN / 64; ++i) tc::tma_load_3d(sb + i * MN_BOX_BYTES, &tm_b, &full[s], t.n0 + i * 64, k0, t.batch);
-                    } else {
-                        tc::tma_load_3d(sb, &tm_b, &full[s], k0, t.n0, t.batch);
-                    }
-                }
-                __syncwarp();
-                if (++s == STAGES) { s = 0; phase ^= 1; }
-            }
-        }
-    } else if (warp == 1) {
-        constexpr uint32_t idesc = instr_desc_f16(BM, BN, A_MN, B_MN);
-        constexpr uint32_t a_lbo = A_MN ? MN_BOX_BYTES : 16, b_lbo = B_MN ? MN_BOX_BYTES : 16;
-        constexpr uint32_t a_step = A_MN ? 2048 : 32, b_step = B_MN ? 2048 : 32;
-        const uint64_t desc_a0 = tc::smem_desc(tc::smem_u32(smem), a_lbo, 1024);
-        const uint64_t desc_b0 = tc::smem_desc(tc::smem_u32(smem) + A_BYTES, b_lbo, 1024);
-        uint32_t local = 0, phase = 0, stage_off = 0;
-        int s = 0;
-        bool ok = true;
-        for (int unit = blockIdx.x; unit < n_units && ok; unit += gridDim.x, ++local) {
-            const int buf = local & 1;
-            if (!__all_sync(0xffffffffu, tc::mbar_wait(&tmem_empty[buf], ((local >> 1) & 1) ^ 1, abort_flag, p.err, tc::ERR_WAIT_TMEM_EMPTY))) break;
-            tc::tc_fence_after_sync();
-            const uint32_t d_tmem = tmem_base + buf * BN;
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
-                ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[s], phase, abort_flag, p.err, tc::ERR_WAIT_FULL));
-                if (!ok) break;
-                tc::tc_fence_after_sync();
-                const uint64_t da = desc_a0 + stage_off, db = desc_b0 + stage_off;
-#pragma unroll
-                for (int kk = 0; kk < BK / 16; ++kk)
-                    tc::mma_bf16_elect(d_tmem, da + ((kk * a_step) >> 4), db + ((kk * b_step) >> 4), idesc, (uint32_t)(kb != 0 || kk != 0));
-                tc::mma_commit_elect(&empty[s]);
-                stage_off += STAGE_BYTES >> 4;
-                if (++s == STAGES) { s = 0; phase ^= 1; stage_off = 0; }
-            }
-            if (ok) tc::mma_commit_elect(&tmem_full[buf]);
-        }
-    } else {
-        const int quarter = warp & 3;
-        uint32_t local = 0;
-        for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x, ++local) {
-            const int buf = local & 1;
-            const Tile t = tile_of(p, unit);
-            int ok = 1;
-            if (lane == 0) ok = tc::mbar_wait(&tmem_full[buf], (local >> 1) & 1, abort_flag, p.err, tc::ERR_WAIT_TMEM_FULL) ? 1 : 0;
-            ok = __shfl_sync(0xffffffffu, ok, 0);
-            if (!ok) break;
-            tc::tc_fence_after_sync();
-            const int row = t.m0 + quarter * 32 + lane;
-            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * BN;
-#pragma unroll 1
-            for (int g = 0; g < BN / 32; ++g) {
-                uint32_t acc[32];
-                tc::tmem_ld_32x32(taddr + g * 32, acc);
-                tc::tmem_ld_wait();
-                finish_columns(p, t, lane, row, t.n0 + g * 32, acc);
-            }
-            tc::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&tmem_empty[buf]);
-        }
-    }
-
-    tc::tc_fence_before_sync();
-    __syncthreads();
-    if (warp == 1) {
-        tc::tc_fence_after_sync();
-        tc::tmem_dealloc(tmem_base, TMEM_COLS);
-    }
-}
-
-relay_status_t launch_product(const Product &p, bool a_mn, bool b_mn, const CUtensorMap &ta, const CUtensorMap &tb, int sms, cudaStream_t st)
-{
-    const dim3 grid((unsigned)std::min<long long>((long long)p.units * p.batch, sms));
-#define LAUNCH(AMN, BMN)                                                                                                              \
-    do {                                                                                                                              \
-        RELAY_CUDA(cudaFuncSetAttribute(orth_product_kernel<AMN, BMN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES)); \
-        RELAY_CUDA(launch_pdl(orth_product_kernel<AMN, BMN>, grid, dim3(NUM_THREADS), SMEM_BYTES, st, ta, tb, p));                     \
-    } while (0)
-    if (a_mn && b_mn) LAUNCH(true, true);
-    else if (b_mn) LAUNCH(false, true);
-    else LAUNCH(false, false);
-#undef LAUNCH
-    return check_launch("orthogonalize_product");
 }
 
 // ---- small matrices: one block each -----------------------------------------------------------------------------
@@ -412,14 +254,11 @@ relay_status_t launch_small(const relay_tensor_t *x, const relay_orthogonalize_a
     return check_launch("orthogonalize_small");
 }
 
-// Matrices whose shorter side has at least this many entries go to the two-SM kernel.
-constexpr int64_t kPairSide = 256;
-
 // ---- workspace -------------------------------------------------------------------------------------------------
 struct Plan {
     int64_t L, M, N, m, n;             // matrices; m = min(M, N), n = max(M, N)
     int64_t xld, gld;                  // row strides of X (rows M, N columns) and G, P (m x m), in elements
-    size_t x_bytes, g_bytes, v_bytes, total;
+    size_t x_bytes, g_bytes, v_bytes, n_bytes, total;
     bool small;
 };
 Plan plan_of(const relay_tensor_t *x)
@@ -434,7 +273,8 @@ Plan plan_of(const relay_tensor_t *x)
     p.x_bytes = align_up((size_t)(p.L * p.M * p.xld) * 2, 256);
     p.g_bytes = align_up((size_t)(p.L * p.m * p.gld) * 2, 256);
     p.v_bytes = align_up((size_t)(p.L * p.gld) * 4, 256);
-    p.total = align_up((size_t)p.L * kNormMost * sizeof(double), 256) + 2 * p.x_bytes + 2 * p.g_bytes + 2 * p.v_bytes;
+    p.n_bytes = align_up((size_t)p.L * kNormMost * sizeof(double), 256);
+    p.total = p.n_bytes + 2 * p.x_bytes + 2 * p.g_bytes + 2 * p.v_bytes + align_up((size_t)p.L * 4, 256);
     p.small = small_fits(p.m, p.n);
     if (p.small) p.total = 0;
     return p;
@@ -452,7 +292,7 @@ relay_status_t check_matrices(const relay_tensor_t *x)
 }
 
 template <typename T>
-relay_status_t prepare_x(const relay_tensor_t *x, const Plan &pl, double *partial, float eps, float s, int sms, __half *out, cudaStream_t st)
+relay_status_t prepare_x(const relay_tensor_t *x, const Plan &pl, double *partial, float eps, float s, int sms, __half *out, unsigned int *done, cudaStream_t st)
 {
     const long long size = pl.M * pl.N, each = kNormThreads * 8;
     const int share = (int)std::max<int64_t>(1, 4 * sms / pl.L);             // blocks per matrix that fill the GPU
@@ -461,7 +301,7 @@ relay_status_t prepare_x(const relay_tensor_t *x, const Plan &pl, double *partia
     RELAY_TRY(check_launch("orthogonalize_norm"));
     const dim3 grid((unsigned)std::min<long long>((pl.M * ((pl.N + 7) / 8) + kNormThreads - 1) / kNormThreads, 2 * share), (unsigned)pl.L);
     RELAY_CUDA(launch_pdl(orth_convert_kernel<T>, grid, dim3(kNormThreads), 0, st, (const T *)x->data, (int)pl.M, (int)pl.N, (int)(pl.N % 8 == 0),
-                          (const double *)partial, partials, eps, s, out, (long long)pl.xld));
+                          (const double *)partial, partials, eps, s, out, (long long)pl.xld, done));
     return check_launch("orthogonalize_convert");
 }
 
@@ -516,88 +356,63 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
     if (!err) return fail(RELAY_ERR_CUDA, "no device error word");
 
     char *w = (char *)ws;
-    double *partial = (double *)w;
-    w += align_up((size_t)pl.L * kNormMost * sizeof(double), 256);
-    __half *xa = (__half *)w, *xb = (__half *)(w + pl.x_bytes);
-    __half *g = (__half *)(w + 2 * pl.x_bytes), *q = (__half *)(w + 2 * pl.x_bytes + pl.g_bytes);
-    float *d = (float *)(w + 2 * pl.x_bytes + 2 * pl.g_bytes), *e = (float *)(w + 2 * pl.x_bytes + 2 * pl.g_bytes + pl.v_bytes);
+    auto take = [&](size_t bytes) { char *at = w; w += bytes; return at; };
+    double *partial = (double *)take(pl.n_bytes);
+    __half *x0 = (__half *)take(pl.x_bytes), *x1 = (__half *)take(pl.x_bytes);
+    __half *g = (__half *)take(pl.g_bytes), *q = (__half *)take(pl.g_bytes);
+    float *d = (float *)take(pl.v_bytes), *e = (float *)take(pl.v_bytes);
     const float s = exp2f(roundf(log2f(sqrtf((float)pl.M * (float)pl.N) / 8.0f)));
+
+    Launch l;
+    l.done = (unsigned int *)w;
+    l.tall = pl.M > pl.N; l.steps = at->steps; l.batch = (int)pl.L; l.err = err;
+    l.x[0] = x0; l.x[1] = x1;
+    // operands: boxes of 128 rows (A) or 64 (B) x 64 contiguous contraction elements, or 64 contraction rows x 64 contiguous columns
+    const uint64_t M = pl.M, N = pl.N, m = pl.m, L = pl.L, xld = pl.xld, gld = pl.gld;
+    for (int i = 0; i < 2; ++i) {
+        RELAY_TRY(make_tmap_3d_f16(&l.map[X_K0 + i], l.x[i], N, M, L, xld, M * xld, 64, 128));
+        RELAY_TRY(make_tmap_3d_f16(&l.map[X_K64_0 + i], l.x[i], N, M, L, xld, M * xld, 64, 64));
+        RELAY_TRY(make_tmap_3d_f16(&l.map[X_MN0 + i], l.x[i], N, M, L, xld, M * xld, 64, 64));
+        const __half *sq = i ? q : g;
+        RELAY_TRY(make_tmap_3d_f16(&l.map[i ? P_K : G_K], sq, m, m, L, gld, m * gld, 64, 128));
+        RELAY_TRY(make_tmap_3d_f16(&l.map[i ? P_K64 : G_K64], sq, m, m, L, gld, m * gld, 64, 64));
+    }
+
+    Product &pg = l.product[0], &pp = l.product[1], &px = l.product[2];
+    for (Product &p : l.product) p = Product{};
+    for (Product *p : {&pg, &pp}) {
+        p->rows = p->cols = (int)m;
+        p->symmetric = 1;
+        p->out_ld = gld; p->out_bs = (long long)(m * gld);
+        p->v_bs = gld;
+    }
+    pg.k_blocks = (int)((pl.n + 63) / 64);
+    pg.a_mn = pg.b_mn = l.tall;
+    pg.alpha = 1.0f / (s * s);
+    pg.out = g;
+    pg.diag = d;
+    pp.k_blocks = (int)((m + 63) / 64);
+    pp.alpha = at->c; pp.beta = at->b; pp.gamma = at->c;
+    pp.row_v = pp.col_v = d;
+    pp.add = g; pp.add_ld = gld; pp.add_bs = (long long)(m * gld);
+    pp.out = q;
+    pp.diag = e;
+    pp.q0 = at->a; pp.q1 = at->b; pp.q2 = at->c;
+    px.rows = (int)M; px.cols = (int)N;
+    px.k_blocks = pp.k_blocks;
+    px.b_mn = !l.tall;
+    px.alpha = px.gamma = 1.0f;
+    (l.tall ? px.col_v : px.row_v) = e;
+    px.v_bs = gld;
+    px.add_ld = px.out_ld = xld; px.add_bs = px.out_bs = (long long)(M * xld);
+    l.product[3] = px;
+    l.product[3].alpha = l.product[3].gamma = at->scale / s;
+    l.product[3].out = y->data; l.product[3].out_ld = N; l.product[3].out_bs = (long long)(M * N); l.product[3].out_bf16 = 1;
 
     BoundsReg reg;
     reg.add(x); reg.add(y); reg.add(ws, ws_bytes);
     RELAY_TRY(reg.commit(st));
-    if (x->dtype == RELAY_F32) RELAY_TRY(prepare_x<float>(x, pl, partial, at->eps, s, sms, xa, st));
-    else RELAY_TRY(prepare_x<__nv_bfloat16>(x, pl, partial, at->eps, s, sms, xa, st));
-
-    const bool tall = pl.M > pl.N;
-    // boxes: 128 rows x 64 contiguous contraction elements, or 64 contraction rows x 64 contiguous rows/columns
-    // the two-SM kernel takes its B operand in boxes of 64 rows
-    const bool pair = pl.m >= kPairSide && sms >= 2;
-    CUtensorMap x_k[2], x_mn[2], g_k, q_k, x_k64[2], g_k64, q_k64;
-    for (int i = 0; i < 2; ++i) {
-        const __half *b = i ? xb : xa;
-        RELAY_TRY(make_tmap_3d_f16(&x_k[i], b, pl.N, pl.M, pl.L, pl.xld, pl.M * pl.xld, BK, 128));
-        RELAY_TRY(make_tmap_3d_f16(&x_mn[i], b, pl.N, pl.M, pl.L, pl.xld, pl.M * pl.xld, 64, BK));
-        RELAY_TRY(make_tmap_3d_f16(&x_k64[i], b, pl.N, pl.M, pl.L, pl.xld, pl.M * pl.xld, BK, 64));
-    }
-    RELAY_TRY(make_tmap_3d_f16(&g_k64, g, pl.m, pl.m, pl.L, pl.gld, pl.m * pl.gld, BK, 64));
-    RELAY_TRY(make_tmap_3d_f16(&q_k64, q, pl.m, pl.m, pl.L, pl.gld, pl.m * pl.gld, BK, 64));
-    UnitTable plans[3];                                // of the three products of a step
-    auto product = [&](const Product &p, int kind, bool first, bool a_mn, bool b_mn, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &b64) {
-        if (!pair) return launch_product(p, a_mn, b_mn, a, b, sms, st);
-        if (first) plan_units(p, sms, &plans[kind]);
-        return launch_product_pair(p, a_mn, b_mn, a, b64, plans[kind], sms, st);
-    };
-    RELAY_TRY(make_tmap_3d_f16(&g_k, g, pl.m, pl.m, pl.L, pl.gld, pl.m * pl.gld, BK, 128));
-    RELAY_TRY(make_tmap_3d_f16(&q_k, q, pl.m, pl.m, pl.L, pl.gld, pl.m * pl.gld, BK, 128));
-
-    const int tm = (int)((pl.m + 127) / 128);
-    const long long v_ld = pl.gld;
-    Product sym{};                                     // G and P
-    sym.rows = sym.cols = (int)pl.m;
-    sym.tiles_m = sym.tiles_n = tm;
-    sym.units = tm * (tm + 1) / 2;
-    sym.batch = (int)pl.L;
-    sym.symmetric = 1;
-    sym.out_ld = pl.gld; sym.out_bs = pl.m * pl.gld;
-    sym.v_bs = v_ld;
-    sym.err = err;
-    Product up{};                                      // X
-    up.rows = (int)pl.M; up.cols = (int)pl.N;
-    up.tiles_m = (int)((pl.M + 127) / 128); up.tiles_n = (int)((pl.N + 127) / 128);
-    up.units = up.tiles_m * up.tiles_n;
-    up.batch = (int)pl.L;
-    up.k_blocks = (int)((pl.m + BK - 1) / BK);
-    up.v_bs = v_ld;
-    (tall ? up.col_v : up.row_v) = e;
-    up.err = err;
-    for (int k = 0; k < at->steps; ++k) {
-        const int cur = k & 1;
-        const bool last = k + 1 == at->steps;
-        Product p = sym;
-        p.k_blocks = (int)((pl.n + BK - 1) / BK);
-        p.alpha = 1.0f / (s * s);
-        p.out = g;
-        p.diag = d;
-        if (tall) RELAY_TRY(product(p, 0, k == 0, true, true, x_mn[cur], x_mn[cur], x_mn[cur]));
-        else RELAY_TRY(product(p, 0, k == 0, false, false, x_k[cur], x_k[cur], x_k64[cur]));
-        p = sym;
-        p.k_blocks = (int)((pl.m + BK - 1) / BK);
-        p.alpha = at->c; p.beta = at->b; p.gamma = at->c;
-        p.row_v = p.col_v = d;
-        p.diag = e;
-        p.q0 = at->a; p.q1 = at->b; p.q2 = at->c;
-        p.add = g; p.add_ld = pl.gld; p.add_bs = pl.m * pl.gld;
-        p.out = q;
-        RELAY_TRY(product(p, 1, k == 0, false, false, g_k, g_k, g_k64));
-        p = up;
-        const float f = last ? at->scale / s : 1.0f;
-        p.alpha = p.gamma = f;
-        p.add = cur ? xb : xa; p.add_ld = pl.xld; p.add_bs = pl.M * pl.xld;
-        if (last) { p.out = y->data; p.out_ld = pl.N; p.out_bs = pl.M * pl.N; p.out_bf16 = 1; }
-        else { p.out = cur ? xa : xb; p.out_ld = pl.xld; p.out_bs = pl.M * pl.xld; }
-        if (tall) RELAY_TRY(product(p, 2, k == 0, false, false, x_k[cur], q_k, q_k64));
-        else RELAY_TRY(product(p, 2, k == 0, false, true, q_k, x_mn[cur], x_mn[cur]));
-    }
-    return RELAY_OK;
+    if (x->dtype == RELAY_F32) RELAY_TRY(prepare_x<float>(x, pl, partial, at->eps, s, sms, x0, l.done, st));
+    else RELAY_TRY(prepare_x<__nv_bfloat16>(x, pl, partial, at->eps, s, sms, x0, l.done, st));
+    return launch_products(l, sms, st);
 }
