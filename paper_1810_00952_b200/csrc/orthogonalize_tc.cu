@@ -202,11 +202,21 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
     return r;
 }
 
+// What the epilogue keeps of a unit's product in registers (the launch's description lies in constant memory and would be
+// indexed by the phase at every use): pointers are the matrix's own.
+struct Terms {
+    float alpha, gamma;
+    int rows, cols, add_ld, out_ld;
+    const __half *add;
+    uint16_t *out;
+    const float *col_v;
+    float *diag;
+};
 // What a group needs from memory, requested a group ahead (past L1: other SMs write it): the addend, four lanes to a row, and the
 // columns' vector, a lane each.  Rows and vectors of the workspace are padded to whole 16-byte pieces.
 struct Fetched { uint4 add[4]; float col; };
 template <int KIND>
-__device__ __forceinline__ void fetch(const Product &p, const void *add, int batch, int row0, int c0, int lane, Fetched &f)
+__device__ __forceinline__ void fetch(const Terms &p, int row0, int c0, int lane, Fetched &f)
 {
     if (KIND == IS_G) return;
     const int c = c0 + (lane & 3) * 8;
@@ -214,15 +224,15 @@ __device__ __forceinline__ void fetch(const Product &p, const void *add, int bat
     for (int i = 0; i < 4; ++i) {
         const int r = row0 + i * 8 + (lane >> 2);
         f.add[i] = uint4{};
-        if (r < p.rows && c < p.cols) f.add[i] = __ldcg(reinterpret_cast<const uint4 *>((const __half *)add + batch * p.add_bs + (long long)r * p.add_ld + c));
+        if (r < p.rows && c < p.cols) f.add[i] = __ldcg(reinterpret_cast<const uint4 *>(p.add + (long long)r * p.add_ld + c));
     }
     f.col = 0.0f;
-    if ((KIND == IS_P || KIND == IS_X_COLUMNS) && c0 + lane < p.cols) f.col = __ldcg(p.col_v + batch * p.v_bs + c0 + lane);
+    if ((KIND == IS_P || KIND == IS_X_COLUMNS) && c0 + lane < p.cols) f.col = __ldcg(p.col_v + c0 + lane);
 }
-struct Block { int batch, row0, c0; bool mirror; };
+struct Block { int row0, c0; bool mirror; };
 template <int KIND, bool LAST>
-__device__ __forceinline__ void finish_block(const Product &p, void *out, uint8_t *stage, const Block &t, int lane, float of_row, float d_row, const Fetched &f,
-                                             const uint32_t (&acc)[32])
+__device__ __forceinline__ void finish_block(const Terms &p, const Product &whole, uint8_t *stage, const Block &t, int lane, float of_row, float d_row,
+                                             const Fetched &f, const uint32_t (&acc)[32])
 {
     constexpr bool ADD = KIND != IS_G, COLUMN = KIND == IS_P || KIND == IS_X_COLUMNS, SYMMETRIC = KIND == IS_G || KIND == IS_P;
     uint8_t *in = stage, *res = stage + 2048;
@@ -269,7 +279,7 @@ __device__ __forceinline__ void finish_block(const Product &p, void *out, uint8_
             if (lane == 2 * j + 1) { mine = hi; hi = 0.0f; }
             v[j] = pair_of(lo, hi);
         }
-        if (row < p.rows) p.diag[t.batch * p.v_bs + row] = mine + p.q0 + d_row * (p.q1 + p.q2 * d_row);
+        if (row < p.rows) p.diag[row] = mine + whole.q0 + d_row * (whole.q1 + whole.q2 * d_row);
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -296,39 +306,46 @@ __device__ __forceinline__ void finish_block(const Product &p, void *out, uint8_
         __syncwarp();
     }
     if (LAST && p.out_ld % 8 != 0) {                       // the caller's rows of an odd width: element by element
-        __nv_bfloat16 *to = (__nv_bfloat16 *)out + t.batch * p.out_bs + t.c0 + lane;
+        __nv_bfloat16 *to = (__nv_bfloat16 *)p.out + t.c0 + lane;
         const int rows = min(32, p.rows - t.row0);
         for (int r = 0; r < rows; ++r)
             if (t.c0 + lane < p.cols) to[(long long)(t.row0 + r) * p.out_ld] = *reinterpret_cast<const __nv_bfloat16 *>(piece(res, r, lane >> 3) + (lane & 7) * 2);
         return;
     }
-    uint16_t *to = (uint16_t *)out + t.batch * p.out_bs;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = i * 8 + sub;
         const uint4 x = *reinterpret_cast<const uint4 *>(piece(res, r, part));
-        if (t.row0 + r < p.rows && t.c0 + part * 8 < p.cols) *reinterpret_cast<uint4 *>(to + (long long)(t.row0 + r) * p.out_ld + t.c0 + part * 8) = x;
+        if (t.row0 + r < p.rows && t.c0 + part * 8 < p.cols) *reinterpret_cast<uint4 *>(p.out + (long long)(t.row0 + r) * p.out_ld + t.c0 + part * 8) = x;
     }
     if (SYMMETRIC && t.mirror) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = i * 8 + sub;
             const uint4 x = *reinterpret_cast<const uint4 *>(piece(in, c, part));
-            if (t.c0 + c < p.cols && t.row0 + part * 8 < p.rows) *reinterpret_cast<uint4 *>(to + (long long)(t.c0 + c) * p.out_ld + t.row0 + part * 8) = x;
+            if (t.c0 + c < p.cols && t.row0 + part * 8 < p.rows) *reinterpret_cast<uint4 *>(p.out + (long long)(t.c0 + c) * p.out_ld + t.row0 + part * 8) = x;
         }
     }
 }
 
 // One unit's epilogue by one warp; false: gave up
 template <int KIND, bool LAST>
-__device__ __forceinline__ bool finish_unit(const Product &p, const Unit &w, const void *add, void *out, uint8_t *stage, int row0, int slot, int lane, uint32_t tmem_base,
+__device__ __forceinline__ bool finish_unit(const Product &whole, const Unit &w, const void *add, void *out, uint8_t *stage, int row0, int slot, int lane, uint32_t tmem_base,
                                             int quarter, uint64_t *tmem_full, uint64_t *tmem_empty, uint32_t &t_local, volatile int *abort_flag, int *err)
 {
     const int items = w.width > BN ? 2 : 1;                // accumulators of this unit
-    const float d_row = (KIND == IS_P || KIND == IS_X_ROWS) && row0 + lane < p.rows ? __ldcg(p.row_v + w.batch * p.v_bs + row0 + lane) : 0.0f;
-    const float of_row = fmaf(p.gamma, d_row, p.beta);
+    Terms p;
+    const long long v_at = w.batch * whole.v_bs;
+    p.alpha = whole.alpha; p.gamma = whole.gamma;
+    p.rows = whole.rows; p.cols = whole.cols;
+    p.add_ld = (int)whole.add_ld; p.out_ld = (int)whole.out_ld;
+    p.add = (const __half *)add + w.batch * whole.add_bs;
+    p.out = (uint16_t *)out + w.batch * whole.out_bs;
+    p.col_v = whole.col_v + v_at; p.diag = whole.diag + v_at;
+    const float d_row = (KIND == IS_P || KIND == IS_X_ROWS) && row0 + lane < p.rows ? __ldcg(whole.row_v + v_at + row0 + lane) : 0.0f;
+    const float of_row = fmaf(p.gamma, d_row, whole.beta);
     Fetched now;                                           // the first group's, before the accumulator is awaited
-    fetch<KIND>(p, add, w.batch, row0, w.n0 + slot * (min(w.width, BN) / 64) * 32, lane, now);
+    fetch<KIND>(p, row0, w.n0 + slot * (min(w.width, BN) / 64) * 32, lane, now);
     for (int item = 0; item < items; ++item, ++t_local) {
         const int buf = t_local & 1;
         const int n0 = w.n0 + item * BN, width = item == 0 ? min(w.width, BN) : w.width - BN;
@@ -343,11 +360,11 @@ __device__ __forceinline__ bool finish_unit(const Product &p, const Unit &w, con
             Fetched next;
             const int c0 = n0 + g * 32;
             const int then = g + 1 < slot * per + per ? c0 + 32 : n0 + BN + slot * ((w.width - BN) / 64) * 32;
-            if (g + 1 < slot * per + per || item + 1 < items) fetch<KIND>(p, add, w.batch, row0, then, lane, next);
+            if (g + 1 < slot * per + per || item + 1 < items) fetch<KIND>(p, row0, then, lane, next);
             tc::tmem_ld_wait();
             // right of the diagonal's 256 x 256 block the mirrored place is not computed by anyone
-            const Block t{w.batch, row0, c0, c0 >= w.m0 + 256};
-            if (row0 < p.rows && c0 < p.cols) finish_block<KIND, LAST>(p, out, stage, t, lane, of_row, d_row, now, acc);
+            const Block t{row0, c0, c0 >= w.m0 + 256};
+            if (row0 < p.rows && c0 < p.cols) finish_block<KIND, LAST>(p, whole, stage, t, lane, of_row, d_row, now, acc);
             now = next;
         }
         tc::tc_fence_before_sync();
