@@ -134,6 +134,7 @@ struct Walk {
     }
 };
 // every lane waits until matrix b's units of the phases before are done (and their stores can be read by TMA too); bounded
+template <bool LOADER>
 __device__ __forceinline__ bool wait_done(const unsigned int *done, unsigned int need, volatile int *abort_flag, int *err)
 {
     if (need == 0) return true;
@@ -146,7 +147,7 @@ __device__ __forceinline__ bool wait_done(const unsigned int *done, unsigned int
                 atomicCAS(err, 0, tc::ERR_WAIT_STEP);
                 return false;
             }
-            __nanosleep(64);
+            if (!LOADER) __nanosleep(100);                 // the epilogue is waiting for its accumulator anyway
         }
     }
     tc::fence_proxy_async_global();
@@ -205,12 +206,23 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
 // What the epilogue keeps of a unit's product in registers (the launch's description lies in constant memory and would be
 // indexed by the phase at every use): pointers are the matrix's own.
 struct Terms {
-    float alpha, gamma;
+    float alpha, beta, gamma, q0, q1, q2;
     int rows, cols, add_ld, out_ld;
     const __half *add;
     uint16_t *out;
-    const float *col_v;
+    const float *row_v, *col_v;
     float *diag;
+    __device__ __forceinline__ Terms(const Product &p, int batch, const void *add_, void *out_)
+    {
+        const long long v_at = batch * p.v_bs;
+        alpha = p.alpha; beta = p.beta; gamma = p.gamma;
+        q0 = p.q0; q1 = p.q1; q2 = p.q2;
+        rows = p.rows; cols = p.cols;
+        add_ld = (int)p.add_ld; out_ld = (int)p.out_ld;
+        add = (const __half *)add_ + batch * p.add_bs;
+        out = (uint16_t *)out_ + batch * p.out_bs;
+        row_v = p.row_v + v_at; col_v = p.col_v + v_at; diag = p.diag + v_at;
+    }
 };
 // What a group needs from memory, requested a group ahead (past L1: other SMs write it): the addend, four lanes to a row, and the
 // columns' vector, a lane each.  Rows and vectors of the workspace are padded to whole 16-byte pieces.
@@ -231,7 +243,7 @@ __device__ __forceinline__ void fetch(const Terms &p, int row0, int c0, int lane
 }
 struct Block { int row0, c0; bool mirror; };
 template <int KIND, bool LAST>
-__device__ __forceinline__ void finish_block(const Terms &p, const Product &whole, uint8_t *stage, const Block &t, int lane, float of_row, float d_row,
+__device__ __forceinline__ void finish_block(const Terms &p, uint8_t *stage, const Block &t, int lane, float of_row, float d_row,
                                              const Fetched &f, const uint32_t (&acc)[32])
 {
     constexpr bool ADD = KIND != IS_G, COLUMN = KIND == IS_P || KIND == IS_X_COLUMNS, SYMMETRIC = KIND == IS_G || KIND == IS_P;
@@ -279,7 +291,7 @@ __device__ __forceinline__ void finish_block(const Terms &p, const Product &whol
             if (lane == 2 * j + 1) { mine = hi; hi = 0.0f; }
             v[j] = pair_of(lo, hi);
         }
-        if (row < p.rows) p.diag[row] = mine + whole.q0 + d_row * (whole.q1 + whole.q2 * d_row);
+        if (row < p.rows) p.diag[row] = mine + p.q0 + d_row * (p.q1 + p.q2 * d_row);
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -328,22 +340,17 @@ __device__ __forceinline__ void finish_block(const Terms &p, const Product &whol
     }
 }
 
-// One unit's epilogue by one warp; false: gave up
+// One unit's epilogue by one warp; false: gave up.  Out of line, so that the six instances do not share one allocation of
+// registers; what it gets of the launch comes by value (a reference would turn the constant bank into generic memory).
+struct Place { int row0, m0, n0, width, slot, lane; uint32_t taddr; };
 template <int KIND, bool LAST>
-__device__ __forceinline__ bool finish_unit(const Product &whole, const Unit &w, const void *add, void *out, uint8_t *stage, int row0, int slot, int lane, uint32_t tmem_base,
-                                            int quarter, uint64_t *tmem_full, uint64_t *tmem_empty, uint32_t &t_local, volatile int *abort_flag, int *err)
+__device__ __noinline__ bool finish_unit(const Terms p, const Place w, uint8_t *stage, uint64_t *tmem_full, uint64_t *tmem_empty, uint32_t t_local, volatile int *abort_flag,
+                                         int *err)
 {
+    const int row0 = w.row0, lane = w.lane, slot = w.slot;
     const int items = w.width > BN ? 2 : 1;                // accumulators of this unit
-    Terms p;
-    const long long v_at = w.batch * whole.v_bs;
-    p.alpha = whole.alpha; p.gamma = whole.gamma;
-    p.rows = whole.rows; p.cols = whole.cols;
-    p.add_ld = (int)whole.add_ld; p.out_ld = (int)whole.out_ld;
-    p.add = (const __half *)add + w.batch * whole.add_bs;
-    p.out = (uint16_t *)out + w.batch * whole.out_bs;
-    p.col_v = whole.col_v + v_at; p.diag = whole.diag + v_at;
-    const float d_row = (KIND == IS_P || KIND == IS_X_ROWS) && row0 + lane < p.rows ? __ldcg(whole.row_v + v_at + row0 + lane) : 0.0f;
-    const float of_row = fmaf(p.gamma, d_row, whole.beta);
+    const float d_row = (KIND == IS_P || KIND == IS_X_ROWS) && row0 + lane < p.rows ? __ldcg(p.row_v + row0 + lane) : 0.0f;
+    const float of_row = fmaf(p.gamma, d_row, p.beta);
     Fetched now;                                           // the first group's, before the accumulator is awaited
     fetch<KIND>(p, row0, w.n0 + slot * (min(w.width, BN) / 64) * 32, lane, now);
     for (int item = 0; item < items; ++item, ++t_local) {
@@ -352,7 +359,7 @@ __device__ __forceinline__ bool finish_unit(const Product &whole, const Unit &w,
         const int per = width / 64;                        // 32-column groups per warp: 4 for a 256-column accumulator, 2 for 128
         if (!__all_sync(0xffffffffu, tc::mbar_wait(&tmem_full[buf], (t_local >> 1) & 1, abort_flag, err, tc::ERR_WAIT_TMEM_FULL))) return false;
         tc::tc_fence_after_sync();
-        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * BN;
+        const uint32_t taddr = w.taddr + buf * BN;
 #pragma unroll 1
         for (int g = slot * per; g < slot * per + per; ++g) {
             uint32_t acc[32];
@@ -364,7 +371,7 @@ __device__ __forceinline__ bool finish_unit(const Product &whole, const Unit &w,
             tc::tmem_ld_wait();
             // right of the diagonal's 256 x 256 block the mirrored place is not computed by anyone
             const Block t{row0, c0, c0 >= w.m0 + 256};
-            if (row0 < p.rows && c0 < p.cols) finish_block<KIND, LAST>(p, whole, stage, t, lane, of_row, d_row, now, acc);
+            if (row0 < p.rows && c0 < p.cols) finish_block<KIND, LAST>(p, stage, t, lane, of_row, d_row, now, acc);
             now = next;
         }
         tc::tc_fence_before_sync();
@@ -429,7 +436,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
                 full = bars + cls_bar_base(c); empty = full + n_st;
                 rings.resume(c, s, phase);
             }
-            ok = __all_sync(0xffffffffu, wait_done(l.done + w.batch, walk.need, abort_flag, l.err));
+            ok = __all_sync(0xffffffffu, wait_done<true>(l.done + w.batch, walk.need, abort_flag, l.err));
             if (!ok) break;
             const int which = walk.kind == 1 ? (load_a ? G_K : G_K64)
                               : walk.kind == 0 ? (l.tall ? X_MN0 + walk.cur : load_a ? X_K0 + walk.cur : X_K64_0 + walk.cur)
@@ -541,15 +548,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
             const bool last = walk.phase == 3 * l.steps - 1;
             const void *x = l.x[walk.cur];
             void *x_out = last ? p.out : l.x[walk.cur ^ 1];
-            ok = __all_sync(0xffffffffu, wait_done(l.done + w.batch, walk.need, abort_flag, l.err));
+            ok = __all_sync(0xffffffffu, wait_done<false>(l.done + w.batch, walk.need, abort_flag, l.err));
             if (!ok) break;
-#define FINISH(KIND, LAST, ADD, OUT) \
-    finish_unit<KIND, LAST>(p, w, ADD, OUT, my_stage, row0, slot, lane, tmem_base, quarter, tmem_full, tmem_empty, t_local, abort_flag, l.err)
+            const Place at{row0, w.m0, w.n0, w.width, slot, lane, tmem_base + ((uint32_t)(quarter * 32) << 16)};
+#define FINISH(KIND, LAST, ADD, OUT) finish_unit<KIND, LAST>(Terms(p, w.batch, ADD, OUT), at, my_stage, tmem_full, tmem_empty, t_local, abort_flag, l.err)
             if (walk.kind == 0) ok = FINISH(IS_G, false, nullptr, p.out);
             else if (walk.kind == 1) ok = FINISH(IS_P, false, p.add, p.out);
             else if (l.tall) ok = last ? FINISH(IS_X_COLUMNS, true, x, x_out) : FINISH(IS_X_COLUMNS, false, x, x_out);
             else ok = last ? FINISH(IS_X_ROWS, true, x, x_out) : FINISH(IS_X_ROWS, false, x, x_out);
 #undef FINISH
+            t_local += w.width > BN ? 2 : 1;
             if (!ok) break;
             if (!last) {                                   // this warp's stores are there, for TMA too: count it in
                 tc::fence_proxy_async_global();
