@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -113,6 +114,21 @@ def desc(t: Optional[torch.Tensor], layout: int = ROWMAJOR) -> Optional[TensorDe
     if len(shape) > MAX_RANK:
         raise IndexError(f"rank {len(shape)}: a descriptor has room for {MAX_RANK} extents")
     return TensorDesc(t.data_ptr() or None, dtype, len(shape), shape, layout, 0)
+
+
+_PACK = struct.Struct("=Qii6qii").pack         # relay_tensor_t
+_REST = [(0,) * (MAX_RANK - n) + (ROWMAJOR, 0) for n in range(MAX_RANK + 1)]
+
+
+def _packed(t: Optional[torch.Tensor]) -> Optional[bytes]:
+    """The descriptor of a row-major tensor as the bytes of the C struct, which ctypes passes as a pointer: half the cost of a
+    ctypes.Structure and a reference to it, and calls on single tokens are as short as their marshalling."""
+    if t is None:
+        return None
+    shape = t.shape
+    if t.dtype not in _TORCH2RELAY or not t.is_contiguous() or len(shape) > MAX_RANK:
+        desc(t)                                # raises what is wrong
+    return _PACK(t.data_ptr(), _TORCH2RELAY[t.dtype], len(shape), *shape, *_REST[len(shape)])
 
 
 def desc_of_type(dtype: int, shape: Sequence[int], layout: int = ROWMAJOR, data: int = 0) -> TensorDesc:
@@ -408,38 +424,38 @@ def relay_infer_gated_recurrence(f: TensorDesc, u: Optional[TensorDesc] = None):
 
 def relay_gated_recurrence(f, u, h0, lengths, gate, h_all, h_final):
     """u = None: f holds the column blocks [ f | u ].  h0, lengths and h_final may be None."""
-    _check(lib().relay_gated_recurrence(_ref(desc(f)), _ref(desc(u)), _ref(desc(h0)), _ref(desc(lengths)), int(gate), _ref(desc(h_all)),
-                                        _ref(desc(h_final)), _stream()))
+    _check(lib().relay_gated_recurrence(_packed(f), _packed(u), _packed(h0), _packed(lengths), int(gate), _packed(h_all),
+                                        _packed(h_final), _stream()))
 
 
 def relay_gated_recurrence_grad(f, u, h0, lengths, gate, h_all, dh_all, dh_final, df, du, dh0):
     """u = None goes with du = None: df holds the column blocks [ df | du ].  h0, lengths, dh_final and dh0 may be None."""
-    _check(lib().relay_gated_recurrence_grad(_ref(desc(f)), _ref(desc(u)), _ref(desc(h0)), _ref(desc(lengths)), int(gate), _ref(desc(h_all)),
-                                             _ref(desc(dh_all)), _ref(desc(dh_final)), _ref(desc(df)), _ref(desc(du)), _ref(desc(dh0)),
+    _check(lib().relay_gated_recurrence_grad(_packed(f), _packed(u), _packed(h0), _packed(lengths), int(gate), _packed(h_all),
+                                             _packed(dh_all), _packed(dh_final), _packed(df), _packed(du), _packed(dh0),
                                              _stream()))
 
 
 def relay_token_logprob(scores, tokens, temperature, logp, entropy, lse, top_logp=None, top_ids=None):
     """tokens and logp, top_logp and top_ids go in pairs; each pair, entropy and lse may be None."""
-    _check(lib().relay_token_logprob(_ref(desc(scores)), _ref(desc(tokens)), ctypes.c_float(temperature), _ref(desc(logp)), _ref(desc(entropy)),
-                                     _ref(desc(lse)), _ref(desc(top_logp)), _ref(desc(top_ids)), _stream()))
+    _check(lib().relay_token_logprob(_packed(scores), _packed(tokens), ctypes.c_float(temperature), _packed(logp), _packed(entropy),
+                                     _packed(lse), _packed(top_logp), _packed(top_ids), _stream()))
 
 
 def relay_token_logprob_grad(scores, tokens, temperature, lse, entropy, dlogp, dentropy, dscores):
     """entropy and dentropy may be None together."""
-    _check(lib().relay_token_logprob_grad(_ref(desc(scores)), _ref(desc(tokens)), ctypes.c_float(temperature), _ref(desc(lse)),
-                                          _ref(desc(entropy)), _ref(desc(dlogp)), _ref(desc(dentropy)), _ref(desc(dscores)), _stream()))
+    _check(lib().relay_token_logprob_grad(_packed(scores), _packed(tokens), ctypes.c_float(temperature), _packed(lse),
+                                          _packed(entropy), _packed(dlogp), _packed(dentropy), _packed(dscores), _stream()))
 
 
 def relay_workspace_bytes_orthogonalize(x) -> int:
-    return int(lib().relay_workspace_bytes_orthogonalize(_ref(desc(x))))
+    return int(lib().relay_workspace_bytes_orthogonalize(_packed(x)))
 
 
 def relay_orthogonalize(x, steps, coefficients, eps, scale, y, ws=None):
     """coefficients = (a, b, c) of X <- a X + (b A + c A A) X."""
     wp, wb = _ws(ws)
     at = OrthogonalizeAttrs(int(steps), *[float(v) for v in coefficients], float(eps), float(scale))
-    _check(lib().relay_orthogonalize(_ref(desc(x)), ctypes.byref(at), _ref(desc(y)), wp, wb, _stream()))
+    _check(lib().relay_orthogonalize(_packed(x), ctypes.byref(at), _packed(y), wp, wb, _stream()))
 
 
 # ---- status helpers -----------------------------------------------------------------------------------
