@@ -191,33 +191,66 @@ __device__ __forceinline__ void fill(float x, float (&r)[V])
 // With fp32 gates e and the quotient are within about one unit in the last place (FINE): the state's own rounding is no larger.
 // With bf16 gates the hardware's exponential and reciprocal serve, a few units off.
 // exp of x <= 0: x = n log 2 + z with log 2 in two parts, Taylor's polynomial of degree 7 on |z| <= log(2) / 2 (remainder
-// 0.347^8 / 8! = 5e-9), times 2^n.
-__device__ __forceinline__ float exp_fine(float x)
+// 0.347^8 / 8! = 5e-9), times 2^n.  n comes as the low bits of a sum with 1.5 * 2^23.
+// x is held at -88, where n = -127 and the power's bits are those of zero.
+template <int V>
+__device__ __forceinline__ void exp_fine(float (&x)[V])
 {
-    const float n = rintf(x * 1.44269504f);
-    const float z = fmaf(n, -1.42860677e-6f, fmaf(n, -0.693145752f, x));      // 0.693145752 has 15 bits: its product with n is exact
-    float p = 1.0f / 5040.0f;
-    p = fmaf(p, z, 1.0f / 720.0f);
-    p = fmaf(p, z, 1.0f / 120.0f);
-    p = fmaf(p, z, 1.0f / 24.0f);
-    p = fmaf(p, z, 1.0f / 6.0f);
-    p = fmaf(p, z, 0.5f);
-    p = fmaf(p, z, 1.0f);
-    p = fmaf(p, z, 1.0f);
-    return x < -87.0f ? 0.0f : __int_as_float(__float_as_int(p) + ((int)n << 23));
+    float c[V], t[V], n[V], p[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) asm("max.NaN.f32 %0, %0, 0fC2B00000;" : "+f"(x[i]));       // -88
+    fill(1.44269504f, c);
+    fill(12582912.0f, p);
+    muladd(x, c, p, t);
+    fill(-12582912.0f, c);
+    add(t, c, n);
+    fill(-0.693115234375f, c);                             // 2839 / 4096: its product with n is exact
+    muladd(n, c, x, x);
+    fill(-3.19461849e-5f, c);                              // what log 2 has beyond it
+    muladd(n, c, x, x);
+    const float of[7] = {1.0f / 720.0f, 1.0f / 120.0f, 1.0f / 24.0f, 1.0f / 6.0f, 0.5f, 1.0f, 1.0f};
+    fill(1.0f / 5040.0f, p);
+#pragma unroll
+    for (int k = 0; k < 7; ++k) {
+        fill(of[k], c);
+        muladd(p, x, c, p);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = __int_as_float(0x3f800000 + (__float_as_int(t[i]) << 23));
+    mul(p, t, x);                                          // a product, for NaN to stay NaN
+}
+// the smaller of sigmoid(f) and 1 - sigmoid(f): e / (1 + e), the reciprocal with one Newton step
+template <int V>
+__device__ __forceinline__ void sigmoid_small(const float (&f)[V], float (&small)[V])
+{
+    float e[V], d[V], r[V], c[V], t[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = -fabsf(f[i]);
+    exp_fine(e);
+    fill(-1.0f, c);
+    fill(-1.0f, t);
+    muladd(e, c, t, d);                                    // -(1 + e)
+#pragma unroll
+    for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r[i]) : "f"(-d[i]));
+    fill(1.0f, c);
+    muladd(d, r, c, t);
+    muladd(r, t, r, r);
+    mul(e, r, small);
 }
 template <bool FINE, int V>
 __device__ __forceinline__ void sigmoid_pair(const float (&f)[V], float (&a)[V], float (&one_less)[V])
 {
     if constexpr (FINE) {
+        float small[V], large[V];
+        sigmoid_small(f, small);
+        float c[V], m[V];
+        fill(1.0f, c);
+        fill(-1.0f, m);
+        muladd(small, m, c, large);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float e = exp_fine(-fabsf(f[i])), d = 1.0f + e, r = __fdividef(1.0f, d);
-            const float small = e * fmaf(r, fmaf(-d, r, 1.0f), r);    // one Newton step on the reciprocal
-            const float large = 1.0f - small;
-            a[i] = f[i] >= 0.0f ? large : small;
-            one_less[i] = f[i] >= 0.0f ? small : large;
-            if (f[i] != f[i]) a[i] = one_less[i] = f[i];
+            a[i] = f[i] >= 0.0f ? large[i] : small[i];
+            one_less[i] = f[i] >= 0.0f ? small[i] : large[i];
         }
     } else {
         // 1 - a = 1 / (1 + exp(f)), and a from it: what a loses where it is itself small is lost on a state that it all but
@@ -256,22 +289,34 @@ template <typename T, int GATE, int V> struct Coefficient {
 #pragma unroll
             for (int i = 0; i < V; ++i) k[i] = f[i];
         } else {
-            sigmoid_pair<FINE>(f, k, s);
-            if (SIGNED) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) k[i] = f[i] >= 0.0f ? -s[i] : k[i];
+            if constexpr (SIGNED) {
+                sigmoid_small(f, s);
+                signed_by(f, s, k);
+            } else {
+                sigmoid_pair<FINE>(f, k, s);
             }
         }
+    }
+    // -(1 - a) of an open gate, a of one that is not: the smaller of the two either way, with the opposite of f's sign bit
+    static __device__ __forceinline__ void signed_by(const float (&f)[V], const float (&small)[V], float (&k)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) k[i] = __int_as_float(__float_as_int(small[i]) | (~__float_as_int(f[i]) & 0x80000000));
     }
     static __device__ __forceinline__ void of(const float (&f)[V], const float (&u)[V], float (&k)[V], float (&b)[V])
     {
         if constexpr (GATE == RELAY_GATE_MIX) {
             float s[V];
-            sigmoid_pair<FINE>(f, k, s);
-            mul(s, u, b);
-            if (SIGNED) {
+            if constexpr (SIGNED) {
+                float less[V];
+                sigmoid_small(f, s);
+                signed_by(f, s, k);
 #pragma unroll
-                for (int i = 0; i < V; ++i) k[i] = f[i] >= 0.0f ? -s[i] : k[i];
+                for (int i = 0; i < V; ++i) less[i] = f[i] >= 0.0f ? s[i] : 1.0f - s[i];
+                mul(less, u, b);
+            } else {
+                sigmoid_pair<FINE>(f, k, s);
+                mul(s, u, b);
             }
         } else {
             of(f, k);
@@ -765,7 +810,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) recurrence_grad_spans_kernel(c
 //   - a cluster stays for several tiles of channels, whose slabs follow each other without a gap.
 constexpr int kTile = 64;              // channels
 constexpr int kStages = 3;             // 3 x 32 KB and 17 KB: two blocks fit an SM's 228 KB
-constexpr int tile_blocks(int item) { return item == 2 ? 2 : 1; }        // per SM; fp64 states need the registers of two
+constexpr int kTileBlocks = 2;         // per SM
 constexpr int kTileThreads = 32 * (kWarps + 1);
 
 struct TilePlan {
@@ -860,6 +905,7 @@ struct Exchange {                      // everything but the ring twice, alterna
 template <bool SAFE, int LAG, typename T, typename F, int V, typename Request>
 __device__ __forceinline__ void join_slabs(Exchange<F, V> &x, const Args &p, const TilePlan &q, int lane, const float *initial, float *final, Request request)
 {
+    constexpr int HELD = sizeof(F) == 8 ? 2 : 8;           // maps in registers
     const uint32_t rank = blockIdx.x % q.S;
     Cursor<T> ahead, here;
     ahead.start(p, q, lane);
@@ -882,13 +928,15 @@ __device__ __forceinline__ void join_slabs(Exchange<F, V> &x, const Args &p, con
         // arming may come after a neighbour's first bytes: the phase ends when both are complete
         if (q.S > 1 && lane == 0) tc::mbar_expect_tx(&x.arrived[buf], (uint32_t)(q.S * 32 * sizeof(Map<F, V>)));
         x.wait(&x.handed[buf], turn.phase, p.err, tc::ERR_WAIT_STEP);
-        Map<F, V> m[kWarps];                                          // all loads in flight together
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) m[w] = x.span[buf][w][lane];
         if (done >= LAG) ask();
-        Map<F, V> all = m[0];
+        Map<F, V> m[HELD], all = identity<F, V>();                    // loads in flight together
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) all = then(all, m[w]);
+        for (int w0 = 0; w0 < kWarps; w0 += HELD) {
+#pragma unroll
+            for (int w = 0; w < HELD; ++w) m[w] = x.span[buf][w0 + w][lane];
+#pragma unroll
+            for (int w = 0; w < HELD; ++w) all = then(all, m[w]);
+        }
         if (q.S > 1) {
             const uint32_t to = tc::smem_u32(&x.block[buf][rank][lane]), bar = tc::smem_u32(&x.arrived[buf]);
 #pragma unroll
@@ -897,26 +945,34 @@ __device__ __forceinline__ void join_slabs(Exchange<F, V> &x, const Args &p, con
         }
         Map<F, V> before = identity<F, V>();                          // while the exchange is under way
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            x.span[buf][w][lane] = before;
-            before = then(before, m[w]);
+        for (int w0 = 0; w0 < kWarps; w0 += HELD) {
+#pragma unroll
+            for (int w = 0; w < HELD; ++w) m[w] = x.span[buf][w0 + w][lane];
+#pragma unroll
+            for (int w = 0; w < HELD; ++w) {
+                x.span[buf][w0 + w][lane] = before;
+                before = then(before, m[w]);
+            }
         }
         if (q.S > 1) {
             // A neighbour sends for slab i + 2 only when it has this block's message for slab i + 1, which this warp sends after
             // it has read slab i's: two buffers are enough.
             wait_arrived(&x.arrived[buf], turn.phase, &x.gave_up, p.err);
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if (r < q.S) m[r] = x.block[buf][r][lane];
+            for (int r0 = 0; r0 < 8; r0 += HELD) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if (r < q.S) {
-                    if (r == (int)rank) {
+                for (int r = 0; r < HELD; ++r)
+                    if (r0 + r < q.S) m[r] = x.block[buf][r0 + r][lane];
 #pragma unroll
-                        for (int i = 0; i < V; ++i) x.state[buf][lane].h[i] = state[i];
+                for (int r = 0; r < HELD; ++r)
+                    if (r0 + r < q.S) {
+                        if (r0 + r == (int)rank) {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) x.state[buf][lane].h[i] = state[i];
+                        }
+                        apply<SAFE>(m[r], state);
                     }
-                    apply<SAFE>(m[r], state);
-                }
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) x.state[buf][lane].h[i] = state[i];
@@ -934,7 +990,7 @@ __device__ __forceinline__ void join_slabs(Exchange<F, V> &x, const Args &p, con
 }
 
 template <typename T, typename TH, int GATE, int TS>
-__global__ void __launch_bounds__(kTileThreads, tile_blocks(sizeof(T)))
+__global__ void __launch_bounds__(kTileThreads, kTileBlocks)
 recurrence_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_constant__ CUtensorMap tm_u, const Args p, const TilePlan q)
 {
     constexpr int V = 2, ROWS = kWarps * TS, TILE = ROWS * kTile * (int)sizeof(T);
@@ -1041,7 +1097,7 @@ recurrence_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_c
 }
 
 template <typename T, typename TH, int GATE, int TS>
-__global__ void __launch_bounds__(kTileThreads, tile_blocks(sizeof(T)))
+__global__ void __launch_bounds__(kTileThreads, kTileBlocks)
 recurrence_grad_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_d,
                              const __grid_constant__ CUtensorMap tm_h, const Args p, const TilePlan q)
 {
@@ -1140,16 +1196,16 @@ template <typename T, typename TH, int GATE>
 bool tiles_fit(const Args &p)
 {
     const long long piece = 16 / (long long)sizeof(T);
-    return p.T > 2 * kWarps && p.D % piece == 0 && p.bs % piece == 0 && p.ld < (1ll << 31) && p.C < (1ll << 31) && p.T < (1ll << 30);
+    return p.D % piece == 0 && p.bs % piece == 0 && p.ld < (1ll << 31) && p.C < (1ll << 31) && p.T < (1ll << 30);
 }
 template <typename T, typename TH, int GATE>
 relay_status_t launch_tiles(const Args &p, bool grad, cudaStream_t st)
 {
-    constexpr int TS = 8, TSG = sizeof(T) + sizeof(TH) == 4 ? 8 : 4;
+    constexpr int TS = sizeof(T) == 2 ? 8 : 4, TSG = sizeof(T) + sizeof(TH) == 4 ? 8 : 4;
     int dev = 0, sms = 148;
     RELAY_CUDA(cudaGetDevice(&dev));
     RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    const int rows = kWarps * (grad ? TSG : TS), resident = tile_blocks(sizeof(T)) * sms;
+    const int rows = kWarps * (grad ? TSG : TS), resident = kTileBlocks * sms;
     TilePlan q;
     q.per_row = (int)((p.D + kTile - 1) / kTile);
     q.tiles = (p.C / p.D) * q.per_row;
@@ -1176,8 +1232,11 @@ relay_status_t launch_tiles(const Args &p, bool grad, cudaStream_t st)
     return check_launch("gated_recurrence");
 }
 
-// Sequences of up to kSteps steps run step by step.  Longer ones: the smallest cluster that gives every SM a block.
-constexpr long long kSteps = 32;
+// Sequences of up to kSteps steps run step by step, in the spans kernels' place; of up to kTileSteps, in the tile kernels' place.
+// 64 x 1024 channels in bf16, forward: 12 steps 13.3 us and in tiles 14.3, 16 steps 15.4 and 14.3, 32 steps 23.6 and 14.3; gradient in
+// fp32: 16 steps 21.5 and 24.6, 24 steps 27.7 and 26.6; 8 x 256 channels, forward: 8 steps 9.3 and 8.2, 32 steps 21.5 and 8.2.
+// Longer sequences in spans: the smallest cluster that gives every SM a block.
+constexpr long long kSteps = 32, kTileSteps = 12;
 
 // W channels a thread in the spans kernels, at most two in the step-by-step ones (more threads where there are few steps)
 template <typename T, typename TH, int GATE, int W>
@@ -1211,7 +1270,7 @@ template <typename T, typename TH, int GATE>
 relay_status_t launch_gate(const Args &p, bool grad, cudaStream_t st)
 {
     if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
-    if (p.T > kSteps && tiles_fit<T, TH, GATE>(p)) return launch_tiles<T, TH, GATE>(p, grad, st);
+    if (p.T > kTileSteps && tiles_fit<T, TH, GATE>(p)) return launch_tiles<T, TH, GATE>(p, grad, st);
     // several channels a thread where every row starts at a multiple of them, so that they are one aligned access
     const long long rows = p.D | p.ld | p.bs;
     return rows % 2 == 0 ? launch<T, TH, GATE, 2>(p, grad, st) : launch<T, TH, GATE, 1>(p, grad, st);

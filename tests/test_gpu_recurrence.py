@@ -100,7 +100,7 @@ def check_case(T, Bn, D, dt, gate, packed, ragged, out_dt=None, seed=0, h0=True)
 
 # one step, spans of the sequence around every power of two that a split could use, odd and even channel counts
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 33, 127, 128, 129, 300, 1025])
+@pytest.mark.parametrize("T", [1, 2, 12, 13, 15, 16, 17, 33, 127, 128, 129, 300, 1025])
 @pytest.mark.parametrize("Bn,D", [(1, 1), (3, 64), (2, 67), (5, 130)])
 @pytest.mark.parametrize("dt", [F32, BF16])
 def test_lengths_of_the_sequence(T, Bn, D, dt):
@@ -150,6 +150,31 @@ def test_gates_at_their_ends(T):
         df, du, d0 = run_grad(t, gate, h)
         for got, w in zip((df, du, d0), L.gated_recurrence_grad(f, u, h0, n, gate, to_np(h), to_np(t["dh_all"].float()), to_np(t["dh_final"]))):
             assert_f32(got, w)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 14, 90, 700])
+@pytest.mark.parametrize("Bn,D", [(2, 72), (3, 33)])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("gate", GATES)
+def test_nan_stays_in_its_channel_and_after_its_step(T, Bn, D, dt, gate):
+    t = make(T, Bn, D, dt, gate, False, False, 31)
+
+    def forward(t):
+        h, last = torch.zeros(T, Bn, D, dtype=dt, device=DEV), torch.zeros(Bn, D, device=DEV)
+        B.relay_gated_recurrence(on(t["f"]), on(t["u"]), on(t["h0"]), None, gate, h, last)
+        return h.cpu(), last.cpu()
+
+    clean = forward(t)[0]
+    at = T // 2
+    for name, channel in (("f", 3), ("u", 17)):
+        v = t[name].clone()
+        v[at, 1, channel] = float("nan")
+        h, last = forward(dict(t, **{name: v}))
+        bad = torch.zeros(T, Bn, D, dtype=torch.bool)
+        bad[at:, 1, channel] = True
+        assert torch.equal(torch.isnan(h), bad) and torch.equal(torch.isnan(last), bad[-1])
+        assert torch.equal(h[~bad], clean[~bad])
 
 
 @pytest.mark.gpu
