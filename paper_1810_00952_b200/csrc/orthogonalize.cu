@@ -33,38 +33,6 @@ using namespace orth;
 constexpr int kNormThreads = 256;
 constexpr int kNormMost = 256;                         // partial sums per matrix, at most
 
-template <typename T>
-__device__ __forceinline__ float element(const T *p)
-{
-    if (!relay_in_bounds(p, sizeof(T))) return 0.0f;
-    if constexpr (sizeof(T) == 2) return __bfloat162float(*p);
-    else return *p;
-}
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
-{
-    __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<uint32_t *>(&v);
-}
-// eight consecutive elements; whole: they are 16-byte aligned
-template <typename T>
-__device__ __forceinline__ void eight(const T *p, bool whole, int n, float (&x)[8])
-{
-    if (whole) {
-        if constexpr (sizeof(T) == 2) {
-            unpack(ld_stream(p), x);
-        } else {
-            float lo[4], hi[4];
-            unpack(ld_stream(p), lo);
-            unpack(ld_stream(p + 4), hi);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { x[i] = lo[i]; x[4 + i] = hi[i]; }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < n ? element(p + i) : 0.0f;
-    }
-}
-
 // The sum of squares in fp64: a square of any finite element fits, and the sum does not depend on the elements' scale.
 template <typename T>
 __global__ void __launch_bounds__(kNormThreads) orth_norm_kernel(const T *__restrict__ x, long long size, int even, double *__restrict__ partial)
@@ -112,11 +80,8 @@ __global__ void __launch_bounds__(kNormThreads) orth_convert_kernel(const T *__r
     __syncthreads();
     sum = 0.0;
     for (int i = 0; i < kNormThreads / 32; ++i) sum += warp_sum[i];
-    // in two factors, each of them within fp32's range where the whole may not be
-    const double f = (double)s / (sqrt(sum) + (double)eps);
-    int e;
-    const float lo = (float)frexp(f, &e);
-    const float f1 = ldexpf(lo, e / 2), f2 = ldexpf(1.0f, e - e / 2);
+    float f1, f2;
+    normalizer(sum, eps, s, f1, f2);
     const int per_row = (cols + 7) / 8;
     const long long items = (long long)rows * per_row;
     x += b * rows * cols;
@@ -259,7 +224,7 @@ struct Plan {
     int64_t L, M, N, m, n;             // matrices; m = min(M, N), n = max(M, N)
     int64_t xld, gld;                  // row strides of X (rows M, N columns) and G, P (m x m), in elements
     size_t x_bytes, g_bytes, v_bytes, n_bytes, total;
-    bool small;
+    bool small, resident;              // one block's fp32 kernel; one cluster's
 };
 Plan plan_of(const relay_tensor_t *x)
 {
@@ -276,7 +241,8 @@ Plan plan_of(const relay_tensor_t *x)
     p.n_bytes = align_up((size_t)p.L * kNormMost * sizeof(double), 256);
     p.total = p.n_bytes + 2 * p.x_bytes + 2 * p.g_bytes + 2 * p.v_bytes + align_up((size_t)p.L * 4, 256);
     p.small = small_fits(p.m, p.n);
-    if (p.small) p.total = 0;
+    p.resident = !p.small && resident_fits(p.m, p.n);
+    if (p.small || p.resident) p.total = 0;
     return p;
 }
 
@@ -349,6 +315,8 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
         if (x->dtype == RELAY_F32) return launch_small<float>(x, at, y, pl.L, (int)pl.M, (int)pl.N, st);
         return launch_small<__nv_bfloat16>(x, at, y, pl.L, (int)pl.M, (int)pl.N, st);
     }
+    const float s = exp2f(roundf(log2f(sqrtf((float)pl.M * (float)pl.N) / 8.0f)));
+    if (pl.resident) return launch_resident(x, at, y, pl.L, (int)pl.M, (int)pl.N, s, st);
     int dev = 0, sms = 148;
     RELAY_CUDA(cudaGetDevice(&dev));
     RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -361,7 +329,6 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
     __half *x0 = (__half *)take(pl.x_bytes), *x1 = (__half *)take(pl.x_bytes);
     __half *g = (__half *)take(pl.g_bytes), *q = (__half *)take(pl.g_bytes);
     float *d = (float *)take(pl.v_bytes), *e = (float *)take(pl.v_bytes);
-    const float s = exp2f(roundf(log2f(sqrtf((float)pl.M * (float)pl.N) / 8.0f)));
 
     Launch l;
     l.done = (unsigned int *)w;

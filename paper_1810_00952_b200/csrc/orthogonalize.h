@@ -1,8 +1,10 @@
 // The products of an orthogonalisation: what the host describes and the tensor-core kernel (orthogonalize_tc.cu) runs.
 #pragma once
 #include <cuda.h>
+#include <cuda_fp16.h>
 
 #include "common.h"
+#include "ewise_kernels.cuh"
 
 namespace relay {
 namespace orth {
@@ -49,6 +51,57 @@ struct Launch {
 };
 
 relay_status_t launch_products(Launch &l, int sms, cudaStream_t st);
+
+// Matrices that stay on the chip (orthogonalize_resident.cu): all of a call in one launch, without a workspace.
+bool resident_fits(int64_t m, int64_t n);
+relay_status_t launch_resident(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *at, const relay_tensor_t *y, int64_t L, int M, int N, float s, cudaStream_t st);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ uint32_t instr_desc_f16(int m, int n, int a_mn, int b_mn)
+{   // fp32 accumulator, fp16 A and B (format 0), majorness, N / 8, M / 16
+    return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+template <typename T>
+__device__ __forceinline__ float element(const T *p)
+{
+    if (!relay_in_bounds(p, sizeof(T))) return 0.0f;
+    if constexpr (sizeof(T) == 2) return __bfloat162float(*p);
+    else return *p;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
+{
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&v);
+}
+// eight consecutive elements; whole: they are 16-byte aligned
+template <typename T>
+__device__ __forceinline__ void eight(const T *p, bool whole, int n, float (&x)[8])
+{
+    if (whole) {
+        if constexpr (sizeof(T) == 2) {
+            unpack(ld_stream(p), x);
+        } else {
+            float lo[4], hi[4];
+            unpack(ld_stream(p), lo);
+            unpack(ld_stream(p + 4), hi);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { x[i] = lo[i]; x[4 + i] = hi[i]; }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < n ? element(p + i) : 0.0f;
+    }
+}
+// s / (norm + eps) in two factors, each of them within fp32's range where the whole may not be
+__device__ __forceinline__ void normalizer(double squares, float eps, float s, float &f1, float &f2)
+{
+    const double f = (double)s / (sqrt(squares) + (double)eps);
+    int e;
+    const float lo = (float)frexp(f, &e);
+    f1 = ldexpf(lo, e / 2);
+    f2 = ldexpf(1.0f, e - e / 2);
+}
+#endif
 
 }  // namespace orth
 

@@ -1,0 +1,361 @@
+// Orthogonalised updates of matrices that stay on the chip: at most 128 rows (columns, where M > N), all steps in one launch.
+//
+// One cluster of S = 1..8 blocks per matrix.  Each block keeps a slice of at most 256 of the n columns of X (of X^T where M > N) in
+// shared memory as fp16, and copies of G and P: a product's operands never leave the SM.  The slice's layout, groups of 64 columns
+// with 128-byte rows swizzled, is K-major for G = X X^T and MN-major for P X at once.  Per step:
+//   G      over the slice's columns, accumulated in TMEM; with S > 1 the blocks' parts are sent to the block that owns the row
+//          (128 / S rows each), added there in the order of the blocks, and the sum in fp16 is sent to all
+//   P      = b G + c G G by every block for itself: 128^3 products are less than an exchange
+//   X      <- e X + offdiag(P) X in place
+// with the diagonals apart in fp32, as in the products of larger matrices.  Every phase ends in a barrier of the block (twice a
+// step of the cluster), so what bounds a step is its chain of latencies: three times MMA, TMEM to registers, shared memory.
+#include <algorithm>
+
+#include "common.h"
+#include "orthogonalize.h"
+#include "tc_common.cuh"
+
+namespace relay {
+namespace orth {
+namespace {
+
+constexpr int kThreads = 512, kRows = 128, kWidest = 256, kMostBlocks = 8;
+constexpr int kGroup = kRows * 128;                        // bytes of 64 columns
+
+struct Resident {
+    int M, N, m, n, tall, S, w, steps; // w: columns of a slice, a multiple of 32
+    float a, b, c, eps, s, scale;
+    int *err;
+};
+struct Scalars {                       // behind the matrices in shared memory
+    float d[kRows], e[kRows];          // the diagonals of G and of a I + P
+    double warp_sum[kThreads / 32], norm[kMostBlocks];
+    uint64_t bar;
+    uint32_t tmem;
+    int gave_up;
+};
+// byte offset of an element (of the 16 bytes that begin with it) in a swizzled matrix of 128 rows
+__device__ __forceinline__ uint32_t place(int row, int col)
+{
+    return (uint32_t)((col >> 6) * kGroup + row * 128 + ((((col >> 3) & 7) ^ (row & 7)) << 4) + (col & 7) * 2);
+}
+__device__ __forceinline__ void unpack_half(const uint4 &v, float (&x)[8])
+{
+    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&r[i]));
+        x[2 * i] = f.x; x[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ uint4 pack_half(const float (&x)[8])
+{
+    return make_uint4(pack_half2(x[0], x[1]), pack_half2(x[2], x[3]), pack_half2(x[4], x[5]), pack_half2(x[6], x[7]));
+}
+__device__ __forceinline__ void st_cluster(uint32_t to, const uint4 &v)
+{
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// what was stored to a neighbour's shared memory is to be read by its tensor core
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// Visits the slice in pieces of eight elements that lie together in memory: row i, columns j to j + 7 of X, or, where M > N, column j,
+// rows i to i + 7.  Neighbouring threads take pieces next to each other in shared memory.
+template <typename T, typename Do>
+__device__ __forceinline__ void visit(const Resident &q, const T *x, int n0, int cols, Do act)
+{
+    const bool whole = q.N % 8 == 0;
+    const int across = q.tall ? cols : (cols + 7) / 8, items = across * (q.tall ? (q.m + 7) / 8 : q.m);
+    constexpr int AT_ONCE = 4;
+    for (int i0 = threadIdx.x; i0 < items; i0 += AT_ONCE * kThreads) {
+        float v[AT_ONCE][8];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int it = i0 + u * kThreads;
+            if (it >= items) continue;
+            const int hi = it / across, lo = it - hi * across;
+            if (q.tall) eight(x + (long long)(n0 + lo) * q.N + 8 * hi, whole, q.m - 8 * hi, v[u]);
+            else eight(x + (long long)hi * q.N + n0 + 8 * lo, whole, cols - 8 * lo, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int it = i0 + u * kThreads;
+            if (it >= items) continue;
+            const int hi = it / across, lo = it - hi * across;
+            if (q.tall) act(8 * hi, lo, v[u]);
+            else act(hi, 8 * lo, v[u]);
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__restrict__ x, __nv_bfloat16 *__restrict__ y, const Resident q)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *X = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int groups = (q.w + 63) / 64;
+    uint8_t *G = X + groups * kGroup, *P = G + 2 * kGroup, *parts = P + 2 * kGroup;     // parts: [block][row of 128 / S][128 floats]
+    Scalars &sc = *reinterpret_cast<Scalars *>(parts + (q.S > 1 ? kRows * 512 : 0));
+
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const int rank = (int)(blockIdx.x % (unsigned)q.S), mp = (q.m + 31) / 32 * 32;
+    const int n0 = rank * q.w, cols = max(0, min(q.w, q.n - n0));
+    const long long b = blockIdx.x / (unsigned)q.S;
+    const uint32_t tmem_cols = q.w > 128 ? 512 : 256;
+    if (tid == 0) {
+        tc::mbar_init(&sc.bar, 1);
+        sc.gave_up = 0;
+        tc::fence_barrier_init();
+    }
+    if (warp == 0) {
+        tc::tmem_alloc(&sc.tmem, tmem_cols);
+        tc::tmem_relinquish();
+    }
+    for (int i = tid; i < groups * kGroup / 16; i += kThreads) reinterpret_cast<uint4 *>(X)[i] = make_uint4(0, 0, 0, 0);
+    tc::tc_fence_before_sync();
+    __syncthreads();
+    if (q.S > 1) tc::cluster_sync();                       // all blocks of the cluster run from here on
+    tc::tc_fence_after_sync();
+    const uint32_t tmem = sc.tmem;
+    pdl_wait();
+
+    // the norm, then the slice as fp16; the second reading is the L2's
+    x += b * q.M * q.N;
+    y += b * q.M * q.N;
+    double s = 0.0;
+    visit(q, x, n0, cols, [&](int, int, const float (&v)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { const double d = v[k]; s = fma(d, d, s); }
+    });
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (lane == 0) sc.warp_sum[warp] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int i = 0; i < kThreads / 32; ++i) s += sc.warp_sum[i];
+    if (q.S > 1) {
+        if (tid < q.S) asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(tc::mapa(tc::smem_u32(&sc.norm[rank]), (uint32_t)tid)), "d"(s) : "memory");
+        tc::cluster_sync();
+        s = 0.0;
+        for (int i = 0; i < q.S; ++i) s += sc.norm[i];
+    }
+    float f1, f2;
+    normalizer(s, q.eps, q.s, f1, f2);
+    visit(q, x, n0, cols, [&](int i, int j, float (&v)[8]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = v[k] * f1 * f2;
+        if (q.tall) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i + k < q.m) *reinterpret_cast<__half *>(X + place(i + k, j)) = __float2half_rn(v[k]);
+        } else {
+            *reinterpret_cast<uint4 *>(X + place(i, j)) = pack_half(v);
+        }
+    });
+    tc::fence_proxy_async();
+    __syncthreads();
+
+    const int quarter = warp & 3, row = quarter * 32 + lane, c0 = (warp >> 2) * 32;
+    const bool mine = quarter * 32 < mp;                   // rows behind mp hold nothing that is read
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t idesc_m = instr_desc_f16(128, mp, 0, 0), idesc_x = instr_desc_f16(128, q.w, 0, 1);
+    const uint64_t desc_x = tc::smem_desc(tc::smem_u32(X), 16, 1024), desc_g = tc::smem_desc(tc::smem_u32(G), 16, 1024),
+                   desc_p = tc::smem_desc(tc::smem_u32(P), 16, 1024), desc_xn = tc::smem_desc(tc::smem_u32(X), kGroup, 1024);
+    auto deep = [](int kk) { return (uint64_t)(((kk >> 2) * kGroup + (kk & 3) * 32) >> 4); };     // 16 contraction indices further, K-major
+    uint32_t phase = 0;
+    auto wait = [&] {                                      // for the products of this phase, by all
+        if (warp == 0) tc::mma_commit_elect(&sc.bar);
+        tc::mbar_wait(&sc.bar, phase, &sc.gave_up, q.err, tc::ERR_WAIT_TMEM_FULL);
+        phase ^= 1;
+        __syncwarp();
+        tc::tc_fence_after_sync();
+    };
+    auto handover = [&] {                                  // of shared memory to the tensor core and of TMEM's columns
+        tc::fence_proxy_async();
+        tc::tc_fence_before_sync();
+        __syncthreads();
+        tc::tc_fence_after_sync();
+    };
+    const float alpha = 1.0f / (q.s * q.s);
+    const int k_x = (max(cols, 1) + 15) / 16, k_m = mp / 16, owned = kRows / q.S;
+    for (int step = 0; step < q.steps; ++step) {
+        const bool last = step + 1 == q.steps;
+        if (warp == 0)
+            for (int kk = 0; kk < k_x; ++kk) tc::mma_bf16_elect(tmem, desc_x + deep(kk), desc_x + deep(kk), idesc_m, kk != 0);
+        wait();
+        if (mine && c0 < mp) {
+            uint32_t acc[32];
+            tc::tmem_ld_32x32(tmem + lanes + c0, acc);
+            tc::tmem_ld_wait();
+            if (q.S == 1) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                    float v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        v[k] = alpha * __uint_as_float(acc[j + k]);
+                        if (c0 + j + k == row) { sc.d[row] = v[k]; v[k] = 0.0f; }
+                    }
+                    *reinterpret_cast<uint4 *>(G + place(row, c0 + j)) = pack_half(v);
+                }
+            } else {
+                const int owner = row / owned, at = row - owner * owned;
+                const uint32_t to = tc::mapa(tc::smem_u32(parts), (uint32_t)owner) + (uint32_t)(rank * owned + at) * 512;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    st_cluster(to + (uint32_t)(((c0 / 4 + j) ^ (at & 7)) << 4), make_uint4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]));
+            }
+        }
+        if (q.S > 1) {
+            tc::tc_fence_before_sync();
+            tc::cluster_sync();
+            for (int i = tid; i < owned * (mp / 8); i += kThreads) {
+                const int at = i / (mp / 8), c = (i - at * (mp / 8)) * 8, r = rank * owned + at;
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = 0.0f;
+                for (int o = 0; o < q.S; ++o) {
+                    const uint8_t *from = parts + (o * owned + at) * 512;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float4 t = *reinterpret_cast<const float4 *>(from + (((c / 4 + h) ^ (at & 7)) << 4));
+                        v[4 * h] += t.x; v[4 * h + 1] += t.y; v[4 * h + 2] += t.z; v[4 * h + 3] += t.w;
+                    }
+                }
+                const bool diagonal = r >= c && r < c + 8;
+                float d = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] *= alpha;
+                    if (c + k == r) { d = v[k]; v[k] = 0.0f; }
+                }
+                const uint4 g = pack_half(v);
+                for (int o = 0; o < q.S; ++o) {
+                    st_cluster(tc::mapa(tc::smem_u32(G + place(r, c)), (uint32_t)o), g);
+                    if (diagonal) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(tc::mapa(tc::smem_u32(&sc.d[r]), (uint32_t)o)), "f"(d) : "memory");
+                }
+            }
+            fence_proxy_async_all();
+            tc::cluster_sync();
+            fence_proxy_async_all();
+            tc::tc_fence_after_sync();
+        } else {
+            handover();
+        }
+
+        if (warp == 0)
+            for (int kk = 0; kk < k_m; ++kk) tc::mma_bf16_elect(tmem, desc_g + deep(kk), desc_g + deep(kk), idesc_m, kk != 0);
+        wait();
+        if (mine && c0 < mp) {
+            uint32_t acc[32];
+            tc::tmem_ld_32x32(tmem + lanes + c0, acc);
+            const float d_row = sc.d[row];
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+                float v[8];
+                unpack_half(*reinterpret_cast<const uint4 *>(G + place(row, c0 + j)), v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float gg = __uint_as_float(acc[j + k]);
+                    v[k] = fmaf(q.c, gg, fmaf(q.c, d_row + sc.d[c0 + j + k], q.b) * v[k]);
+                    if (c0 + j + k == row) {
+                        sc.e[row] = q.a + d_row * q.b + q.c * fmaf(d_row, d_row, gg);
+                        v[k] = 0.0f;
+                    }
+                }
+                *reinterpret_cast<uint4 *>(P + place(row, c0 + j)) = pack_half(v);
+            }
+        }
+        handover();
+
+        if (warp == 0)
+            for (int kk = 0; kk < k_m; ++kk) tc::mma_bf16_elect(tmem + 128, desc_p + deep(kk), desc_xn + (uint64_t)(kk * 2048 >> 4), idesc_x, kk != 0);
+        wait();
+        if (mine) {
+            const float e_row = sc.e[row], out = q.scale / q.s;
+            for (int c = c0; c < q.w; c += 128) {
+                uint32_t acc[32];
+                tc::tmem_ld_32x32(tmem + 128 + lanes + c, acc);
+                tc::tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                    uint4 *at = reinterpret_cast<uint4 *>(X + place(row, c + j));
+                    float v[8];
+                    unpack_half(*at, v);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = fmaf(e_row, v[k], __uint_as_float(acc[j + k]));
+                    if (!last) {
+                        *at = pack_half(v);
+                        continue;
+                    }
+                    __nv_bfloat16 h[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) h[k] = __float2bfloat16_rn(out * v[k]);
+                    if (q.tall) {                          // a warp's rows lie next to each other in y
+                        __nv_bfloat16 *to = y + (long long)(n0 + c + j) * q.N + row;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (row < q.m && c + j + k < cols && relay_in_bounds(to + (long long)k * q.N, 2)) to[(long long)k * q.N] = h[k];
+                    } else {
+                        *at = *reinterpret_cast<const uint4 *>(h);
+                    }
+                }
+            }
+        }
+        handover();
+    }
+    if (!q.tall) {
+        if (q.N % 8 == 0) {
+            const int across = cols / 8;
+            for (int i = tid; i < q.m * across; i += kThreads) {
+                const int r = i / across, c = (i - r * across) * 8;
+                __nv_bfloat16 *to = y + (long long)r * q.N + n0 + c;
+                if (relay_in_bounds(to, 16)) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(X + place(r, c));
+            }
+        } else {
+            for (int i = tid; i < q.m * cols; i += kThreads) {
+                const int r = i / cols, c = i - r * cols;
+                __nv_bfloat16 *to = y + (long long)r * q.N + n0 + c;
+                if (relay_in_bounds(to, 2)) *to = *reinterpret_cast<const __nv_bfloat16 *>(X + place(r, c));
+            }
+        }
+    }
+    __syncthreads();
+    if (warp == 0) tc::tmem_dealloc(tmem, tmem_cols);
+}
+
+template <typename T>
+relay_status_t launch(const relay_tensor_t *x, const relay_tensor_t *y, int64_t L, const Resident &q, size_t smem, cudaStream_t st)
+{
+    RELAY_CUDA(cudaFuncSetAttribute(orth_resident_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    RELAY_CUDA(launch_pdl_cluster(orth_resident_kernel<T>, dim3((unsigned)(L * q.S)), dim3(kThreads), dim3((unsigned)q.S), smem, st, (const T *)x->data,
+                                  (__nv_bfloat16 *)y->data, q));
+    return check_launch("orthogonalize_resident");
+}
+
+}  // namespace
+
+bool resident_fits(int64_t m, int64_t n) { return m <= kRows && n <= (int64_t)kMostBlocks * kWidest; }
+
+relay_status_t launch_resident(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *at, const relay_tensor_t *y, int64_t L, int M, int N, float s, cudaStream_t st)
+{
+    Resident q;
+    q.M = M; q.N = N; q.m = std::min(M, N); q.n = std::max(M, N);
+    q.tall = M > N; q.steps = at->steps;
+    q.S = 1;
+    while (q.S * kWidest < q.n) q.S *= 2;
+    q.w = ((q.n + q.S - 1) / q.S + 31) / 32 * 32;
+    q.a = at->a; q.b = at->b; q.c = at->c; q.eps = at->eps; q.s = s; q.scale = at->scale;
+    q.err = device_error_word();
+    if (!q.err) return fail(RELAY_ERR_CUDA, "no device error word");
+    const size_t smem = 1024 + (size_t)((q.w + 63) / 64 + 4) * kGroup + (q.S > 1 ? kRows * 512 : 0) + sizeof(Scalars);
+    BoundsReg reg;
+    reg.add(x); reg.add(y);
+    RELAY_TRY(reg.commit(st));
+    if (x->dtype == RELAY_F32) return launch<float>(x, y, L, q, smem, st);
+    return launch<__nv_bfloat16>(x, y, L, q, smem, st);
+}
+
+}  // namespace orth
+}  // namespace relay

@@ -44,16 +44,6 @@ __host__ __device__ constexpr int cls_stage_bytes(int c) { return A_BYTES + c * 
 __host__ __device__ constexpr int cls_bar_base(int c) { return c == 1 ? 0 : c == 2 ? 16 : c == 3 ? 28 : 36; }   // full[], then empty[]
 constexpr int BAR_TMEM = 44;                               // tmem_full[2], tmem_empty[2]
 
-__device__ __forceinline__ uint32_t instr_desc_f16(int m, int n, int a_mn, int b_mn)
-{   // fp32 accumulator, fp16 A and B (format 0), majorness, N / 8, M / 16
-    return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
-{
-    __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<uint32_t *>(&v);
-}
-
 // Each width class has barriers of its own over the same shared memory.  A class that is left and taken up again goes on where it
 // stood: its barriers remember how often their stages went round.
 struct Rings {
