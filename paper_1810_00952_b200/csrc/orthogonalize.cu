@@ -99,10 +99,10 @@ __global__ void __launch_bounds__(kNormThreads) orth_convert_kernel(const T *__r
 
 // ---- small matrices: one block each -----------------------------------------------------------------------------
 constexpr int kSmallThreads = 256;
-constexpr int64_t kSmallSide = 64, kSmallSize = 64 * 96;
+constexpr int64_t kSmallSize = 512;
 // rows of shared memory: whole float4, an odd number of them, so that rows next to each other start on other banks
 __host__ __device__ inline int small_ld(int n) { return ((n + 3) / 4 | 1) * 4; }
-inline bool small_fits(int64_t m, int64_t n) { return m <= kSmallSide && m * n <= kSmallSize; }
+inline bool small_fits(int64_t m, int64_t n) { return m * n <= kSmallSize; }
 inline size_t small_smem(int m, int n)
 {
     const int rm = (m + 3) / 4 * 4;

@@ -3,12 +3,13 @@
 // One cluster of S = 1..8 blocks per matrix.  Each block keeps a slice of at most 256 of the n columns of X (of X^T where M > N) in
 // shared memory as fp16, and copies of G and P: a product's operands never leave the SM.  The slice's layout, groups of 64 columns
 // with 128-byte rows swizzled, is K-major for G = X X^T and MN-major for P X at once.  Per step:
-//   G      over the slice's columns, accumulated in TMEM; with S > 1 the blocks' parts are sent to the block that owns the row
-//          (128 / S rows each), added there in the order of the blocks, and the sum in fp16 is sent to all
+//   G      over the slice's columns, accumulated in TMEM; with S > 1 the blocks' parts are sent to the block that owns the row, added
+//          there in the order of the blocks, and the sum is sent to all as fp16
 //   P      = b G + c G G by every block for itself: 128^3 products are less than an exchange
 //   X      <- e X + offdiag(P) X in place
-// with the diagonals apart in fp32, as in the products of larger matrices.  Every phase ends in a barrier of the block (twice a
-// step of the cluster), so what bounds a step is its chain of latencies: three times MMA, TMEM to registers, shared memory.
+// with the diagonals apart in fp32, as in the products of larger matrices.  Every phase ends in a barrier of the block, so what
+// bounds a step is its chain of latencies: three times MMA, TMEM to registers, shared memory (4.7 us at 128 x 256); and the exchange
+// of G (3.3 us between two blocks, 5 between eight; by st.async, whose every 16 bytes update a barrier, 5 and 5).
 #include <algorithm>
 
 #include "common.h"
@@ -59,34 +60,37 @@ __device__ __forceinline__ void st_cluster(uint32_t to, const uint4 &v)
 // what was stored to a neighbour's shared memory is to be read by its tensor core
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
-// Visits the slice in pieces of eight elements that lie together in memory: row i, columns j to j + 7 of X, or, where M > N, column j,
-// rows i to i + 7.  Neighbouring threads take pieces next to each other in shared memory.
-template <typename T, typename Do>
-__device__ __forceinline__ void visit(const Resident &q, const T *x, int n0, int cols, Do act)
-{
-    const bool whole = q.N % 8 == 0;
-    const int across = q.tall ? cols : (cols + 7) / 8, items = across * (q.tall ? (q.m + 7) / 8 : q.m);
-    constexpr int AT_ONCE = 4;
-    for (int i0 = threadIdx.x; i0 < items; i0 += AT_ONCE * kThreads) {
-        float v[AT_ONCE][8];
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const int it = i0 + u * kThreads;
-            if (it >= items) continue;
-            const int hi = it / across, lo = it - hi * across;
-            if (q.tall) eight(x + (long long)(n0 + lo) * q.N + 8 * hi, whole, q.m - 8 * hi, v[u]);
-            else eight(x + (long long)hi * q.N + n0 + 8 * lo, whole, cols - 8 * lo, v[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const int it = i0 + u * kThreads;
-            if (it >= items) continue;
-            const int hi = it / across, lo = it - hi * across;
-            if (q.tall) act(8 * hi, lo, v[u]);
-            else act(hi, 8 * lo, v[u]);
-        }
+// The slice in registers, as pieces of eight elements that lie together in memory: columns j to j + 7 of row i of X, or, where
+// M > N, rows i to i + 7 of column j.  A warp's pieces are next to each other in memory, or four of them by sixteen columns, two
+// to a thread: what it stores side by side then shares few banks.
+constexpr int kPieces = kRows * kWidest / 8 / kThreads;
+struct Pieces {
+    int i, j;                          // of the present piece
+    int hi, lo, across, by_hi, by_lo, tall;
+    __device__ __forceinline__ explicit Pieces(const Resident &q)
+    {
+        tall = q.tall;
+        across = tall ? q.w / 16 : q.w / 8;
+        const int first = tall ? (int)(threadIdx.x >> 5) : (int)threadIdx.x, by = tall ? kThreads / 32 : kThreads;
+        hi = first / across; lo = first - hi * across;
+        by_hi = by / across; by_lo = by - by_hi * across;
+        set(0);
     }
-}
+    __device__ __forceinline__ void set(int u)
+    {
+        const int lane = threadIdx.x & 31;
+        i = tall ? 8 * (hi * 4 + (lane >> 3)) : hi;
+        j = tall ? lo * 16 + (lane & 7) * 2 + (u & 1) : lo * 8;
+    }
+    __device__ __forceinline__ void next(int u)                       // on from piece u
+    {
+        if (!tall || (u & 1)) {
+            hi += by_hi; lo += by_lo;
+            if (lo >= across) { lo -= across; ++hi; }
+        }
+        set(u + 1);
+    }
+};
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__restrict__ x, __nv_bfloat16 *__restrict__ y, const Resident q)
@@ -94,7 +98,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
     extern __shared__ uint8_t smem_raw[];
     uint8_t *X = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int groups = (q.w + 63) / 64;
-    uint8_t *G = X + groups * kGroup, *P = G + 2 * kGroup, *parts = P + 2 * kGroup;     // parts: [block][row of 128 / S][128 floats]
+    uint8_t *G = X + groups * kGroup, *P = G + 2 * kGroup, *parts = P + 2 * kGroup;     // parts: [block][row][128 floats]
     Scalars &sc = *reinterpret_cast<Scalars *>(parts + (q.S > 1 ? kRows * 512 : 0));
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -119,14 +123,34 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
     const uint32_t tmem = sc.tmem;
     pdl_wait();
 
-    // the norm, then the slice as fp16; the second reading is the L2's
+    // the slice, its norm, and the slice as fp16
     x += b * q.M * q.N;
     y += b * q.M * q.N;
-    double s = 0.0;
-    visit(q, x, n0, cols, [&](int, int, const float (&v)[8]) {
+    float v[kPieces][8];
+    const bool whole = q.N % 8 == 0;
+    float most = 0.0f;
+    Pieces in(q);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { const double d = v[k]; s = fma(d, d, s); }
-    });
+    for (int u = 0; u < kPieces; ++u, in.next(u - 1)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[u][k] = 0.0f;
+        if (in.i >= q.m || in.j >= cols) continue;
+        if (q.tall) eight(x + (long long)(n0 + in.j) * q.N + in.i, whole, q.m - in.i, v[u]);
+        else eight(x + (long long)in.i * q.N + n0 + in.j, whole, cols - in.j, v[u]);
+    }
+    // a thread's squares in fp32, of values scaled to the largest one's exponent; their sum goes on in fp64, where any square fits
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(v[u][k]));
+    const int exponent = min(__float_as_int(most) >> 23, 253);
+    const float unit = __int_as_float((254 - exponent) << 23);
+    float squares = 0.0f;
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { const float t = v[u][k] * unit; squares = fmaf(t, t, squares); }
+    double s = (double)squares * __longlong_as_double((long long)(1023 + 2 * (exponent - 127)) << 52);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
     if (lane == 0) sc.warp_sum[warp] = s;
@@ -141,17 +165,21 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
     }
     float f1, f2;
     normalizer(s, q.eps, q.s, f1, f2);
-    visit(q, x, n0, cols, [&](int i, int j, float (&v)[8]) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = v[k] * f1 * f2;
-        if (q.tall) {
+    for (int u = 0; u < kPieces; ++u)
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (i + k < q.m) *reinterpret_cast<__half *>(X + place(i + k, j)) = __float2half_rn(v[k]);
-        } else {
-            *reinterpret_cast<uint4 *>(X + place(i, j)) = pack_half(v);
+        for (int k = 0; k < 8; ++k) v[u][k] = v[u][k] * f1 * f2;
+    Pieces to(q);
+#pragma unroll
+    for (int u = 0; u < kPieces; ++u, to.next(u - 1)) {
+        if (to.i >= q.m || to.j >= cols) continue;
+        if (!q.tall) {
+            *reinterpret_cast<uint4 *>(X + place(to.i, to.j)) = pack_half(v[u]);
+        } else if (u % 2 == 0) {                           // its second column is zero behind the last
+#pragma unroll
+            for (int k = 0; k < 8; ++k) *reinterpret_cast<uint32_t *>(X + place(to.i + k, to.j)) = pack_half2(v[u][k], v[u + 1][k]);
         }
-    });
+    }
     tc::fence_proxy_async();
     __syncthreads();
 
@@ -177,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
         tc::tc_fence_after_sync();
     };
     const float alpha = 1.0f / (q.s * q.s);
-    const int k_x = (max(cols, 1) + 15) / 16, k_m = mp / 16, owned = kRows / q.S;
+    const int k_x = (max(cols, 1) + 15) / 16, k_m = mp / 16, owned = mp / q.S;
     for (int step = 0; step < q.steps; ++step) {
         const bool last = step + 1 == q.steps;
         if (warp == 0)
@@ -203,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
                 const uint32_t to = tc::mapa(tc::smem_u32(parts), (uint32_t)owner) + (uint32_t)(rank * owned + at) * 512;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    st_cluster(to + (uint32_t)(((c0 / 4 + j) ^ (at & 7)) << 4), make_uint4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]));
+                    st_cluster(to + (uint32_t)(((c0 / 4 + j) ^ (row & 7)) << 4), make_uint4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]));
             }
         }
         if (q.S > 1) {
@@ -218,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
                     const uint8_t *from = parts + (o * owned + at) * 512;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float4 t = *reinterpret_cast<const float4 *>(from + (((c / 4 + h) ^ (at & 7)) << 4));
+                        const float4 t = *reinterpret_cast<const float4 *>(from + (((c / 4 + h) ^ (r & 7)) << 4));
                         v[4 * h] += t.x; v[4 * h + 1] += t.y; v[4 * h + 2] += t.z; v[4 * h + 3] += t.w;
                     }
                 }
@@ -235,6 +263,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
                     if (diagonal) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(tc::mapa(tc::smem_u32(&sc.d[r]), (uint32_t)o)), "f"(d) : "memory");
                 }
             }
+            // Behind this barrier every block has read its parts: they may be sent again.  G is sent again only behind the next
+            // step's first barrier, which follows every block's last look at this one.
             fence_proxy_async_all();
             tc::cluster_sync();
             fence_proxy_async_all();

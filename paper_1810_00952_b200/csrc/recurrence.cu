@@ -521,28 +521,6 @@ __device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map<F, V> 
     for (int i = 0; i < (int)(sizeof(m) / 8); ++i)
         asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.u32 [%0], {%1, %2}, [%3];" ::"r"(to + 8 * i), "r"(w[i].x), "r"(w[i].y), "r"(bar) : "memory");
 }
-__device__ __forceinline__ bool try_wait_cluster(uint64_t *bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred P;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 P, [%1], %2;\n\tselp.u32 %0, 1, 0, P;\n\t}\n"
-                 : "=r"(ok) : "r"(tc::smem_u32(bar)), "r"(parity) : "memory");
-    return ok != 0;
-}
-// Bounded: a warp that gives up records it, and this block's later waits end at once (its results are then not to be used).
-__device__ __forceinline__ void wait_arrived(uint64_t *bar, uint32_t parity, int *gave_up, int *err)
-{
-    if (try_wait_cluster(bar, parity)) return;
-    const long long began = clock64();
-    while (!try_wait_cluster(bar, parity)) {
-        if (*(volatile int *)gave_up) return;
-        if (clock64() - began > tc::kWaitLimitCycles) {
-            *(volatile int *)gave_up = 1;
-            atomicCAS(err, 0, tc::ERR_WAIT_EXCHANGE);
-            return;
-        }
-    }
-}
-
 // Joins the maps of all threads of a lane's channels over the slab.  Warp 0 does it for the block (eight warps doing it each for
 // themselves would execute more instructions than the steps do); its `state` is the state before the slab on entry, behind it on
 // return.  The result is the state before this thread's own span.
@@ -576,7 +554,7 @@ __device__ __forceinline__ void join_slab(Joints<F, V> &j, const Map<F, V> &mine
                 if (r < S) send(tc::mapa(to, (uint32_t)r), tc::mapa(bar, (uint32_t)r), all);
             // A neighbour sends for slab i + 2 only when it has this block's message for slab i + 1, which this warp sends after it
             // has read slab i's: two buffers are enough.
-            wait_arrived(&j.arrived[buf], (slab >> 1) & 1, &j.gave_up, err);
+            tc::wait_arrived(&j.arrived[buf], (slab >> 1) & 1, &j.gave_up, err);
 #pragma unroll
             for (int r = 0; r < 8; ++r)
                 if (r < S) m[r] = j.block[buf][r][lane];
@@ -957,7 +935,7 @@ __device__ __forceinline__ void join_slabs(Exchange<F, V> &x, const Args &p, con
         if (q.S > 1) {
             // A neighbour sends for slab i + 2 only when it has this block's message for slab i + 1, which this warp sends after
             // it has read slab i's: two buffers are enough.
-            wait_arrived(&x.arrived[buf], turn.phase, &x.gave_up, p.err);
+            tc::wait_arrived(&x.arrived[buf], turn.phase, &x.gave_up, p.err);
 #pragma unroll
             for (int r0 = 0; r0 < 8; r0 += HELD) {
 #pragma unroll

@@ -69,6 +69,29 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
     return true;
 }
 
+// What blocks of a cluster send each other with st.async: the bytes and the count that completes the receiver's barrier travel together.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred P;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 P, [%1], %2;\n\tselp.u32 %0, 1, 0, P;\n\t}\n"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded: a warp that gives up records it, and this block's later waits end at once (its results are then not to be used).
+__device__ __forceinline__ void wait_arrived(uint64_t *bar, uint32_t parity, int *gave_up, int *err)
+{
+    if (mbar_try_wait_cluster(bar, parity)) return;
+    const long long began = clock64();
+    while (!mbar_try_wait_cluster(bar, parity)) {
+        if (*(volatile int *)gave_up) return;
+        if (clock64() - began > kWaitLimitCycles) {
+            *(volatile int *)gave_up = 1;
+            atomicCAS(err, 0, ERR_WAIT_EXCHANGE);
+            return;
+        }
+    }
+}
+
 // cross-block hand-over through global memory: a counter written with release and polled with acquire
 __device__ __forceinline__ unsigned int ld_acquire_u32(const unsigned int *p)
 {

@@ -64,6 +64,17 @@ def test_shapes(M, N, dt):
     close(run(x), L.orthogonalize(to_np(x), 5, QUINTIC, 1e-7, 1.0))
 
 
+# either side of the sizes at which another kernel takes over: 512 elements, 128 rows, 256 columns for each of 1, 2, 4, 8 blocks
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(16, 32), (19, 27), (1, 512), (1, 513), (32, 32), (1, 1025), (33, 33), (2, 600), (16, 65), (40, 40), (97, 97), (128, 256), (256, 128), (128, 257), (257, 128),
+                                   (31, 513), (128, 1000), (1000, 128), (128, 1024), (1025, 97), (120, 2048), (2048, 120), (3, 2047), (2047, 3), (128, 2049),
+                                   (129, 129), (9, 40, 300), (20, 300, 40), (30, 128, 2048)])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_sizes_at_which_the_kernel_changes(shape, dt):
+    x = matrices(shape, dt, sum(shape))
+    close(run(x), L.orthogonalize(to_np(x), 5, QUINTIC, 1e-7, 1.0))
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", [(3, 70, 90), (2, 3, 90, 70), (5, 130, 130), (40, 16, 16), (2, 2, 2, 2, 33, 65), (1, 600, 600), (200, 8, 40)])
 @pytest.mark.parametrize("dt", [F32, BF16])
