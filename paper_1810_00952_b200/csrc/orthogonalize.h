@@ -34,7 +34,7 @@ struct Product {
 struct UnitTable {
     static constexpr int kMax = 640;
     int n;
-    uint32_t e[kMax];                  // row block (256 rows) | first 128-column chunk << 8 | chunks << 17
+    uint32_t e[kMax];                  // row block (256 rows) | first piece of 64 columns << 8 | pieces << 19
 };
 
 // tensor maps of one launch: X in both buffers, with its columns or its rows as contraction index, G and P (64: boxes for B)

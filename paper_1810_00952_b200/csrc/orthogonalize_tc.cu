@@ -4,7 +4,8 @@
 // What bounds a product here is how fast an SM can fill its shared memory (about 48 bytes a cycle): a k-step of 64 over 256 x 128 c
 // columns costs a pair max(256 c cycles of MMA, (16 + 8 c) KB per SM / 48 B).  256 x 512 (c = 4) balances the two, but fills both
 // TMEM accumulators, so its epilogue is not overlapped; c <= 2 leaves the other accumulator to the next unit.  The host cuts each
-// product into units of c = 1..4 chunks of 128 columns, whichever cut finishes first (see plan below).  Symmetric products have
+// product into units of 64 columns or c = 1..4 chunks of 128, whichever cut finishes first (see plan below): small matrices into
+// units of 64, whose epilogue, the part of a phase that nothing hides, is the shortest.  Symmetric products have
 // units on and above the diagonal only.
 //
 // The pairs run through all units of all phases (three per step) in one order.  A unit of matrix b needs every unit of b's phase
@@ -12,6 +13,11 @@
 // Matrices of a batch so run into each other's phases, and between two phases of one matrix lie a few microseconds instead of the
 // end of one kernel and the start of the next.  All pairs are resident (the grid is what fits at once), every unit's needs come
 // before it in the order, and all waits are bounded.
+//
+// Measured at 4096 x 4096: 1.33 ms, 1.04 PFLOP/s; per step of 222 us the MMAs take 163 (at the power-limited clock) and the three
+// changes of phase 59, in which the last unit's epilogue runs with all SMs storing at once.  One launch per product: 1.39 ms for 8 x 1024
+// x 4096 against 0.85, 194 us for 3 x 500 x 333 against 122 (112 since units of 64 columns).  Epilogues with TMA stores, with sixteen warps, or in line with the roles
+// were slower (sixteen warps and the in-line form spill registers).
 //
 // Roles per block: warp 0 loads A, the last warp loads B, warp 1 of the leader issues the MMAs, eight warps are the epilogue.  full[] lives
 // in the leader; empty[] and tmem_full[] in each block, by multicast commits; tmem_empty[] in the leader.
@@ -104,8 +110,8 @@ struct Walk {
             w.batch = (int)(unit / t.n);                   // matrix by matrix: while the last ones are in this phase, the first have
             const uint32_t e = t.e[unit - (long long)w.batch * t.n];       // long been counted and can enter the next
             w.m0 = (int)(e & 0xffu) * 256;
-            w.n0 = (int)((e >> 8) & 0x1ffu) * 128;
-            w.width = (int)(e >> 17) * 128;
+            w.n0 = (int)((e >> 8) & 0x7ffu) * 64;
+            w.width = (int)(e >> 19) * 64;
             return w;
         }
         const Product &p = l.product[kind];
@@ -413,7 +419,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
         for (Walk walk(l, pair, pairs); walk.more() && ok; walk.next()) {
             const Unit w = walk.at();
             const Product &p = walk.product();
-            const int c = w.width >> 7;
+            const int c = max(1, w.width >> 7);
             if (c != cur) {
                 rings.leave(cur, s, phase);
                 // the new class's stages lie over the old one's: every old stage must have been released
@@ -433,10 +439,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
                               : l.tall ? (load_a ? X_K0 + walk.cur : (int)P_K64) : (load_a ? (int)P_K : X_MN0 + walk.cur);
             const CUtensorMap *map = &l.map[which];
             // the first MMA of a 16-deep step covers 2 h0 columns, the second 2 h1; this block holds h0 + h1 of them
-            const int h0 = c == 1 ? 64 : 128, h1 = c == 3 ? 64 : c == 4 ? 128 : 0;
+            const int h0 = w.width == 64 ? 32 : c == 1 ? 64 : 128, h1 = c == 3 ? 64 : c == 4 ? 128 : 0;
             const int m0 = w.m0 + (int)rank * 128;
             const int na = w.n0 + (int)rank * h0, nb = w.n0 + 2 * h0 + (int)rank * h1;
-            const int boxes0 = h0 >> 6, boxes = (h0 + h1) >> 6;
+            const int boxes0 = max(1, h0 >> 6), boxes = boxes0 + (h1 >> 6);         // 64 columns: of one box only the first half is used
             const uint32_t tx = 2u * (uint32_t)st_bytes;                            // bytes of both blocks
             for (int kb = 0; kb < p.k_blocks; ++kb) {
                 ok = __all_sync(0xffffffffu, tc::mbar_wait(&empty[s], phase ^ 1, abort_flag, l.err, tc::ERR_WAIT_EMPTY));
@@ -476,7 +482,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
             for (Walk walk(l, pair, pairs); walk.more() && ok; walk.next()) {
                 const Unit w = walk.at();
                 const Product &p = walk.product();
-                const int c = w.width >> 7;
+                const int c = max(1, w.width >> 7);
                 if (c != cur) {
                     rings.leave(cur, s, phase);
                     cur = c; n_st = cls_stages(c); st_bytes = cls_stage_bytes(c);
@@ -489,7 +495,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
                 const uint32_t a_step = p.a_mn ? 2048 : 32, b_step = p.b_mn ? 2048 : 32;
                 const uint64_t desc_a0 = tc::smem_desc(tc::smem_u32(smem), p.a_mn ? MN_BOX_BYTES : 16, 1024);
                 const uint64_t desc_b0 = tc::smem_desc(tc::smem_u32(smem) + A_BYTES, p.b_mn ? MN_BOX_BYTES : 16, 1024);
-                const uint32_t idesc_256 = instr_desc_f16(256, 256, p.a_mn, p.b_mn), idesc_128 = instr_desc_f16(256, 128, p.a_mn, p.b_mn);
+                const uint32_t idesc_256 = instr_desc_f16(256, 256, p.a_mn, p.b_mn), idesc_128 = instr_desc_f16(256, 128, p.a_mn, p.b_mn), idesc_64 = instr_desc_f16(256, 64, p.a_mn, p.b_mn);
                 const bool both = c >= 3;                  // both accumulators, in the order in which they come free
                 const int buf = t_local & 1;
                 if (!__all_sync(0xffffffffu, tc::mbar_wait(&tmem_empty[buf], ((t_local >> 1) & 1) ^ 1, abort_flag, l.err, tc::ERR_WAIT_TMEM_EMPTY))) break;
@@ -497,7 +503,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
                     break;
                 tc::tc_fence_after_sync();
                 const uint32_t d0 = tmem_base + buf * BN, d1 = tmem_base + (buf ^ 1) * BN;
-                const uint32_t idesc0 = c == 1 ? idesc_128 : idesc_256, idesc1 = c == 3 ? idesc_128 : idesc_256;
+                const uint32_t idesc0 = w.width == 64 ? idesc_64 : c == 1 ? idesc_128 : idesc_256, idesc1 = c == 3 ? idesc_128 : idesc_256;
                 for (int kb = 0; kb < p.k_blocks; ++kb) {
                     ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[s], phase, abort_flag, l.err, tc::ERR_WAIT_FULL));
                     if (!ok) break;
@@ -566,62 +572,66 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
     }
 }
 
-// ---- plan --------------------------------------------------------------------------------------------------------------
-double main_cycles(int c, int k_blocks) { return k_blocks * std::max(256.0 * c, (16.0 + 8.0 * c) * 1024.0 / 48.0); }
-double epilogue_cycles(int c) { return 1500.0 + 2500.0 * c; }
+// ---- plan: widths c in pieces of 64 columns, 1 or an even number up to 8 -----------------------------------------------------
+double main_cycles(int c, int k_blocks) { return k_blocks * std::max(128.0 * c, (16.0 + 4.0 * std::max(c, 2)) * 1024.0 / 48.0); }
+double epilogue_cycles(int c) { return 1500.0 + 1250.0 * c; }
+constexpr int kWidths[] = {1, 2, 4, 6, 8};
+int width_of(long long pieces) { return pieces <= 1 ? 1 : (int)((pieces + 1) / 2 * 2); }
 
-// Cuts the rows of chunks of one matrix into units, taking widths from `rounds` (one width for each `quota` units, the last one
+// Cuts the rows of pieces of one matrix into units, taking widths from `rounds` (one width for each `quota` units, the last one
 // for whatever follows); false if they are more than the table holds.
 bool cut(const Product &p, int quota0, const std::vector<int> &rounds, std::vector<uint32_t> *units)
 {
-    const int cpr = (p.cols + 127) / 128;
+    const int per_row = (p.cols + 63) / 64;
     units->clear();
     size_t r = 0;
     int quota = quota0;
     for (int m = 0; m < p.tiles_m; ++m) {
-        int at = p.symmetric ? 2 * m : 0;
-        while (at < cpr) {
-            const int c = std::min(rounds[std::min(r, rounds.size() - 1)], cpr - at);
+        int at = p.symmetric ? 4 * m : 0;
+        while (at < per_row) {
+            const int c = std::min(rounds[std::min(r, rounds.size() - 1)], width_of(per_row - at));
             if (units->size() == (size_t)UnitTable::kMax) return false;
-            units->push_back((uint32_t)m | ((uint32_t)at << 8) | ((uint32_t)c << 17));
+            units->push_back((uint32_t)m | ((uint32_t)at << 8) | ((uint32_t)c << 19));
             at += c;
             if (--quota == 0) { quota = quota0; ++r; }
         }
     }
-    std::stable_sort(units->begin(), units->end(), [](uint32_t a, uint32_t b) { return (a >> 17) > (b >> 17); });
+    std::stable_sort(units->begin(), units->end(), [](uint32_t a, uint32_t b) { return (a >> 19) > (b >> 19); });
     return true;
 }
 // The phase's length: each round over the pairs takes as long as its widest unit; a wide unit's epilogue is in the way of the next
-// unit, and the last unit's is always in the way of the next phase.
+// unit, and the last unit's is always in the way of the next phase.  A matrix's units come widest first, so the widest of a round is
+// its first or, where another matrix begins in it, the widest of all.  Of very many rounds the first few stand for all.
 double finish_time(const std::vector<uint32_t> &units, int batch, int pairs, int k_blocks)
 {
+    constexpr long long kLook = 256;
     double t = 0, last = 0;
-    const long long n = (long long)units.size() * batch;
-    for (long long i = 0; i < n; i += pairs) {
-        int c = 0;
-        for (long long k = i; k < std::min<long long>(n, i + pairs); ++k) c = std::max(c, (int)(units[(size_t)(k % (long long)units.size())] >> 17));
-        if (c >= 3 && last > 0) t += last;
+    const long long size = (long long)units.size(), n = size * batch, rounds = (n + pairs - 1) / pairs;
+    for (long long r = 0; r < std::min(rounds, kLook); ++r) {
+        const long long at = r * pairs % size;
+        const int c = (int)(units[at + std::min<long long>(pairs, n - r * pairs) > size ? 0 : (size_t)at] >> 19);
+        if (c >= 6 && last > 0) t += last;
         t += main_cycles(c, k_blocks);
         last = epilogue_cycles(c);
     }
-    return t + last;
+    return (t + last) * std::max(1.0, (double)rounds / (double)kLook);
 }
-// the cut that finishes first: one width throughout, or as many chunks as a pair's share has, the widest first
+// the cut that finishes first: one width throughout, or as many pieces as a pair's share has, the widest first
 void plan(Product *p, int batch, int pairs, UnitTable *tb)
 {
     p->tiles_m = (p->rows + 255) / 256;
     p->units = p->symmetric ? p->tiles_m * (p->tiles_m + 1) / 2 : p->tiles_m * ((p->cols + 255) / 256);
     tb->n = 0;
-    const int cpr = (p->cols + 127) / 128;
+    const int per_row = (p->cols + 63) / 64;
     long long total = 0;
-    for (int m = 0; m < p->tiles_m; ++m) total += std::max(0, cpr - (p->symmetric ? 2 * m : 0));
+    for (int m = 0; m < p->tiles_m; ++m) total += std::max(0, per_row - (p->symmetric ? 4 * m : 0));
     const int quota = std::max(1, pairs / batch);
     std::vector<uint32_t> units, best;
     double best_time = 0;
-    for (int widest = 1; widest <= 4; ++widest)
+    for (int widest : kWidths)
         for (int share = 0; share < 2; ++share) {
             std::vector<int> rounds;
-            if (share) for (long long left = (total + quota - 1) / quota; left > 0; left -= rounds.back()) rounds.push_back((int)std::min<long long>(widest, left));
+            if (share) for (long long left = (total + quota - 1) / quota; left > 0; left -= rounds.back()) rounds.push_back(std::min(widest, width_of(left)));
             else rounds.push_back(widest);
             if (!cut(*p, quota, rounds, &units)) continue;
             const double t = finish_time(units, batch, pairs, p->k_blocks);

@@ -1,5 +1,13 @@
 // Gated linear recurrence over a sequence, h_t = a_t h_{t-1} + b_t per channel, and its gradient group (Section 4.2 of the
 // paper: reverse mode through the recursion over time).  Elementwise steps: HBM-bound where the channels fill the GPU.
+//
+// Bytes: the forward group reads f and u and writes h once, the gradient reads f, u, h, dh and writes df, du once.  Measured against
+// a copy at 6.53 TB/s: 16384 x 1 x 4096 in bf16 80 us (5.0 TB/s), gradient of 4096 x 8 x 1024 in bf16 83 us (4.85 TB/s), the same
+// forward in fp32 115 us (3.5 TB/s, bound by its instructions, fp64 states among them).  Short of that the length of the chain counts:
+// 128 x 64 x 1024 in bf16 15 us (3.4 TB/s), one step of 64 x 1024 7.5 us, nearly all of it the call and the launch.
+//
+// Three forms: step by step, a thread per channel (few steps); the time axis cut into spans that stay in registers (rows that are not
+// whole 16-byte pieces); the same with tiles fetched ahead by TMA and a warp that only joins (all others).
 #include <algorithm>
 #include <type_traits>
 
@@ -786,6 +794,8 @@ __global__ void __launch_bounds__(32 * kWarps, 2) recurrence_grad_spans_kernel(c
 //   - a ninth warp joins: it takes the spans' maps, tells the cluster, collects its blocks' maps and hands the state back, while
 //     the other warps already compose the next slab and only then run the current one;
 //   - a cluster stays for several tiles of channels, whose slabs follow each other without a gap.
+// 16384 x 1 x 4096 in bf16: spans in registers 122 us, tiles with all warps joining 140 (8 steps a thread) and 100 (16), with the
+// joining warp and one slab composed ahead 80.  4096 x 13 x D, forward in bf16: D = 336 in tiles 35 us, D = 333 in spans 43.
 constexpr int kTile = 64;              // channels
 constexpr int kStages = 3;             // 3 x 32 KB and 17 KB: two blocks fit an SM's 228 KB
 constexpr int kTileBlocks = 2;         // per SM
