@@ -248,7 +248,10 @@ Plan plan_of(const relay_tensor_t *x)
     p.total = p.n_bytes + 2 * p.x_bytes + 2 * p.g_bytes + 2 * p.v_bytes + align_up((size_t)p.L * 4, 256);
     p.small = small_fits(p.m, p.n);
     p.resident = !p.small && resident_fits(p.m, p.n);
-    if (p.small || p.resident) p.total = 0;
+    // On the chip nothing is kept in the workspace.  The smallest one is asked for all the same: above kSmallSize elements every call
+    // has to bring a workspace, whichever form takes its size.
+    if (p.resident) p.total = 256;
+    if (p.small) p.total = 0;
     return p;
 }
 

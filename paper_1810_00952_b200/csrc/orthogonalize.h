@@ -52,7 +52,7 @@ struct Launch {
 
 relay_status_t launch_products(Launch &l, int sms, cudaStream_t st);
 
-// Matrices that stay on the chip (orthogonalize_resident.cu): all of a call in one launch, without a workspace.
+// Matrices that stay on the chip (orthogonalize_resident.cu): all of a call in one launch.
 bool resident_fits(int64_t m, int64_t n);
 relay_status_t launch_resident(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *at, const relay_tensor_t *y, int64_t L, int M, int N, float s, cudaStream_t st);
 
