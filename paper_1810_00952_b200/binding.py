@@ -435,6 +435,14 @@ def relay_gated_recurrence_grad(f, u, h0, lengths, gate, h_all, dh_all, dh_final
                                              _stream()))
 
 
+def relay_debug_recurrence_form(f: TensorDesc, u: Optional[TensorDesc], h_all: TensorDesc, ragged: bool = False) -> int:
+    """Which form of the recurrence's kernels these sizes take: 0 step by step, 1 spans in registers, 2 tiles (no GPU needed)."""
+    r = int(lib().relay_debug_recurrence_form(_ref(f), _ref(u), _ref(h_all), 1 if ragged else 0))
+    if r < 0:
+        raise ValueError("relay_debug_recurrence_form: types or shapes that the calls refuse")
+    return r
+
+
 def relay_token_logprob(scores, tokens, temperature, logp, entropy, lse, top_logp=None, top_ids=None):
     """tokens and logp, top_logp and top_ids go in pairs; each pair, entropy and lse may be None."""
     _check(lib().relay_token_logprob(_packed(scores), _packed(tokens), ctypes.c_float(temperature), _packed(logp), _packed(entropy),

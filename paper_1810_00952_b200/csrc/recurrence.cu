@@ -1181,12 +1181,6 @@ recurrence_grad_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __g
 }
 
 template <typename T, typename TH, int GATE>
-bool tiles_fit(const Args &p)
-{
-    const long long piece = 16 / (long long)sizeof(T);
-    return p.D % piece == 0 && p.bs % piece == 0 && p.ld < (1ll << 31) && p.C < (1ll << 31) && p.T < (1ll << 30);
-}
-template <typename T, typename TH, int GATE>
 relay_status_t launch_tiles(const Args &p, bool grad, cudaStream_t st)
 {
     constexpr int TS = sizeof(T) == 2 ? 8 : 4, TSG = sizeof(T) + sizeof(TH) == 4 ? 8 : 4;
@@ -1220,19 +1214,28 @@ relay_status_t launch_tiles(const Args &p, bool grad, cudaStream_t st)
     return check_launch("gated_recurrence");
 }
 
-// Sequences of up to kSteps steps run step by step, in the spans kernels' place; of up to kTileSteps, in the tile kernels' place.
+// Which form takes a call.  Sequences of up to kSteps steps run step by step, in the spans kernels' place; of up to kTileSteps, in the
+// tile kernels' place.
 // 64 x 1024 channels in bf16, forward: 12 steps 13.3 us and in tiles 14.3, 16 steps 15.4 and 14.3, 32 steps 23.6 and 14.3; gradient in
 // fp32: 16 steps 21.5 and 24.6, 24 steps 27.7 and 26.6; 8 x 256 channels, forward: 8 steps 9.3 and 8.2, 32 steps 21.5 and 8.2.
 // Longer sequences in spans: the smallest cluster that gives every SM a block.
+// Tiles and spans keep byte offsets within a step's row of f and u in 32 bits (spans those of h too): wider rows, of which only few
+// steps fit the GPU's memory, run step by step.
 constexpr long long kSteps = 32, kTileSteps = 12;
+enum Form { STEPS, SPANS, TILES };
+Form form_of(const Args &p, long long of_t, long long of_h)
+{
+    const long long piece = 16 / of_t;
+    if (p.ld * of_t >= (1ll << 32)) return STEPS;
+    if (p.T > kTileSteps && p.D % piece == 0 && p.bs % piece == 0 && p.C < (1ll << 31) && p.T < (1ll << 30)) return TILES;
+    return p.T > kSteps && p.C * of_h < (1ll << 32) ? SPANS : STEPS;
+}
 
 // W channels a thread in the spans kernels, at most two in the step-by-step ones (more threads where there are few steps)
 template <typename T, typename TH, int GATE, int W>
 relay_status_t launch(const Args &p, bool grad, cudaStream_t st)
 {
-    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
-    const bool narrow = p.ld * (long long)sizeof(T) < (1ll << 32) && p.C * (long long)sizeof(TH) < (1ll << 32);   // a row's offsets fit 32 bits
-    if (p.T > kSteps && narrow) {
+    if (form_of(p, sizeof(T), sizeof(TH)) == SPANS) {
         constexpr int TS = (sizeof(T) == 2 ? 32 : 16) / (W == 1 ? 2 : W), TSG = (sizeof(T) + sizeof(TH) == 4 ? 16 : 8) / (W == 1 ? 2 : W);
         int dev = 0, sms = 148;
         RELAY_CUDA(cudaGetDevice(&dev));
@@ -1258,7 +1261,7 @@ template <typename T, typename TH, int GATE>
 relay_status_t launch_gate(const Args &p, bool grad, cudaStream_t st)
 {
     if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
-    if (p.T > kTileSteps && tiles_fit<T, TH, GATE>(p)) return launch_tiles<T, TH, GATE>(p, grad, st);
+    if (form_of(p, sizeof(T), sizeof(TH)) == TILES) return launch_tiles<T, TH, GATE>(p, grad, st);
     // several channels a thread where every row starts at a multiple of them, so that they are one aligned access
     const long long rows = p.D | p.ld | p.bs;
     return rows % 2 == 0 ? launch<T, TH, GATE, 2>(p, grad, st) : launch<T, TH, GATE, 1>(p, grad, st);
@@ -1333,18 +1336,23 @@ relay_status_t check_gate(int32_t gate)
     return RELAY_OK;
 }
 
-Args make_args(const relay_tensor_t *f, const relay_tensor_t *u, const relay_tensor_t *h0, const relay_tensor_t *lengths, const Sizes &s)
+Args sizes_of(const Sizes &s, bool ragged)
 {
     Args p{};
-    p.f = f->data;
-    p.u = s.packed ? (const char *)f->data + s.D * dtype_size(f->dtype) : u->data;
     p.T = s.T; p.C = s.B * s.D; p.D = s.D;
     p.bs = s.packed ? 2 * s.D : s.D;
     p.ld = s.B * p.bs;
+    if (!s.packed && !ragged) p.D = p.bs = p.C;    // nothing depends on the batch element: one row of channels
+    return p;
+}
+Args make_args(const relay_tensor_t *f, const relay_tensor_t *u, const relay_tensor_t *h0, const relay_tensor_t *lengths, const Sizes &s)
+{
+    Args p = sizes_of(s, lengths != nullptr);
+    p.f = f->data;
+    p.u = s.packed ? (const char *)f->data + s.D * dtype_size(f->dtype) : u->data;
     p.h0 = h0 ? (const float *)h0->data : nullptr;
     p.lengths = lengths ? (const int *)lengths->data : nullptr;
     p.err = device_error_word();
-    if (!s.packed && !lengths) p.D = p.bs = p.C;   // nothing depends on the batch element: one row of channels
     return p;
 }
 
@@ -1441,4 +1449,14 @@ extern "C" relay_status_t relay_gated_recurrence_grad(const relay_tensor_t *f, c
     for (const relay_tensor_t *t : outs) reg.add(t);
     RELAY_TRY(reg.commit((cudaStream_t)stream));
     return launch_any(p, f->dtype, h_all->dtype, gate, true, (cudaStream_t)stream);
+}
+
+// Which form the call takes: 0 step by step, 1 spans in registers, 2 tiles; -1 where the types or shapes are refused.  Host only.
+extern "C" int32_t relay_debug_recurrence_form(const relay_tensor_t *f, const relay_tensor_t *u, const relay_tensor_t *h_all, int32_t ragged)
+{
+    clear_error();
+    Sizes s;
+    if (!f || !h_all || check_inputs(f, u, &s) != RELAY_OK || check_sequence(h_all, f->dtype, RELAY_F32, s, s.D, "h_all") != RELAY_OK) return -1;
+    if (s.B == 0 || s.D == 0) return STEPS;
+    return form_of(sizes_of(s, ragged != 0), (long long)dtype_size(f->dtype), (long long)dtype_size(h_all->dtype));
 }
