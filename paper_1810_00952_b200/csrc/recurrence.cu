@@ -2,7 +2,7 @@
 // paper: reverse mode through the recursion over time).  Elementwise steps: HBM-bound where the channels fill the GPU.
 //
 // Bytes: the forward group reads f and u and writes h once, the gradient reads f, u, h, dh and writes df, du once.  Measured against
-// a copy at 6.53 TB/s: 16384 x 1 x 4096 in bf16 80 us (5.0 TB/s), gradient of 4096 x 8 x 1024 in bf16 83 us (4.85 TB/s), the same
+// a copy at 6.53 TB/s: 16384 x 1 x 4096 in bf16 85 us (4.7 TB/s), gradient of 4096 x 8 x 1024 in bf16 87 us (4.6 TB/s), the same
 // forward in fp32 115 us (3.5 TB/s, bound by its instructions, fp64 states among them).  Short of that the length of the chain counts:
 // 128 x 64 x 1024 in bf16 15 us (3.4 TB/s), one step of 64 x 1024 7.5 us, nearly all of it the call and the launch.
 //
@@ -261,20 +261,28 @@ __device__ __forceinline__ void sigmoid_pair(const float (&f)[V], float (&a)[V],
             one_less[i] = f[i] >= 0.0f ? small[i] : large[i];
         }
     } else {
-        // 1 - a = 1 / (1 + exp(f)), and a from it: what a loses where it is itself small is lost on a state that it all but
-        // erases.  An infinite exponential gives exactly 0.
-        float y[V], c[V];
+        // 1 - a = 1 / (1 + exp(f)).  Where the gate is shut a is the smaller one and is exp(f) times that; where it is open a is one
+        // minus that, also where the exponential is infinite.  (One minus it everywhere: 81 us against 85 at 16384 x 1 x 4096, but a has
+        // an absolute error of 6e-8 then: nothing is left of it, or of the gate's partial, at f = -17.)
+        float y[V], c[V], shut[V];
         fill(1.44269504f, c);
         mul(f, c, y);
 #pragma unroll
         for (int i = 0; i < V; ++i) asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(y[i]));
+        float d[V];
         fill(1.0f, c);
-        add(y, c, y);
+        add(y, c, d);
 #pragma unroll
-        for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(one_less[i]) : "f"(y[i]));
+        for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(one_less[i]) : "f"(d[i]));
         float m[V];
         fill(-1.0f, m);
         muladd(one_less, m, c, a);
+        mul(y, one_less, shut);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {                      // by f's sign; a compare and a select were slower
+            const int k = __float_as_int(f[i]) >> 31;
+            a[i] = __int_as_float((__float_as_int(a[i]) & ~k) | (__float_as_int(shut[i]) & k));
+        }
     }
 }
 // A step's coefficient and the type F that states are carried in: fp32; beside fp32 gates fp64, rounded where a state is stored,

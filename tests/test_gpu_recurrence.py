@@ -12,7 +12,7 @@ import torch
 from oracle import language as L
 from paper_1810_00952_b200 import binding as B
 
-from parity import Guarded, assert_bf16, assert_f32, to_np
+from parity import Guarded, assert_bf16, assert_f32, bf16_ulp, to_np
 
 DEV = "cuda:0"
 F32, BF16 = torch.float32, torch.bfloat16
@@ -150,6 +150,47 @@ def test_gates_at_their_ends(T):
         df, du, d0 = run_grad(t, gate, h)
         for got, w in zip((df, du, d0), L.gated_recurrence_grad(f, u, h0, n, gate, to_np(h), to_np(t["dh_all"].float()), to_np(t["dh_final"]))):
             assert_f32(got, w)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,D", [(9, 64), (9, 33), (40, 64), (40, 33), (40, 34), (300, 64), (300, 33)])
+@pytest.mark.parametrize("dt,out_dt", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("gate", [B.GATE_SIGMOID, B.GATE_MIX])
+def test_shut_gates_keep_their_relative_precision(T, D, dt, out_dt, gate):
+    """One step whose gates are shut (f from -8 to -30) among open ones, values of zero and partials of one sign, so that no sum
+    cancels: states and partials there are products with the small coefficient.  Relative error: of the exponential and its argument
+    at most 4e-6, of the reciprocal and the products 1e-6, of the sums over the open steps (a = 0.95, some 20 of them) 3e-6; the bound is
+    2e-5, and half a unit in the last place where the result is bf16."""
+    t = make(T, 2, D, dt, gate, False, False, 41)
+    at = T // 2
+    t["lengths"] = torch.full((2,), T, dtype=torch.int32)                 # rows of D channels, not of 2 D
+    t["f"][:] = 3.0
+    t["f"][at] = torch.linspace(-8.0, -30.0, D).to(dt)
+    t["u"][:] = 0.0
+    if gate == B.GATE_MIX:
+        t["u"][at - 1] = 1.0                                              # a state that has not decayed
+    else:
+        t["u"][at - 1] = 2.0
+    t["dh_all"], t["dh_final"] = t["dh_all"].abs() + 0.1, t["dh_final"].abs()
+    t["h0"] = t["h0"].abs() + 0.1
+    f, u, h0, n = expect(t, gate)
+
+    def near(got, want, what):
+        g = to_np(got)
+        slack = 0.5 * bf16_ulp(want) if got.dtype == BF16 else 0.0
+        assert np.all(np.abs(g - want) <= 2e-5 * np.abs(want) + slack), (what, np.max(np.abs(g - want) / np.maximum(np.abs(want), 1e-300)))
+
+    h, _ = run_forward(t, gate, out_dt)
+    near(h[at], L.gated_recurrence(f, u, h0, n, gate)[0][at], "h")
+    df, du, d0 = run_grad(t, gate, h)
+    want = L.gated_recurrence_grad(f, u, h0, n, gate, to_np(h), to_np(t["dh_all"].to(out_dt)), to_np(t["dh_final"]))
+    near(df[at], want[0][at], "df"); near(du[at], want[1][at], "du")
+    # one step alone: what reaches the initial state is a g and nothing else
+    t1 = {k: v[at:at + 1].contiguous() if k in ("f", "u", "dh_all") else v for k, v in t.items()}
+    t1["lengths"] = None
+    h, _ = run_forward(t1, gate, out_dt)
+    near(run_grad(t1, gate, h)[2], L.gated_recurrence_grad(f[at:at + 1], u[at:at + 1], h0, None, gate, to_np(h), to_np(t1["dh_all"].to(out_dt)),
+                                                         to_np(t["dh_final"]))[2], "dh0")
 
 
 @pytest.mark.gpu
