@@ -197,8 +197,9 @@ __device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigne
 
 // One thread's running sums, in pairs, N vectors at a time: the maximum over all of them is looked at first, and only where it is
 // larger than the one so far are the sums scaled down (some ln(row / N) times a row).
-// Differences from -inf: the scores are raised to the lowest finite value first, so that 0 times the distance is 0; only where the
-// maximum itself is that low (masks of the lowest value and nothing else) are the elements looked at one by one.
+// Differences from -inf: the scores are raised to the lowest finite value first, so that 0 times the distance is 0.  That holds as
+// long as the distance is finite: where the maximum is so low (masks of the lowest value and nothing else) or so high that it may
+// not be, the elements are looked at one by one.
 struct Running {
     float m = -INFINITY;
     unsigned long long s = 0, w = 0;                       // two partial sums each
@@ -225,7 +226,7 @@ struct Running {
             for (int n = N - 1; n >= 0; --n)
                 if (top[n] == most) best_at = j + n * stride;
         }
-        if (m < -1.0e36f) {
+        if (!(fabsf(m) < 1.0e30f)) {                       // also NaN: what the sums are then does not matter
             if (m == -INFINITY) return most;               // nothing but -inf so far
             for (int n = 0; n < N; ++n) {
                 float x[E], s0, s1, w0, w1;
@@ -233,7 +234,7 @@ struct Running {
                 unpair(s, s0, s1); unpair(w, w0, w1);
                 for (int i = 0; i < E; ++i)
                     if (x[i] != -INFINITY) {
-                        const float d = x[i] - m, e = exp2_(d * k.log2e);
+                        const float d = below(x[i], m), e = exp2_(d * k.log2e);
                         s0 += e;
                         w0 = fmaf(e, d, w0);
                     }

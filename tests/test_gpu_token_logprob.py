@@ -148,6 +148,27 @@ def test_masked_rows_infinities_and_nan(V, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V", [2, 7, 1000, 33001, 200000])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("temperature", [1.0, 0.6])
+def test_large_maxima_beside_masked_classes(V, dt, temperature):
+    """The distance from a large maximum to a masked class is not a finite number: such a class adds nothing to the entropy."""
+    low = torch.finfo(dt).min
+    z = torch.empty(8, V, dtype=dt)
+    for row, (m, rest) in enumerate([(1e32, -INF), (1e32, low), (3e37, -INF), (3e37, low), (1e30, low), (1e29, -INF), (-1e32, -INF), (-1e37, low)]):
+        z[row] = rest
+        z[row, V // 2] = m
+        z[row, ::97] = m                                   # several equal ones: the entropy is the logarithm of their number
+    z[7, -1] = low
+    tok = torch.full((8,), V // 2, dtype=torch.int32)
+    o, w = forward(z, tok, temperature, 1), L.token_logprob(to_np(z), tok.numpy(), stored(temperature), 1)
+    np.testing.assert_array_equal(o["top_ids"].cpu().numpy(), w["top_ids"])
+    with np.errstate(over="ignore"):
+        for k in ("logp", "entropy", "lse", "top_logp"):
+            same(o[k], w[k].astype(np.float32), k)         # as stored: what is below the type's range is -inf
+
+
+@pytest.mark.gpu
 def test_every_output_alone_leading_axes_and_wide_tokens():
     z, tok, _ = scores(24, 1003, BF16, 3)
     o = forward(z, tok, 1.0, 4)
