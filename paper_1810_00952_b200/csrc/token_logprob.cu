@@ -628,6 +628,9 @@ struct RowPieces {
     }
 };
 
+// Log-probabilities are held at kNothing, where exp is zero: its product with a slope is zero unless that is above 1e35.
+constexpr float kNothing = -1.0e3f;
+
 // With q = exp(lp):  dscores = -(d + e (lp + h)) q / temperature,  d = dlogp, e = dentropy; at the token d (1 - q) in place of -d q
 template <typename T>
 __global__ void __launch_bounds__(kThreads) token_logprob_grad_kernel(const GradArgs p, int parts)
@@ -662,7 +665,7 @@ __global__ void __launch_bounds__(kThreads) token_logprob_grad_kernel(const Grad
             float l0, l1, t0, t1;
             const unsigned long long v = pair(x[c], x[c + 1]);
             unpair(fma2(pair(y[c], y[c + 1]), pair(p.k.inv_lo, p.k.inv_lo), fma2(v, pair(p.k.inv, p.k.inv), pair(-lse, -lse))), l0, l1);
-            l0 = max_nan(l0, -1.0e30f); l1 = max_nan(l1, -1.0e30f);
+            l0 = max_nan(l0, kNothing); l1 = max_nan(l1, kNothing);
             const unsigned long long lp = pair(l0, l1);
             unpair(mul2(lp, pair(1.44269504f, 1.44269504f)), t0, t1);
             if (FINE) { t0 = __expf(l0); t1 = __expf(l1); }

@@ -169,6 +169,30 @@ def test_large_maxima_beside_masked_classes(V, dt, temperature):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V", [3, 1000, 33001])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("temperature,weight", [(1e-10, 1.0), (1e-5, 1e20), (1.0, 1e25)])
+def test_gradient_of_impossible_classes_under_steep_slopes(V, dt, temperature, weight):
+    """dentropy / temperature of 1e10 to 1e25 times a log-probability far below any exponential's range: the partials there are zero.
+    The other classes' scores differ by no more than the temperature, so that they have probabilities.  Their term lp + H cancels to
+    rounding where they are all equal, so one of them stands apart; the tolerance is the parity tests' own."""
+    low = torch.finfo(dt).min
+    z = torch.zeros(4, V, dtype=dt)
+    z[:, 0] = temperature                                  # one class e times as probable
+    z[:, -1] = torch.tensor([-INF, low, -1e20, -1e4])
+    tok = torch.zeros(4, dtype=torch.int32)
+    o = forward(z, tok, temperature)
+    dlogp, dent = torch.full((4,), weight), torch.full((4,), weight)
+    dz = Guarded((4, V), dt, DEV)
+    B.relay_token_logprob_grad(z.to(DEV), tok.to(DEV), temperature, o["lse"], o["entropy"], dlogp.to(DEV), dent.to(DEV), dz.t)
+    torch.cuda.synchronize()
+    got = dz.check()
+    assert not bool(got[:, -1].any())
+    want = L.token_logprob_grad(to_np(z), tok.numpy(), stored(temperature), to_np(o["lse"]), to_np(o["entropy"]), to_np(dlogp), to_np(dent))
+    (assert_f32 if dt == F32 else assert_bf16)(got, want, what="dscores")
+
+
+@pytest.mark.gpu
 def test_every_output_alone_leading_axes_and_wide_tokens():
     z, tok, _ = scores(24, 1003, BF16, 3)
     o = forward(z, tok, 1.0, 4)
