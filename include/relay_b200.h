@@ -431,7 +431,8 @@ relay_status_t relay_gated_recurrence_grad(const relay_tensor_t *f, const relay_
  *   lse[i] = log sum_j exp(z[i,j]),  z = scores / temperature;   logp[i] = z[i,tokens[i]] - lse[i]
  *   entropy[i] = - sum_j p[i,j] log p[i,j]
  *   top_ids[i,:], top_logp[i,:]: the K tokens of the largest scores, largest first, equal scores by the lower id
- *   scores:(..,V) f32 or bf16, rank 1..6, the leading axes are the rows;  tokens:(..) i32 or i64;  temperature > 0
+ *   scores:(..,V) f32 or bf16, rank 1..6, the leading axes are the rows;  tokens:(..) i32 or i64;  temperature > 0 (a subnormal one
+ *   counts as the smallest normal number)
  *   -> logp, entropy, lse:(..) f32;  top_logp:(..,K) f32, top_ids:(..,K) i32, 1 <= K <= min(V, RELAY_MAX_TOP).
  * tokens and logp may be NULL together, top_logp and top_ids too, entropy and lse each (not all outputs at once).
  * Arithmetic in f32.  A token outside [0,V) names no class: its logp is 0.  Scores of -inf are classes that cannot occur; a

@@ -5,6 +5,7 @@
 //   8 x 131072 bf16, K = 20     10.4 us, 0.2 TB/s: the launch, the exchange between a row's blocks and the choice of the largest
 //   gradient, 4096 x 32768 bf16 with the entropy's term  93 us, 5.8 TB/s;  509 x 50021 f32  34 us, 6.0 TB/s: HBM
 #include <algorithm>
+#include <cfloat>
 
 #include "common.h"
 #include "ewise_kernels.cuh"
@@ -30,15 +31,26 @@ __device__ __forceinline__ int token_of(const void *tokens, int is_i64, long lon
 }
 
 // ---- temperature ---------------------------------------------------------------------------------------------------
-// 1 / temperature as a sum of two floats, and log2(e) / temperature
-struct Scale { float inv, inv_lo, log2e; };
+// 1 / temperature as a sum of two floats.  Distances d of two scores are kept in units of 1 / unit: one, but 2^64 where the temperature is
+// so high that classes far apart share the probability; then a sum of distances stays finite, and `limit` sends every row to the
+// path that looks at its elements one by one (elsewhere a distance of 1e30 is as good as an infinite one).
+struct Scale {
+    float inv, inv_lo;
+    float unit, inv_d, inv_2d, log2e_d;                    // 1, 2 and log2(e) over the temperature, per unit of d
+    float limit;                                           // of the largest score's size on the short path
+};
 inline Scale scale_of(float temperature)
 {
-    const double inv = 1.0 / (double)temperature;
+    const bool high = temperature > 1.0e20f;
+    const double inv = 1.0 / std::max((double)temperature, (double)FLT_MIN), unit = high ? 0x1p-64 : 1.0;
     Scale k;
     k.inv = (float)inv;
     k.inv_lo = (float)(inv - (double)k.inv);
-    k.log2e = (float)(1.4426950408889634 * inv);
+    k.unit = (float)unit;
+    k.inv_d = (float)(inv / unit);
+    k.inv_2d = 2.0f * k.inv_d;
+    k.log2e_d = (float)(1.4426950408889634 * inv / unit);
+    k.limit = high ? 0.0f : 1.0e30f;
     return k;
 }
 // z / temperature - lse with one rounding of the result's own size: the product stays exact inside the multiply-add, so a
@@ -48,7 +60,7 @@ __device__ __forceinline__ float log_prob(float z, float lse, const Scale &k)
     return fmaf(fmaxf(z, -3.0e38f), k.inv_lo, fmaf(z, k.inv, -lse));
 }
 
-// ---- sums of one row, joinable in any order of parts, d = z - m ----------------------------------------------------------
+// ---- sums of one row, joinable in any order of parts, d = z - m (times `unit`) ----------------------------------------------
 //   m = max z,  s = sum exp(d / temperature),  w = sum exp(d / temperature) d
 //   lse = m / temperature + log s;   logp = d / temperature - log s;   entropy = log s - w / (s temperature)
 // Everything but lse itself is free of m's size.  A part without a score above -inf has m = -inf, s = w = 0; a NaN stays in m.
@@ -67,8 +79,8 @@ __device__ __forceinline__ float exp2_(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// a finite difference even where a score or the maximum is infinite: its exponential is 0 and its product with that too
-__device__ __forceinline__ float below(float z, float m) { return fmaxf(z - m, -1.0e30f); }
+// a finite distance even where a score or the maximum is infinite: its exponential is 0 and its product with that too
+__device__ __forceinline__ float below(float z, float m, const Scale &k) { return fmaxf(fmaf(z, k.unit, -(m * k.unit)), -1.0e30f); }
 
 // the sums of a warp's lanes together, in every lane; written out with intrinsics, so that every kernel rounds alike
 __device__ __forceinline__ Sums join_lanes(Sums a, const Scale &k)
@@ -76,7 +88,7 @@ __device__ __forceinline__ Sums join_lanes(Sums a, const Scale &k)
     float m = a.m;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, d));
-    const float d = below(a.m, m), f = exp2_(d * k.log2e);
+    const float d = below(a.m, m, k), f = exp2_(d * k.log2e_d);
     float s = __fmul_rn(f, a.s), w = __fmul_rn(f, fmaf(d, a.s, a.w));
 #pragma unroll
     for (int d2 = 16; d2 > 0; d2 >>= 1) {
@@ -94,13 +106,13 @@ struct Row {
         m = a.m;
         log_s = logf(a.s);
         lse = fmaf(a.m, k.inv, log_s);
-        entropy = log_s - __fdiv_rn(__fmul_rn(a.w, k.inv), a.s);
+        entropy = log_s - __fdiv_rn(__fmul_rn(a.w, k.inv_d), a.s);
         if (a.m == -INFINITY) { lse = -INFINITY; entropy = 0.0f; }
         else if (!(a.m < INFINITY)) lse = entropy = log_s = __int_as_float(0x7fc00000);
     }
     __device__ __forceinline__ float logp(float z, const Scale &k) const
     {
-        return m == -INFINITY ? -INFINITY : fmaf(z - m, k.inv, -log_s);
+        return m == -INFINITY ? -INFINITY : fmaf((0.5f * z - 0.5f * m) * k.unit, k.inv_2d, -log_s);   // half the distance: finite
     }
 };
 
@@ -216,7 +228,7 @@ struct Running {
         for (int n = 1; n < N; ++n) most = max_nan(most, top[n]);
         if (best_at < 0) best_at = j;
         if (!(most <= m)) {                                // larger, or NaN
-            const float d = below(m, most), f = exp2_(d * k.log2e);
+            const float d = below(m, most, k), f = exp2_(d * k.log2e_d);
             float s0, s1, w0, w1;
             unpair(s, s0, s1); unpair(w, w0, w1);
             w = pair(f * fmaf(d, s0, w0), f * fmaf(d, s1, w1));
@@ -226,7 +238,7 @@ struct Running {
             for (int n = N - 1; n >= 0; --n)
                 if (top[n] == most) best_at = j + n * stride;
         }
-        if (!(fabsf(m) < 1.0e30f)) {                       // also NaN: what the sums are then does not matter
+        if (!(fabsf(m) < k.limit)) {                       // also NaN: what the sums are then does not matter
             if (m == -INFINITY) return most;               // nothing but -inf so far
             for (int n = 0; n < N; ++n) {
                 float x[E], s0, s1, w0, w1;
@@ -234,7 +246,7 @@ struct Running {
                 unpair(s, s0, s1); unpair(w, w0, w1);
                 for (int i = 0; i < E; ++i)
                     if (x[i] != -INFINITY) {
-                        const float d = below(x[i], m), e = exp2_(d * k.log2e);
+                        const float d = below(x[i], m, k), e = exp2_(d * k.log2e_d);
                         s0 += e;
                         w0 = fmaf(e, d, w0);
                     }
@@ -242,7 +254,7 @@ struct Running {
             }
             return most;
         }
-        const unsigned long long nm = pair(-m, -m), c = pair(k.log2e, k.log2e);
+        const unsigned long long nm = pair(-m, -m), c = pair(k.log2e_d, k.log2e_d);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             float x[E];

@@ -193,6 +193,36 @@ def test_gradient_of_impossible_classes_under_steep_slopes(V, dt, temperature, w
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V", [5, 1000, 33001])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("temperature", [1e-45, 2e-38, 1e-20, 9e19, 1e21, 1e30, 1e38, 3e38])
+def test_temperatures_at_the_ends_of_their_range(V, dt, temperature):
+    """Scores at the temperature's own scale beside masks of -inf and of the lowest value: at 1e38 the lowest value is no mask, and
+    -inf still is."""
+    t = max(stored(temperature), float(np.finfo(np.float32).tiny))
+    r = np.random.default_rng(V)
+    x = np.clip(2 * t * r.normal(size=(7, V)), -3e38, 3e38)
+    masked = r.random(V) < 0.5
+    masked[0] = False
+    x[1, masked] = -np.inf
+    z = torch.from_numpy(x).to(dt)
+    low = torch.finfo(dt).min
+    z[2, torch.from_numpy(masked)] = low
+    z[3] = 0.0; z[3, -1] = -INF
+    z[4] = low
+    z[5] = -INF; z[5, 0] = 0.0
+    if t >= 1e30:
+        z[6, ::2] = 3e38; z[6, 1::2] = -3e38
+    tok = torch.from_numpy(r.integers(0, V, 7)).to(torch.int32)
+    top = min(V, 5)
+    o, w = forward(z, tok, temperature, top), L.token_logprob(to_np(z), tok.numpy(), t, top)
+    np.testing.assert_array_equal(o["top_ids"].cpu().numpy(), w["top_ids"])
+    with np.errstate(over="ignore"):
+        for k in ("logp", "entropy", "lse", "top_logp"):
+            same(o[k], w[k].astype(np.float32), k)
+
+
+@pytest.mark.gpu
 def test_every_output_alone_leading_axes_and_wide_tokens():
     z, tok, _ = scores(24, 1003, BF16, 3)
     o = forward(z, tok, 1.0, 4)
