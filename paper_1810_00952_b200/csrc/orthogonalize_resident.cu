@@ -355,10 +355,13 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
     if (warp == 0) tc::tmem_dealloc(tmem, tmem_cols);
 }
 
+constexpr size_t smem_bytes(int w, bool parts) { return 1024 + (size_t)((w + 63) / 64 + 4) * kGroup + (parts ? kRows * 512 : 0) + sizeof(Scalars); }
+
 template <typename T>
 relay_status_t launch(const relay_tensor_t *x, const relay_tensor_t *y, int64_t L, const Resident &q, size_t smem, cudaStream_t st)
 {
-    RELAY_CUDA(cudaFuncSetAttribute(orth_resident_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    // the most that any shape needs: the attribute is the kernel's, and another thread may be launching a larger matrix
+    RELAY_CUDA(cudaFuncSetAttribute(orth_resident_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(kWidest, true)));
     RELAY_CUDA(launch_pdl_cluster(orth_resident_kernel<T>, dim3((unsigned)(L * q.S)), dim3(kThreads), dim3((unsigned)q.S), smem, st, (const T *)x->data,
                                   (__nv_bfloat16 *)y->data, q));
     return check_launch("orthogonalize_resident");
@@ -379,12 +382,11 @@ relay_status_t launch_resident(const relay_tensor_t *x, const relay_orthogonaliz
     q.a = at->a; q.b = at->b; q.c = at->c; q.eps = at->eps; q.s = s; q.scale = at->scale;
     q.err = device_error_word();
     if (!q.err) return fail(RELAY_ERR_CUDA, "no device error word");
-    const size_t smem = 1024 + (size_t)((q.w + 63) / 64 + 4) * kGroup + (q.S > 1 ? kRows * 512 : 0) + sizeof(Scalars);
     BoundsReg reg;
     reg.add(x); reg.add(y);
     RELAY_TRY(reg.commit(st));
-    if (x->dtype == RELAY_F32) return launch<float>(x, y, L, q, smem, st);
-    return launch<__nv_bfloat16>(x, y, L, q, smem, st);
+    if (x->dtype == RELAY_F32) return launch<float>(x, y, L, q, smem_bytes(q.w, q.S > 1), st);
+    return launch<__nv_bfloat16>(x, y, L, q, smem_bytes(q.w, q.S > 1), st);
 }
 
 }  // namespace orth

@@ -1,6 +1,7 @@
 """Calls that overlap: on two streams, or from two host threads, each with buffers of its own.  Results have the bits of the same call
 alone."""
 import ctypes
+import threading
 
 import pytest
 import torch
@@ -53,8 +54,17 @@ def check_overlap(first, second, rounds=20):
             assert all(torch.equal(a, b) for a, b in zip(w, call.outs))
 
 
-def kernel_attributes(graph, attribute):
-    """Of every kernel node of a captured graph that was not run."""
+def capture(call):
+    g = torch.cuda.CUDAGraph(keep_graph=True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        call()
+    return g
+
+
+def kernel_nodes(graph):
+    """The kernel nodes of a captured graph that need not have been run, and the driver library."""
     cu = ctypes.CDLL("libcuda.so.1")
     n = ctypes.c_size_t(0)
     g = ctypes.c_void_p(graph.raw_cuda_graph())
@@ -66,10 +76,13 @@ def kernel_attributes(graph, attribute):
         kind = ctypes.c_int(-1)
         assert cu.cuGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0
         if kind.value == 0:                                   # CU_GRAPH_NODE_TYPE_KERNEL
-            value = (ctypes.c_int * 16)()                     # CUlaunchAttributeValue: 64 bytes
-            assert cu.cuGraphKernelNodeGetAttribute(ctypes.c_void_p(node), attribute, value) == 0
-            out.append(value[0])
-    return out
+            out.append(ctypes.c_void_p(node))
+    return out, cu
+
+
+class KernelNodeParams(ctypes.Structure):                     # CUDA_KERNEL_NODE_PARAMS_v2
+    _fields_ = [("func", ctypes.c_void_p), ("dims", ctypes.c_uint * 6), ("shared_bytes", ctypes.c_uint), ("params", ctypes.c_void_p),
+                ("extra", ctypes.c_void_p), ("kern", ctypes.c_void_p), ("ctx", ctypes.c_void_p)]
 
 
 @pytest.mark.parametrize("shape", [(300, 500), (2048, 2048)])
@@ -78,12 +91,13 @@ def test_products_whose_blocks_wait_for_one_another_are_launched_cooperatively(s
     run; then replayed."""
     call = Orthogonalize(shape, 1)
     want = alone(call)                                        # also loads the module and sets the kernel's attributes
-    g = torch.cuda.CUDAGraph(keep_graph=True)
-    s = torch.cuda.Stream()
-    s.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.graph(g, stream=s):
-        call()
-    cooperative = kernel_attributes(g, 2)                     # CU_LAUNCH_ATTRIBUTE_COOPERATIVE
+    g = capture(call)
+    nodes, cu = kernel_nodes(g)
+    cooperative = []
+    for node in nodes:
+        value = (ctypes.c_int * 16)()                         # CUlaunchAttributeValue: 64 bytes
+        assert cu.cuGraphKernelNodeGetAttribute(node, 2, value) == 0          # CU_LAUNCH_ATTRIBUTE_COOPERATIVE
+        cooperative.append(value[0])
     assert len(cooperative) == 3 and cooperative.count(1) == 1, cooperative
     call.y.fill_(7)
     g.instantiate()
@@ -97,3 +111,50 @@ def test_products_whose_blocks_wait_for_one_another_are_launched_cooperatively(s
 @pytest.mark.parametrize("first,second", [((300, 500), (500, 300)), ((2048, 2048), (1024, 2048)), ((8, 512, 1024), (300, 300))])
 def test_orthogonalised_updates_on_two_streams(first, second):
     check_overlap(Orthogonalize(first, 1), Orthogonalize(second, 2, F32))
+
+
+def test_a_small_matrix_on_the_chip_leaves_room_for_a_large_one():
+    """The limit of dynamic shared memory is the kernel's, whichever thread set it last."""
+    small, large = Orthogonalize((40, 40), 1), Orthogonalize((128, 2048), 2)
+    alone(large)
+    g = capture(large)
+    nodes, cu = kernel_nodes(g)
+    p = KernelNodeParams()
+    assert len(nodes) == 1 and cu.cuGraphKernelNodeGetParams_v2(nodes[0], ctypes.byref(p)) == 0
+    func = ctypes.c_void_p(p.func)
+    if not p.func:
+        assert cu.cuKernelGetFunction(ctypes.byref(func), ctypes.c_void_p(p.kern)) == 0
+    limit = ctypes.c_int(0)
+    for call in (large, small):
+        alone(call)
+        assert cu.cuFuncGetAttribute(ctypes.byref(limit), 8, func) == 0       # CU_FUNC_ATTRIBUTE_MAX_DYNAMIC_SHARED_SIZE_BYTES
+        assert limit.value >= p.shared_bytes > 150 * 1024, (limit.value, p.shared_bytes)
+
+
+def test_matrices_on_the_chip_from_two_host_threads():
+    """They share a kernel and differ in the shared memory that they ask for."""
+    calls = [Orthogonalize((40, 40), 1), Orthogonalize((128, 2048), 2)]
+    want = [alone(c) for c in calls]
+    for t in (calls[0].y, calls[1].y):
+        t.fill_(7)
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(call):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(3000):
+                    call()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:                                # shown by the assertion below
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    B.relay_poll_status()
+    for w, c in zip(want, calls):
+        assert torch.equal(w[0], c.y)
