@@ -9,6 +9,7 @@
 // Three forms: step by step, a thread per channel (few steps); the time axis cut into spans that stay in registers (rows that are not
 // whole 16-byte pieces); the same with tiles fetched ahead by TMA and a warp that only joins (all others).
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "common.h"
@@ -805,8 +806,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) recurrence_grad_spans_kernel(c
 // 16384 x 1 x 4096 in bf16: spans in registers 122 us, tiles with all warps joining 140 (8 steps a thread) and 100 (16), with the
 // joining warp and one slab composed ahead 80.  4096 x 13 x D, forward in bf16: D = 336 in tiles 35 us, D = 333 in spans 43.
 constexpr int kTile = 64;              // channels
-constexpr int kStages = 3;             // 3 x 32 KB and 17 KB: two blocks fit an SM's 228 KB
-constexpr int kTileBlocks = 2;         // per SM
+constexpr int kStages = 3;
 constexpr int kTileThreads = 32 * (kWarps + 1);
 
 struct TilePlan {
@@ -985,11 +985,23 @@ __device__ __forceinline__ void join_slabs(Exchange<F, V> &x, const Args &p, con
     __syncwarp();
 }
 
-template <typename T, typename TH, int GATE, int TS>
-__global__ void __launch_bounds__(kTileThreads, kTileBlocks)
+// Steps a thread takes of a slab, a block's ring of tiles in bytes, and how many blocks an SM's 228 KB hold (1 KB of each is the
+// system's): 96 KB and 17 KB of maps in bf16, 48 and 34 in fp32, two of them; 96 and 34 for the fp32 gradient, one.
+template <typename T, typename TH, bool GRAD> struct TileShape {
+    using F = std::conditional_t<sizeof(T) == 4, double, float>;
+    static constexpr int TS = (GRAD ? sizeof(T) + sizeof(TH) == 4 : sizeof(T) == 2) ? 8 : 4;
+    static constexpr int ROWS = kWarps * TS;
+    static constexpr size_t RING = (size_t)kStages * ROWS * kTile * 2 * (sizeof(T) + (GRAD ? sizeof(TH) : 0));
+    static constexpr size_t BYTES = RING + sizeof(Exchange<F, 2>) + 128 + 1024;
+    static constexpr int BLOCKS = 2 * BYTES <= 228 * 1024 ? 2 : 1;
+};
+
+template <typename T, typename TH, int GATE>
+__global__ void __launch_bounds__(kTileThreads, (TileShape<T, TH, false>::BLOCKS))
 recurrence_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_constant__ CUtensorMap tm_u, const Args p, const TilePlan q)
 {
-    constexpr int V = 2, ROWS = kWarps * TS, TILE = ROWS * kTile * (int)sizeof(T);
+    using Shape = TileShape<T, TH, false>;
+    constexpr int V = 2, TS = Shape::TS, ROWS = Shape::ROWS, TILE = ROWS * kTile * (int)sizeof(T);
     constexpr bool SAFE = GATE == RELAY_GATE_GIVEN;
     using K = Coefficient<T, GATE, V>;
     using F = typename K::F;
@@ -1092,12 +1104,13 @@ recurrence_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_c
     tc::cluster_sync();                // no block leaves while another may still send to it
 }
 
-template <typename T, typename TH, int GATE, int TS>
-__global__ void __launch_bounds__(kTileThreads, kTileBlocks)
+template <typename T, typename TH, int GATE>
+__global__ void __launch_bounds__(kTileThreads, (TileShape<T, TH, true>::BLOCKS))
 recurrence_grad_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __grid_constant__ CUtensorMap tm_u, const __grid_constant__ CUtensorMap tm_d,
                              const __grid_constant__ CUtensorMap tm_h, const Args p, const TilePlan q)
 {
-    constexpr int V = 2, ROWS = kWarps * TS, TILE = ROWS * kTile * (int)sizeof(T), TILE_H = ROWS * kTile * (int)sizeof(TH), STAGE = 2 * (TILE + TILE_H);
+    using Shape = TileShape<T, TH, true>;
+    constexpr int V = 2, TS = Shape::TS, ROWS = Shape::ROWS, TILE = ROWS * kTile * (int)sizeof(T), TILE_H = ROWS * kTile * (int)sizeof(TH), STAGE = 2 * (TILE + TILE_H);
     constexpr bool SAFE = GATE == RELAY_GATE_GIVEN;
     using K = Coefficient<T, GATE, V>;
     using F = typename K::F;
@@ -1188,22 +1201,56 @@ recurrence_grad_tiles_kernel(const __grid_constant__ CUtensorMap tm_f, const __g
     tc::cluster_sync();
 }
 
+// Clusters of S blocks of a kernel that are resident at once on the present device; asked for once per size.
+template <typename Kernel>
+int resident_clusters(Kernel kernel, std::atomic<int> (&known)[64][9], int dev, int S, size_t smem)
+{
+    if (dev < 0 || dev >= 64) return 1;
+    int n = known[dev][S].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)S); cfg.blockDim = dim3(kTileThreads); cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)S; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+    n = std::max(n, 1);
+    known[dev][S].store(n, std::memory_order_relaxed);
+    return n;
+}
+
 template <typename T, typename TH, int GATE>
 relay_status_t launch_tiles(const Args &p, bool grad, cudaStream_t st)
 {
-    constexpr int TS = sizeof(T) == 2 ? 8 : 4, TSG = sizeof(T) + sizeof(TH) == 4 ? 8 : 4;
-    int dev = 0, sms = 148;
+    using Forward = TileShape<T, TH, false>;
+    using Gradient = TileShape<T, TH, true>;
+    int dev = 0;
     RELAY_CUDA(cudaGetDevice(&dev));
-    RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    const int rows = kWarps * (grad ? TSG : TS), resident = kTileBlocks * sms;
+    const int rows = grad ? Gradient::ROWS : Forward::ROWS;
     TilePlan q;
     q.per_row = (int)((p.D + kTile - 1) / kTile);
     q.tiles = (p.C / p.D) * q.per_row;
-    // as many blocks per tile as find room at once and have something to do; no more clusters than find room
-    q.S = (int)std::max<long long>(1, std::min<long long>({8, resident / q.tiles, (p.T + rows - 1) / rows}));
+    const size_t smem = grad ? Gradient::RING : Forward::RING;
+    static std::atomic<int> known[2][64][9];
+    if (grad) RELAY_CUDA(cudaFuncSetAttribute(recurrence_grad_tiles_kernel<T, TH, GATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    else RELAY_CUDA(cudaFuncSetAttribute(recurrence_tiles_kernel<T, TH, GATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    // Blocks per tile: the fewest rounds over the clusters that are resident at once, each of a tile's slabs and one more for its first,
+    // which nothing hides; from three blocks on the exchange costs 2 % a block.  Two blocks also where they are 2 % behind one: at 128
+    // tiles on 148 SMs they keep all of them busy in the first of two rounds (fp32 gradient of 4096 x 8 x 1024: 232 us against 247; 128 x
+    // 64 x 1024 in bf16, 14 % behind: 16.4 against 15.4).
+    long long clusters = 1;
+    double best = 0;
+    q.S = 1;
+    for (int S = 1; S <= 8 && (S == 1 || (long long)(S - 1) * rows < p.T); ++S) {
+        const long long room = grad ? resident_clusters(recurrence_grad_tiles_kernel<T, TH, GATE>, known[1], dev, S, smem)
+                                    : resident_clusters(recurrence_tiles_kernel<T, TH, GATE>, known[0], dev, S, smem);
+        const long long rounds = (q.tiles + room - 1) / room, slabs = (p.T + (long long)S * rows - 1) / ((long long)S * rows);
+        const double cost = (double)rounds * (double)(slabs + 1) * (S > 2 ? 1.0 + 0.02 * S : 1.0);
+        if (S == 1 || cost < best * (S == 2 ? 1.02 : 1.0)) { best = cost; q.S = S; clusters = std::min(room, q.tiles); }
+    }
     q.slabs = (int)((p.T + (long long)q.S * rows - 1) / ((long long)q.S * rows));
-    const size_t smem = (size_t)kStages * rows * kTile * 2 * (sizeof(T) + (grad ? sizeof(TH) : 0));
-    const dim3 grid((unsigned)(std::min<long long>(q.tiles, resident / q.S) * q.S)), block(kTileThreads), cluster((unsigned)q.S);
+    const dim3 grid((unsigned)(clusters * q.S)), block(kTileThreads), cluster((unsigned)q.S);
     const bool t32 = sizeof(T) == 4, h32 = sizeof(TH) == 4;
     CUtensorMap f, u, d, h;
     const uint64_t ld = (uint64_t)p.ld;
@@ -1211,13 +1258,11 @@ relay_status_t launch_tiles(const Args &p, bool grad, cudaStream_t st)
     RELAY_TRY(make_tmap_2d(&f, t32, p.f, ld, p.T, ld, kTile, rows, false));
     RELAY_TRY(make_tmap_2d(&u, t32, p.u, ld - (p.bs == 2 * p.D ? p.D : 0), p.T, ld, kTile, rows, false));
     if (!grad) {
-        RELAY_CUDA(cudaFuncSetAttribute(recurrence_tiles_kernel<T, TH, GATE, TS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        RELAY_CUDA(launch_pdl_cluster(recurrence_tiles_kernel<T, TH, GATE, TS>, grid, block, cluster, smem, st, f, u, p, q));
+        RELAY_CUDA(launch_pdl_cluster(recurrence_tiles_kernel<T, TH, GATE>, grid, block, cluster, smem, st, f, u, p, q));
     } else {
         RELAY_TRY(make_tmap_2d(&d, h32, p.dh, p.C, p.T, p.C, kTile, rows, false));
         RELAY_TRY(make_tmap_2d(&h, h32, p.h, p.C, p.T, p.C, kTile, rows, false));
-        RELAY_CUDA(cudaFuncSetAttribute(recurrence_grad_tiles_kernel<T, TH, GATE, TSG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        RELAY_CUDA(launch_pdl_cluster(recurrence_grad_tiles_kernel<T, TH, GATE, TSG>, grid, block, cluster, smem, st, f, u, d, h, p, q));
+        RELAY_CUDA(launch_pdl_cluster(recurrence_grad_tiles_kernel<T, TH, GATE>, grid, block, cluster, smem, st, f, u, d, h, p, q));
     }
     return check_launch("gated_recurrence");
 }

@@ -85,6 +85,15 @@ class KernelNodeParams(ctypes.Structure):                     # CUDA_KERNEL_NODE
                 ("extra", ctypes.c_void_p), ("kern", ctypes.c_void_p), ("ctx", ctypes.c_void_p)]
 
 
+class LaunchAttribute(ctypes.Structure):                      # CUlaunchAttribute
+    _fields_ = [("id", ctypes.c_int), ("pad", ctypes.c_int), ("value", ctypes.c_uint * 16)]
+
+
+class LaunchConfig(ctypes.Structure):                         # CUlaunchConfig
+    _fields_ = [("dims", ctypes.c_uint * 6), ("shared_bytes", ctypes.c_uint), ("stream", ctypes.c_void_p),
+                ("attributes", ctypes.POINTER(LaunchAttribute)), ("n", ctypes.c_uint)]
+
+
 @pytest.mark.parametrize("shape", [(300, 500), (2048, 2048)])
 def test_products_whose_blocks_wait_for_one_another_are_launched_cooperatively(shape):
     """The last kernel of the call (norm, copy, products) must be placed whole or not at all: seen on a captured graph before it is
@@ -158,3 +167,37 @@ def test_matrices_on_the_chip_from_two_host_threads():
     B.relay_poll_status()
     for w, c in zip(want, calls):
         assert torch.equal(w[0], c.y)
+
+
+@pytest.mark.parametrize("dt,out_dt", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("tiles", [8, 35, 72, 128, 160, 512])
+def test_persistent_clusters_of_the_recurrence_are_planned_for_the_room_they_find(dt, out_dt, grad, tiles):
+    """A cluster walks over tiles, so a grid that does not fit at once makes the last clusters wait for a whole share.  What fits is the
+    driver's answer for this kernel, its cluster size and its shared memory."""
+    T, D = 512, 64 * tiles
+    f, u, h, dh = (torch.zeros(T, 1, D, dtype=t, device=DEV) for t in (dt, dt, out_dt, out_dt))
+    df, du = torch.empty_like(f), torch.empty_like(u)
+
+    def call():
+        if grad:
+            B.relay_gated_recurrence_grad(f, u, None, None, B.GATE_MIX, h, dh, None, df, du, None)
+        else:
+            B.relay_gated_recurrence(f, u, None, None, B.GATE_MIX, h, None)
+
+    call()
+    g = capture(call)
+    nodes, cu = kernel_nodes(g)
+    p = KernelNodeParams()
+    assert len(nodes) == 1 and cu.cuGraphKernelNodeGetParams_v2(nodes[0], ctypes.byref(p)) == 0
+    func = ctypes.c_void_p(p.func)
+    if not p.func:
+        assert cu.cuKernelGetFunction(ctypes.byref(func), ctypes.c_void_p(p.kern)) == 0
+    size = (ctypes.c_uint * 16)()
+    assert cu.cuGraphKernelNodeGetAttribute(nodes[0], 4, size) == 0           # CU_LAUNCH_ATTRIBUTE_CLUSTER_DIMENSION
+    attribute = LaunchAttribute(id=4)
+    attribute.value[:3] = size[:3]
+    config = LaunchConfig(dims=p.dims, shared_bytes=p.shared_bytes, attributes=ctypes.pointer(attribute), n=1)
+    clusters = ctypes.c_int(0)
+    assert cu.cuOccupancyMaxActiveClusters(ctypes.byref(clusters), func, ctypes.byref(config)) == 0
+    assert p.dims[0] // size[0] <= clusters.value, (p.dims[0], size[0], clusters.value)
