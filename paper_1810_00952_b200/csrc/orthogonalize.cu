@@ -7,9 +7,10 @@
 // Three products a step on the tensor cores (tcgen05, kind::f16).  G and P are symmetric: only the tiles on and above the
 // diagonal are computed, each stored to both places, so a step costs m m n + m m m + 2 m m n operations.  The operands lie in
 // the workspace as fp16: at the tensor rate of bf16 it keeps 10 fraction bits instead of 7, and with them an update that is 1e-3
-// instead of 1e-2 off.  Range is no concern: singular values never leave [0, 1.3], X is kept times a power of two,
-// S = 2^round(log2(sqrt(M N) / 8)), which puts its elements around 1/8 at the start and below 0.16 sqrt(M N) ever after, and
-// what is too small for fp16 in G and P is small against the diagonal.  The diagonals of G and P, whose entries grow to 1 and -2.7
+// instead of 1e-2 off.  Their range: with the usual coefficients singular values never leave [0, 1.3]; X is kept times a power of two,
+// S = 2^round(log2(sqrt(M N) / 8)), which puts its elements around 1/8 at the start and below 0.16 sqrt(M N) ever after; other
+// coefficients may let X grow or shrink, and further powers of two per step follow that (steps_of).  What is too small for fp16 in G
+// and P is small against the diagonal.  The diagonals of G and P, whose entries grow to 1 and -2.7
 // and whose rounding would move whole rows, are kept apart in fp32: with G = D + O,
 //   P = b O + c (D O + O D + O O) off the diagonal,  e = a + b d + c (d d + diag(O O)) on it,   X <- e X + offdiag(P) X
 // (one multiplier per row of X, per column where M > N), all of it in the products' epilogues.
@@ -135,8 +136,7 @@ __device__ __forceinline__ void dot_rows(const float *a, const float *b, int ld,
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSmallThreads) orth_small_kernel(const T *__restrict__ x, int M, int N, int steps, float a, float b, float c, float eps, float scale,
-                                                                  __nv_bfloat16 *__restrict__ y)
+__global__ void __launch_bounds__(kSmallThreads) orth_small_kernel(const T *__restrict__ x, int M, int N, const Steps step, float eps, __nv_bfloat16 *__restrict__ y)
 {
     extern __shared__ float4 smem4[];
     __shared__ double warp_sum[kSmallThreads / 32];
@@ -166,7 +166,8 @@ __global__ void __launch_bounds__(kSmallThreads) orth_small_kernel(const T *__re
         X[tall ? q * ldx + r : r * ldx + q] = (float)(f * (double)element(x + i));
     }
     __syncthreads();
-    for (int k = 0; k < steps; ++k) {
+    for (int k = 0; k < step.n; ++k) {
+        const float a = step.a[k], b = step.b[k], c = step.c[k];
         float t[4][4];
         for (int u = tid; u < mt * mt; u += kSmallThreads) {                          // G = X X^T
             const int i0 = u / mt * 4, j0 = u % mt * 4;
@@ -211,19 +212,55 @@ __global__ void __launch_bounds__(kSmallThreads) orth_small_kernel(const T *__re
     }
     for (int i = tid; i < M * N; i += kSmallThreads) {
         const int r = i / N, q = i - r * N;
-        if (relay_in_bounds(y + i, 2)) y[i] = __float2bfloat16_rn(scale * X[tall ? q * ldx + r : r * ldx + q]);
+        if (relay_in_bounds(y + i, 2)) y[i] = __float2bfloat16_rn(step.scale * X[tall ? q * ldx + r : r * ldx + q]);
     }
 }
 
 template <typename T>
-relay_status_t launch_small(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *at, const relay_tensor_t *y, int64_t L, int M, int N, cudaStream_t st)
+relay_status_t launch_small(const relay_tensor_t *x, const Steps &steps, float eps, const relay_tensor_t *y, int64_t L, int M, int N, cudaStream_t st)
 {
     const size_t smem = small_smem(std::min(M, N), std::max(M, N));
     RELAY_CUDA(cudaFuncSetAttribute(orth_small_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024));
-    RELAY_CUDA(launch_pdl(orth_small_kernel<T>, dim3((unsigned)L), dim3(kSmallThreads), smem, st, (const T *)x->data, M, N, at->steps, at->a, at->b, at->c, at->eps,
-                          at->scale, (__nv_bfloat16 *)y->data));
+    RELAY_CUDA(launch_pdl(orth_small_kernel<T>, dim3((unsigned)L), dim3(kSmallThreads), smem, st, (const T *)x->data, M, N, steps, eps, (__nv_bfloat16 *)y->data));
     return check_launch("orthogonalize_small");
 }
+
+}  // namespace
+
+// Singular values start in [0, 1]; a step takes t to t (a + b t^2 + c t^4), so g, the largest absolute value that the steps can have made,
+// is known beforehand.  Where 2^-r g leaves [1/4, 16], or 16-bit elements of s X may leave their range, X is kept times 2^-r from
+// there on, which is a change of each step's coefficients.  With the usual coefficients g is 1.2 and r stays 0.  A g that single
+// values near one may reach, but none near zero (those grow by a a step), is followed for 2^10 only: most elements would be lost.
+orth::Steps orth::steps_of(const relay_orthogonalize_attrs_t &at, double s)
+{
+    Steps p{};
+    p.n = at.steps;
+    const double a = at.a, b = at.b, c = at.c, most = std::min(16.0, 32768.0 / s);
+    double g = 1.0, grown = 0.0;                           // log2 of what values near zero have grown by
+    int r = 0;
+    for (int k = 0; k < at.steps; ++k) {
+        auto value = [&](double t) { const double q = t * t; return std::fabs(t * (a + q * (b + c * q))); };
+        double next = value(g);
+        const double root = 9.0 * b * b - 20.0 * a * c;    // extrema: a + 3 b t^2 + 5 c t^4 = 0
+        for (int sign = -1; sign <= 1 && root >= 0.0; sign += 2) {
+            const double q = c != 0.0 ? (-3.0 * b + sign * std::sqrt(root)) / (10.0 * c) : b != 0.0 ? -a / (3.0 * b) : 0.0;
+            if (q > 0.0 && q < g * g) next = std::max(next, value(std::sqrt(q)));
+        }
+        g = std::min(std::max(next, 1e-300), 1e300);
+        grown += std::log2(std::max(std::fabs(a), 1e-30));
+        int to = 0;
+        if (g > most) to = std::min((int)std::ceil(std::log2(g / most)), (int)std::max(0.0, std::floor(grown)) + 10);
+        else if (g < 0.25) to = (int)std::ceil(std::log2(g));
+        p.a[k] = (float)std::ldexp(a, r - to);
+        p.b[k] = (float)std::ldexp(b, 3 * r - to);
+        p.c[k] = (float)std::ldexp(c, 5 * r - to);
+        r = to;
+    }
+    p.scale = (float)std::ldexp((double)at.scale, r);
+    return p;
+}
+
+namespace {
 
 // ---- workspace -------------------------------------------------------------------------------------------------
 struct Plan {
@@ -321,11 +358,13 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
         BoundsReg reg;
         reg.add(x); reg.add(y);
         RELAY_TRY(reg.commit(st));
-        if (x->dtype == RELAY_F32) return launch_small<float>(x, at, y, pl.L, (int)pl.M, (int)pl.N, st);
-        return launch_small<__nv_bfloat16>(x, at, y, pl.L, (int)pl.M, (int)pl.N, st);
+        const Steps steps = steps_of(*at, 1.0);
+        if (x->dtype == RELAY_F32) return launch_small<float>(x, steps, at->eps, y, pl.L, (int)pl.M, (int)pl.N, st);
+        return launch_small<__nv_bfloat16>(x, steps, at->eps, y, pl.L, (int)pl.M, (int)pl.N, st);
     }
     const float s = exp2f(roundf(log2f(sqrtf((float)pl.M * (float)pl.N) / 8.0f)));
-    if (pl.resident) return launch_resident(x, at, y, pl.L, (int)pl.M, (int)pl.N, s, st);
+    const Steps steps = steps_of(*at, s);
+    if (pl.resident) return launch_resident(x, steps, at->eps, y, pl.L, (int)pl.M, (int)pl.N, s, st);
     int dev = 0, sms = 148;
     RELAY_CUDA(cudaGetDevice(&dev));
     RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -341,7 +380,7 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
 
     Launch l;
     l.done = (unsigned int *)w;
-    l.tall = pl.M > pl.N; l.steps = at->steps; l.batch = (int)pl.L; l.err = err;
+    l.tall = pl.M > pl.N; l.step = steps; l.batch = (int)pl.L; l.err = err;
     l.x[0] = x0; l.x[1] = x1;
     // operands: boxes of 128 rows (A) or 64 (B) x 64 contiguous contraction elements, or 64 contraction rows x 64 contiguous columns
     const uint64_t M = pl.M, N = pl.N, m = pl.m, L = pl.L, xld = pl.xld, gld = pl.gld;
@@ -368,12 +407,10 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
     pg.out = g;
     pg.diag = d;
     pp.k_blocks = (int)((m + 63) / 64);
-    pp.alpha = at->c; pp.beta = at->b; pp.gamma = at->c;
     pp.row_v = pp.col_v = d;
     pp.add = g; pp.add_ld = gld; pp.add_bs = (long long)(m * gld);
     pp.out = q;
-    pp.diag = e;
-    pp.q0 = at->a; pp.q1 = at->b; pp.q2 = at->c;
+    pp.diag = e;                                           // its coefficients are the step's
     px.rows = (int)M; px.cols = (int)N;
     px.k_blocks = pp.k_blocks;
     px.b_mn = !l.tall;
@@ -382,7 +419,7 @@ extern "C" relay_status_t relay_orthogonalize(const relay_tensor_t *x, const rel
     px.v_bs = gld;
     px.add_ld = px.out_ld = xld; px.add_bs = px.out_bs = (long long)(M * xld);
     l.product[3] = px;
-    l.product[3].alpha = l.product[3].gamma = at->scale / s;
+    l.product[3].alpha = l.product[3].gamma = steps.scale / s;
     l.product[3].out = y->data; l.product[3].out_ld = N; l.product[3].out_bs = (long long)(M * N); l.product[3].out_bf16 = 1;
 
     BoundsReg reg;

@@ -9,6 +9,15 @@
 namespace relay {
 namespace orth {
 
+// The coefficients of each step.  X is kept times 2^-r, r by step, where the iteration leaves the 16-bit operands' range: see steps_of.
+constexpr int kMostSteps = 16;
+struct Steps {
+    int n;
+    float a[kMostSteps], b[kMostSteps], c[kMostSteps];
+    float scale;                       // of the result
+};
+Steps steps_of(const relay_orthogonalize_attrs_t &at, double s);
+
 // One product on a batch of fp16 matrices:
 //   out[r,c] = alpha sum_k A(r,k) B(k,c) + (beta + gamma (row_v[r] + col_v[c])) add[r,c]
 // and, for the symmetric ones, the diagonal apart from it in fp32 (out then has a zero there):
@@ -45,8 +54,9 @@ struct Launch {
     Product product[4];                // G, P, X; X of the last step
     void *x[2];                        // X's buffers: step k reads x[k & 1] and writes the other
     UnitTable table[3];
+    Steps step;
     unsigned int *done;                // per matrix, zero at the start: epilogue warps that have finished a unit
-    int tall, steps, batch;
+    int tall, batch;
     int *err;
 };
 
@@ -54,7 +64,7 @@ relay_status_t launch_products(Launch &l, int sms, cudaStream_t st);
 
 // Matrices that stay on the chip (orthogonalize_resident.cu): all of a call in one launch.
 bool resident_fits(int64_t m, int64_t n);
-relay_status_t launch_resident(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *at, const relay_tensor_t *y, int64_t L, int M, int N, float s, cudaStream_t st);
+relay_status_t launch_resident(const relay_tensor_t *x, const Steps &steps, float eps, const relay_tensor_t *y, int64_t L, int M, int N, float s, cudaStream_t st);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ uint32_t instr_desc_f16(int m, int n, int a_mn, int b_mn)

@@ -24,8 +24,9 @@ constexpr int kThreads = 512, kRows = 128, kWidest = 256, kMostBlocks = 8;
 constexpr int kGroup = kRows * 128;                        // bytes of 64 columns
 
 struct Resident {
-    int M, N, m, n, tall, S, w, steps; // w: columns of a slice, a multiple of 32
-    float a, b, c, eps, s, scale;
+    int M, N, m, n, tall, S, w;        // w: columns of a slice, a multiple of 32
+    Steps step;
+    float eps, s;
     int *err;
 };
 struct Scalars {                       // behind the matrices in shared memory
@@ -206,8 +207,9 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
     };
     const float alpha = 1.0f / (q.s * q.s);
     const int k_x = (max(cols, 1) + 15) / 16, k_m = mp / 16, owned = mp / q.S;
-    for (int step = 0; step < q.steps; ++step) {
-        const bool last = step + 1 == q.steps;
+    for (int step = 0; step < q.step.n; ++step) {
+        const bool last = step + 1 == q.step.n;
+        const float ka = q.step.a[step], kb = q.step.b[step], kc = q.step.c[step];
         if (warp == 0)
             for (int kk = 0; kk < k_x; ++kk) tc::mma_bf16_elect(tmem, desc_x + deep(kk), desc_x + deep(kk), idesc_m, kk != 0);
         wait();
@@ -288,9 +290,9 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const float gg = __uint_as_float(acc[j + k]);
-                    v[k] = fmaf(q.c, gg, fmaf(q.c, d_row + sc.d[c0 + j + k], q.b) * v[k]);
+                    v[k] = fmaf(kc, gg, fmaf(kc, d_row + sc.d[c0 + j + k], kb) * v[k]);
                     if (c0 + j + k == row) {
-                        sc.e[row] = q.a + d_row * q.b + q.c * fmaf(d_row, d_row, gg);
+                        sc.e[row] = ka + d_row * kb + kc * fmaf(d_row, d_row, gg);
                         v[k] = 0.0f;
                     }
                 }
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
             for (int kk = 0; kk < k_m; ++kk) tc::mma_bf16_elect(tmem + 128, desc_p + deep(kk), desc_xn + (uint64_t)(kk * 2048 >> 4), idesc_x, kk != 0);
         wait();
         if (mine) {
-            const float e_row = sc.e[row], out = q.scale / q.s;
+            const float e_row = sc.e[row], out = q.step.scale / q.s;
             for (int c = c0; c < q.w; c += 128) {
                 uint32_t acc[32];
                 tc::tmem_ld_32x32(tmem + 128 + lanes + c, acc);
@@ -371,15 +373,15 @@ relay_status_t launch(const relay_tensor_t *x, const relay_tensor_t *y, int64_t 
 
 bool resident_fits(int64_t m, int64_t n) { return m <= kRows && n <= (int64_t)kMostBlocks * kWidest; }
 
-relay_status_t launch_resident(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *at, const relay_tensor_t *y, int64_t L, int M, int N, float s, cudaStream_t st)
+relay_status_t launch_resident(const relay_tensor_t *x, const Steps &steps, float eps, const relay_tensor_t *y, int64_t L, int M, int N, float s, cudaStream_t st)
 {
     Resident q;
     q.M = M; q.N = N; q.m = std::min(M, N); q.n = std::max(M, N);
-    q.tall = M > N; q.steps = at->steps;
+    q.tall = M > N;
     q.S = 1;
     while (q.S * kWidest < q.n) q.S *= 2;
     q.w = ((q.n + q.S - 1) / q.S + 31) / 32 * 32;
-    q.a = at->a; q.b = at->b; q.c = at->c; q.eps = at->eps; q.s = s; q.scale = at->scale;
+    q.step = steps; q.eps = eps; q.s = s;
     q.err = device_error_word();
     if (!q.err) return fail(RELAY_ERR_CUDA, "no device error word");
     BoundsReg reg;

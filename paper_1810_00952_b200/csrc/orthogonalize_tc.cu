@@ -82,7 +82,7 @@ struct Walk {
     {
         enter();
     }
-    __device__ __forceinline__ const Product &product() const { return l.product[phase == 3 * l.steps - 1 ? 3 : kind]; }
+    __device__ __forceinline__ const Product &product() const { return l.product[phase == 3 * l.step.n - 1 ? 3 : kind]; }
     __device__ __forceinline__ int per_matrix() const { return l.product[kind].units; }
     __device__ __forceinline__ void enter()
     {
@@ -96,9 +96,9 @@ struct Walk {
             units = (long long)per_matrix() * l.batch;
             unit = pair - first;
             if (unit < 0) unit += pairs;
-        } while (unit >= units && phase < 3 * l.steps);
+        } while (unit >= units && phase < 3 * l.step.n);
     }
-    __device__ __forceinline__ bool more() const { return phase < 3 * l.steps; }
+    __device__ __forceinline__ bool more() const { return phase < 3 * l.step.n; }
     __device__ __forceinline__ void next()
     {
         unit += pairs;
@@ -210,6 +210,11 @@ struct Terms {
     uint16_t *out;
     const float *row_v, *col_v;
     float *diag;
+    __device__ __forceinline__ Terms(const Product &p, int batch, const void *add_, void *out_, const Steps &s, int step)
+        : Terms(p, batch, add_, out_)
+    {
+        q0 = s.a[step]; beta = q1 = s.b[step]; alpha = gamma = q2 = s.c[step];
+    }
     __device__ __forceinline__ Terms(const Product &p, int batch, const void *add_, void *out_)
     {
         const long long v_at = batch * p.v_bs;
@@ -543,7 +548,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
             const Unit w = walk.at();
             const Product &p = walk.product();
             const int row0 = w.m0 + (int)rank * 128 + quarter * 32;
-            const bool last = walk.phase == 3 * l.steps - 1;
+            const bool last = walk.phase == 3 * l.step.n - 1;
             const void *x = l.x[walk.cur];
             void *x_out = last ? p.out : l.x[walk.cur ^ 1];
             ok = __all_sync(0xffffffffu, wait_done<false>(l.done + w.batch, walk.need, abort_flag, l.err));
@@ -551,7 +556,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
             const Place at{row0, w.m0, w.n0, w.width, slot, lane, tmem_base + ((uint32_t)(quarter * 32) << 16)};
 #define FINISH(KIND, LAST, ADD, OUT) finish_unit<KIND, LAST>(Terms(p, w.batch, ADD, OUT), at, my_stage, tmem_full, tmem_empty, t_local, abort_flag, l.err)
             if (walk.kind == 0) ok = FINISH(IS_G, false, nullptr, p.out);
-            else if (walk.kind == 1) ok = FINISH(IS_P, false, p.add, p.out);
+            else if (walk.kind == 1) ok = finish_unit<IS_P, false>(Terms(p, w.batch, p.add, p.out, l.step, walk.phase / 3), at, my_stage, tmem_full, tmem_empty, t_local, abort_flag, l.err);
             else if (l.tall) ok = last ? FINISH(IS_X_COLUMNS, true, x, x_out) : FINISH(IS_X_COLUMNS, false, x, x_out);
             else ok = last ? FINISH(IS_X_ROWS, true, x, x_out) : FINISH(IS_X_ROWS, false, x, x_out);
 #undef FINISH

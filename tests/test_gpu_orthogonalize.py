@@ -97,6 +97,18 @@ def test_steps_coefficients_and_scale(steps, coef):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("coef,steps", [((10, 0, 0), 6), ((10, 0, 0), 16), ((0.1, 0, 0), 6), ((0.1, 0, 0), 16), ((-3, 0, 0), 9), ((1e4, 0, 0), 3), ((1e-4, 0, 0), 3),
+                                        ((2, 0.5, 0), 4), ((3, 1, 0), 3), ((4, -1, 0), 3)])
+@pytest.mark.parametrize("shape", [(16, 20), (90, 150), (150, 90), (40, 600), (300, 200), (200, 300), (600, 900)])
+def test_coefficients_that_let_the_matrix_grow_or_shrink(coef, steps, shape):
+    """From 1e-19 to 1e14 of the norm, far outside the 16-bit operands' own range.  Rounding the operands of the fp64 iteration on the
+    CPU, kept in range by powers of two, gives errors of 1.4e-4 to 8.6e-4 of the result's norm over these cases: the bounds above hold."""
+    x = matrices(shape, F32, steps)
+    c = tuple(float(np.float32(v)) for v in coef)
+    close(run(x, steps, coef, 0.0, 1.0), L.orthogonalize(to_np(x), steps, c, 0.0, 1.0))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e12, 1e30])
 def test_only_the_direction_counts(scale):
     x = matrices((140, 200), F32, 3)
