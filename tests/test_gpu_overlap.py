@@ -28,6 +28,36 @@ class Orthogonalize:
         B.relay_orthogonalize(self.x, 5, QUINTIC, 1e-7, 1.0, self.y, self.ws)
 
 
+class Recurrence:
+    """The forward call and its gradient group, one after the other."""
+
+    def __init__(self, T, Bn, D, seed, dt=BF16):
+        self.f, self.u, self.dh = (randn(T, Bn, D, dt=dt, seed=seed + k) for k in range(3))
+        self.h0 = randn(Bn, D, dt=F32, seed=seed + 3)
+        self.h, self.df, self.du = (torch.empty_like(self.f) for _ in range(3))
+        self.last, self.dh0 = torch.empty_like(self.h0), torch.empty_like(self.h0)
+        self.outs = [self.h, self.last, self.df, self.du, self.dh0]
+
+    def __call__(self):
+        B.relay_gated_recurrence(self.f, self.u, self.h0, None, B.GATE_MIX, self.h, self.last)
+        B.relay_gated_recurrence_grad(self.f, self.u, self.h0, None, B.GATE_MIX, self.h, self.dh, self.h0, self.df, self.du, self.dh0)
+
+
+class TokenLogprob:
+    def __init__(self, N, V, top, seed, dt=BF16):
+        self.z = randn(N, V, dt=dt, seed=seed)
+        self.tok = torch.arange(N, device=DEV, dtype=torch.int32) % V
+        self.d = randn(N, dt=F32, seed=seed + 1)
+        self.logp, self.entropy, self.lse = (torch.empty(N, device=DEV) for _ in range(3))
+        self.top, self.ids = torch.empty(N, top, device=DEV), torch.empty(N, top, device=DEV, dtype=torch.int32)
+        self.dz = torch.empty_like(self.z)
+        self.outs = [self.logp, self.entropy, self.lse, self.top, self.ids, self.dz]
+
+    def __call__(self):
+        B.relay_token_logprob(self.z, self.tok, 0.8, self.logp, self.entropy, self.lse, self.top, self.ids)
+        B.relay_token_logprob_grad(self.z, self.tok, 0.8, self.lse, self.entropy, self.d, self.d, self.dz)
+
+
 def alone(call):
     call()
     torch.cuda.synchronize()
@@ -201,3 +231,15 @@ def test_persistent_clusters_of_the_recurrence_are_planned_for_the_room_they_fin
     clusters = ctypes.c_int(0)
     assert cu.cuOccupancyMaxActiveClusters(ctypes.byref(clusters), func, ctypes.byref(config)) == 0
     assert p.dims[0] // size[0] <= clusters.value, (p.dims[0], size[0], clusters.value)
+
+
+@pytest.mark.parametrize("first,second", [
+    (lambda: Recurrence(3000, 1, 512, 1), lambda: Recurrence(700, 4, 1024, 11, F32)),
+    (lambda: Recurrence(900, 3, 333, 1), lambda: Recurrence(8, 64, 1024, 11)),
+    (lambda: TokenLogprob(8, 131072, 20, 1), lambda: TokenLogprob(600, 5003, 5, 11, F32)),
+    (lambda: Recurrence(3000, 1, 512, 1), lambda: TokenLogprob(8, 131072, 20, 11)),
+    (lambda: Orthogonalize((300, 500), 1), lambda: Recurrence(3000, 1, 512, 11, F32)),
+    (lambda: Orthogonalize((128, 2048), 1), lambda: TokenLogprob(600, 5003, 64, 11))],
+    ids=["tiles", "spans and steps", "log-probabilities", "recurrence and log-probabilities", "products and recurrence", "on the chip and log-probabilities"])
+def test_operators_of_a_language_model_on_two_streams(first, second):
+    check_overlap(first(), second())
