@@ -285,8 +285,8 @@ Plan plan_of(const relay_tensor_t *x)
     p.total = p.n_bytes + 2 * p.x_bytes + 2 * p.g_bytes + 2 * p.v_bytes + align_up((size_t)p.L * 4, 256);
     p.small = small_fits(p.m, p.n);
     p.resident = !p.small && resident_fits(p.m, p.n);
-    // On the chip nothing is kept in the workspace.  The smallest one is asked for all the same: above kSmallSize elements every call
-    // has to bring a workspace, whichever form takes its size.
+    // No kernel reads or writes the 256 bytes of a matrix that stays on the chip: they are the documented minimum above kSmallSize, which
+    // a caller meets whichever form takes the size, and which may come to be used.
     if (p.resident) p.total = 256;
     if (p.small) p.total = 0;
     return p;

@@ -205,3 +205,24 @@ def test_refusals_leave_the_output_untouched(monkeypatch):
         f(x=same, y=same, ws=torch.zeros(1 << 18, dtype=torch.uint8))
     assert e.value.status_name == "ERR_ATTR"
     assert B.relay_launch_count() == n0 and bool((y == 5).all())
+
+
+@pytest.mark.parametrize("shape", [(200, 333), (333, 200), (2, 3, 200, 333)])
+def test_products_refuse_a_workspace_that_is_too_small_or_misaligned(monkeypatch, shape):
+    """Sizes whose workspace the kernels write; refused on the host, before a launch (host memory)."""
+    monkeypatch.setattr(B, "_stream", lambda: ctypes.c_void_p(None))
+    x, y = torch.zeros(shape), torch.full(shape, 5, dtype=BF16)
+    n = B.relay_workspace_bytes_orthogonalize(x)
+    m, k = min(shape[-2:]), max(shape[-2:])
+    batch = int(np.prod(shape[:-2], initial=1))
+    assert n >= batch * 2 * (2 * m * k + 2 * m * m)                       # X twice, G and P in 16 bits
+    less = B.relay_workspace_bytes_orthogonalize(torch.zeros(*shape[:-2], 190, 333))
+    assert less < n
+    ws = torch.zeros(n + 64, dtype=torch.uint8)
+    ws = ws[(-ws.data_ptr()) % 16:]
+    n0 = B.relay_launch_count()
+    for bad in (None, ws[:0], ws[:16], ws[:n - 1], ws[:less], ws[8:8 + n], ws[1:1 + n]):
+        with pytest.raises(B.RelayError) as e:
+            B.relay_orthogonalize(x, 5, QUINTIC, 1e-7, 1.0, y, bad)
+        assert e.value.status_name == "ERR_WORKSPACE"
+    assert B.relay_launch_count() == n0 and bool((y == 5).all())
