@@ -226,3 +226,30 @@ def test_products_refuse_a_workspace_that_is_too_small_or_misaligned(monkeypatch
             B.relay_orthogonalize(x, 5, QUINTIC, 1e-7, 1.0, y, bad)
         assert e.value.status_name == "ERR_WORKSPACE"
     assert B.relay_launch_count() == n0 and bool((y == 5).all())
+
+
+# Singular values that fall off, as those of gradients do.  Rounding the operands of the fp64 iteration on the CPU gives, over the
+# sizes here, at most these errors over the result's norm; the results' own rounding adds 1.7e-3, and a fifth is left for the order of sums.
+DECAY = {"1/i": 0.0033, "1/i^2": 0.0204, "rank 8 and noise of 1 %": 0.0230, "rank 16": 0.0478}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spectrum", list(DECAY))
+@pytest.mark.parametrize("shape", [(96, 160), (128, 1000), (333, 500), (512, 768), (768, 512)])
+def test_singular_values_that_fall_off(spectrum, shape):
+    x = falling(shape, spectrum)
+    w = L.orthogonalize(to_np(x), 5, tuple(float(np.float32(v)) for v in QUINTIC), 1e-7, 1.0)
+    g = to_np(run(x))
+    assert rms(g - w) <= (1.2 * DECAY[spectrum] + 1.7e-3) * rms(w), rms(g - w) / rms(w)
+
+
+def falling(shape, spectrum):
+    r = np.random.default_rng(shape[0] + shape[1])
+    n = min(shape)
+    u, v = np.linalg.qr(r.normal(size=(shape[0], n)))[0], np.linalg.qr(r.normal(size=(shape[1], n)))[0]
+    i = np.arange(1, n + 1)
+    s = {"1/i": 1.0 / i, "1/i^2": 1.0 / i ** 2, "rank 8 and noise of 1 %": np.where(i <= 8, 1.0, 0.0), "rank 16": np.where(i <= 16, 1.0, 0.0)}[spectrum]
+    x = (u * s) @ v.T
+    if spectrum.startswith("rank 8"):
+        x = x + 0.01 * np.linalg.norm(x) / np.sqrt(x.size) * r.normal(size=shape)
+    return torch.from_numpy(x).to(F32)
