@@ -1284,25 +1284,33 @@ Form form_of(const Args &p, long long of_t, long long of_h)
     return p.T > kSteps && p.C * of_h < (1ll << 32) ? SPANS : STEPS;
 }
 
-// W channels a thread in the spans kernels, at most two in the step-by-step ones (more threads where there are few steps)
-template <typename T, typename TH, int GATE, int W>
-relay_status_t launch(const Args &p, bool grad, cudaStream_t st)
+// V channels a lane.  Two, where rows allow it: bf16, and the fp32 forward call where all steps of a lane's channels are one slab or two;
+// not where there are too few channels to give every SM a block then.  The steps a lane keeps in registers are as many as fit without
+// spilling to memory (a few words in the fp32 instances).  4096 steps of 13 x 334 channels, one and two a lane: bf16 forward 39.7 and 34.0
+// us, gradient 79.6 and 62.0; fp32 60.8 and 89, gradient 116 and 157.  64 steps of 64 x 1022: bf16 27.9 and 17.3, fp32 29.5 and 24.9, its
+// gradient 40.4 and 36.8.  16384 x 1 x 66 in bf16: 32 and 59.
+constexpr long long kShortSpans = 64;
+template <typename T, typename TH, int GATE, int V>
+relay_status_t launch_spans(const Args &p, bool grad, int sms, cudaStream_t st)
 {
-    if (form_of(p, sizeof(T), sizeof(TH)) == SPANS) {
-        constexpr int TS = (sizeof(T) == 2 ? 32 : 16) / (W == 1 ? 2 : W), TSG = (sizeof(T) + sizeof(TH) == 4 ? 16 : 8) / (W == 1 ? 2 : W);
-        int dev = 0, sms = 148;
-        RELAY_CUDA(cudaGetDevice(&dev));
-        RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-        const long long tiles = (p.C + 32 * W - 1) / (32 * W), steps = kWarps * (grad ? TSG : TS);
-        int S = 1;
-        while (S < 8 && tiles * S < sms && p.T > S * steps) S *= 2;
-        if (tiles * S > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "gated_recurrence: %lld channels", p.C);
-        const dim3 grid((unsigned)(tiles * S)), block(32 * kWarps), cluster((unsigned)S);
-        if (grad) RELAY_CUDA(launch_pdl_cluster(recurrence_grad_spans_kernel<T, TH, GATE, W, TSG>, grid, block, cluster, 0, st, p, S));
-        else RELAY_CUDA(launch_pdl_cluster(recurrence_spans_kernel<T, TH, GATE, W, TS>, grid, block, cluster, 0, st, p, S));
-        return check_launch("gated_recurrence");
+    constexpr int TS = (sizeof(T) == 2 ? 16 : 8) / V, TSG = sizeof(T) + sizeof(TH) == 4 ? 8 / V : 4;
+    const long long tiles = (p.C + 32 * V - 1) / (32 * V), steps = kWarps * (grad ? TSG : TS);
+    int S = 1;
+    while (S < 8 && tiles * S < sms && p.T > S * steps) S *= 2;
+    if (tiles * S > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "gated_recurrence: %lld channels", p.C);
+    const dim3 grid((unsigned)(tiles * S)), block(32 * kWarps), cluster((unsigned)S);
+    if constexpr (sizeof(T) == 2 || V == 1) {
+        if (grad) {
+            RELAY_CUDA(launch_pdl_cluster(recurrence_grad_spans_kernel<T, TH, GATE, V, TSG>, grid, block, cluster, 0, st, p, S));
+            return check_launch("gated_recurrence");
+        }
     }
-    constexpr int V = W == 1 ? 1 : 2;
+    RELAY_CUDA(launch_pdl_cluster(recurrence_spans_kernel<T, TH, GATE, V, TS>, grid, block, cluster, 0, st, p, S));
+    return check_launch("gated_recurrence");
+}
+template <typename T, typename TH, int GATE, int V>
+relay_status_t launch_steps(const Args &p, bool grad, cudaStream_t st)
+{
     const long long blocks = (p.C / V + kThreads - 1) / kThreads;
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "gated_recurrence: %lld channels", p.C);
     const dim3 grid((unsigned)blocks);
@@ -1314,10 +1322,16 @@ template <typename T, typename TH, int GATE>
 relay_status_t launch_gate(const Args &p, bool grad, cudaStream_t st)
 {
     if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
-    if (form_of(p, sizeof(T), sizeof(TH)) == TILES) return launch_tiles<T, TH, GATE>(p, grad, st);
-    // several channels a thread where every row starts at a multiple of them, so that they are one aligned access
-    const long long rows = p.D | p.ld | p.bs;
-    return rows % 2 == 0 ? launch<T, TH, GATE, 2>(p, grad, st) : launch<T, TH, GATE, 1>(p, grad, st);
+    const Form form = form_of(p, sizeof(T), sizeof(TH));
+    if (form == TILES) return launch_tiles<T, TH, GATE>(p, grad, st);
+    // two channels a thread where every row starts at a multiple of them, so that they are one aligned access
+    const bool even = (p.D | p.ld | p.bs) % 2 == 0;
+    if (form == STEPS) return even ? launch_steps<T, TH, GATE, 2>(p, grad, st) : launch_steps<T, TH, GATE, 1>(p, grad, st);
+    int dev = 0, sms = 148;
+    RELAY_CUDA(cudaGetDevice(&dev));
+    RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const bool two = even && (p.C + 63) / 64 * 8 >= sms && (sizeof(T) == 2 || (!grad && p.T <= kShortSpans));
+    return two ? launch_spans<T, TH, GATE, 2>(p, grad, sms, st) : launch_spans<T, TH, GATE, 1>(p, grad, sms, st);
 }
 template <typename T, typename TH>
 relay_status_t launch_typed(const Args &p, int32_t gate, bool grad, cudaStream_t st)
