@@ -374,6 +374,11 @@ __device__ __forceinline__ void store_remote(uint32_t at, uint32_t v) { asm vola
 // the number of larger ones.
 constexpr int kList = 512;             // listed elements; expected -G ln(1 - K / G): 31 for K = 20, G = 32, 89 for K = 64, G = 128
 
+// Up to how many alternatives 32 groups bound them, in blocks of 128 and of 512 threads.  More groups list fewer elements, but finding
+// their K-th largest takes longer.  32 groups against 128: 8192 x 4000 bf16 (128 threads) K = 20 52 and 62 us, 24 60 and 63, 28 67 and
+// 65, 31 87 and 67; 4096 x 32768 74 and 77, 78 and 78, 84 and 80, 98 and 82; 8 x 131072 (512 threads) K = 20 10.5 and 19.3, 28 11.9 and
+// 20.2, 31 14 and 20.5.  32 groups cannot bound more than 31.
+constexpr int kFewGroups128 = 24, kFewGroups512 = 31;
 template <int NT>
 struct Lists {
     unsigned long long largest[NT];    // per thread: a key not above its largest element's
@@ -404,7 +409,7 @@ template <int NT, typename T, bool EVEN, typename Meanwhile>
 __device__ __forceinline__ bool list_largest(Lists<NT> &l, const RowVectors<T, EVEN> &r, int v0, int v1, int K, unsigned long long mine, int per, int used, Meanwhile meanwhile)
 {
     constexpr int E = Vec<T>::E;
-    const int tid = threadIdx.x, groups = K <= 20 ? 32 : 128;          // group: the threads of equal tid mod groups
+    const int tid = threadIdx.x, groups = K <= (NT == 128 ? kFewGroups128 : kFewGroups512) ? 32 : 128;     // group: the threads of equal tid mod groups
     if (tid == 0) l.count = l.eighths = 0;
     bool is_bound = false;
     if (tid < groups) {

@@ -110,6 +110,22 @@ def test_many_rows(N, V):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("N,V", [(5, 100), (5, 9001), (2, 60000), (320, 2000), (320, 601)])
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("top", [20, 21, 24, 25, 31, 32, 33, 63, 64])
+def test_numbers_of_alternatives_around_the_changes_of_their_bound(N, V, dt, top):
+    r = np.random.default_rng(V + top)
+    z = torch.from_numpy(r.normal(0, 3, (N, V))).to(dt)
+    z[0] = torch.arange(V).to(dt)                        # rising; in bf16 with many equal ones
+    z[1, : V - 3] = -INF                                 # fewer than asked for can occur
+    some = [0, 1, N // 2, N - 1]
+    o = forward(z, torch.zeros(N, dtype=torch.int32), 1.0, top)
+    w = L.token_logprob(to_np(z[some]), np.zeros(len(some), int), 1.0, top)
+    np.testing.assert_array_equal(o["top_ids"][some].cpu().numpy(), w["top_ids"])
+    same(o["top_logp"][some], w["top_logp"], "top_logp")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("V", [11, 300, 5003, 40000])
 @pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("top", [1, 8, 64])
