@@ -505,6 +505,18 @@ def relay_debug_plan_units(M: int, N: int, K: int, sms: int, max_units: int = 10
     return [(int(e) & 0xFFF, (int(e) >> 12) & 0xFFF, int(e) >> 24) for e in buf[:n]]
 
 
+def relay_debug_orthogonalize_units(rows: int, cols: int, symmetric: bool, k_blocks: int, batch: int, pairs: int):
+    """Unit plan of one product of the orthogonalised update as (row block of 256, first piece of 64 columns, pieces) triples, or None
+    when the kernel would follow its fixed scheme."""
+    buf = (ctypes.c_uint32 * 640)()
+    n = int(lib().relay_debug_orthogonalize_units(int(rows), int(cols), 1 if symmetric else 0, int(k_blocks), int(batch), int(pairs), buf, 640))
+    if n == -1:
+        return None
+    if n < 0:
+        raise ValueError("relay_debug_orthogonalize_units: bad arguments")
+    return [(int(e) & 0xFF, (int(e) >> 8) & 0x7FF, int(e) >> 19) for e in buf[:n]]
+
+
 def relay_launch_count() -> int:
     return int(lib().relay_launch_count())
 

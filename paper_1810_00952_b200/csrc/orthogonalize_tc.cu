@@ -25,7 +25,6 @@
 // in the leader; empty[] and tmem_full[] in each block, by multicast commits; tmem_empty[] in the leader.
 #include <algorithm>
 #include <cuda_fp16.h>
-#include <vector>
 
 #include "common.h"
 #include "ewise_kernels.cuh"
@@ -585,45 +584,56 @@ double epilogue_cycles(int c) { return 1500.0 + 1250.0 * c; }
 constexpr int kWidths[] = {1, 2, 4, 6, 8};
 int width_of(long long pieces) { return pieces <= 1 ? 1 : (int)((pieces + 1) / 2 * 2); }
 
-// Cuts the rows of pieces of one matrix into units, taking widths from `rounds` (one width for each `quota` units, the last one
-// for whatever follows); false if they are more than the table holds.
-bool cut(const Product &p, int quota0, const std::vector<int> &rounds, std::vector<uint32_t> *units)
+// The widths of a cut's rounds: one throughout, or (share) as many pieces as are left of a pair's share, the widest first.
+struct Widths {
+    int widest;
+    bool share;
+    long long left;                    // of the share
+    int now() const { return share ? std::min(widest, width_of(left)) : widest; }
+    void next() { if (share && left > now()) left -= now(); }
+};
+// Cuts the rows of pieces of one matrix into units, a width for each `quota0` of them, widest first in the table; false if they are
+// more than it holds.  Nothing here allocates: a call cannot fail for want of host memory.
+bool cut(const Product &p, int quota0, Widths width, UnitTable *units)
 {
+    UnitTable cut;
+    cut.n = 0;
     const int per_row = (p.cols + 63) / 64;
-    units->clear();
-    size_t r = 0;
     int quota = quota0;
     for (int m = 0; m < p.tiles_m; ++m) {
         int at = p.symmetric ? 4 * m : 0;
         while (at < per_row) {
-            const int c = std::min(rounds[std::min(r, rounds.size() - 1)], width_of(per_row - at));
-            if (units->size() == (size_t)UnitTable::kMax) return false;
-            units->push_back((uint32_t)m | ((uint32_t)at << 8) | ((uint32_t)c << 19));
+            const int c = std::min(width.now(), width_of(per_row - at));
+            if (cut.n == UnitTable::kMax) return false;
+            cut.e[cut.n++] = (uint32_t)m | ((uint32_t)at << 8) | ((uint32_t)c << 19);
             at += c;
-            if (--quota == 0) { quota = quota0; ++r; }
+            if (--quota == 0) { quota = quota0; width.next(); }
         }
     }
-    std::stable_sort(units->begin(), units->end(), [](uint32_t a, uint32_t b) { return (a >> 19) > (b >> 19); });
+    units->n = 0;
+    for (int k = (int)(sizeof kWidths / sizeof *kWidths) - 1; k >= 0; --k)
+        for (int i = 0; i < cut.n; ++i)
+            if ((int)(cut.e[i] >> 19) == kWidths[k]) units->e[units->n++] = cut.e[i];
     return true;
 }
 // The phase's length: each round over the pairs takes as long as its widest unit; a wide unit's epilogue is in the way of the next
 // unit, and the last unit's is always in the way of the next phase.  A matrix's units come widest first, so the widest of a round is
 // its first or, where another matrix begins in it, the widest of all.  Of very many rounds the first few stand for all.
-double finish_time(const std::vector<uint32_t> &units, int batch, int pairs, int k_blocks)
+double finish_time(const UnitTable &units, int batch, int pairs, int k_blocks)
 {
     constexpr long long kLook = 256;
     double t = 0, last = 0;
-    const long long size = (long long)units.size(), n = size * batch, rounds = (n + pairs - 1) / pairs;
+    const long long size = units.n, n = size * batch, rounds = (n + pairs - 1) / pairs;
     for (long long r = 0; r < std::min(rounds, kLook); ++r) {
         const long long at = r * pairs % size;
-        const int c = (int)(units[at + std::min<long long>(pairs, n - r * pairs) > size ? 0 : (size_t)at] >> 19);
+        const int c = (int)(units.e[at + std::min<long long>(pairs, n - r * pairs) > size ? 0 : at] >> 19);
         if (c >= 6 && last > 0) t += last;
         t += main_cycles(c, k_blocks);
         last = epilogue_cycles(c);
     }
     return (t + last) * std::max(1.0, (double)rounds / (double)kLook);
 }
-// the cut that finishes first: one width throughout, or as many pieces as a pair's share has, the widest first
+// the cut that finishes first
 void plan(Product *p, int batch, int pairs, UnitTable *tb)
 {
     p->tiles_m = (p->rows + 255) / 256;
@@ -633,20 +643,15 @@ void plan(Product *p, int batch, int pairs, UnitTable *tb)
     long long total = 0;
     for (int m = 0; m < p->tiles_m; ++m) total += std::max(0, per_row - (p->symmetric ? 4 * m : 0));
     const int quota = std::max(1, pairs / batch);
-    std::vector<uint32_t> units, best;
+    UnitTable units;
     double best_time = 0;
     for (int widest : kWidths)
         for (int share = 0; share < 2; ++share) {
-            std::vector<int> rounds;
-            if (share) for (long long left = (total + quota - 1) / quota; left > 0; left -= rounds.back()) rounds.push_back(std::min(widest, width_of(left)));
-            else rounds.push_back(widest);
-            if (!cut(*p, quota, rounds, &units)) continue;
+            if (!cut(*p, quota, Widths{widest, share != 0, (total + quota - 1) / quota}, &units)) continue;
             const double t = finish_time(units, batch, pairs, p->k_blocks);
-            if (best.empty() || t < best_time) { best = units; best_time = t; }
+            if (tb->n == 0 || t < best_time) { *tb = units; best_time = t; }
         }
-    if (best.empty()) return;
-    tb->n = p->units = (int)best.size();
-    std::copy(best.begin(), best.end(), tb->e);
+    if (tb->n > 0) p->units = tb->n;
 }
 
 // pairs that are resident at once on this device
@@ -688,3 +693,20 @@ relay_status_t launch_products(Launch &l, int sms, cudaStream_t st)
 
 }  // namespace orth
 }  // namespace relay
+
+// Host-only view of the plan of one product (rows x cols results per matrix, contraction steps of 64): units as in UnitTable, widest
+// first; -1 where 256 x 256 units in order would run, -2 for bad arguments.
+extern "C" int32_t relay_debug_orthogonalize_units(int32_t rows, int32_t cols, int32_t symmetric, int32_t k_blocks, int32_t batch, int32_t pairs, uint32_t *units,
+                                                   int32_t max_units)
+{
+    using namespace relay::orth;
+    if (rows < 1 || cols < 1 || rows > 65536 || cols > 65536 || k_blocks < 1 || batch < 1 || pairs < 1 || !units || (symmetric && rows != cols)) return -2;
+    Product p{};
+    p.rows = rows; p.cols = cols; p.symmetric = symmetric != 0; p.k_blocks = k_blocks;
+    UnitTable tb;
+    plan(&p, batch, pairs, &tb);
+    if (tb.n == 0) return -1;
+    if (tb.n > max_units) return -2;
+    std::copy(tb.e, tb.e + tb.n, units);
+    return tb.n;
+}
