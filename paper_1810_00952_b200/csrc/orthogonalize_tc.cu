@@ -477,6 +477,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1) orth
                 if (++s == n_st) { s = 0; phase ^= 1; }
             }
         }
+        // Neither block leaves before the copies into both have landed, whoever gave up; bounded, for a stage that lacks a part.
+        if (rank == 0 && load_a)
+            for (int i = 0; i < n_st; ++i)
+                for (int k = 0; k < 100000 && !tc::mbar_try_wait(&full[i], i < s ? phase : phase ^ 1); ++k) {}
     } else if (warp == 1) {
         if (rank == 0) {
             constexpr uint32_t b1_off = (2 * CHUNK_BYTES) >> 4;   // the second MMA's columns follow the first's 128 in this block
