@@ -18,12 +18,13 @@
 //
 // Measured at 4096 x 4096: 1.33 ms, 1.04 PFLOP/s; per step of 222 us the MMAs take 163 (at the power-limited clock) and the three
 // changes of phase 59, in which the last unit's epilogue runs with all SMs storing at once.  One launch per product: 1.39 ms for 8 x 1024
-// x 4096 against 0.85, 194 us for 3 x 500 x 333 against 122 (112 since units of 64 columns).  Epilogues with TMA stores, with sixteen warps, or in line with the roles
-// were slower (sixteen warps and the in-line form spill registers).
+// x 4096 against 0.84, 194 us for 3 x 500 x 333 against 122 (114 since units of 64 columns).  Epilogues with TMA stores, with sixteen warps
+// (whose registers spill in every unit), or in line with the roles were slower; this form keeps some 100 bytes of a unit's terms on the stack.
 //
 // Roles per block: warp 0 loads A, the last warp loads B, warp 1 of the leader issues the MMAs, eight warps are the epilogue.  full[] lives
 // in the leader; empty[] and tmem_full[] in each block, by multicast commits; tmem_empty[] in the leader.
 #include <algorithm>
+#include <atomic>
 #include <cuda_fp16.h>
 
 #include "common.h"
@@ -661,10 +662,10 @@ void plan(Product *p, int batch, int pairs, UnitTable *tb)
 // pairs that are resident at once on this device
 int resident_pairs(int sms)
 {
-    static int known[64] = {0};
+    static std::atomic<int> known[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    if (known[dev] == 0) {
+    if (known[dev].load(std::memory_order_relaxed) == 0) {
         if (cudaFuncSetAttribute(orth_products_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES) != cudaSuccess) { cudaGetLastError(); return 0; }
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(sms / 2 * 2)); cfg.blockDim = dim3(NUM_THREADS); cfg.dynamicSmemBytes = SMEM_BYTES;
@@ -674,9 +675,9 @@ int resident_pairs(int sms)
         cfg.attrs = attr; cfg.numAttrs = 1;
         int n = 0;
         if (cudaOccupancyMaxActiveClusters(&n, orth_products_kernel, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
-        known[dev] = n;
+        known[dev].store(n, std::memory_order_relaxed);
     }
-    return std::min(known[dev], sms / 2);
+    return std::min(known[dev].load(std::memory_order_relaxed), sms / 2);
 }
 
 }  // namespace

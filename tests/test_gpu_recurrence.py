@@ -125,6 +125,16 @@ def test_long_and_wide(T, Bn, D, ragged):
     check_case(T, Bn, D, F32, B.GATE_MIX, False, ragged, seed=5)
 
 
+# rows of an even width that are not whole 16-byte pieces, with enough channels for two a lane: either side of every rule
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [33, 64, 65, 200])
+@pytest.mark.parametrize("Bn,D", [(2, 1022), (1, 66), (7, 170)])
+@pytest.mark.parametrize("dt,out_dt", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("gate,packed,ragged", [(B.GATE_GIVEN, True, False), (B.GATE_SIGMOID, False, True), (B.GATE_MIX, True, True)])
+def test_even_rows_that_are_not_whole_pieces(T, Bn, D, dt, out_dt, gate, packed, ragged):
+    check_case(T, Bn, D, dt, gate, packed, ragged, out_dt)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("T", [1, 40, 700])
 def test_absent_states_are_zero(T):
