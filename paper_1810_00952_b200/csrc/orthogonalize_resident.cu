@@ -8,7 +8,7 @@
 //   P      = b G + c G G by every block for itself: 128^3 products are less than an exchange
 //   X      <- e X + offdiag(P) X in place
 // with the diagonals apart in fp32, as in the products of larger matrices.  Every phase ends in a barrier of the block, so what
-// bounds a step is its chain of latencies: three times MMA, TMEM to registers, shared memory (4.7 us at 128 x 256); and the exchange
+// bounds a step is its chain of latencies: three times MMA, TMEM to registers, shared memory (4.8 us at 128 x 256); and the exchange
 // of G (3.3 us between two blocks, 5 between eight; by st.async, whose every 16 bytes update a barrier, 5 and 5).
 #include <algorithm>
 
@@ -25,12 +25,14 @@ constexpr int kGroup = kRows * 128;                        // bytes of 64 column
 
 struct Resident {
     int M, N, m, n, tall, S, w;        // w: columns of a slice, a multiple of 32
-    Steps step;
-    float eps, s;
+    float eps, s, scale;
+    int steps;
     int *err;
+    Steps step;
 };
 struct Scalars {                       // behind the matrices in shared memory
     float d[kRows], e[kRows];          // the diagonals of G and of a I + P
+    float a[kMostSteps], b[kMostSteps], c[kMostSteps];     // the steps' coefficients (indexing the parameters by step instead: 0.1 us a step more)
     double warp_sum[kThreads / 32], norm[kMostBlocks];
     uint64_t bar;
     uint32_t tmem;
@@ -116,6 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
         tc::tmem_alloc(&sc.tmem, tmem_cols);
         tc::tmem_relinquish();
     }
+    if (tid < kMostSteps) { sc.a[tid] = q.step.a[tid]; sc.b[tid] = q.step.b[tid]; sc.c[tid] = q.step.c[tid]; }
     for (int i = tid; i < groups * kGroup / 16; i += kThreads) reinterpret_cast<uint4 *>(X)[i] = make_uint4(0, 0, 0, 0);
     tc::tc_fence_before_sync();
     __syncthreads();
@@ -207,9 +210,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
     };
     const float alpha = 1.0f / (q.s * q.s);
     const int k_x = (max(cols, 1) + 15) / 16, k_m = mp / 16, owned = mp / q.S;
-    for (int step = 0; step < q.step.n; ++step) {
-        const bool last = step + 1 == q.step.n;
-        const float ka = q.step.a[step], kb = q.step.b[step], kc = q.step.c[step];
+    for (int step = 0; step < q.steps; ++step) {
+        const bool last = step + 1 == q.steps;
         if (warp == 0)
             for (int kk = 0; kk < k_x; ++kk) tc::mma_bf16_elect(tmem, desc_x + deep(kk), desc_x + deep(kk), idesc_m, kk != 0);
         wait();
@@ -281,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
         if (mine && c0 < mp) {
             uint32_t acc[32];
             tc::tmem_ld_32x32(tmem + lanes + c0, acc);
-            const float d_row = sc.d[row];
+            const float d_row = sc.d[row], ka = sc.a[step], kb = sc.b[step], kc = sc.c[step];
             tc::tmem_ld_wait();
 #pragma unroll
             for (int j = 0; j < 32; j += 8) {
@@ -305,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_resident_kernel(const T *__r
             for (int kk = 0; kk < k_m; ++kk) tc::mma_bf16_elect(tmem + 128, desc_p + deep(kk), desc_xn + (uint64_t)(kk * 2048 >> 4), idesc_x, kk != 0);
         wait();
         if (mine) {
-            const float e_row = sc.e[row], out = q.step.scale / q.s;
+            const float e_row = sc.e[row], out = q.scale / q.s;
             for (int c = c0; c < q.w; c += 128) {
                 uint32_t acc[32];
                 tc::tmem_ld_32x32(tmem + 128 + lanes + c, acc);
@@ -381,7 +383,7 @@ relay_status_t launch_resident(const relay_tensor_t *x, const Steps &steps, floa
     q.S = 1;
     while (q.S * kWidest < q.n) q.S *= 2;
     q.w = ((q.n + q.S - 1) / q.S + 31) / 32 * 32;
-    q.step = steps; q.eps = eps; q.s = s;
+    q.step = steps; q.steps = steps.n; q.scale = steps.scale; q.eps = eps; q.s = s;
     q.err = device_error_word();
     if (!q.err) return fail(RELAY_ERR_CUDA, "no device error word");
     BoundsReg reg;
