@@ -7,7 +7,7 @@
 // Three products a step on the tensor cores (tcgen05, kind::f16).  G and P are symmetric: only the tiles on and above the
 // diagonal are computed, each stored to both places, so a step costs m m n + m m m + 2 m m n operations.  The operands lie in
 // the workspace as fp16: at the tensor rate of bf16 it keeps 10 fraction bits instead of 7, and with them an update that is 1e-3
-// instead of 1e-2 off (where singular values fall off, 0.3 to 5 % instead of 3 to 43: see the entry point).  Their range: with the usual coefficients singular values never leave [0, 1.3]; X is kept times a power of two,
+// instead of 1e-2 off (where singular values fall off, 0.3 to 5 % instead of 3 to 38: see the entry point).  Their range: with the usual coefficients singular values never leave [0, 1.3]; X is kept times a power of two,
 // S = 2^round(log2(sqrt(M N) / 8)), which puts its elements around 1/8 at the start and below 0.16 sqrt(M N) ever after; other
 // coefficients may let X grow or shrink, and further powers of two per step follow that (steps_of).  What is too small for fp16 in G
 // and P is small against the diagonal.  The diagonals of G and P, whose entries grow to 1 and -2.7
@@ -21,7 +21,7 @@
 //   up to 128 x 2048            a cluster that keeps the matrix on the chip (orthogonalize_resident.cu): 128 x 256 32 us against 86
 //   all others                  pairs of SMs over the products' units (orthogonalize_tc.cu), after two passes for norm and copy
 // Measured: 4096 x 4096 1.33 ms = 1.04 PFLOP/s of the operations above (cuBLAS on a plain product: 1.63 burst, 1.38 sustained);
-// 8 x 1024 x 4096 0.85 ms = 0.66 PFLOP/s; 3 x 500 x 333 112 us, a step 19 to 21: three phases of 6 to 7 us each, whatever their size.
+// 8 x 1024 x 4096 0.84 ms = 0.66 PFLOP/s; 3 x 500 x 333 114 us, a step 19 to 21: three phases of 6 to 7 us each, whatever their size.
 #include <algorithm>
 #include <cmath>
 #include <cuda_fp16.h>

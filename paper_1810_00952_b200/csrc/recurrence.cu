@@ -2,12 +2,13 @@
 // paper: reverse mode through the recursion over time).  Elementwise steps: HBM-bound where the channels fill the GPU.
 //
 // Bytes: the forward group reads f and u and writes h once, the gradient reads f, u, h, dh and writes df, du once.  Measured against
-// a copy at 6.53 TB/s: 16384 x 1 x 4096 in bf16 85 us (4.7 TB/s), gradient of 4096 x 8 x 1024 in bf16 87 us (4.6 TB/s), the same
-// forward in fp32 115 us (3.5 TB/s, bound by its instructions, fp64 states among them).  Short of that the length of the chain counts:
-// 128 x 64 x 1024 in bf16 15 us (3.4 TB/s), one step of 64 x 1024 7.5 us, nearly all of it the call and the launch.
+// a copy at 6.53 TB/s: 16384 x 1 x 4096 in bf16 85 us (4.7 TB/s), gradient of 4096 x 8 x 1024 in bf16 87 us (4.6 TB/s); the same
+// in fp32, with fp64 states, 108 us forward (3.7 TB/s) and 233 the gradient (3.5 TB/s, one block an SM).  Short of that the length of the
+// chain counts: 128 x 64 x 1024 in bf16 15.4 us (3.3 TB/s), 16384 steps of 64 channels 38 us forward (eight blocks at most work on them), one
+// step of 64 x 1024 7.4 us, nearly all of it the call and the launch.
 //
-// Three forms: step by step, a thread per channel (few steps); the time axis cut into spans that stay in registers (rows that are not
-// whole 16-byte pieces); the same with tiles fetched ahead by TMA and a warp that only joins (all others).
+// Three forms: step by step, a thread per one or two channels (few steps); the time axis cut into spans that stay in registers (rows that
+// are not whole 16-byte pieces); the same with tiles fetched ahead by TMA and a warp that only joins (all others).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -804,7 +805,9 @@ __global__ void __launch_bounds__(32 * kWarps, 2) recurrence_grad_spans_kernel(c
 //     the other warps already compose the next slab and only then run the current one;
 //   - a cluster stays for several tiles of channels, whose slabs follow each other without a gap.
 // 16384 x 1 x 4096 in bf16: spans in registers 122 us, tiles with all warps joining 140 (8 steps a thread) and 100 (16), with the
-// joining warp and one slab composed ahead 80.  4096 x 13 x D, forward in bf16: D = 336 in tiles 35 us, D = 333 in spans 43.
+// joining warp and one slab composed ahead 85.  4096 x 13 x D, forward and gradient in bf16: D = 336 in tiles 32 and 60 us, in spans 34 and
+// 61; 4096 x 8 x 1024 43 and 86 against 57 and 109.  In fp32 tiles are ahead at few steps (128 x 64 x 1024: 30 and 59 against 39 and 62),
+// spans at many (4096 x 8 x 1024: 108 and 232 against 99 and 202); with rows of whole pieces fp32 takes tiles throughout.
 constexpr int kTile = 64;              // channels
 constexpr int kStages = 3;
 constexpr int kTileThreads = 32 * (kWarps + 1);

@@ -1,9 +1,11 @@
 // Log-probabilities of given tokens, entropies and the most probable tokens of rows of scores, and the gradient group.
 // The forward call reads every score once, the gradient reads and writes it once.  Measured against a copy at 6.53 TB/s:
-//   4096 x 32768 bf16, K = 8    67 us, 4.0 TB/s: bound by its instructions (of the active cycles the exponentials' pipe is busy 50 %
-//                               and 60 % issue); two register buffers, a bulk-copy ring and several blocks a row were no faster
+//   4096 x 32768 bf16, K = 8    68 us, 4.0 TB/s: no pipe is full (of the active cycles the exponentials' is busy 50 % and 60 % issue, with 44 %
+//                               of the warps there are: a row ends in barriers); without alternatives 55 us, 4.9 TB/s; two register buffers, a
+//                               bulk-copy ring and several blocks a row were no faster
+//   4096 x 32768 f32            93 us, 5.8 TB/s: HBM
 //   8 x 131072 bf16, K = 20     10.4 us, 0.2 TB/s: the launch, the exchange between a row's blocks and the choice of the largest
-//   gradient, 4096 x 32768 bf16 with the entropy's term  93 us, 5.8 TB/s;  509 x 50021 f32  34 us, 6.0 TB/s: HBM
+//   gradient, 4096 x 32768 bf16 with the entropy's term  94 us, 5.7 TB/s;  509 x 50021 f32  34 us, 6.0 TB/s: HBM
 #include <algorithm>
 #include <cfloat>
 
