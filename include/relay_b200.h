@@ -408,7 +408,7 @@ relay_status_t relay_sgd_update(const relay_tensor_t *const *params, const relay
  * h_final is the state after its last step, and what f and u hold there is not used.  T = 1 is the step of a decoder.
  * B = 0 or D = 0 is a no-op; T = 0 gives h_final = h0.  No workspace.
  * Long sequences are summed in spans that are joined afterwards: with GIVEN coefficients whose products over a span
- * overflow, a state can become infinite or NaN where a step-by-step sum would not. */
+ * overflow, a state can become infinite or NaN where a step-by-step sum would not; an infinite state can become NaN. */
 relay_status_t relay_infer_gated_recurrence(const relay_tensor_t *f, const relay_tensor_t *u, relay_tensor_t *h_all, relay_tensor_t *h_final);
 relay_status_t relay_gated_recurrence(const relay_tensor_t *f, const relay_tensor_t *u, const relay_tensor_t *h0, const relay_tensor_t *lengths,
                                       int32_t gate, const relay_tensor_t *h_all, const relay_tensor_t *h_final, void *stream);
@@ -455,7 +455,8 @@ relay_status_t relay_token_logprob_grad(const relay_tensor_t *scores, const rela
  * towards the nearest matrix with singular values near one by products,
  *   X <- x / (|x|_F + eps);   `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X   (A = X^T X and X <- a X + X (b A + c A A)
  *   where M > N);   y = scale X
- *   x:(..,M,N) f32 or bf16, rank 2..6, each leading index a matrix of its own -> y: the same shape, bf16.
+ *   x:(..,M,N) f32 or bf16, rank 2..6, each leading index a matrix of its own -> y: the same shape, bf16.  At most 65535 matrices, M and
+ *   N at most 65536 (RELAY_ERR_SHAPE).
  * The products' operands are 16-bit floats with 10 fraction bits, whatever x's type, but for the diagonals of A and of a + b A + c A A,
  * which are f32; sums are f32.  Against 64 bits, with the usual five steps and before y's own rounding (1.7e-3 of the norm), the result is
  * off by about 1e-3 of its norm where x's singular values are of one size.  Directions whose singular values are below 1e-3 of the
