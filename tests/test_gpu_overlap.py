@@ -203,8 +203,8 @@ def test_matrices_on_the_chip_from_two_host_threads():
 @pytest.mark.parametrize("grad", [False, True])
 @pytest.mark.parametrize("tiles", [8, 35, 72, 128, 160, 512])
 def test_persistent_clusters_of_the_recurrence_are_planned_for_the_room_they_find(dt, out_dt, grad, tiles):
-    """A cluster walks over tiles, so a grid that does not fit at once makes the last clusters wait for a whole share.  What fits is the
-    driver's answer for this kernel, its cluster size and its shared memory."""
+    """A cluster walks over tiles, so a grid that does not fit at once makes the last clusters wait for a whole share.  What fits is
+    CUDA's occupancy query for this kernel, its cluster size and its shared memory."""
     T, D = 512, 64 * tiles
     f, u, h, dh = (torch.zeros(T, 1, D, dtype=t, device=DEV) for t in (dt, dt, out_dt, out_dt))
     df, du = torch.empty_like(f), torch.empty_like(u)
