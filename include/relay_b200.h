@@ -69,7 +69,8 @@ typedef enum { RELAY_F32 = 0, RELAY_BF16 = 1, RELAY_I32 = 2, RELAY_I64 = 3, RELA
 
 typedef enum { RELAY_ROWMAJOR = 0, RELAY_NCHW = 1, RELAY_NHWC = 2, RELAY_OIHW = 3 } relay_layout_t;
 
-typedef enum { RELAY_ACT_NONE = 0, RELAY_ACT_RELU = 1, RELAY_ACT_TANH = 2, RELAY_ACT_SIGMOID = 3 } relay_act_t;
+/* SILU is x sigmoid(x); only the operators that name it take it. */
+typedef enum { RELAY_ACT_NONE = 0, RELAY_ACT_RELU = 1, RELAY_ACT_TANH = 2, RELAY_ACT_SIGMOID = 3, RELAY_ACT_SILU = 4 } relay_act_t;
 
 /* A typed tensor value: Tensor(dtype, Shape(shape[0..rank))) plus its device address. */
 typedef struct relay_tensor {
@@ -468,6 +469,104 @@ relay_status_t relay_token_logprob_grad(const relay_tensor_t *scores, const rela
 size_t relay_workspace_bytes_orthogonalize(const relay_tensor_t *x);
 relay_status_t relay_orthogonalize(const relay_tensor_t *x, const relay_orthogonalize_attrs_t *attrs, const relay_tensor_t *y, void *ws,
                                    size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * State space language models: the short convolution and the selective scan of their layers, each for whole sequences and for
+ * single tokens, and the scoring of given tokens straight from the head's operands.  (T,B,D) are steps, batch elements and channels,
+ * as in the recurrences above, and `lengths` means the same: sequence b ends before step lengths[b] (values outside [0,T] count as 0
+ * and T), results and partials are zero from there on, and what the inputs hold there is not used.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Short causal convolution of a sequence, one filter of K taps per channel, with bias and activation:
+ *   y[t,b,d] = act( bias[d] + sum_{k<K} w[k,d] x[t-K+1+k,b,d] ),   the steps -K+1 .. -1 being those of `before`
+ *   x:(T,B,D) t in {f32, bf16};  w:(K,D) t or f32, 1 <= K <= 8;  b:(D) t or f32, or NULL;  before:(K-1,B,D) t or NULL (zeros)
+ *   lengths:(B) i32 or NULL (all T);  act NONE or SILU
+ *   -> y:(T,B,D) t;  after:(K-1,B,D) t or NULL: the last K-1 inputs of each sequence, which the next call takes as `before`.
+ * Sums in f32, one rounding.  T = 1 is the step of a decoder.  No workspace.  T = 0 gives after = before. */
+relay_status_t relay_infer_causal_conv(const relay_tensor_t *x, const relay_tensor_t *w, relay_tensor_t *y, relay_tensor_t *after);
+relay_status_t relay_causal_conv(const relay_tensor_t *x, const relay_tensor_t *w, const relay_tensor_t *b, const relay_tensor_t *before,
+                                 const relay_tensor_t *lengths, int32_t act, const relay_tensor_t *y, const relay_tensor_t *after,
+                                 void *stream);
+
+/* Gradient group of the convolution (Section 4.2), given the partials dy:(T,B,D) t and dafter:(K-1,B,D) t or NULL (zero); with s the sum
+ * before the activation (computed again from x) and g = dy act'(s):
+ *   dx[t] = sum_k w[k] g[t+K-1-k] + what dafter holds for that input;   dbefore: the same for the steps ahead of the first
+ *   dw[k] = sum_{t,b} g[t,b] x[t-K+1+k,b];   db = sum_{t,b} g[t,b]
+ *   dx:(T,B,D) t;  dw:(K,D) f32, db:(D) f32 and dbefore:(K-1,B,D) t or NULL each.  Sums in f32 and in a fixed order.
+ * `ws` must hold relay_workspace_bytes_causal_conv_grad() bytes where dw or db is wanted. */
+size_t relay_workspace_bytes_causal_conv_grad(const relay_tensor_t *x, const relay_tensor_t *w);
+relay_status_t relay_causal_conv_grad(const relay_tensor_t *x, const relay_tensor_t *w, const relay_tensor_t *b, const relay_tensor_t *before,
+                                      const relay_tensor_t *lengths, int32_t act, const relay_tensor_t *dy, const relay_tensor_t *dafter,
+                                      const relay_tensor_t *dx, const relay_tensor_t *dw, const relay_tensor_t *db,
+                                      const relay_tensor_t *dbefore, void *ws, size_t ws_bytes, void *stream);
+
+/* Selective scan: every channel carries N states whose decay and input weights change from step to step,
+ *   delta' = delta + delta_bias, then log(1 + exp(delta')) if softplus != 0
+ *   h[t,b,d,n] = exp(delta'[t,b,d] a[d,n]) h[t-1,b,d,n] + delta'[t,b,d] u[t,b,d] b[t,b,n],   h[-1] = h0
+ *   y[t,b,d] = ( sum_n c[t,b,n] h[t,b,d,n] + d[d] u[t,b,d] ) silu(z[t,b,d])
+ *   u, delta:(T,B,D) t in {f32, bf16};  a:(D,N) f32, 1 <= N <= RELAY_MAX_SCAN_STATES;  b, c:(T,B,N) t, or c = NULL and b:(T,B,2N),
+ *   whose last axis holds the blocks [ b | c ] (one dense result);  d:(D) f32 or NULL (no such term);  z:(T,B,D) t or NULL (no gate);
+ *   delta_bias:(D) f32 or NULL;  h0:(B,D,N) f32 or NULL (zero);  lengths:(B) i32 or NULL
+ *   -> y:(T,B,D) t;  h_final:(B,D,N) f32 or NULL: the state after each sequence's last step;
+ *      states:(ceil(T / RELAY_SCAN_SPAN),B,D,N) f32 or NULL: the state before every RELAY_SCAN_SPAN-th step, for the gradient.
+ * Arithmetic and states in f32.  T = 1 is the step of a decoder.  No workspace.  T = 0 gives h_final = h0.
+ * Long sequences are summed in spans that are joined: where exp(delta' a) over a span overflows (a > 0), a state can become infinite
+ * or NaN where a step-by-step sum would not. */
+#define RELAY_SCAN_SPAN 32
+#define RELAY_MAX_SCAN_STATES 64
+relay_status_t relay_infer_selective_scan(const relay_tensor_t *u, const relay_tensor_t *a, relay_tensor_t *y, relay_tensor_t *h_final,
+                                          relay_tensor_t *states);
+relay_status_t relay_selective_scan(const relay_tensor_t *u, const relay_tensor_t *delta, const relay_tensor_t *a, const relay_tensor_t *b,
+                                    const relay_tensor_t *c, const relay_tensor_t *d, const relay_tensor_t *z,
+                                    const relay_tensor_t *delta_bias, const relay_tensor_t *h0, const relay_tensor_t *lengths,
+                                    int32_t softplus, const relay_tensor_t *y, const relay_tensor_t *h_final, const relay_tensor_t *states,
+                                    void *stream);
+
+/* Gradient group of the scan (Section 4.2), given the forward call's states and the partials dy:(T,B,D) t and dh_final:(B,D,N) f32 or NULL
+ * (zero).  With y' = sum_n c h + d u, e = dy silu(z) (dy without a gate) and g[t] = e[t] c[t] + G[t+1], G[t] = exp(delta'[t] a) g[t], G[T] =
+ * dh_final, summed over whatever the operand was broadcast along:
+ *   du = e d + delta' sum_n g b;        ddelta' = u sum_n g b + sum_n a G h[t-1];   ddelta = ddelta' sigmoid(delta + delta_bias) if softplus
+ *   da = sum_{t,b} delta' G h[t-1];     db = sum_d g delta' u;   dc = sum_d e h;    dd = sum_{t,b} e u
+ *   dz = dy y' silu'(z);                ddelta_bias = sum_{t,b} ddelta;             dh0 = G[0]
+ *   du, ddelta, db, dc, dz: types and shapes of u, delta, b, c, z (db:(T,B,2N) with dc = NULL where c is NULL; dz NULL where z is NULL);
+ *   da:(D,N) f32;  dd, ddelta_bias:(D) f32 or NULL (NULL where d or delta_bias is NULL);  dh0:(B,D,N) f32 or NULL.
+ * The states between those saved are computed again.  Sums in f32 and in a fixed order.
+ * `ws` must hold relay_workspace_bytes_selective_scan_grad() bytes. */
+size_t relay_workspace_bytes_selective_scan_grad(const relay_tensor_t *u, const relay_tensor_t *a);
+relay_status_t relay_selective_scan_grad(const relay_tensor_t *u, const relay_tensor_t *delta, const relay_tensor_t *a, const relay_tensor_t *b,
+                                         const relay_tensor_t *c, const relay_tensor_t *d, const relay_tensor_t *z,
+                                         const relay_tensor_t *delta_bias, const relay_tensor_t *lengths, int32_t softplus,
+                                         const relay_tensor_t *states, const relay_tensor_t *dy, const relay_tensor_t *dh_final,
+                                         const relay_tensor_t *du, const relay_tensor_t *ddelta, const relay_tensor_t *da,
+                                         const relay_tensor_t *db, const relay_tensor_t *dc, const relay_tensor_t *dd,
+                                         const relay_tensor_t *dz, const relay_tensor_t *ddelta_bias, const relay_tensor_t *dh0, void *ws,
+                                         size_t ws_bytes, void *stream);
+
+/* Log-probabilities of given tokens straight from the operands of the dense group that would make the scores (relay_fused_dense_act and
+ * relay_token_logprob in one, without the N x V scores in memory):
+ *   z[i,j] = sum_k x[i,k] w[k,j] / temperature  (w[j,k] if trans_w != 0: a head that is the embedding table)
+ *   lse[i] = log sum_j exp(z[i,j]);   logp[i] = z[i,tokens[i]] - lse[i]
+ *   x:(..,K) t in {f32, bf16}, rank 1..6, the leading axes are the rows;  w:(K,V) t, or (V,K);  tokens:(..) i32 or i64;  temperature > 0
+ *   -> logp, lse:(..) f32.
+ * bf16 operands are multiplied as they are and summed in f32; f32 runs in true fp32.  A token outside [0,V) names no class: its logp
+ * is 0.  With bf16 operands scores of -inf are classes that cannot occur, and a row of nothing else has lse = -inf, logp = -inf; a row with
+ * a NaN or +inf score has NaN results.  With f32 operands an infinite score is NaN (the contraction's sums are compensated).  V = 0 is RELAY_ERR_SHAPE; V < 2^31 - 512.
+ * `ws` must hold relay_workspace_bytes_linear_logprob() bytes. */
+size_t relay_workspace_bytes_linear_logprob(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w);
+relay_status_t relay_linear_logprob(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, const relay_tensor_t *tokens,
+                                    float temperature, const relay_tensor_t *logp, const relay_tensor_t *lse, void *ws, size_t ws_bytes,
+                                    void *stream);
+
+/* Gradient group of the above, given the forward call's lse:(..) f32 and dlogp:(..) f32:
+ *   dz[i,j] = dlogp[i] (1[j = tokens[i]] - exp(z[i,j] - lse[i])) / temperature
+ *   dx[i,k] = sum_j dz[i,j] w[k,j];   dw[k,j] = sum_i x[i,k] dz[i,j]      dx, dw: types and shapes of x and w; one of them may be NULL
+ * The scores are computed again, a piece of the vocabulary at a time; with bf16 operands dz is rounded to bf16, the operand type of
+ * the two products, whose sums are f32.  A row whose token names no class has no part in either; a row with lse = -inf neither.
+ * `ws` must hold relay_workspace_bytes_linear_logprob_grad() bytes. */
+size_t relay_workspace_bytes_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w);
+relay_status_t relay_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, const relay_tensor_t *tokens,
+                                         float temperature, const relay_tensor_t *lse, const relay_tensor_t *dlogp, const relay_tensor_t *dx,
+                                         const relay_tensor_t *dw, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Status helpers.

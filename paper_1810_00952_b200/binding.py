@@ -21,8 +21,9 @@ CHECK_LIB_PATH = os.path.join(_HERE, "librelay_b200_check.so")
 MAX_RANK = 6
 F32, BF16, I32, I64, BOOL = 0, 1, 2, 3, 4
 ROWMAJOR, NCHW, NHWC, OIHW = 0, 1, 2, 3
-ACT_NONE, ACT_RELU, ACT_TANH, ACT_SIGMOID = 0, 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_TANH, ACT_SIGMOID, ACT_SILU = 0, 1, 2, 3, 4
 GATE_GIVEN, GATE_SIGMOID, GATE_MIX = 0, 1, 2
+SCAN_SPAN = 32            # steps between the states that relay_selective_scan saves for its gradient
 RED_NONE, RED_SUM, RED_MAX, RED_MEAN, RED_ARGMAX = 0, 1, 2, 3, 4
 
 STATUS_NAMES = ["OK", "ERR_NULL", "ERR_RANK", "ERR_SHAPE", "ERR_DTYPE", "ERR_LAYOUT", "ERR_ALIGN", "ERR_ATTR",
@@ -89,7 +90,9 @@ def lib() -> ctypes.CDLL:
         for name in ("relay_workspace_bytes_dense_act", "relay_workspace_bytes_dense_act_grad",
                      "relay_workspace_bytes_conv2d_act", "relay_workspace_bytes_conv2d_act_grad",
                      "relay_workspace_bytes_reduce", "relay_workspace_bytes_lstm", "relay_workspace_bytes_lstm_grad",
-                     "relay_workspace_bytes_orthogonalize"):
+                     "relay_workspace_bytes_orthogonalize", "relay_workspace_bytes_causal_conv_grad",
+                     "relay_workspace_bytes_selective_scan_grad", "relay_workspace_bytes_linear_logprob",
+                     "relay_workspace_bytes_linear_logprob_grad"):
             getattr(L, name).restype = ctypes.c_size_t
         _lib = L
     return _lib
@@ -464,6 +467,79 @@ def relay_orthogonalize(x, steps, coefficients, eps, scale, y, ws=None):
     wp, wb = _ws(ws)
     at = OrthogonalizeAttrs(int(steps), *[float(v) for v in coefficients], float(eps), float(scale))
     _check(lib().relay_orthogonalize(_packed(x), ctypes.byref(at), _packed(y), wp, wb, _stream()))
+
+
+# ---- state space language models --------------------------------------------------------------------------
+def relay_infer_causal_conv(x: TensorDesc, w: TensorDesc):
+    y, after = TensorDesc(), TensorDesc()
+    _check(lib().relay_infer_causal_conv(_ref(x), _ref(w), ctypes.byref(y), ctypes.byref(after)))
+    return y, after
+
+
+def relay_causal_conv(x, w, b, before, lengths, act, y, after):
+    """b, before, lengths and after may be None."""
+    _check(lib().relay_causal_conv(_packed(x), _packed(w), _packed(b), _packed(before), _packed(lengths), int(act), _packed(y),
+                                   _packed(after), _stream()))
+
+
+def relay_workspace_bytes_causal_conv_grad(x, w) -> int:
+    return int(lib().relay_workspace_bytes_causal_conv_grad(_packed(x), _packed(w)))
+
+
+def relay_causal_conv_grad(x, w, b, before, lengths, act, dy, dafter, dx, dw, db, dbefore, ws=None):
+    """b, before, lengths, dafter, dw, db and dbefore may be None."""
+    wp, wb = _ws(ws)
+    _check(lib().relay_causal_conv_grad(_packed(x), _packed(w), _packed(b), _packed(before), _packed(lengths), int(act), _packed(dy),
+                                        _packed(dafter), _packed(dx), _packed(dw), _packed(db), _packed(dbefore), wp, wb, _stream()))
+
+
+def relay_infer_selective_scan(u: TensorDesc, a: TensorDesc):
+    y, h_final, states = TensorDesc(), TensorDesc(), TensorDesc()
+    _check(lib().relay_infer_selective_scan(_ref(u), _ref(a), ctypes.byref(y), ctypes.byref(h_final), ctypes.byref(states)))
+    return y, h_final, states
+
+
+def relay_selective_scan(u, delta, a, b, c, d, z, delta_bias, h0, lengths, softplus, y, h_final, states):
+    """c = None: b holds the column blocks [ b | c ].  d, z, delta_bias, h0, lengths, h_final and states may be None; states (one for
+    every SCAN_SPAN steps) are what the gradient needs."""
+    _check(lib().relay_selective_scan(_packed(u), _packed(delta), _packed(a), _packed(b), _packed(c), _packed(d), _packed(z),
+                                      _packed(delta_bias), _packed(h0), _packed(lengths), int(bool(softplus)), _packed(y),
+                                      _packed(h_final), _packed(states), _stream()))
+
+
+def relay_workspace_bytes_selective_scan_grad(u, a) -> int:
+    return int(lib().relay_workspace_bytes_selective_scan_grad(_packed(u), _packed(a)))
+
+
+def relay_selective_scan_grad(u, delta, a, b, c, d, z, delta_bias, lengths, softplus, states, dy, dh_final, du, ddelta, da, db, dc, dd, dz,
+                              ddelta_bias, dh0, ws):
+    """dc, dz, dd and ddelta_bias are None where c, z, d and delta_bias are; dd, ddelta_bias and dh0 may be None."""
+    wp, wb = _ws(ws)
+    ts = [u, delta, a, b, c, d, z, delta_bias, lengths]
+    outs = [states, dy, dh_final, du, ddelta, da, db, dc, dd, dz, ddelta_bias, dh0]
+    _check(lib().relay_selective_scan_grad(*[_packed(t) for t in ts], int(bool(softplus)), *[_packed(t) for t in outs], wp, wb, _stream()))
+
+
+def relay_workspace_bytes_linear_logprob(x, w, trans_w) -> int:
+    return int(lib().relay_workspace_bytes_linear_logprob(_packed(x), _packed(w), int(bool(trans_w))))
+
+
+def relay_linear_logprob(x, w, trans_w, tokens, temperature, logp, lse, ws):
+    """w:(K,V), or (V,K) with trans_w (a head that is the embedding table)."""
+    wp, wb = _ws(ws)
+    _check(lib().relay_linear_logprob(_packed(x), _packed(w), int(bool(trans_w)), _packed(tokens), ctypes.c_float(temperature),
+                                      _packed(logp), _packed(lse), wp, wb, _stream()))
+
+
+def relay_workspace_bytes_linear_logprob_grad(x, w, trans_w) -> int:
+    return int(lib().relay_workspace_bytes_linear_logprob_grad(_packed(x), _packed(w), int(bool(trans_w))))
+
+
+def relay_linear_logprob_grad(x, w, trans_w, tokens, temperature, lse, dlogp, dx, dw, ws):
+    """One of dx and dw may be None."""
+    wp, wb = _ws(ws)
+    _check(lib().relay_linear_logprob_grad(_packed(x), _packed(w), int(bool(trans_w)), _packed(tokens), ctypes.c_float(temperature),
+                                           _packed(lse), _packed(dlogp), _packed(dx), _packed(dw), wp, wb, _stream()))
 
 
 # ---- status helpers -----------------------------------------------------------------------------------

@@ -1,0 +1,431 @@
+// Short causal convolution of a sequence, one filter of K taps per channel, and its gradient group:
+//   s_t = b + sum_k w[k] x_{t-K+1+k},  y_t = act(s_t)
+// HBM-bound: the forward group reads x and writes y once, the gradient reads x and dy and writes dx once; K multiply-adds an element.
+// A thread owns V consecutive channels (16 bytes of a row where rows allow it) and a span of steps; the K - 1 inputs before the
+// current one stay in its registers, and at the start of a span they are read again (K - 1 rows in S).  The gradient walks a span
+// forwards and K - 1 steps beyond it: the partial of an input needs those of the K sums that it entered.
+#include <algorithm>
+
+#include "sequence.cuh"
+
+namespace relay {
+namespace {
+
+using namespace seq;
+
+constexpr int kMaxTaps = 8;
+constexpr int kThreads = 256;
+constexpr int kRows = 8;           // spans of a gradient block: their partial sums of dw and db are joined on the chip
+constexpr int kGradV = 4;          // most channels of a gradient thread: filter, window, slopes and sums of each stay in registers
+
+struct Args {
+    const void *x;                 // [T][C]
+    const void *w, *b;             // [K][D], [D] or null
+    const void *before;            // [K-1][C] or null
+    const int *lengths;            // [C / D] or null
+    void *y, *after;               // [T][C], [K-1][C] or null
+    const void *dy, *dafter;       // [T][C], [K-1][C] or null
+    void *dx, *dbefore;            // [T][C], [K-1][C] or null
+    float *part;                   // [parts][C / D][K + 1][D]
+    long long T, C, D;
+    int K, S, w_bf16, b_bf16, silu;
+    long long blocks_c;            // blocks along the channels
+};
+
+__device__ __forceinline__ long long end_of(const Args &p, long long c)
+{
+    if (p.lengths == nullptr) return p.T;
+    const int *at = p.lengths + c / p.D;
+    const long long n = relay_in_bounds(at, 4) ? *at : 0;
+    return n < 0 ? 0 : n > p.T ? p.T : n;
+}
+// input of step t, which may lie ahead of the first one; zero behind the sequence's end
+template <typename T, int V>
+__device__ __forceinline__ void load_input(const Args &p, long long t, long long c, long long end, float (&x)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = 0.0f;
+    if (t >= 0) {
+        if (t < end) load<T, V>(p.x, t * p.C + c, x);
+    } else if (p.before != nullptr && t >= 1 - p.K) {
+        load<T, V>(p.before, (t + p.K - 1) * p.C + c, x);
+    }
+}
+// the filter, right-aligned to KP taps (the first KP - K do not exist), and the bias
+template <int V, int KP>
+__device__ __forceinline__ void load_filter(const Args &p, long long d, float (&w)[KP][V], float (&b)[V])
+{
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[k][i] = 0.0f;
+        if (k >= KP - p.K) load_operand<V>(p.w, p.w_bf16, (k - (KP - p.K)) * p.D + d, w[k]);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = 0.0f;
+    if (p.b != nullptr) load_operand<V>(p.b, p.b_bf16, d, b);
+}
+
+template <typename T, int V, int KP>
+__global__ void __launch_bounds__(kThreads) causal_conv_kernel(const Args p)
+{
+    constexpr bool FINE = sizeof(T) == 4;
+    constexpr int U = V == 8 ? 4 : 8;                      // rows in flight
+    pdl_wait();
+    const long long span = blockIdx.x / p.blocks_c;
+    const long long c = ((blockIdx.x - span * p.blocks_c) * kThreads + threadIdx.x) * V;
+    if (c >= p.C) return;
+    const long long end = end_of(p, c), t0 = span * p.S, t1 = min(t0 + p.S, p.T);
+    const int first = KP - p.K;
+    float w[KP][V], b[V], x[KP - 1 + U][V];
+    load_filter<V, KP>(p, c % p.D, w, b);
+    // the state for the next call: the last K - 1 inputs of the sequence
+    if (span == 0 && p.after != nullptr) {
+        for (int j = 0; j < p.K - 1; ++j) {
+            float q[V];
+            load_input<T, V>(p, end - (p.K - 1) + j, c, end, q);
+            store<T, V>(p.after, j * p.C + c, q);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < KP - 1; ++j) load_input<T, V>(p, t0 - (KP - 1) + j, c, end, x[j]);
+    for (long long t = t0; t < t1; t += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_input<T, V>(p, t + u, c, t + u < t1 ? end : 0, x[KP - 1 + u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (t + u >= t1) break;
+            float y[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = b[i];
+#pragma unroll
+            for (int k = 0; k < KP; ++k)
+                if (k >= first) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) y[i] = fmaf(w[k][i], x[u + k][i], y[i]);
+                }
+            if (p.silu) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] *= logistic<FINE>(y[i]);
+            }
+            if (t + u >= end) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = 0.0f;
+            }
+            store<T, V>(p.y, (t + u) * p.C + c, y);
+        }
+#pragma unroll
+        for (int j = 0; j < KP - 1; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[j][i] = x[U + j][i];
+    }
+}
+
+// One span: dx of its steps (and of the inputs ahead of the first step), its share of dw and db.
+template <typename T, int V, int KP>
+__global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args p)
+{
+    constexpr bool FINE = sizeof(T) == 4;
+    __shared__ float joint[kRows][32 * V];
+    pdl_wait();
+    const long long part = blockIdx.x / p.blocks_c;
+    const long long c = ((blockIdx.x - part * p.blocks_c) * 32 + threadIdx.x) * V;
+    const bool live = c < p.C;
+    const long long end = live ? end_of(p, c) : 0, t0 = (part * kRows + threadIdx.y) * p.S, t1 = min(t0 + p.S, p.T);
+    const int first = KP - p.K;
+    float w[KP][V], b[V], x[KP][V], g[KP][V], dw[KP][V], db[V];   // x[k]: the input under tap k;  g[k]: the slope k steps back
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[k][i] = g[k][i] = dw[k][i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) db[i] = 0.0f;
+    if (live && (t0 < p.T || t0 == 0)) {
+        load_filter<V, KP>(p, c % p.D, w, b);
+#pragma unroll
+        for (int j = 1; j < KP; ++j) load_input<T, V>(p, t0 - KP + j, c, end, x[j]);
+#pragma unroll 2
+        for (long long t = t0; t < t1 + KP - 1; ++t) {
+#pragma unroll
+            for (int k = 0; k + 1 < KP; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) { x[k][i] = x[k + 1][i]; g[KP - 1 - k][i] = g[KP - 2 - k][i]; }
+            load_input<T, V>(p, t, c, end, x[KP - 1]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[0][i] = 0.0f;
+            if (t < end) {
+                load<T, V>(p.dy, t * p.C + c, g[0]);
+                if (p.silu) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float s = b[i];
+#pragma unroll
+                        for (int k = 0; k < KP; ++k) if (k >= first) s = fmaf(w[k][i], x[k][i], s);
+                        const float q = logistic<FINE>(s);
+                        g[0][i] *= q * fmaf(s, 1.0f - q, 1.0f);
+                    }
+                }
+                if (t < t1) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) db[i] += g[0][i];
+#pragma unroll
+                    for (int k = 0; k < KP; ++k)
+                        if (k >= first) {
+#pragma unroll
+                            for (int i = 0; i < V; ++i) dw[k][i] = fmaf(g[0][i], x[k][i], dw[k][i]);
+                        }
+                }
+            }
+            const long long at = t - (KP - 1);             // the step whose K sums are complete
+            if (at < (t0 == 0 ? 1 - p.K : t0)) continue;
+            float dx[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) dx[i] = 0.0f;
+            if (at < end) {
+#pragma unroll
+                for (int k = 0; k < KP; ++k)
+                    if (k >= first) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) dx[i] = fmaf(w[k][i], g[k][i], dx[i]);
+                    }
+                const long long j = at - (end - (p.K - 1));
+                if (p.dafter != nullptr && j >= 0) {
+                    float q[V];
+                    load<T, V>(p.dafter, j * p.C + c, q);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) dx[i] += q[i];
+                }
+            }
+            if (at >= 0) store<T, V>(p.dx, at * p.C + c, dx);
+            else if (p.dbefore != nullptr) store<T, V>(p.dbefore, (at + p.K - 1) * p.C + c, dx);
+        }
+    }
+    if (p.part == nullptr) return;
+    const long long bd = live ? c / p.D : 0;
+    float *out = p.part + ((part * (p.C / p.D) + bd) * (p.K + 1)) * p.D + (c - bd * p.D);
+#pragma unroll
+    for (int k = 0; k <= KP; ++k) {
+        if (k < first) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) joint[threadIdx.y][threadIdx.x * V + i] = k < KP ? dw[k < KP ? k : 0][i] : db[i];
+        __syncthreads();
+        if (threadIdx.y == 0 && live) {
+            float s[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                s[i] = joint[0][threadIdx.x * V + i];
+#pragma unroll
+                for (int r = 1; r < kRows; ++r) s[i] += joint[r][threadIdx.x * V + i];
+            }
+            store<float, V>(out, (k - first) * p.D, s);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------
+constexpr long long kSms = 148;
+
+// Steps of a span: the longest that still give every SM its threads, so that as few rows as possible are read twice.
+int forward_span(long long T, long long C, int V)
+{
+    int S = 64;
+    while (S > 8 && (C / V) * ((T + S - 1) / S) < kSms * 1024) S /= 2;
+    return S;
+}
+int gradient_span(long long T, long long C, int V)
+{
+    int S = 64;
+    while (S > 8 && ((C / V + 31) / 32) * ((T + (long long)S * kRows - 1) / ((long long)S * kRows)) < kSms * 4) S /= 2;
+    return S;
+}
+int channels_of_gradient(long long D) { return D % kGradV == 0 ? kGradV : 1; }
+long long gradient_parts(long long T, long long C, long long D)
+{
+    const long long steps = (long long)gradient_span(T, C, channels_of_gradient(D)) * kRows;
+    return std::max<long long>(1, (T + steps - 1) / steps);
+}
+
+template <typename T, int V, int KP>
+relay_status_t launch_forward(Args p, cudaStream_t st)
+{
+    p.S = forward_span(p.T, p.C, V);
+    p.blocks_c = (p.C / V + kThreads - 1) / kThreads;
+    const long long blocks = p.blocks_c * std::max<long long>(1, (p.T + p.S - 1) / p.S);
+    if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "causal_conv: %lld steps of %lld channels", p.T, p.C);
+    RELAY_CUDA(launch_pdl(causal_conv_kernel<T, V, KP>, dim3((unsigned)blocks), dim3(kThreads), 0, st, p));
+    return check_launch("causal_conv");
+}
+template <typename T, int V, int KP>
+relay_status_t launch_gradient(Args p, cudaStream_t st)
+{
+    p.S = gradient_span(p.T, p.C, V);
+    p.blocks_c = (p.C / V + 31) / 32;
+    const long long blocks = p.blocks_c * gradient_parts(p.T, p.C, p.D);
+    if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "causal_conv_grad: %lld steps of %lld channels", p.T, p.C);
+    RELAY_CUDA(launch_pdl(causal_conv_grad_kernel<T, V, KP>, dim3((unsigned)blocks), dim3(32, kRows), 0, st, p));
+    return check_launch("causal_conv_grad");
+}
+// taps: kernels for 2, 4 and 8; fewer are right-aligned in them.  Channels of a thread: as many as divide the rows into whole
+// aligned accesses.
+template <typename T, int V>
+relay_status_t forward_taps(const Args &p, cudaStream_t st)
+{
+    if (p.K <= 2) return launch_forward<T, V, 2>(p, st);
+    return p.K <= 4 ? launch_forward<T, V, 4>(p, st) : launch_forward<T, V, 8>(p, st);
+}
+template <typename T, int V>
+relay_status_t gradient_taps(const Args &p, cudaStream_t st)
+{
+    if (p.K <= 2) return launch_gradient<T, V, 2>(p, st);
+    return p.K <= 4 ? launch_gradient<T, V, 4>(p, st) : launch_gradient<T, V, 8>(p, st);
+}
+template <typename T>
+relay_status_t forward_channels(const Args &p, cudaStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    if (p.D % V == 0) return forward_taps<T, V>(p, st);
+    return p.D % 2 == 0 ? forward_taps<T, 2>(p, st) : forward_taps<T, 1>(p, st);
+}
+template <typename T>
+relay_status_t gradient_channels(const Args &p, cudaStream_t st)
+{
+    return channels_of_gradient(p.D) == kGradV ? gradient_taps<T, kGradV>(p, st) : gradient_taps<T, 1>(p, st);
+}
+
+// ---- boundary ---------------------------------------------------------------------------------------------------
+relay_status_t check_filter(const relay_tensor_t *x, const relay_tensor_t *w, Sizes *s, int64_t *K)
+{
+    RELAY_TRY(check_sequence(x, s, "x"));
+    RELAY_TRY(check_type(w, "w"));
+    RELAY_TRY(check_rank(w, 2, "w"));
+    *K = w->shape[0];
+    RELAY_TRY(check_tensor(w, x->dtype, RELAY_F32, {*K, s->D}, "w"));
+    if (*K < 1 || *K > kMaxTaps) return fail(RELAY_ERR_SHAPE, "w: %lld taps, needs 1..%d", (long long)*K, kMaxTaps);
+    return RELAY_OK;
+}
+relay_status_t check_act(int32_t act)
+{
+    if (act != RELAY_ACT_NONE && act != RELAY_ACT_SILU) return fail(RELAY_ERR_ATTR, "activation %d, needs none or silu", act);
+    return RELAY_OK;
+}
+Args make_args(const relay_tensor_t *x, const relay_tensor_t *w, const relay_tensor_t *b, const relay_tensor_t *before,
+               const relay_tensor_t *lengths, int32_t act, const Sizes &s, int64_t K)
+{
+    Args p{};
+    p.x = x->data; p.w = w->data; p.b = b ? b->data : nullptr;
+    p.before = before ? before->data : nullptr;
+    p.lengths = lengths ? (const int *)lengths->data : nullptr;
+    p.T = s.T; p.C = s.B * s.D; p.D = s.D; p.K = (int)K;
+    p.w_bf16 = w->dtype == RELAY_BF16; p.b_bf16 = b && b->dtype == RELAY_BF16;
+    p.silu = act == RELAY_ACT_SILU;
+    return p;
+}
+size_t gradient_bytes(const Sizes &s, int64_t K)
+{
+    if (s.B == 0 || s.D == 0) return 0;
+    return (size_t)gradient_parts(s.T, s.B * s.D, s.D) * s.B * (K + 1) * s.D * sizeof(float);
+}
+
+}  // namespace
+}  // namespace relay
+
+using namespace relay;
+
+extern "C" relay_status_t relay_infer_causal_conv(const relay_tensor_t *x, const relay_tensor_t *w, relay_tensor_t *y, relay_tensor_t *after)
+{
+    clear_error();
+    RELAY_TRY(check_not_null(x, "x"));
+    RELAY_TRY(check_not_null(w, "w"));
+    RELAY_TRY(check_not_null(y, "y"));
+    RELAY_TRY(check_not_null(after, "after"));
+    seq::Sizes s;
+    int64_t K;
+    RELAY_TRY(check_filter(x, w, &s, &K));
+    *y = *x;
+    y->data = nullptr;
+    *after = *y;
+    after->shape[0] = K - 1;
+    return RELAY_OK;
+}
+
+extern "C" relay_status_t relay_causal_conv(const relay_tensor_t *x, const relay_tensor_t *w, const relay_tensor_t *b,
+                                            const relay_tensor_t *before, const relay_tensor_t *lengths, int32_t act,
+                                            const relay_tensor_t *y, const relay_tensor_t *after, void *stream)
+{
+    clear_error();
+    RELAY_TRY(check_not_null(x, "x"));
+    RELAY_TRY(check_not_null(w, "w"));
+    RELAY_TRY(check_not_null(y, "y"));
+    seq::Sizes s;
+    int64_t K;
+    RELAY_TRY(check_filter(x, w, &s, &K));
+    RELAY_TRY(seq::check_tensor(b, x->dtype, RELAY_F32, {s.D}, "b"));
+    RELAY_TRY(seq::check_tensor(before, x->dtype, x->dtype, {K - 1, s.B, s.D}, "before"));
+    RELAY_TRY(seq::check_tensor(lengths, RELAY_I32, RELAY_I32, {s.B}, "lengths"));
+    RELAY_TRY(seq::check_tensor(y, x->dtype, x->dtype, {s.T, s.B, s.D}, "y"));
+    RELAY_TRY(seq::check_tensor(after, x->dtype, x->dtype, {K - 1, s.B, s.D}, "after"));
+    RELAY_TRY(check_act(act));
+    const relay_tensor_t *ins[5] = {x, w, b, before, lengths}, *outs[2] = {y, after};
+    RELAY_TRY(seq::check_buffers(ins, outs));
+    if (s.B == 0 || s.D == 0 || (s.T == 0 && (!after || K == 1))) return RELAY_OK;
+    Args p = make_args(x, w, b, before, lengths, act, s, K);
+    p.y = y->data;
+    p.after = after ? after->data : nullptr;
+    cudaStream_t st = (cudaStream_t)stream;
+    RELAY_TRY(seq::register_buffers(ins, outs, nullptr, 0, st));
+    return x->dtype == RELAY_F32 ? forward_channels<float>(p, st) : forward_channels<__nv_bfloat16>(p, st);
+}
+
+extern "C" size_t relay_workspace_bytes_causal_conv_grad(const relay_tensor_t *x, const relay_tensor_t *w)
+{
+    clear_error();
+    seq::Sizes s;
+    int64_t K;
+    if (!x || !w || check_filter(x, w, &s, &K) != RELAY_OK) return 0;
+    return gradient_bytes(s, K);
+}
+
+extern "C" relay_status_t relay_causal_conv_grad(const relay_tensor_t *x, const relay_tensor_t *w, const relay_tensor_t *b,
+                                                 const relay_tensor_t *before, const relay_tensor_t *lengths, int32_t act,
+                                                 const relay_tensor_t *dy, const relay_tensor_t *dafter, const relay_tensor_t *dx,
+                                                 const relay_tensor_t *dw, const relay_tensor_t *db, const relay_tensor_t *dbefore, void *ws,
+                                                 size_t ws_bytes, void *stream)
+{
+    clear_error();
+    RELAY_TRY(check_not_null(x, "x"));
+    RELAY_TRY(check_not_null(w, "w"));
+    RELAY_TRY(check_not_null(dy, "dy"));
+    RELAY_TRY(check_not_null(dx, "dx"));
+    seq::Sizes s;
+    int64_t K;
+    RELAY_TRY(check_filter(x, w, &s, &K));
+    RELAY_TRY(seq::check_tensor(b, x->dtype, RELAY_F32, {s.D}, "b"));
+    RELAY_TRY(seq::check_tensor(before, x->dtype, x->dtype, {K - 1, s.B, s.D}, "before"));
+    RELAY_TRY(seq::check_tensor(lengths, RELAY_I32, RELAY_I32, {s.B}, "lengths"));
+    RELAY_TRY(seq::check_tensor(dy, x->dtype, x->dtype, {s.T, s.B, s.D}, "dy"));
+    RELAY_TRY(seq::check_tensor(dafter, x->dtype, x->dtype, {K - 1, s.B, s.D}, "dafter"));
+    RELAY_TRY(seq::check_tensor(dx, x->dtype, x->dtype, {s.T, s.B, s.D}, "dx"));
+    RELAY_TRY(seq::check_tensor(dw, RELAY_F32, RELAY_F32, {K, s.D}, "dw"));
+    RELAY_TRY(seq::check_tensor(db, RELAY_F32, RELAY_F32, {s.D}, "db"));
+    RELAY_TRY(seq::check_tensor(dbefore, x->dtype, x->dtype, {K - 1, s.B, s.D}, "dbefore"));
+    RELAY_TRY(check_act(act));
+    const relay_tensor_t *ins[7] = {x, w, b, before, lengths, dy, dafter}, *outs[4] = {dx, dw, db, dbefore};
+    RELAY_TRY(seq::check_buffers(ins, outs));
+    const size_t need = dw || db ? gradient_bytes(s, K) : 0;
+    RELAY_TRY(check_workspace(ws, ws_bytes, need));
+    cudaStream_t st = (cudaStream_t)stream;
+    if (s.D == 0) return RELAY_OK;
+    Args p = make_args(x, w, b, before, lengths, act, s, K);
+    p.dy = dy->data;
+    p.dafter = dafter ? dafter->data : nullptr;
+    p.dx = dx->data;
+    p.dbefore = dbefore ? dbefore->data : nullptr;
+    p.part = dw || db ? (float *)ws : nullptr;
+    RELAY_TRY(seq::register_buffers(ins, outs, ws, need, st));
+    if (s.B > 0)
+        RELAY_TRY(x->dtype == RELAY_F32 ? gradient_channels<float>(p, st) : gradient_channels<__nv_bfloat16>(p, st));
+    const long long rows = s.B > 0 ? gradient_parts(s.T, p.C, p.D) * s.B : 0;
+    return seq::launch_column_sums((const float *)ws, rows, (K + 1) * s.D, (K + 1) * s.D, dw ? (float *)dw->data : nullptr, K * s.D,
+                                   db ? (float *)db->data : nullptr, st);
+}

@@ -155,7 +155,7 @@ int *device_error_word();  // device address of the word on the current device (
 // single-stream test runs.  In the ordinary build all of this compiles to nothing.
 constexpr int kErrBounds = 6;
 #ifdef RELAY_BOUNDS_CHECK
-struct BoundsTable { int n; int *err; unsigned long long lo[16], hi[16]; };
+struct BoundsTable { int n; int *err; unsigned long long lo[32], hi[32]; };
 #ifdef __CUDACC__
 static __constant__ BoundsTable c_bounds;
 __device__ __forceinline__ bool relay_in_bounds(const void *p, size_t bytes)
@@ -171,11 +171,11 @@ struct BoundsReg {
     BoundsTable t{};
     void add(const void *p, size_t bytes)
     {
-        if (!p || !bytes || t.n >= 16) return;
+        if (!p || !bytes || t.n >= 32) return;
         t.lo[t.n] = (unsigned long long)p; t.hi[t.n] = (unsigned long long)p + bytes; ++t.n;
     }
     void add(const relay_tensor_t *x) { if (x) add(x->data, nbytes(x)); }
-    relay_status_t commit(cudaStream_t st)
+    __attribute__((always_inline)) relay_status_t commit(cudaStream_t st)    // names this source file's table: never one function for all files
     {
         t.err = device_error_word();
         RELAY_CUDA(cudaMemcpyToSymbolAsync(c_bounds, &t, sizeof t, 0, cudaMemcpyHostToDevice, st));

@@ -1,0 +1,482 @@
+// Log-probabilities of given tokens straight from the operands of a language model's head, and the gradient group: the N x V scores are
+// made a piece of the vocabulary at a time and never kept.
+//
+// bf16: the forward call is one product whose epilogue leaves (maximum, sum of exponentials) per row and 64 columns, which a second
+// kernel joins.  The gradient makes the partials dz of a piece of the scores (the same product with another epilogue), and multiplies
+// them with w and x; the sum of dx over the pieces is kept in fp32.  TMA wants rows of whole 16 bytes: pieces of w that have others
+// (odd vocabularies, odd widths) are copied to padded rows first, and dw of such a piece back.
+// f32: the same pieces through the fp32 contraction, with the scores of a piece in the workspace.
+#include <algorithm>
+#include <cfloat>
+
+#include "gemm.h"
+#include "linear_logprob.h"
+#include "sequence.cuh"
+
+namespace relay {
+namespace {
+
+using head::Piece;
+
+constexpr long long kPieceElements = 1ll << 27;            // scores (or copied weights) of a piece, at most
+
+// ---- small kernels -----------------------------------------------------------------------------------------------
+// Joins the partial statistics of a row: eight groups of them, each in its order.
+__global__ void __launch_bounds__(256) join_stats_kernel(const float2 *part, long long ld, long long parts, const float *at, const void *tokens,
+                                                         int tokens_i64, long long rows, long long V, float inv_temperature, float *logp,
+                                                         float *lse)
+{
+    __shared__ float2 joint[8][32];
+    pdl_wait();
+    const long long row = (long long)blockIdx.x * 32 + threadIdx.x;
+    float m = -INFINITY, s = 0.0f;
+    auto add = [&](const float2 &q) {
+        const float top = fmaxf(m, q.x), off = top == -INFINITY ? 0.0f : top;
+        s = s * exp2f(m - off) + q.y * exp2f(q.x - off);
+        m = top;
+    };
+    if (row < rows) {
+#pragma unroll 4
+        for (long long j = threadIdx.y; j < parts; j += 8) {
+            const float2 *from = part + j * ld + row;
+            if (relay_in_bounds(from, 8)) add(__ldcs(from));
+        }
+    }
+    joint[threadIdx.y][threadIdx.x] = make_float2(m, s);
+    __syncthreads();
+    if (threadIdx.y != 0 || row >= rows) return;
+#pragma unroll
+    for (int g = 1; g < 8; ++g) add(joint[g][threadIdx.x]);
+    const float l = m == -INFINITY && s == 0.0f ? -INFINITY : fmaf(m, 0.693147181f, logf(s));
+    float lp = 0.0f;
+    if (head::token_in_piece(tokens, tokens_i64, row, V, 0, V) >= 0 && relay_in_bounds(at + row, 4))
+        lp = l == -INFINITY ? l : fmaf(at[row], inv_temperature, -l);
+    if (relay_in_bounds(logp + row, 4)) logp[row] = lp;
+    if (relay_in_bounds(lse + row, 4)) lse[row] = l;
+}
+
+// to (to_rows, to_cols) <- from (rows, cols), zero beyond; rows whose token names no class are zero too where tokens are given: whatever x
+// holds there (NaN too) takes no part in dw
+template <typename T>
+__global__ void __launch_bounds__(256) copy_padded_kernel(const T *from, long long ld_from, long long rows, long long cols, T *to, long long ld_to,
+                                                          long long to_rows, long long to_cols, const void *tokens, int tokens_i64, long long V)
+{
+    pdl_wait();
+    for (long long r = blockIdx.y; r < to_rows; r += gridDim.y) {
+        const bool live = r < rows && (tokens == nullptr || head::token_in_piece(tokens, tokens_i64, r, V, 0, V) >= 0);
+        for (long long c = (long long)blockIdx.x * 256 + threadIdx.x; c < to_cols; c += (long long)gridDim.x * 256) {
+            const T *p = from + r * ld_from + c;
+            T *q = to + r * ld_to + c;
+            const T x = live && c < cols && relay_in_bounds(p, sizeof(T)) ? *p : T(0.0f);
+            if (relay_in_bounds(q, sizeof(T))) *q = x;
+        }
+    }
+}
+// out (rows, cols) <- a + b, both fp32 (b may be null), rounded once
+template <typename T>
+__global__ void __launch_bounds__(256) add_kernel(const float *a, const float *b, long long ld, T *out, long long ld_out, long long rows,
+                                                  long long cols)
+{
+    pdl_wait();
+    for (long long r = blockIdx.y; r < rows; r += gridDim.y)
+        for (long long c = (long long)blockIdx.x * 256 + threadIdx.x; c < cols; c += (long long)gridDim.x * 256) {
+            const long long at = r * ld + c;
+            if (!relay_in_bounds(a + at, 4)) continue;
+            const float x = a[at] + (b != nullptr && relay_in_bounds(b + at, 4) ? b[at] : 0.0f);
+            T *q = out + r * ld_out + c;
+            if (!relay_in_bounds(q, sizeof(T))) continue;
+            if constexpr (sizeof(T) == 2) *q = __float2bfloat16_rn(x);
+            else *q = x;
+        }
+}
+
+// f32: statistics of a piece of scores in memory, one block a row (base 2, as the other path's)
+__global__ void __launch_bounds__(256) stats_kernel(const float *z, long long ld, const Piece p, float scale, float2 *part, float *at)
+{
+    __shared__ float2 joint[256];
+    pdl_wait();
+    const long long row = blockIdx.x;
+    const float *zr = z + row * ld;
+    float m = -INFINITY, s = 0.0f;
+    auto add = [&](float qm, float qs) {
+        const float top = fmaxf(m, qm), off = top == -INFINITY ? 0.0f : top;
+        s = s * exp2f(m - off) + qs * exp2f(qm - off);
+        m = top;
+    };
+    for (long long j = threadIdx.x; j < p.classes; j += 256) {
+        const float v = relay_in_bounds(zr + j, 4) ? zr[j] * scale : 0.0f;
+        if (v == -INFINITY) continue;
+        add(v, v != v ? v : 1.0f);
+    }
+    joint[threadIdx.x] = make_float2(m, s);
+    __syncthreads();
+    for (int n = 128; n > 0; n >>= 1) {
+        if (threadIdx.x < n) {
+            m = joint[threadIdx.x].x; s = joint[threadIdx.x].y;
+            add(joint[threadIdx.x + n].x, joint[threadIdx.x + n].y);
+            joint[threadIdx.x] = make_float2(m, s);
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x != 0) return;
+    if (relay_in_bounds(part + row, 8)) part[row] = make_float2(m, s);
+    const int t = head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, p.first, p.classes);
+    if (t >= 0 && relay_in_bounds(zr + t, 4) && relay_in_bounds(at + row, 4)) at[row] = zr[t];
+}
+// f32: dz of a piece, over its scores
+__global__ void __launch_bounds__(256) slopes_kernel(float *z, long long ld, const Piece p, const float *lse, const float *dlogp)
+{
+    pdl_wait();
+    for (long long row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        const int t = head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, p.first, p.classes);
+        const float l = relay_in_bounds(lse + row, 4) ? lse[row] : 0.0f;
+        const bool nothing = l == -INFINITY || head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, 0, p.V) < 0;
+        const float slope = nothing || !relay_in_bounds(dlogp + row, 4) ? 0.0f : dlogp[row] * p.inv_temperature;
+        for (long long j = (long long)blockIdx.x * 256 + threadIdx.x; j < p.classes; j += (long long)gridDim.x * 256) {
+            float *q = z + row * ld + j;
+            if (!relay_in_bounds(q, 4)) continue;
+            const float lp = fmaf(*q, p.inv_temperature, -l);
+            *q = nothing ? 0.0f : -slope * (j == t ? expm1f(lp) : expf(lp));
+        }
+    }
+}
+
+dim3 grid_of(long long rows, long long cols)
+{
+    return dim3((unsigned)std::min<long long>(std::max<long long>(1, (cols + 255) / 256), 64), (unsigned)std::min<long long>(std::max<long long>(1, rows), 16384));
+}
+template <typename T>
+relay_status_t copy_padded(const void *from, long long ld_from, long long rows, long long cols, void *to, long long ld_to, long long to_rows,
+                           long long to_cols, const Piece *masked, cudaStream_t st)
+{
+    RELAY_CUDA(launch_pdl(copy_padded_kernel<T>, grid_of(to_rows, to_cols), dim3(256), 0, st, (const T *)from, ld_from, rows, cols, (T *)to, ld_to,
+                          to_rows, to_cols, masked ? masked->tokens : nullptr, masked ? masked->tokens_i64 : 0, masked ? masked->V : 0));
+    return check_launch("linear_logprob");
+}
+template <typename T>
+relay_status_t add(const float *a, const float *b, long long ld, void *out, long long ld_out, long long rows, long long cols, cudaStream_t st)
+{
+    RELAY_CUDA(launch_pdl(add_kernel<T>, grid_of(rows, cols), dim3(256), 0, st, a, b, ld, (T *)out, ld_out, rows, cols));
+    return check_launch("linear_logprob");
+}
+
+// ---- sizes and the workspace --------------------------------------------------------------------------------------
+struct Sizes { int64_t rows, K, V; int rank; };            // rank of the row vectors
+
+int64_t padded(int64_t n) { return std::max<int64_t>(64, (n + 7) / 8 * 8); }
+// classes of a piece, whole tiles of 256: pieces of nearly the same size
+int64_t piece_of(int64_t V, int64_t other)
+{
+    const int64_t most = std::max<int64_t>(256, kPieceElements / std::max<int64_t>(1, other) / 256 * 256), n = (V + most - 1) / most;
+    return std::min<int64_t>((V + 255) / 256 * 256, ((V + n - 1) / n + 255) / 256 * 256);
+}
+bool rows_fit(const Sizes &s, bool trans_w) { return (trans_w ? s.K : s.V) % 8 == 0; }                // rows of w are whole 16 bytes
+
+struct Layout {
+    int64_t piece, pieces;                 // classes of a piece
+    int64_t N, K, C;                       // padded rows, width and classes of a piece (bf16)
+    bool copy_x, copy_w;
+    size_t part, at, x, w, z, dx, dx_more, dw, bytes;
+};
+Layout forward_layout(const Sizes &s, bool trans_w, bool bf16)
+{
+    Layout q{};
+    q.copy_x = bf16 && s.K % 8 != 0;
+    q.copy_w = bf16 && !rows_fit(s, trans_w);
+    q.K = padded(s.K); q.N = s.rows;
+    q.piece = !bf16 ? piece_of(s.V, s.rows) : q.copy_w ? piece_of(s.V, q.K) : s.V;
+    q.pieces = (s.V + q.piece - 1) / q.piece;
+    q.C = padded(q.piece);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
+    q.part = take((size_t)(bf16 ? head::parts_of(q.piece) : 1) * q.pieces * s.rows * sizeof(float2));
+    q.at = take((size_t)s.rows * 4);
+    q.x = take(q.copy_x ? (size_t)s.rows * q.K * 2 : 0);
+    q.w = take(q.copy_w ? (size_t)q.K * q.C * 2 : 0);
+    q.z = take(bf16 ? 0 : (size_t)s.rows * q.piece * 4);
+    q.bytes = at;
+    return q;
+}
+Layout gradient_layout(const Sizes &s, bool trans_w, bool bf16)
+{
+    Layout q{};
+    q.N = bf16 ? padded(s.rows) : s.rows; q.K = bf16 ? padded(s.K) : s.K;
+    q.piece = piece_of(s.V, std::max(q.N, q.K));
+    q.pieces = (s.V + q.piece - 1) / q.piece;
+    q.C = bf16 ? padded(q.piece) : q.piece;
+    q.copy_x = true;                                       // masked
+    const int64_t last = s.V - (q.pieces - 1) * q.piece;   // the pieces before it are whole tiles
+    q.copy_w = bf16 && (!rows_fit(s, trans_w) || padded(last) != last || q.K != s.K);                     // some piece is copied
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
+    q.x = take((size_t)q.N * q.K * (bf16 ? 2 : 4));
+    q.z = take((size_t)q.N * q.C * (bf16 ? 2 : 4));
+    q.dx = take(bf16 ? (size_t)q.N * q.K * 4 : 0);
+    q.dx_more = take(q.pieces > 1 ? (size_t)q.N * q.K * 4 : 0);
+    q.w = take(q.copy_w ? (size_t)q.K * q.C * 2 : 0);
+    q.dw = take(q.copy_w ? (size_t)q.K * q.C * 2 : 0);
+    q.bytes = at;
+    return q;
+}
+
+// ---- the calls --------------------------------------------------------------------------------------------------------
+GemmDesc product(int64_t M, int64_t N, int64_t K, const void *a, int64_t a_sm, int64_t a_sk, const void *b, int64_t b_sk, int64_t b_sn, void *c,
+                 int64_t ldc, int32_t in, int32_t out)
+{
+    GemmDesc g;
+    g.M = M; g.N = N; g.K = K;
+    g.a = a; g.a_sm = a_sm; g.a_sk = a_sk;
+    g.b = b; g.b_sk = b_sk; g.b_sn = b_sn;
+    g.c = c; g.ldc = ldc;
+    g.in_dtype = in; g.out_dtype = out;
+    return g;
+}
+
+// the piece of w that starts at class `first`: as it is, or copied to padded rows
+relay_status_t weights_of(Piece *p, const Sizes &s, const char *w, const Layout &q, char *ws, bool copy, cudaStream_t st)
+{
+    p->w = w + (p->trans_w ? p->first * s.K : p->first) * 2;
+    p->ldw = p->trans_w ? s.K : s.V;
+    if (!copy) return RELAY_OK;
+    const int64_t rows = p->trans_w ? p->classes : s.K, cols = p->trans_w ? s.K : p->classes;
+    const int64_t to_rows = p->trans_w ? padded(p->classes) : q.K, to_cols = p->trans_w ? q.K : padded(p->classes);
+    RELAY_TRY(copy_padded<__nv_bfloat16>(p->w, p->ldw, rows, cols, ws + q.w, to_cols, to_rows, to_cols, nullptr, st));
+    p->w = ws + q.w;
+    p->ldw = to_cols;
+    return RELAY_OK;
+}
+
+relay_status_t run_forward(Piece p, const Sizes &s, const void *w, bool bf16, float *logp, float *lse, char *ws, cudaStream_t st)
+{
+    const Layout q = forward_layout(s, p.trans_w, bf16);
+    float2 *part = (float2 *)(ws + q.part);
+    float *at = (float *)(ws + q.at);
+    const float scale = (float)(1.4426950408889634 * (double)p.inv_temperature);
+    const long long per_piece = bf16 ? head::parts_of(q.piece) : 1;
+    long long parts = 0;
+    if (q.copy_x) {
+        RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, ws + q.x, q.K, s.rows, q.K, nullptr, st));
+        p.x = ws + q.x;
+        p.ldx = q.K;
+    }
+    for (p.first = 0; p.first < s.V; p.first += q.piece) {
+        p.classes = std::min<int64_t>(q.piece, s.V - p.first);
+        if (bf16) {
+            RELAY_TRY(weights_of(&p, s, (const char *)w, q, ws, q.copy_w, st));
+            RELAY_TRY(head::launch_stats(p, part + p.first / q.piece * per_piece * s.rows, s.rows, at, st));
+            parts += (p.classes + 127) / 128 * 2;
+        } else {
+            const float *b = (const float *)w + (p.trans_w ? p.first * s.K : p.first);
+            RELAY_TRY(launch_gemm(product(s.rows, p.classes, s.K, p.x, s.K, 1, b, p.trans_w ? 1 : s.V, p.trans_w ? s.K : 1, ws + q.z, q.piece,
+                                          RELAY_F32, RELAY_F32), st));
+            RELAY_CUDA(launch_pdl(stats_kernel, dim3((unsigned)s.rows), dim3(256), 0, st, (const float *)(ws + q.z), (long long)q.piece, p, scale,
+                                  part + p.first / q.piece * s.rows, at));
+            RELAY_TRY(check_launch("linear_logprob"));
+            parts += 1;
+        }
+    }
+    RELAY_CUDA(launch_pdl(join_stats_kernel, dim3((unsigned)((s.rows + 31) / 32)), dim3(32, 8), 0, st, (const float2 *)part, (long long)s.rows, parts,
+                          (const float *)at, p.tokens, p.tokens_i64, (long long)s.rows, (long long)s.V, p.inv_temperature, logp, lse));
+    return check_launch("linear_logprob");
+}
+
+relay_status_t run_gradient_f32(Piece p, const Sizes &s, const float *w, const float *lse, const float *dlogp, float *dx, float *dw, char *ws,
+                                cudaStream_t st)
+{
+    const Layout q = gradient_layout(s, p.trans_w, false);
+    float *x = (float *)(ws + q.x), *z = (float *)(ws + q.z), *more = (float *)(ws + q.dx_more);
+    RELAY_TRY(copy_padded<float>(p.x, s.K, s.rows, s.K, x, s.K, s.rows, s.K, &p, st));
+    for (p.first = 0; p.first < s.V; p.first += q.piece) {
+        p.classes = std::min<int64_t>(q.piece, s.V - p.first);
+        const int64_t at = p.trans_w ? p.first * s.K : p.first, w_k = p.trans_w ? 1 : s.V, w_v = p.trans_w ? s.K : 1;
+        RELAY_TRY(launch_gemm(product(s.rows, p.classes, s.K, x, s.K, 1, w + at, w_k, w_v, z, q.piece, RELAY_F32, RELAY_F32), st));
+        RELAY_CUDA(launch_pdl(slopes_kernel, grid_of(s.rows, p.classes), dim3(256), 0, st, z, (long long)q.piece, p, lse, dlogp));
+        RELAY_TRY(check_launch("linear_logprob_grad"));
+        if (dx) {
+            float *to = p.first == 0 ? dx : more;
+            RELAY_TRY(launch_gemm(product(s.rows, s.K, p.classes, z, q.piece, 1, w + at, w_v, w_k, to, s.K, RELAY_F32, RELAY_F32), st));
+            if (to == more) RELAY_TRY(add<float>(dx, more, s.K, dx, s.K, s.rows, s.K, st));
+        }
+        if (!dw) continue;
+        if (p.trans_w) RELAY_TRY(launch_gemm(product(p.classes, s.K, s.rows, z, 1, q.piece, x, s.K, 1, dw + at, s.K, RELAY_F32, RELAY_F32), st));
+        else RELAY_TRY(launch_gemm(product(s.K, p.classes, s.rows, x, 1, s.K, z, q.piece, 1, dw + at, s.V, RELAY_F32, RELAY_F32), st));
+    }
+    return RELAY_OK;
+}
+
+relay_status_t run_gradient_bf16(Piece p, const Sizes &s, const void *w, const float *lse, const float *dlogp, __nv_bfloat16 *dx, __nv_bfloat16 *dw,
+                                 char *ws, cudaStream_t st)
+{
+    const Layout q = gradient_layout(s, p.trans_w, true);
+    void *x = ws + q.x, *z = ws + q.z;
+    float *sum = (float *)(ws + q.dx), *more = (float *)(ws + q.dx_more);
+    RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, x, q.K, q.N, q.K, &p, st));
+    p.x = x;
+    p.ldx = q.K;
+    for (p.first = 0; p.first < s.V; p.first += q.piece) {
+        p.classes = std::min<int64_t>(q.piece, s.V - p.first);
+        const int64_t C = padded(p.classes), at = p.trans_w ? p.first * s.K : p.first;
+        const bool copy = !rows_fit(s, p.trans_w) || C != p.classes || q.K != s.K;
+        RELAY_TRY(weights_of(&p, s, (const char *)w, q, ws, copy, st));
+        RELAY_TRY(head::launch_slopes(p, lse, dlogp, z, C, q.N, C, st));
+        const int64_t w_k = p.trans_w ? 1 : p.ldw, w_v = p.trans_w ? p.ldw : 1;
+        if (dx) {
+            float *to = p.first == 0 ? sum : more;
+            RELAY_TRY(launch_gemm(product(q.N, q.K, C, z, C, 1, p.w, w_v, w_k, to, q.K, RELAY_BF16, RELAY_F32), st));
+            const bool last = p.first + q.piece >= s.V;
+            const float *b = to == more ? more : nullptr;
+            if (last) RELAY_TRY(add<__nv_bfloat16>(sum, b, q.K, dx, s.K, s.rows, s.K, st));
+            else if (b) RELAY_TRY(add<float>(sum, b, q.K, sum, q.K, q.N, q.K, st));
+        }
+        if (!dw) continue;
+        void *to = copy ? (void *)(ws + q.dw) : (void *)(dw + at);
+        const int64_t ld = copy ? (p.trans_w ? q.K : C) : p.ldw;
+        if (p.trans_w) RELAY_TRY(launch_gemm(product(C, q.K, q.N, z, 1, C, x, q.K, 1, to, ld, RELAY_BF16, RELAY_BF16), st));
+        else RELAY_TRY(launch_gemm(product(q.K, C, q.N, x, 1, q.K, z, C, 1, to, ld, RELAY_BF16, RELAY_BF16), st));
+        if (copy) {
+            const int64_t rows = p.trans_w ? p.classes : s.K, cols = p.trans_w ? s.K : p.classes;
+            RELAY_TRY(copy_padded<__nv_bfloat16>(to, ld, rows, cols, dw + at, p.trans_w ? s.K : s.V, rows, cols, nullptr, st));
+        }
+    }
+    return RELAY_OK;
+}
+
+// ---- boundary -----------------------------------------------------------------------------------------------------------
+relay_status_t check_operands(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, Sizes *s)
+{
+    RELAY_TRY(check_type(x, "x"));
+    RELAY_TRY(check_type(w, "w"));
+    if (x->rank < 1) return fail(RELAY_ERR_RANK, "x: rank 0, a row is needed");
+    RELAY_TRY(check_rank(w, 2, "w"));
+    if (!is_float(x->dtype)) return fail(RELAY_ERR_DTYPE, "x: base type %s, needs f32 or bf16", dtype_name(x->dtype));
+    RELAY_TRY(check_dtype(w, x->dtype, "w"));
+    RELAY_TRY(check_layout(x, RELAY_ROWMAJOR, RELAY_ROWMAJOR, "x"));
+    RELAY_TRY(check_layout(w, RELAY_ROWMAJOR, RELAY_ROWMAJOR, "w"));
+    s->rank = x->rank - 1;
+    s->K = x->shape[s->rank];
+    s->rows = 1;
+    for (int d = 0; d < s->rank; ++d) s->rows *= x->shape[d];
+    s->V = w->shape[trans_w ? 0 : 1];
+    if (w->shape[trans_w ? 1 : 0] != s->K)
+        return fail(RELAY_ERR_SHAPE, "w: contraction extent %lld, x has %lld", (long long)w->shape[trans_w ? 1 : 0], (long long)s->K);
+    if (s->V == 0) return fail(RELAY_ERR_SHAPE, "w: a row without classes has no softmax");
+    if (s->K == 0) return fail(RELAY_ERR_SHAPE, "x: a contraction over nothing");
+    if (s->V > INT32_MAX - 512) return fail(RELAY_ERR_SHAPE, "w: %lld classes do not fit an i32", (long long)s->V);
+    if (s->K > (1 << 20) || s->rows > (1 << 28)) return fail(RELAY_ERR_UNSUPPORTED, "x: %lld rows of %lld", (long long)s->rows, (long long)s->K);
+    return RELAY_OK;
+}
+relay_status_t check_rows(const relay_tensor_t *t, const relay_tensor_t *x, const Sizes &s, int32_t d0, int32_t d1, const char *name)
+{
+    RELAY_TRY(check_type(t, name));
+    RELAY_TRY(check_rank(t, s.rank, name));
+    if (t->dtype != d0 && t->dtype != d1) return fail(RELAY_ERR_DTYPE, "%s: base type %s", name, dtype_name(t->dtype));
+    RELAY_TRY(check_layout(t, RELAY_ROWMAJOR, RELAY_ROWMAJOR, name));
+    return check_shape_n(t, x->shape, s.rank, name);
+}
+relay_status_t check_temperature(float t)
+{
+    if (!(t > 0.0f) || t > 3.0e38f) return fail(RELAY_ERR_ATTR, "temperature = %g, needs a positive finite number", (double)t);
+    return RELAY_OK;
+}
+Piece make_piece(const relay_tensor_t *x, const relay_tensor_t *tokens, int32_t trans_w, float temperature, const Sizes &s)
+{
+    Piece p{};
+    p.x = x->data; p.ldx = s.K;
+    p.trans_w = trans_w != 0;
+    p.rows = s.rows; p.K = s.K; p.V = s.V;
+    p.tokens = tokens->data; p.tokens_i64 = tokens->dtype == RELAY_I64;
+    p.inv_temperature = 1.0f / std::max(temperature, FLT_MIN);
+    return p;
+}
+
+}  // namespace
+}  // namespace relay
+
+using namespace relay;
+
+extern "C" size_t relay_workspace_bytes_linear_logprob(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w)
+{
+    clear_error();
+    Sizes s;
+    if (!x || !w || check_operands(x, w, trans_w, &s) != RELAY_OK || s.rows == 0) return 0;
+    return forward_layout(s, trans_w != 0, x->dtype == RELAY_BF16).bytes;
+}
+extern "C" size_t relay_workspace_bytes_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w)
+{
+    clear_error();
+    Sizes s;
+    if (!x || !w || check_operands(x, w, trans_w, &s) != RELAY_OK || s.rows == 0) return 0;
+    return gradient_layout(s, trans_w != 0, x->dtype == RELAY_BF16).bytes;
+}
+
+extern "C" relay_status_t relay_linear_logprob(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, const relay_tensor_t *tokens,
+                                               float temperature, const relay_tensor_t *logp, const relay_tensor_t *lse, void *ws, size_t ws_bytes,
+                                               void *stream)
+{
+    clear_error();
+    RELAY_TRY(check_not_null(x, "x"));
+    RELAY_TRY(check_not_null(w, "w"));
+    RELAY_TRY(check_not_null(tokens, "tokens"));
+    RELAY_TRY(check_not_null(logp, "logp"));
+    RELAY_TRY(check_not_null(lse, "lse"));
+    Sizes s;
+    RELAY_TRY(check_operands(x, w, trans_w, &s));
+    RELAY_TRY(check_rows(tokens, x, s, RELAY_I32, RELAY_I64, "tokens"));
+    RELAY_TRY(check_rows(logp, x, s, RELAY_F32, RELAY_F32, "logp"));
+    RELAY_TRY(check_rows(lse, x, s, RELAY_F32, RELAY_F32, "lse"));
+    RELAY_TRY(check_temperature(temperature));
+    const relay_tensor_t *ins[3] = {x, w, tokens}, *outs[2] = {logp, lse};
+    RELAY_TRY(seq::check_buffers(ins, outs));
+    if (s.rows == 0) return RELAY_OK;
+    const bool bf16 = x->dtype == RELAY_BF16;
+    const size_t need = forward_layout(s, trans_w != 0, bf16).bytes;
+    RELAY_TRY(check_workspace(ws, ws_bytes, need));
+    cudaStream_t st = (cudaStream_t)stream;
+    RELAY_TRY(seq::register_buffers(ins, outs, ws, need, st));
+    return run_forward(make_piece(x, tokens, trans_w, temperature, s), s, w->data, bf16, (float *)logp->data, (float *)lse->data, (char *)ws, st);
+}
+
+extern "C" relay_status_t relay_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, const relay_tensor_t *tokens,
+                                                    float temperature, const relay_tensor_t *lse, const relay_tensor_t *dlogp,
+                                                    const relay_tensor_t *dx, const relay_tensor_t *dw, void *ws, size_t ws_bytes, void *stream)
+{
+    clear_error();
+    RELAY_TRY(check_not_null(x, "x"));
+    RELAY_TRY(check_not_null(w, "w"));
+    RELAY_TRY(check_not_null(tokens, "tokens"));
+    RELAY_TRY(check_not_null(lse, "lse"));
+    RELAY_TRY(check_not_null(dlogp, "dlogp"));
+    if (!dx && !dw) return fail(RELAY_ERR_NULL, "no output is wanted");
+    Sizes s;
+    RELAY_TRY(check_operands(x, w, trans_w, &s));
+    RELAY_TRY(check_rows(tokens, x, s, RELAY_I32, RELAY_I64, "tokens"));
+    RELAY_TRY(check_rows(lse, x, s, RELAY_F32, RELAY_F32, "lse"));
+    RELAY_TRY(check_rows(dlogp, x, s, RELAY_F32, RELAY_F32, "dlogp"));
+    for (const auto &o : {std::make_pair(dx, x), std::make_pair(dw, w)}) {
+        if (!o.first) continue;
+        const char *name = o.second == x ? "dx" : "dw";
+        RELAY_TRY(check_type(o.first, name));
+        RELAY_TRY(check_rank(o.first, o.second->rank, name));
+        RELAY_TRY(check_dtype(o.first, o.second->dtype, name));
+        RELAY_TRY(check_layout(o.first, RELAY_ROWMAJOR, RELAY_ROWMAJOR, name));
+        RELAY_TRY(check_shape_n(o.first, o.second->shape, o.second->rank, name));
+    }
+    RELAY_TRY(check_temperature(temperature));
+    const relay_tensor_t *ins[5] = {x, w, tokens, lse, dlogp}, *outs[2] = {dx, dw};
+    RELAY_TRY(seq::check_buffers(ins, outs));
+    cudaStream_t st = (cudaStream_t)stream;
+    if (s.rows == 0) {                                     // a sum over no rows
+        if (dw) RELAY_CUDA(cudaMemsetAsync(dw->data, 0, nbytes(dw), st));
+        return RELAY_OK;
+    }
+    const bool bf16 = x->dtype == RELAY_BF16;
+    const size_t need = gradient_layout(s, trans_w != 0, bf16).bytes;
+    RELAY_TRY(check_workspace(ws, ws_bytes, need));
+    RELAY_TRY(seq::register_buffers(ins, outs, ws, need, st));
+    const Piece p = make_piece(x, tokens, trans_w, temperature, s);
+    if (bf16)
+        return run_gradient_bf16(p, s, w->data, (const float *)lse->data, (const float *)dlogp->data, dx ? (__nv_bfloat16 *)dx->data : nullptr,
+                                 dw ? (__nv_bfloat16 *)dw->data : nullptr, (char *)ws, st);
+    return run_gradient_f32(p, s, (const float *)w->data, (const float *)lse->data, (const float *)dlogp->data, dx ? (float *)dx->data : nullptr,
+                            dw ? (float *)dw->data : nullptr, (char *)ws, st);
+}

@@ -1,0 +1,198 @@
+// The products of a language model's head with what becomes of their scores: softmax statistics per row (forward) or the partials
+// of the scores (gradient), on the main loop of the two-SM contraction (gemm_tc2.cuh).  The scores live in TMEM alone: an epilogue warp
+// holds 32 rows x 64 columns of them in registers, one row a lane.
+#include "gemm_tc2.cuh"
+#include "linear_logprob.h"
+
+namespace relay {
+
+relay_status_t make_tmap_2d_sw64(CUtensorMap *m, bool f32, const void *base, uint64_t inner, uint64_t outer, uint64_t row_stride,
+                                 uint32_t box_outer);
+relay_status_t make_tmap_2d_bf16(CUtensorMap *m, const void *base, uint64_t inner, uint64_t outer, uint64_t row_stride,
+                                 uint32_t box_inner, uint32_t box_outer);
+
+namespace {
+
+using namespace gemm_tc2;
+
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+struct HeadParams : gemm_tc::Params {
+    const void *tokens;
+    int tokens_i64;
+    long long rows, V, first, classes;
+    float scale;                           // log2(e) / temperature
+    float inv_temperature;
+    float2 *part;                          // statistics
+    long long ld;
+    float *at;
+    const float *lse, *dlogp;              // slopes
+};
+
+// Each warp takes 64 neighbouring columns of its 32 rows: of a 128-column accumulator only the first two of the four slots have some.
+struct StatsEpilogue {
+    using Params = HeadParams;
+    int token;
+    __device__ __forceinline__ void prepare(const Params &p, int lane, int row0, int, int)
+    {
+        token = -1;
+        if (row0 + lane < p.rows) token = head::token_in_piece(p.tokens, p.tokens_i64, row0 + lane, p.V, p.first, p.classes);
+    }
+    __device__ __forceinline__ void drain(const Params &p, const CUtensorMap *, uint32_t taddr, uint8_t *, int lane, int row0, int n0, int width,
+                                          int slot)
+    {
+        const int c0 = slot * head::kPartColumns;
+        if (c0 >= width) return;
+        uint32_t r[2][32];
+        tc::tmem_ld_32x32(taddr + c0, r[0]);
+        tc::tmem_ld_32x32(taddr + c0 + 32, r[1]);
+        tc::tmem_ld_wait();
+        const int n = n0 + c0;
+        if (n + 64 > p.classes) {                          // warp-uniform: columns that do not exist
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+                if (n + j >= p.classes) r[j >> 5][j & 31] = 0xff800000u;
+        }
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 64; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(r[j >> 5][j & 31]));
+        const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale, off = m == -INFINITY ? 0.0f : -m;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 64; ++j) s[j & 3] += ex2(fmaf(__uint_as_float(r[j >> 5][j & 31]), p.scale, off));
+        const long long row = row0 + lane;
+        if (row < p.rows) p.part[(long long)(n / head::kPartColumns) * p.ld + row] = make_float2(m, (s[0] + s[1]) + (s[2] + s[3]));
+        const int hit = token - n;
+        if (hit >= 0 && hit < 64) {
+            float z = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 64; ++j) if (j == hit) z = __uint_as_float(r[j >> 5][j & 31]);
+            p.at[row] = z;
+        }
+    }
+    __device__ __forceinline__ void finish() {}
+};
+
+struct SlopeEpilogue {
+    using Params = HeadParams;
+    int token;
+    float off, slope, lse;                 // -lse log2(e), dlogp / temperature
+    bool nothing;                          // no token, or no class that can occur: no partials
+    __device__ __forceinline__ void prepare(const Params &p, int lane, int row0, int, int)
+    {
+        const long long row = row0 + lane;
+        token = -1;
+        nothing = true;
+        slope = off = lse = 0.0f;
+        if (row >= p.rows) return;
+        lse = p.lse[row];
+        token = head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, p.first, p.classes);
+        nothing = lse == -INFINITY || head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, 0, p.V) < 0;
+        if (nothing) return;
+        slope = p.dlogp[row] * p.inv_temperature;
+        off = -lse * 1.44269504f;
+    }
+    __device__ __forceinline__ void drain(const Params &p, const CUtensorMap *tm_c, uint32_t taddr, uint8_t *stage, int lane, int row0, int n0,
+                                          int width, int slot)
+    {
+        const int c0 = slot * 64;
+        if (c0 >= width) return;
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            const int n = n0 + c0 + 32 * half;
+            if (n >= p.N) break;                           // warp-uniform; p.N: columns of the stored piece
+            uint32_t r[32];
+            tc::tmem_ld_32x32(taddr + c0 + 32 * half, r);
+            tc::tmem_ld_wait();
+            const int hit = nothing ? -1 : token - n;
+            float v[32], own = 0.0f;
+            if (hit >= 0 && hit < 32) {                    // 1 - p of a class that is nearly certain keeps its precision
+#pragma unroll
+                for (int j = 0; j < 32; ++j) if (j == hit) own = __uint_as_float(r[j]);
+                own = -slope * expm1f(fmaf(own, p.inv_temperature, -lse));
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                v[j] = -slope * ex2(fmaf(__uint_as_float(r[j]), p.scale, off));
+                if (j == hit) v[j] = own;
+                if (nothing || n + j >= p.classes) v[j] = 0.0f;
+            }
+            const int sw = (lane >> 1) & 3;
+            if (tc::elect_one()) tc::tma_store_wait_read<0>();
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ sw) << 4)) =
+                    make_uint4(pack2(v[8 * c], v[8 * c + 1]), pack2(v[8 * c + 2], v[8 * c + 3]), pack2(v[8 * c + 4], v[8 * c + 5]),
+                               pack2(v[8 * c + 6], v[8 * c + 7]));
+            tc::fence_proxy_async();
+            __syncwarp();
+            if (tc::elect_one()) {
+                tc::tma_store_2d(tm_c, stage, n, row0);
+                tc::tma_store_commit();
+            }
+        }
+    }
+    __device__ __forceinline__ void finish() { if (tc::elect_one()) tc::tma_store_wait_all<0>(); }
+};
+
+template <typename Epi>
+relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, void *c, int64_t ldc, cudaStream_t st)
+{
+    int dev = 0, sms = 148;
+    RELAY_CUDA(cudaGetDevice(&dev));
+    RELAY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    CUtensorMap tm_a, tm_b, tm_c;
+    RELAY_TRY(make_tmap_2d_bf16(&tm_a, q.x, q.K, q.rows, q.ldx, BK, 128));
+    if (q.trans_w) RELAY_TRY(make_tmap_2d_bf16(&tm_b, q.w, q.K, q.classes, q.ldw, BK, 64));
+    else RELAY_TRY(make_tmap_2d_bf16(&tm_b, q.w, q.classes, q.K, q.ldw, 64, BK));
+    tm_c = tm_a;                                           // statistics are not stored by tile
+    if (c) RELAY_TRY(make_tmap_2d_sw64(&tm_c, false, c, N, M, ldc, 32));
+    p.M = (int)M; p.N = (int)N; p.K = (int)q.K;
+    p.tiles_m = (int)((M + 255) / 256); p.tiles_n = (int)((N + BN - 1) / BN); p.k_blocks = (int)((q.K + BK - 1) / BK);
+    p.err = device_error_word();
+    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
+    p.tokens = q.tokens; p.tokens_i64 = q.tokens_i64;
+    p.rows = q.rows; p.V = q.V; p.first = q.first; p.classes = q.classes;
+    p.inv_temperature = q.inv_temperature;
+    p.scale = (float)(1.4426950408889634 * (double)q.inv_temperature);
+    const int n_tiles = p.tiles_m * p.tiles_n, pairs = std::min(n_tiles, sms / 2);
+    static thread_local UnitTable tb;
+    tb.n = 0;
+    p.tail_split = 1;
+    if (!plan_units(p.tiles_m, (int)((N + 127) / 128), pairs, p.k_blocks, &tb)) {
+        tb.n = 0;
+        const int wide_rounds = p.k_blocks >= kWideMinKBlocks ? std::min(n_tiles / (2 * pairs), (p.tiles_m * (p.tiles_n / 2)) / pairs) : 0;
+        p.wide_units = wide_rounds * pairs;
+        const int narrow = n_tiles - 2 * p.wide_units, rem = narrow % pairs;
+        p.tail_split = (rem > 0 && 2 * rem <= pairs) ? 2 : 1;
+        p.full_tiles = p.tail_split == 2 ? narrow - rem : narrow;
+    }
+    auto go = [&](auto kernel) -> relay_status_t {
+        RELAY_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES));
+        RELAY_CUDA(launch_pdl(kernel, dim3(2 * pairs), dim3(NUM_THREADS), SMEM_BYTES, st, tm_a, tm_b, tm_c, p, tb));
+        return check_launch("linear_logprob");
+    };
+    return q.trans_w ? go(gemm_tc2_kernel<false, false, Epi>) : go(gemm_tc2_kernel<false, true, Epi>);
+}
+
+}  // namespace
+
+namespace head {
+
+relay_status_t launch_stats(const Piece &q, float2 *part, long long ld, float *at, cudaStream_t st)
+{
+    HeadParams p{};
+    p.part = part; p.ld = ld; p.at = at;
+    return launch<StatsEpilogue>(q, p, q.rows, q.classes, nullptr, 0, st);
+}
+relay_status_t launch_slopes(const Piece &q, const float *lse, const float *dlogp, void *dz, long long ld, long long padded_rows,
+                             long long padded_classes, cudaStream_t st)
+{
+    HeadParams p{};
+    p.lse = lse; p.dlogp = dlogp;
+    return launch<SlopeEpilogue>(q, p, padded_rows, padded_classes, dz, ld, st);
+}
+
+}  // namespace head
+}  // namespace relay
