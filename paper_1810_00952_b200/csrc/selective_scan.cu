@@ -4,6 +4,10 @@
 #include "selective_scan.cuh"
 
 namespace relay {
+
+relay_status_t make_tmap_2d(CUtensorMap *m, bool f32, const void *base, uint64_t inner, uint64_t outer, uint64_t row_stride,
+                            uint32_t box_inner, uint32_t box_outer, bool swizzle128);
+
 namespace {
 
 using namespace scan;
@@ -14,6 +18,7 @@ constexpr int kStepThreads = 128;
 template <typename T, int NB>
 __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(const Args p)
 {
+    constexpr bool FINE = sizeof(T) == 4;
     pdl_wait();
     const long long at = ((long long)blockIdx.x * kStepThreads + threadIdx.x) >> 2;      // b * D + d
     const int nl = threadIdx.x & 3;
@@ -37,17 +42,22 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
         }
         if (t < end) {
             u = load_weight<T>(p.u, row + d);
-            float step = load_weight<T>(p.delta, row + d) + bias, slope;
-            if (p.softplus) step = softplus_(step, slope);
+            float step = load_weight<T>(p.delta, row + d) + bias, other;
+            if (p.softplus) unpair(softplus2(pair(step, step)).value, step, other);
             const long long bc = (t * p.B + i) * p.ld_bc;
 #pragma unroll
             for (int k = 0; k < NB; ++k)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int n = k * 16 + nl * 4 + j;
-                    if (n >= p.N) continue;
-                    h[k][j] = fmaf(exp2_(step * a[k][j] * kLog2e), h[k][j], step * u * load_weight<T>(p.b, bc + n));
-                    y = fmaf(load_weight<T>(p.c, bc + n), h[k][j], y);
+                for (int j = 0; j < 4; j += 2) {
+                    float decay[2];
+                    unpair(decay2<FINE>(pair(step * (a[k][j] * kLog2e), step * (a[k][j + 1] * kLog2e))), decay[0], decay[1]);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int n = k * 16 + nl * 4 + j + q;
+                        if (n >= p.N) continue;
+                        h[k][j + q] = fmaf(decay[q], h[k][j + q], step * u * load_weight<T>(p.b, bc + n));
+                        y = fmaf(load_weight<T>(p.c, bc + n), h[k][j + q], y);
+                    }
                 }
         }
         y += __shfl_xor_sync(0xffffffffu, y, 1);
@@ -58,7 +68,7 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
                 out[0] = fmaf(skip, u, y);
                 if (p.z) {
                     const float z = load_weight<T>(p.z, row + d);
-                    out[0] *= z * logistic<sizeof(T) == 4>(z);
+                    out[0] *= z * logistic<FINE>(z);
                 }
             }
             store<T, 1>(p.y, row + d, out);
@@ -70,175 +80,313 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
 }
 
 // ---- chunks -----------------------------------------------------------------------------------------------------------
-// A block: WC warps of eight channels side by side, WT rows of them, each with a run of RUN steps of the chunk.
-constexpr int RUN = 8;
+// A block: WC warps of eight channels side by side, WT rows of them; four lanes a channel, each with four neighbouring states of every
+// sixteen.  A chunk's rows are fetched a chunk ahead by TMA.  Three phases: steps and weights are made fp32, four channels a thread, each
+// step and step times u twice over, as the scan's paired instructions take them; the scan itself; and skip, gate and rounding of the
+// results, whose four partial sums a channel the scan leaves side by side.  Several blocks on an SM are in different phases.
+// WT = 1: a warp takes its channels through the whole chunk.  WT > 1: each row of warps has a run of RUN steps.
+constexpr int RUN = 8, STAGES = 2;
 
-template <int WT, int WC, int NB>
+template <typename T, int WT, int WC, int NB, int TD>
 struct Tile {
-    static constexpr int THREADS = 32 * WT * WC, CHANNELS = 8 * WC, STEPS = RUN * WT, NP = 16 * NB;
-    float2 step[STEPS][CHANNELS];          // delta, delta u
-    float b[STEPS][NP], c[STEPS][NP];
-    float y[STEPS][CHANNELS];
-    float4 decay[2][WT][WC][32], sum[2][WT][WC][32];
+    static constexpr int THREADS = 32 * WT * WC, CHANNELS = 8 * TD * WC, STEPS = RUN * WT < 32 ? 32 : RUN * WT, NP = 16 * NB;
+    struct Stage { alignas(128) T u[STEPS][CHANNELS]; alignas(128) T delta[STEPS][CHANNELS]; alignas(128) T z[STEPS][CHANNELS]; alignas(128) T bc[STEPS * 2 * NP]; };
+    Stage stage[STAGES];
+    alignas(16) float2 step[STEPS][CHANNELS];              // delta, delta u
+    alignas(16) float b[STEPS][NP], c[STEPS][NP];
+    alignas(16) float y[STEPS][4][CHANNELS];               // the four lanes' parts of sum_n c h
+    float4 decay[WT == 1 ? 1 : 2][WT][WC][WT == 1 ? 1 : 32], sum[WT == 1 ? 1 : 2][WT][WC][WT == 1 ? 1 : 32];
+    uint64_t full[STAGES];
+    int gave_up;
 };
 
-template <typename T, int WT, int WC, int NB>
-__global__ void __launch_bounds__(32 * WT * WC, NB == 1 ? 2 : 1) selective_scan_kernel(const Args p)
+template <typename T, int WT, int WC, int NB, int TD>
+__global__ void __launch_bounds__(32 * WT * WC) selective_scan_kernel(const Args p, const __grid_constant__ Maps maps)
 {
-    using S = Tile<WT, WC, NB>;
+    using S = Tile<T, WT, WC, NB, TD>;
     constexpr bool FINE = sizeof(T) == 4;
-    constexpr int WEIGHTS = S::STEPS * S::NP / S::THREADS;                 // values of b (and of c) that a thread fetches per chunk
-    extern __shared__ uint4 shared_raw[];
-    S &s = *reinterpret_cast<S *>(shared_raw);
-    pdl_wait();
+    extern __shared__ uint8_t shared_raw[];
+    S &s = *reinterpret_cast<S *>(((uintptr_t)shared_raw + 127) & ~(uintptr_t)127);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wt = warp / WC, wc = warp % WC, nl = lane & 3, cl = lane >> 2;
     const long long i = blockIdx.x / p.groups;
     const long long c0 = (blockIdx.x - i * p.groups) * S::CHANNELS;
-    const long long end = end_of(p, i);
-    // this thread's states: of channel mine
-    const int ch = wc * 8 + cl;
-    const long long mine = c0 + ch;
-    const bool live = mine < p.D;
-    f32x2 a[NB][2], h[NB][2];                                              // a log2(e); the state at the chunk's start
-#pragma unroll
-    for (int k = 0; k < NB; ++k) {
-        float x[4];
-        load_states(p, live ? p.a : nullptr, mine * p.N, k * 16 + nl * 4, x);
-        a[k][0] = pair(x[0] * kLog2e, x[1] * kLog2e);
-        a[k][1] = pair(x[2] * kLog2e, x[3] * kLog2e);
-        load_states(p, live ? p.h0 : nullptr, (i * p.D + mine) * p.N, k * 16 + nl * 4, x);
-        h[k][0] = pair(x[0], x[1]);
-        h[k][1] = pair(x[2], x[3]);
+    if (tid == 0) {
+        for (int q = 0; q < STAGES; ++q) tc::mbar_init(&s.full[q], 1);
+        s.gave_up = 0;
+        tc::fence_barrier_init();
     }
-    // this thread's pair of channels and step of the chunk in what surrounds the scan
-    const int pt = tid / (S::CHANNELS / 2), pc = 2 * (tid % (S::CHANNELS / 2));
-    const long long two = c0 + pc;
-    float skip[2] = {0.0f, 0.0f}, bias[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-        if (two + j < p.D) {
-            if (p.d && relay_in_bounds(p.d + two + j, 4)) skip[j] = p.d[two + j];
-            if (p.delta_bias && relay_in_bounds(p.delta_bias + two + j, 4)) bias[j] = p.delta_bias[two + j];
+    __syncthreads();
+    pdl_wait();
+    const long long end = end_of(p, i);
+    const int live_chunks = (int)((end + S::STEPS - 1) / S::STEPS);
+    // rows of chunk k into its stage, by TMA (one thread) or by everyone's plain loads
+    auto fetch = [&](int k) {
+        typename S::Stage &g = s.stage[k % STAGES];
+        const long long t0 = (long long)k * S::STEPS;
+        if (tid == 0 && (p.tma_x || p.tma_w)) {
+            const uint32_t x = p.tma_x ? (p.z ? 3u : 2u) * (uint32_t)sizeof(g.u) : 0u, w = p.tma_w ? (uint32_t)(S::STEPS * 2 * p.N * sizeof(T)) : 0u;
+            tc::mbar_expect_tx(&s.full[k % STAGES], x + w);
+            const int col = (int)(i * p.D + c0), row = (int)t0;
+            if (p.tma_x) {
+                tc::tma_load_2d(g.u, &maps.u, &s.full[k % STAGES], col, row);
+                tc::tma_load_2d(g.delta, &maps.delta, &s.full[k % STAGES], col, row);
+                if (p.z) tc::tma_load_2d(g.z, &maps.z, &s.full[k % STAGES], col, row);
+            }
+            if (p.tma_w) {
+                tc::tma_load_2d(g.bc, &maps.b, &s.full[k % STAGES], (int)(i * p.ld_bc), row);
+                if (p.ld_bc == p.N) tc::tma_load_2d(g.bc + S::STEPS * p.N, &maps.c, &s.full[k % STAGES], (int)(i * p.ld_bc), row);
+            }
         }
-    float u[2], raw[2], z[2], wb[WEIGHTS], wc_[WEIGHTS];
-    auto fetch = [&](long long t0) {
-        const long long t = t0 + pt;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) u[j] = raw[j] = z[j] = 0.0f;
-        if (t < end && two < p.D) {
-            const long long row = (t * p.B + i) * p.D;
-            load_channels<T>(p, p.u, row, two, u);
-            load_channels<T>(p, p.delta, row, two, raw);
-            if (p.z) load_channels<T>(p, p.z, row, two, z);
+        if (!p.tma_x) {
+#pragma unroll 4
+            for (int e = tid; e < S::STEPS * S::CHANNELS; e += S::THREADS) {
+                const int t = e / S::CHANNELS, c = e % S::CHANNELS;
+                const long long at = ((t0 + t) * p.B + i) * p.D + c0 + c;
+                if (t0 + t < end && c0 + c < p.D) {
+                    g.u[t][c] = load_raw_one<T>(p.u, at);
+                    g.delta[t][c] = load_raw_one<T>(p.delta, at);
+                    if (p.z) g.z[t][c] = load_raw_one<T>(p.z, at);
+                }
+            }
         }
-#pragma unroll
-        for (int k = 0; k < WEIGHTS; ++k) {
-            const int e = tid + k * S::THREADS, tt = e / S::NP, n = e % S::NP;
-            wb[k] = wc_[k] = 0.0f;
-            if (t0 + tt < end && n < p.N) {
-                const long long at = ((t0 + tt) * p.B + i) * p.ld_bc + n;
-                wb[k] = load_weight<T>(p.b, at);
-                wc_[k] = load_weight<T>(p.c, at);
+        if (!p.tma_w) {
+            const bool packed = p.ld_bc != p.N;
+#pragma unroll 4
+            for (int e = tid; e < S::STEPS * p.N; e += S::THREADS) {
+                const int t = e / p.N, n = e - t * p.N;
+                const long long at = ((t0 + t) * p.B + i) * p.ld_bc + n;
+                if (t0 + t < end) {
+                    g.bc[packed ? t * 2 * p.N + n : e] = load_raw_one<T>(p.b, at);
+                    g.bc[packed ? t * 2 * p.N + p.N + n : S::STEPS * p.N + e] = load_raw_one<T>(p.c, at);
+                }
             }
         }
     };
-    fetch(0);
-    for (long long t0 = 0; t0 < p.T; t0 += S::STEPS) {
-        const bool inside = t0 + pt < end;
-        float un[2], zn[2];
+    for (int k = 0; k < STAGES && k < live_chunks; ++k) fetch(k);
+    // this thread's states: of channels mine .. mine + TD - 1
+    const int ch = (wc * 8 + cl) * TD;
+    const long long mine = c0 + ch;
+    f32x2 a[TD][NB][2], h[TD][NB][2];                      // a log2(e); the state
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float step = raw[j] + bias[j], slope;
-            if (p.softplus) step = softplus_(step, slope);
-            if (!inside || two + j >= p.D) step = 0.0f;                    // nothing decays and nothing is added
-            s.step[pt][pc + j] = make_float2(step, step * u[j]);
-            un[j] = u[j];
-            zn[j] = z[j];
-        }
-#pragma unroll
-        for (int k = 0; k < WEIGHTS; ++k) {
-            const int e = tid + k * S::THREADS;
-            (&s.b[0][0])[e] = wb[k];
-            (&s.c[0][0])[e] = wc_[k];
-        }
-        __syncthreads();
-        if (t0 + S::STEPS < p.T) fetch(t0 + S::STEPS);
-        float y[RUN];
-#pragma unroll
-        for (int r = 0; r < RUN; ++r) y[r] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-            f32x2 da[RUN][2], x[RUN][2], P[2], H[2];                       // decays; what is added, then the states
-            P[0] = P[1] = pair(1.0f, 1.0f);
-            H[0] = H[1] = pair(0.0f, 0.0f);
-#pragma unroll
-            for (int r = 0; r < RUN; ++r) {
-                const float2 st = s.step[wt * RUN + r][ch];
-                const float4 b = *reinterpret_cast<const float4 *>(&s.b[wt * RUN + r][k * 16 + nl * 4]);
-                const f32x2 dd = pair(st.x, st.x), du = pair(st.y, st.y);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float lo, hi;
-                    unpair(mul2(dd, a[k][q]), lo, hi);
-                    da[r][q] = pair(exp2_(lo), exp2_(hi));
-                    x[r][q] = mul2(du, q ? pair(b.z, b.w) : pair(b.x, b.y));
-                    H[q] = fma2(da[r][q], H[q], x[r][q]);
-                    P[q] = mul2(da[r][q], P[q]);
-                }
-            }
-            const int slot = k & 1;
-            float4 v;
-            unpair(P[0], v.x, v.y); unpair(P[1], v.z, v.w);
-            s.decay[slot][wt][wc][lane] = v;
-            unpair(H[0], v.x, v.y); unpair(H[1], v.z, v.w);
-            s.sum[slot][wt][wc][lane] = v;
-            __syncthreads();
-            f32x2 from[2] = {h[k][0], h[k][1]};                            // the state at the start of this run
-#pragma unroll
-            for (int w = 0; w < WT; ++w) {
-                const float4 pw = s.decay[slot][w][wc][lane], hw = s.sum[slot][w][wc][lane];
-                if (w == wt) { from[0] = h[k][0]; from[1] = h[k][1]; }
-                h[k][0] = fma2(pair(pw.x, pw.y), h[k][0], pair(hw.x, hw.y));
-                h[k][1] = fma2(pair(pw.z, pw.w), h[k][1], pair(hw.z, hw.w));
-            }
-            if (p.states && live && t0 + wt * RUN < p.T && (t0 + wt * RUN) % kSpan == 0) {
-                float g[4];
-                unpair(from[0], g[0], g[1]); unpair(from[1], g[2], g[3]);
-                store_states(p, p.states, (((t0 + wt * RUN) / kSpan * p.B + i) * p.D + mine) * p.N, k * 16 + nl * 4, g);
-            }
-#pragma unroll
-            for (int r = 0; r < RUN; ++r) {
-                const float4 c = *reinterpret_cast<const float4 *>(&s.c[wt * RUN + r][k * 16 + nl * 4]);
-                f32x2 sum;
-                from[0] = fma2(da[r][0], from[0], x[r][0]);
-                from[1] = fma2(da[r][1], from[1], x[r][1]);
-                sum = fma2(pair(c.z, c.w), from[1], mul2(pair(c.x, c.y), from[0]));
-                y[r] += sum2(sum);
-            }
-        }
-        float yr[RUN / 4];
-        reduce_lanes<RUN, 1, 4>(y, lane, yr);
-#pragma unroll
-        for (int j = 0; j < RUN / 4; ++j) s.y[wt * RUN + 4 * j + nl][ch] = yr[j];
-        __syncthreads();
-        if (t0 + pt < p.T && two < p.D) {
-            float out[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                out[j] = inside ? fmaf(skip[j], un[j], s.y[pt][pc + j]) : 0.0f;
-                if (p.z) out[j] *= zn[j] * logistic<FINE>(zn[j]);
-            }
-            store_channels<T>(p, p.y, ((t0 + pt) * p.B + i) * p.D, two, out);
-        }
-    }
-    if (wt == 0 && live) {
+    for (int d = 0; d < TD; ++d)
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
             float x[4];
-            unpair(h[k][0], x[0], x[1]); unpair(h[k][1], x[2], x[3]);
-            store_states(p, p.h_final, (i * p.D + mine) * p.N, k * 16 + nl * 4, x);
+            load_states(p, mine + d < p.D ? p.a : nullptr, (mine + d) * p.N, k * 16 + nl * 4, x);
+            a[d][k][0] = pair(x[0] * kLog2e, x[1] * kLog2e);
+            a[d][k][1] = pair(x[2] * kLog2e, x[3] * kLog2e);
+            load_states(p, mine + d < p.D ? p.h0 : nullptr, (i * p.D + mine + d) * p.N, k * 16 + nl * 4, x);
+            h[d][k][0] = pair(x[0], x[1]);
+            h[d][k][1] = pair(x[2], x[3]);
         }
+    auto write = [&](float *to, long long first, int d, int k, const f32x2 (&v)[2]) {
+        float g[4];
+        unpair(v[0], g[0], g[1]); unpair(v[1], g[2], g[3]);
+        if (mine + d < p.D) store_states(p, to, (first + mine + d) * p.N, k * 16 + nl * 4, g);
+    };
+    auto save = [&](long long t, int d, int k, const f32x2 (&v)[2]) {
+        if (p.states && t < p.T && t % kSpan == 0) write(p.states, (t / kSpan * p.B + i) * p.D, d, k, v);
+    };
+    // four channels that this thread turns into steps, and whose results it finishes: always the same ones
+    constexpr int FOURS = S::CHANNELS / 4, PASSES = (S::STEPS * FOURS + S::THREADS - 1) / S::THREADS;
+    static_assert(S::THREADS % FOURS == 0, "a thread's channels are the same in every row");
+    const int pc = 4 * (tid % FOURS);
+    f32x2 skip[2], bias[2];
+    {
+        float x[4], y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool in = c0 + pc + j < p.D;
+            x[j] = p.d && in && relay_in_bounds(p.d + c0 + pc + j, 4) ? p.d[c0 + pc + j] : 0.0f;
+            y[j] = p.delta_bias && in && relay_in_bounds(p.delta_bias + c0 + pc + j, 4) ? p.delta_bias[c0 + pc + j] : 0.0f;
+        }
+        skip[0] = pair(x[0], x[1]); skip[1] = pair(x[2], x[3]);
+        bias[0] = pair(y[0], y[1]); bias[1] = pair(y[2], y[3]);
     }
+    for (int chunk = 0; chunk < live_chunks; ++chunk) {
+        typename S::Stage &g = s.stage[chunk % STAGES];
+        const long long t0 = (long long)chunk * S::STEPS;
+        if (p.tma_x || p.tma_w) tc::mbar_wait(&s.full[chunk % STAGES], (chunk / STAGES) & 1, &s.gave_up, p.err, tc::ERR_WAIT_FULL);
+        if (!p.tma_x || !p.tma_w) __syncthreads();         // everyone's plain loads
+        const int in = (int)min((long long)S::STEPS, end - t0);              // steps of the chunk that are inside the sequence
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k) {
+            const int t = tid / FOURS + k * (S::THREADS / FOURS);
+            if (t >= S::STEPS) break;
+            float u[4], x[4];
+            widen_shared(&g.u[t][pc], u);
+            widen_shared(&g.delta[t][pc], x);
+            f32x2 step[2] = {add2(pair(x[0], x[1]), bias[0]), add2(pair(x[2], x[3]), bias[1])};
+            if (p.softplus) { step[0] = softplus2(step[0]).value; step[1] = softplus2(step[1]).value; }
+            if (t >= in) {                                 // behind the end nothing decays and nothing is added
+                step[0] = step[1] = 0;
+                u[0] = u[1] = u[2] = u[3] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float lo, hi, ulo, uhi;
+                unpair(step[j], lo, hi);
+                unpair(mul2(step[j], pair(u[2 * j], u[2 * j + 1])), ulo, uhi);
+                *reinterpret_cast<float4 *>(&s.step[t][pc + 2 * j]) = make_float4(lo, ulo, hi, uhi);
+            }
+        }
+        if (p.N == S::NP) {                                // four states at a time
+            for (int e = tid; e < S::STEPS * S::NP / 4; e += S::THREADS) {
+                const int t = e / (S::NP / 4), n = e % (S::NP / 4) * 4;
+                float b[4], c[4];
+                widen_shared(p.ld_bc != p.N ? &g.bc[t * 2 * S::NP + n] : &g.bc[t * S::NP + n], b);
+                widen_shared(p.ld_bc != p.N ? &g.bc[t * 2 * S::NP + S::NP + n] : &g.bc[S::STEPS * S::NP + t * S::NP + n], c);
+                if (t >= in) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) b[j] = c[j] = 0.0f;
+                }
+                *reinterpret_cast<float4 *>(&s.b[t][n]) = make_float4(b[0], b[1], b[2], b[3]);
+                *reinterpret_cast<float4 *>(&s.c[t][n]) = make_float4(c[0], c[1], c[2], c[3]);
+            }
+        } else {
+            for (int e = tid; e < S::STEPS * S::NP; e += S::THREADS) {
+                const int t = e / S::NP, n = e % S::NP;
+                const bool on = t < in && n < p.N, packed = p.ld_bc != p.N;
+                s.b[t][n] = on ? to_f32(g.bc[packed ? t * 2 * p.N + n : t * p.N + n]) : 0.0f;
+                s.c[t][n] = on ? to_f32(g.bc[packed ? t * 2 * p.N + p.N + n : S::STEPS * p.N + t * p.N + n]) : 0.0f;
+            }
+        }
+        __syncthreads();
+        if constexpr (WT == 1) {
+#pragma unroll
+            for (int d = 0; d < TD; ++d)
+#pragma unroll
+                for (int k = 0; k < NB; ++k) save(t0, d, k, h[d][k]);
+            // a few steps at a time: first their decays and what they add, all independent, then the chain
+            constexpr int AT_ONCE = NB == 1 ? 8 / TD : 1;
+#pragma unroll 2
+            for (int r0 = 0; r0 < S::STEPS; r0 += AT_ONCE) {
+                f32x2 da[AT_ONCE][TD][NB][2], x[AT_ONCE][TD][NB][2];
+#pragma unroll
+                for (int r = 0; r < AT_ONCE; ++r) {
+                    float2 st[TD];
+                    if constexpr (TD == 1) st[0] = s.step[r0 + r][ch];
+                    else {
+#pragma unroll
+                        for (int d = 0; d < TD; d += 2) *reinterpret_cast<float4 *>(&st[d]) = *reinterpret_cast<const float4 *>(&s.step[r0 + r][ch + d]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < NB; ++k) {
+                        const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
+#pragma unroll
+                        for (int d = 0; d < TD; ++d) {
+                            const f32x2 dd = pair(st[d].x, st[d].x), du = pair(st[d].y, st[d].y);
+                            da[r][d][k][0] = decay2<FINE>(mul2(dd, a[d][k][0]));
+                            da[r][d][k][1] = decay2<FINE>(mul2(dd, a[d][k][1]));
+                            x[r][d][k][0] = mul2(du, b.x);
+                            x[r][d][k][1] = mul2(du, b.y);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < AT_ONCE; ++r) {
+                    float sum[TD];
+#pragma unroll
+                    for (int d = 0; d < TD; ++d) {
+                        f32x2 y = 0;
+#pragma unroll
+                        for (int k = 0; k < NB; ++k) {
+                            const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
+                            h[d][k][0] = fma2(da[r][d][k][0], h[d][k][0], x[r][d][k][0]);
+                            h[d][k][1] = fma2(da[r][d][k][1], h[d][k][1], x[r][d][k][1]);
+                            y = k ? fma2(c.x, h[d][k][0], y) : mul2(c.x, h[d][k][0]);
+                            y = fma2(c.y, h[d][k][1], y);
+                        }
+                        sum[d] = sum2(y);
+                    }
+                    if constexpr (TD == 1) s.y[r0 + r][nl][ch] = sum[0];
+                    else if constexpr (TD == 2) *reinterpret_cast<float2 *>(&s.y[r0 + r][nl][ch]) = make_float2(sum[0], sum[1]);
+                    else *reinterpret_cast<float4 *>(&s.y[r0 + r][nl][ch]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                }
+            }
+        } else {
+            const int r0 = wt * RUN;                       // this warp's run
+            float y[RUN];
+#pragma unroll
+            for (int k = 0; k < NB; ++k) {
+                f32x2 da[RUN][2], x[RUN][2], P[2], H[2];                   // decays; what is added, then the states
+#pragma unroll
+                for (int r = 0; r < RUN; ++r) {
+                    const float2 st = s.step[r0 + r][ch];
+                    const f32x2 dd = pair(st.x, st.x), du = pair(st.y, st.y);
+                    const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        da[r][q] = decay2<FINE>(mul2(dd, a[0][k][q]));
+                        x[r][q] = mul2(du, q ? b.y : b.x);
+                        H[q] = r ? fma2(da[r][q], H[q], x[r][q]) : x[r][q];
+                        P[q] = r ? mul2(da[r][q], P[q]) : da[r][q];
+                    }
+                }
+                const int slot = k & 1;
+                *reinterpret_cast<ulonglong2 *>(&s.decay[slot][wt][wc][lane]) = make_ulonglong2(P[0], P[1]);
+                *reinterpret_cast<ulonglong2 *>(&s.sum[slot][wt][wc][lane]) = make_ulonglong2(H[0], H[1]);
+                __syncthreads();
+                f32x2 from[2];                             // the state at the start of this run
+#pragma unroll
+                for (int w = 0; w < WT; ++w) {
+                    const ulonglong2 pw = *reinterpret_cast<const ulonglong2 *>(&s.decay[slot][w][wc][lane]);
+                    const ulonglong2 hw = *reinterpret_cast<const ulonglong2 *>(&s.sum[slot][w][wc][lane]);
+                    if (w == wt) { from[0] = h[0][k][0]; from[1] = h[0][k][1]; }
+                    h[0][k][0] = fma2(pw.x, h[0][k][0], hw.x);
+                    h[0][k][1] = fma2(pw.y, h[0][k][1], hw.y);
+                }
+                save(t0 + r0, 0, k, from);
+#pragma unroll
+                for (int r = 0; r < RUN; ++r) {
+                    const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
+                    from[0] = fma2(da[r][0], from[0], x[r][0]);
+                    from[1] = fma2(da[r][1], from[1], x[r][1]);
+                    const float v = sum2(fma2(c.y, from[1], mul2(c.x, from[0])));
+                    y[r] = k ? y[r] + v : v;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RUN; ++r) s.y[r0 + r][nl][ch] = y[r];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k) {
+            const int t = tid / FOURS + k * (S::THREADS / FOURS);
+            if (t >= S::STEPS || t0 + t >= p.T) break;
+            f32x2 out[2] = {0, 0};
+            float q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&s.y[t][j][pc]);
+                out[0] = add2(out[0], v.x); out[1] = add2(out[1], v.y);
+            }
+            widen_shared(&g.u[t][pc], q);
+            if (p.d) { out[0] = fma2(skip[0], pair(q[0], q[1]), out[0]); out[1] = fma2(skip[1], pair(q[2], q[3]), out[1]); }
+            if (p.z) {
+                widen_shared(&g.z[t][pc], q);
+                out[0] = mul2(out[0], pair(q[0] * logistic<FINE>(q[0]), q[1] * logistic<FINE>(q[1])));
+                out[1] = mul2(out[1], pair(q[2] * logistic<FINE>(q[2]), q[3] * logistic<FINE>(q[3])));
+            }
+            unpair(out[0], q[0], q[1]); unpair(out[1], q[2], q[3]);
+            if (t >= in) q[0] = q[1] = q[2] = q[3] = 0.0f;
+            store_four<T>(p, p.y, ((t0 + t) * p.B + i) * p.D, c0 + pc, q);
+        }
+        __syncthreads();                                   // the stage is free
+        if (chunk + STAGES < live_chunks) fetch(chunk + STAGES);
+    }
+    // behind the sequence
+    const long long tail = (long long)live_chunks * S::STEPS;
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (long long t = tail + tid / FOURS; t < p.T; t += S::THREADS / FOURS) store_four<T>(p, p.y, (t * p.B + i) * p.D, c0 + pc, zero);
+    if (wt != 0) return;
+#pragma unroll
+    for (int d = 0; d < TD; ++d)
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+            for (long long t = (tail + kSpan - 1) / kSpan * kSpan; t < p.T; t += kSpan) save(t, d, k, h[d][k]);
+            if (p.h_final) write(p.h_final, i * p.D, d, k, h[d][k]);
+        }
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -252,22 +400,28 @@ relay_status_t launch_steps(const Args &p, cudaStream_t st)
     RELAY_CUDA(launch_pdl(selective_scan_steps_kernel<T, NB>, dim3((unsigned)blocks), dim3(kStepThreads), 0, st, p));
     return check_launch("selective_scan");
 }
-template <typename T, int WT, int WC, int NB>
+template <typename T, int WT, int WC, int NB, int TD>
 relay_status_t launch_chunks(Args p, cudaStream_t st)
 {
-    using S = Tile<WT, WC, NB>;
+    using S = Tile<T, WT, WC, NB, TD>;
     p.groups = (int)((p.D + S::CHANNELS - 1) / S::CHANNELS);
     const long long blocks = p.B * p.groups;
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "selective_scan: %lld x %lld channels", p.B, p.D);
-    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_kernel<T, WT, WC, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(S)));
-    RELAY_CUDA(launch_pdl(selective_scan_kernel<T, WT, WC, NB>, dim3((unsigned)blocks), dim3(S::THREADS), sizeof(S), st, p));
+    Maps maps;
+    RELAY_TRY(make_maps(&p, &maps, sizeof(T) == 4, S::CHANNELS, S::STEPS));
+    const size_t bytes = sizeof(S) + 128;
+    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_kernel<T, WT, WC, NB, TD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    RELAY_CUDA(launch_pdl(selective_scan_kernel<T, WT, WC, NB, TD>, dim3((unsigned)blocks), dim3(S::THREADS), bytes, st, p, maps));
     return check_launch("selective_scan");
 }
+// Rows of warps share the channels where there are too few of them to give every SM eight warps.
 template <typename T, int NB>
 relay_status_t launch_form(const Args &p, cudaStream_t st)
 {
     if (p.T <= kFewSteps) return launch_steps<T, NB>(p, st);
-    return launch_chunks<T, 4, 2, NB>(p, st);
+    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
+    if (p.B * p.D < 148 * 64) return launch_chunks<T, NB == 1 ? 8 : 4, 1, NB, 1>(p, st);
+    return launch_chunks<T, 1, 2, NB, 1>(p, st);
 }
 template <typename T>
 relay_status_t launch_states(const Args &p, cudaStream_t st)
@@ -279,6 +433,26 @@ relay_status_t launch_states(const Args &p, cudaStream_t st)
 }  // namespace
 
 namespace scan {
+
+// TMA takes rows of whole 16-byte pieces that start at such pieces for every batch element, and coordinates of 31 bits.
+relay_status_t make_maps(Args *p, Maps *m, bool f32, int channels, int steps)
+{
+    const int64_t e = f32 ? 4 : 2, row = p->B * p->D, weights = p->B * p->ld_bc;
+    p->tma_x = p->D * e % 16 == 0 && row < 0x7fffff00LL && p->T < 0x7fffff00LL;
+    p->tma_w = p->ld_bc * e % 16 == 0 && weights < 0x7fffff00LL && p->T < 0x7fffff00LL;
+    *m = Maps{};
+    if (p->tma_x) {
+        RELAY_TRY(make_tmap_2d(&m->u, f32, p->u, row, p->T, row, channels, steps, false));
+        RELAY_TRY(make_tmap_2d(&m->delta, f32, p->delta, row, p->T, row, channels, steps, false));
+        if (p->z) RELAY_TRY(make_tmap_2d(&m->z, f32, p->z, row, p->T, row, channels, steps, false));
+        if (p->dy) RELAY_TRY(make_tmap_2d(&m->dy, f32, p->dy, row, p->T, row, channels, steps, false));
+    }
+    if (p->tma_w) {
+        RELAY_TRY(make_tmap_2d(&m->b, f32, p->b, weights, p->T, weights, p->ld_bc, steps, false));
+        if (p->ld_bc == p->N) RELAY_TRY(make_tmap_2d(&m->c, f32, p->c, weights, p->T, weights, p->ld_bc, steps, false));
+    }
+    return RELAY_OK;
+}
 
 relay_status_t check_inputs(const Inputs &in, Sizes *s, int64_t *N)
 {
@@ -326,6 +500,8 @@ Args make_args(const Inputs &in, int32_t softplus, const Sizes &s, int64_t N)
     p.ld_bc = (int)(in.c ? N : 2 * N);
     p.softplus = softplus;
     p.pairs = s.D % 2 == 0;
+    p.four = s.D % 4 == 0;
+    p.err = device_error_word();
     p.quads = N % 4 == 0;
     return p;
 }

@@ -6,6 +6,7 @@
 // every warp joins those before its own, and the run is summed again from the state that it really starts with.
 #pragma once
 #include "sequence.cuh"
+#include "tc_common.cuh"
 
 namespace relay {
 namespace scan {
@@ -34,8 +35,13 @@ struct Args {
     long long T, B, D;
     int N, ld_bc, softplus, groups;
     int pairs;                             // two neighbouring channels are one aligned access
+    int four;                              // four are
     int quads;                             // four neighbouring states are one aligned access
+    int tma_x, tma_w;                      // rows of channels, and of b and c, are whole 16-byte pieces: TMA fetches them
+    int *err;
 };
+// what TMA fetches, as (B*D columns, T rows) and (B * ld_bc columns, T rows)
+struct Maps { CUtensorMap u, delta, z, dy, b, c; };
 
 __device__ __forceinline__ long long end_of(const Args &p, long long i)
 {
@@ -44,24 +50,31 @@ __device__ __forceinline__ long long end_of(const Args &p, long long i)
     return n < 0 ? 0 : n > p.T ? p.T : n;
 }
 
-// softplus(x) = max(x, 0) + log(1 + w), w = exp(-|x|) <= 1, and its slope, the logistic function.  log(1 + w) = 2 atanh(s), s = w / (2 + w) <=
-// 1/3, by the series of atanh up to s^13 (the rest is below 3^-15 / 15 = 5e-9 of one): steps are small numbers, and a relative error in one
-// moves a whole state.  w = 2^t with what the rounding of t = -|x| log2(e) left put back.
-__device__ __forceinline__ float softplus_(float x, float &slope)
+// softplus(x) = max(x, 0) + log(1 + w), w = exp(-|x|) <= 1, of two values, and its slope, the logistic function.  log(1 + w) = w q(w), q
+// the expansion of log(1 + w) / w in Chebyshev polynomials on [0,1] up to the ninth (5e-9 off): steps are small numbers, and a relative
+// error in one moves a whole state.  w = 2^t with what the rounding of t = -|x| log2(e) left put back.
+struct Softplus { f32x2 value, w; };
+__device__ __forceinline__ Softplus softplus2(f32x2 x)
 {
-    const float m = -fabsf(x), t = m * kLog2e;
-    const float left = fmaf(m, kLog2e, -t) + m * 1.925963033e-8f;            // log2(e) beyond fp32
-    const float p = exp2_(t), w = fmaf(p, left * 0.693147181f, p);
-    const float s = __fdividef(w, 2.0f + w), q = s * s;
-    float r = fmaf(q, 1.0f / 13.0f, 1.0f / 11.0f);
-    r = fmaf(r, q, 1.0f / 9.0f);
-    r = fmaf(r, q, 1.0f / 7.0f);
-    r = fmaf(r, q, 0.2f);
-    r = fmaf(r, q, 1.0f / 3.0f);
-    r = fmaf(r, q, 1.0f);
+    constexpr float of[10] = {1.0f, -4.999990463e-01f, 3.333000541e-01f, -2.495455891e-01f, 1.967811733e-01f, -1.531186253e-01f, 1.061426476e-01f,
+                              -5.706420168e-02f, 1.990716159e-02f, -3.256378463e-03f};
+    const f32x2 m = x | 0x8000000080000000ull;                             // -|x|
+    const f32x2 t = mul2(m, pair(kLog2e, kLog2e));
+    f32x2 left = fma2(m, pair(kLog2e, kLog2e), neg2(t));
+    left = fma2(m, pair(1.925963033e-8f, 1.925963033e-8f), left);          // log2(e) beyond fp32
+    float a, b;
+    unpair(t, a, b);
+    const f32x2 p = pair(exp2_(a), exp2_(b)), w = fma2(p, mul2(left, pair(0.693147181f, 0.693147181f)), p);
+    f32x2 r = pair(of[9], of[9]);
+#pragma unroll
+    for (int k = 8; k >= 0; --k) r = fma2(r, w, pair(of[k], of[k]));
+    unpair(x, a, b);
+    return Softplus{fma2(r, w, pair(fmaxf(a, 0.0f), fmaxf(b, 0.0f))), w};
+}
+__device__ __forceinline__ float softplus_slope(float x, float w)
+{
     const float small = __fdividef(w, 1.0f + w);
-    slope = x >= 0.0f ? 1.0f - small : small;
-    return fmaxf(x, 0.0f) + 2.0f * s * r;
+    return x >= 0.0f ? 1.0f - small : small;
 }
 
 // two neighbouring channels c, c + 1 of a row that starts at `row`; those from D on are zero
@@ -83,6 +96,64 @@ __device__ __forceinline__ void store_channels(const Args &p, void *base, long l
     store<T, 1>(base, row + c, lo);
     if (c + 1 < p.D) store<T, 1>(base, row + c + 1, hi);
 }
+// four neighbouring channels
+template <typename T>
+__device__ __forceinline__ void store_four(const Args &p, void *base, long long row, long long c, const float (&x)[4])
+{
+    if (p.four) {
+        if (c < p.D) store<T, 4>(base, row + c, x);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float q[1] = {x[j]};
+        if (c + j < p.D) store<T, 1>(base, row + c + j, q);
+    }
+}
+// one value as it is stored
+template <typename T>
+__device__ __forceinline__ T load_raw_one(const void *base, long long at)
+{
+    const T *p = (const T *)base + at;
+    return relay_in_bounds(p, sizeof(T)) ? *p : T(0.0f);
+}
+// four neighbouring values in shared memory, as fp32
+__device__ __forceinline__ void widen_shared(const __nv_bfloat16 *p, float (&x)[4]) { widen(*reinterpret_cast<const uint2 *>(p), x, __nv_bfloat16()); }
+__device__ __forceinline__ void widen_shared(const float *p, float (&x)[4]) { unpack(*reinterpret_cast<const uint4 *>(p), x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(float x) { return x; }
+
+// 2^x of two exponents.  With bf16 data the hardware's exponential serves: a few units of 2^-24 off, 2e-8 low on average.  A state adds
+// that up over the steps in which it forgets, so fp32 data takes a polynomial whose only error beyond 2e-9 is its last rounding: x = n + f with
+// n the nearest whole number (the low bits of a sum with 1.5 * 2^23), 2^f on |f| <= 1/2 by its Chebyshev expansion up to f^6, n added to
+// the exponent's bits.  Exponents below -126 give zero, above 126 infinity comes a little early.
+template <bool FINE>
+__device__ __forceinline__ f32x2 decay2(f32x2 x)
+{
+    float lo, hi;
+    if constexpr (!FINE) {
+        unpair(x, lo, hi);
+        return pair(exp2_(lo), exp2_(hi));
+    } else {
+        float a, b, c, d;
+        unpair(x, lo, hi);
+        a = fminf(fmaxf(lo, -126.0f), 127.0f); b = fminf(fmaxf(hi, -126.0f), 127.0f);
+        const f32x2 y = pair(a, b), t = add2(y, pair(12582912.0f, 12582912.0f)), f = add2(y, neg2(add2(t, pair(-12582912.0f, -12582912.0f))));
+        constexpr float of[7] = {1.0f, 6.931471825e-01f, 2.402265072e-01f, 5.550327152e-02f, 9.618025273e-03f, 1.340043265e-03f, 1.546973217e-04f};
+        f32x2 r = pair(of[6], of[6]);
+#pragma unroll
+        for (int k = 5; k >= 0; --k) r = fma2(r, f, pair(of[k], of[k]));
+        unpair(t, c, d);
+        unpair(r, a, b);
+        a = __int_as_float(__float_as_int(a) + (__float_as_int(c) << 23));
+        b = __int_as_float(__float_as_int(b) + (__float_as_int(d) << 23));
+        // far below zero nothing is left; NaN stays NaN
+        a = lo < -126.0f ? 0.0f : lo != lo ? lo : a;
+        b = hi < -126.0f ? 0.0f : hi != hi ? hi : b;
+        return pair(a, b);
+    }
+}
+
 // four neighbouring states n .. n + 3 of an f32 tensor [..][N] at entry `at`; those from N on are zero
 __device__ __forceinline__ void load_states(const Args &p, const float *base, long long at, int n, float (&x)[4])
 {
@@ -139,6 +210,7 @@ __device__ __forceinline__ void reduce_lanes(float (&x)[V], int lane, float (&ou
 
 // ---- the boundary's part that both calls share ---------------------------------------------------------------------------
 struct Inputs { const relay_tensor_t *u, *delta, *a, *b, *c, *d, *z, *delta_bias, *lengths; };
+relay_status_t make_maps(Args *p, Maps *m, bool f32, int channels, int steps);
 relay_status_t check_sizes(const relay_tensor_t *u, const relay_tensor_t *a, Sizes *s, int64_t *N);
 relay_status_t check_inputs(const Inputs &in, Sizes *s, int64_t *N);
 relay_status_t check_softplus(int32_t softplus);

@@ -140,7 +140,13 @@ __global__ void __launch_bounds__(32 * WT * columns_of(NB), 1) selective_scan_gr
             for (int j = 0; j < 2; ++j) {
                 step[j] = raw[j] + bias[j];
                 slope[j] = 1.0f;
-                if (p.softplus) step[j] = softplus_(step[j], slope[j]);
+                if (p.softplus) {
+                    const Softplus q = softplus2(pair(step[j], step[j]));
+                    float v, w;
+                    unpair(q.w, w, v);
+                    slope[j] = softplus_slope(step[j], w);
+                    unpair(q.value, step[j], v);
+                }
                 if (!inside || two + j >= p.D) step[j] = 0.0f;             // nothing decays and nothing is added
                 e[j] = dy[j];
                 gate[j] = 0.0f;
