@@ -438,8 +438,8 @@ namespace scan {
 relay_status_t make_maps(Args *p, Maps *m, bool f32, int channels, int steps)
 {
     const int64_t e = f32 ? 4 : 2, row = p->B * p->D, weights = p->B * p->ld_bc;
-    p->tma_x = p->D * e % 16 == 0 && row < 0x7fffff00LL && p->T < 0x7fffff00LL;
-    p->tma_w = p->ld_bc * e % 16 == 0 && weights < 0x7fffff00LL && p->T < 0x7fffff00LL;
+    p->tma_x = p->T > 0 && p->D * e % 16 == 0 && row < 0x7fffff00LL && p->T < 0x7fffff00LL;
+    p->tma_w = p->T > 0 && p->ld_bc * e % 16 == 0 && weights < 0x7fffff00LL && p->T < 0x7fffff00LL;
     *m = Maps{};
     if (p->tma_x) {
         RELAY_TRY(make_tmap_2d(&m->u, f32, p->u, row, p->T, row, channels, steps, false));

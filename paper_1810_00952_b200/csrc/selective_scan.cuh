@@ -120,6 +120,8 @@ __device__ __forceinline__ T load_raw_one(const void *base, long long at)
 // four neighbouring values in shared memory, as fp32
 __device__ __forceinline__ void widen_shared(const __nv_bfloat16 *p, float (&x)[4]) { widen(*reinterpret_cast<const uint2 *>(p), x, __nv_bfloat16()); }
 __device__ __forceinline__ void widen_shared(const float *p, float (&x)[4]) { unpack(*reinterpret_cast<const uint4 *>(p), x); }
+__device__ __forceinline__ void widen_two(const __nv_bfloat16 *p, float (&x)[2]) { widen(*reinterpret_cast<const uint32_t *>(p), x, __nv_bfloat16()); }
+__device__ __forceinline__ void widen_two(const float *p, float (&x)[2]) { widen(*reinterpret_cast<const uint2 *>(p), x, float()); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 

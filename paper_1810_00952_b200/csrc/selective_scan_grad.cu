@@ -8,42 +8,100 @@ namespace {
 
 using namespace scan;
 
-// A block: WC warps side by side, of sixteen channels each (two a lane), WT rows of them, each with a run of RUN steps; the chunk is the span
-// whose starting states the forward call saved.
-constexpr int RUN = 4, WT = kSpan / RUN, STEPS = kSpan;
-__host__ __device__ constexpr int columns_of(int NB) { return NB == 1 ? 2 : 1; }
+// A block: sixteen channels of a batch element, eight warps; a lane has two neighbouring channels and four neighbouring states of every sixteen,
+// and each warp a run of RUN steps of the chunk, which is the span whose starting states the forward call saved.  The runs' products and sums
+// meet in shared memory in both directions at once.  Chunks are taken from the last to the first; rows are fetched a chunk ahead by TMA.
+constexpr int RUN = 4, WT = kSpan / RUN, STEPS = kSpan, CHANNELS = 16, THREADS = 32 * WT, STAGES = 2;
 
-template <int NB>
+template <typename T, int NB>
 struct Tile {
-    static constexpr int WC = columns_of(NB), THREADS = 32 * WT * WC, CHANNELS = 16 * WC, NP = 16 * NB, SLOTS = NB == 1 ? 1 : 2;
-    float2 step[STEPS][CHANNELS];                          // delta, delta u
-    float e[STEPS][CHANNELS];                              // dy silu(z)
-    float b[STEPS][NP], c[STEPS][NP];
-    float4 decay[SLOTS][WT][WC][2][32], sum[SLOTS][WT][WC][2][32], back[SLOTS][WT][WC][2][32];
-    float along[STEPS][CHANNELS], kept[STEPS][CHANNELS], plain[STEPS][CHANNELS];   // sum_n g b, sum_n a G h[t-1], sum_n c h
-    float dbc[WC][STEPS][2 * NP];
+    static constexpr int NP = 16 * NB, SLOTS = NB == 1 ? 1 : 2;
+    struct Stage { alignas(128) T u[STEPS][CHANNELS]; alignas(128) T delta[STEPS][CHANNELS]; alignas(128) T z[STEPS][CHANNELS]; alignas(128) T dy[STEPS][CHANNELS]; alignas(128) T bc[STEPS * 2 * NP]; };
+    Stage stage[STAGES];
+    alignas(16) float2 step[STEPS][CHANNELS];              // delta, delta u
+    alignas(16) float e[STEPS][CHANNELS];                  // dy silu(z)
+    alignas(16) float b[STEPS][NP], c[STEPS][NP];
+    ulonglong2 decay[SLOTS][WT][2][32], sum[SLOTS][WT][2][32], back[SLOTS][WT][2][32];
+    ulonglong2 carry[2][NB][2][32];                        // what flows back into the chunk
+    alignas(16) float along[STEPS][CHANNELS], kept[STEPS][CHANNELS], plain[STEPS][CHANNELS];   // sum_n g b, sum_n a G h[t-1], sum_n c h
+    alignas(16) float dbc[STEPS][2 * NP];
     float2 u[THREADS], slope[THREADS], gate[THREADS];      // what a thread needs again at the end of a chunk
-    float4 slots[NB == 1 ? 1 : NB][4][NB == 1 ? 1 : THREADS];   // more than sixteen states: carries and sums of da wait here
+    ulonglong2 da[NB == 1 ? 1 : NB][2][NB == 1 ? 1 : THREADS];   // more than sixteen states: sums of da wait here
+    uint64_t full[STAGES];
+    int gave_up;
 };
 
 template <typename T, int NB>
-__global__ void __launch_bounds__(32 * WT * columns_of(NB), 1) selective_scan_grad_kernel(const Args p)
+__global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_kernel(const Args p, const __grid_constant__ Maps maps)
 {
-    using S = Tile<NB>;
+    using S = Tile<T, NB>;
     constexpr bool FINE = sizeof(T) == 4;
-    constexpr int WC = S::WC, WEIGHTS = (STEPS * S::NP + S::THREADS - 1) / S::THREADS;
-    extern __shared__ uint4 shared_raw[];
-    S &s = *reinterpret_cast<S *>(shared_raw);
-    pdl_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wt = warp / WC, wc = warp % WC, nl = lane & 3, cl = lane >> 2;
+    extern __shared__ uint8_t shared_raw[];
+    S &s = *reinterpret_cast<S *>(((uintptr_t)shared_raw + 127) & ~(uintptr_t)127);
+    const int tid = threadIdx.x, lane = tid & 31, wt = tid >> 5, nl = lane & 3, cl = lane >> 2;
     const long long i = blockIdx.x / p.groups;
     const int group = (int)(blockIdx.x - i * p.groups);
-    const long long c0 = (long long)group * S::CHANNELS, end = end_of(p, i);
-    const int ch = wc * 16 + cl * 2;                       // this lane's channels: ch, ch + 1 of the block
+    const long long c0 = (long long)group * CHANNELS;
+    if (tid == 0) {
+        for (int q = 0; q < STAGES; ++q) tc::mbar_init(&s.full[q], 1);
+        s.gave_up = 0;
+        tc::fence_barrier_init();
+    }
+    __syncthreads();
+    pdl_wait();
+    const long long end = end_of(p, i);
+    const int chunks = (int)((p.T + STEPS - 1) / STEPS), live_chunks = (int)((end + STEPS - 1) / STEPS);
+    // the q-th fetch: rows of chunk live_chunks - 1 - q
+    auto fetch = [&](int q) {
+        typename S::Stage &g = s.stage[q % STAGES];
+        const long long t0 = (long long)(live_chunks - 1 - q) * STEPS;
+        if (tid == 0 && (p.tma_x || p.tma_w)) {
+            uint64_t *full = &s.full[q % STAGES];
+            const uint32_t x = p.tma_x ? (p.z ? 4u : 3u) * (uint32_t)sizeof(g.u) : 0u, w = p.tma_w ? (uint32_t)(STEPS * 2 * p.N * sizeof(T)) : 0u;
+            tc::mbar_expect_tx(full, x + w);
+            const int col = (int)(i * p.D + c0), row = (int)t0;
+            if (p.tma_x) {
+                tc::tma_load_2d(g.u, &maps.u, full, col, row);
+                tc::tma_load_2d(g.delta, &maps.delta, full, col, row);
+                tc::tma_load_2d(g.dy, &maps.dy, full, col, row);
+                if (p.z) tc::tma_load_2d(g.z, &maps.z, full, col, row);
+            }
+            if (p.tma_w) {
+                tc::tma_load_2d(g.bc, &maps.b, full, (int)(i * p.ld_bc), row);
+                if (p.ld_bc == p.N) tc::tma_load_2d(g.bc + STEPS * p.N, &maps.c, full, (int)(i * p.ld_bc), row);
+            }
+        }
+        if (!p.tma_x) {
+#pragma unroll
+            for (int e = tid; e < STEPS * CHANNELS; e += THREADS) {
+                const int t = e / CHANNELS, c = e % CHANNELS;
+                const long long at = ((t0 + t) * p.B + i) * p.D + c0 + c;
+                if (t0 + t < end && c0 + c < p.D) {
+                    g.u[t][c] = load_raw_one<T>(p.u, at);
+                    g.delta[t][c] = load_raw_one<T>(p.delta, at);
+                    g.dy[t][c] = load_raw_one<T>(p.dy, at);
+                    if (p.z) g.z[t][c] = load_raw_one<T>(p.z, at);
+                }
+            }
+        }
+        if (!p.tma_w) {
+            const bool packed = p.ld_bc != p.N;
+#pragma unroll 2
+            for (int e = tid; e < STEPS * p.N; e += THREADS) {
+                const int t = e / p.N, n = e - t * p.N;
+                const long long at = ((t0 + t) * p.B + i) * p.ld_bc + n;
+                if (t0 + t < end) {
+                    g.bc[packed ? t * 2 * p.N + n : e] = load_raw_one<T>(p.b, at);
+                    g.bc[packed ? t * 2 * p.N + p.N + n : STEPS * p.N + e] = load_raw_one<T>(p.c, at);
+                }
+            }
+        }
+    };
+    for (int q = 0; q < STAGES && q < live_chunks; ++q) fetch(q);
+    const int ch = cl * 2;                                 // this lane's channels: ch, ch + 1 of the block
     const long long mine = c0 + ch;
-    // sixteen states: everything that lives from chunk to chunk is in registers
-    f32x2 a1[2][2], G1[2][2], dA1[2][2];                   // a log2(e), what flows back into the chunk, sums of da
-    auto load_a = [&](int k, f32x2 (&a)[2][2]) {
+    f32x2 a[2][2], dA[2][2];                               // a log2(e), sums of da
+    auto load_a = [&](int k) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             float x[4];
@@ -52,212 +110,196 @@ __global__ void __launch_bounds__(32 * WT * columns_of(NB), 1) selective_scan_gr
             a[j][1] = pair(x[2] * kLog2e, x[3] * kLog2e);
         }
     };
-    auto to_slot = [&](int k, int at, const f32x2 (&v)[2][2]) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float4 x;
-            unpair(v[j][0], x.x, x.y); unpair(v[j][1], x.z, x.w);
-            s.slots[k][at + j][tid] = x;
-        }
-    };
-    auto from_slot = [&](int k, int at, f32x2 (&v)[2][2]) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float4 x = s.slots[k][at + j][tid];
-            v[j][0] = pair(x.x, x.y); v[j][1] = pair(x.z, x.w);
-        }
-    };
+    for (int j = 0; j < 2; ++j) dA[j][0] = dA[j][1] = 0;
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+            if constexpr (NB > 1) s.da[k][j][tid] = make_ulonglong2(0, 0);
+            if (wt != 0) continue;
             float x[4];
             load_states(p, mine + j < p.D ? p.dh_final : nullptr, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, x);
-            G1[j][0] = pair(x[0], x[1]); G1[j][1] = pair(x[2], x[3]);
-            dA1[j][0] = dA1[j][1] = pair(0.0f, 0.0f);
+            s.carry[0][k][j][lane] = make_ulonglong2(pair(x[0], x[1]), pair(x[2], x[3]));
         }
-        if constexpr (NB > 1) { to_slot(k, 0, G1); to_slot(k, 2, dA1); }
     }
-    if constexpr (NB == 1) load_a(0, a1);
+    if constexpr (NB == 1) load_a(0);
     // this thread's pair of channels and step of the chunk in what surrounds the scan
-    const int pt = tid / (S::CHANNELS / 2), pc = 2 * (tid % (S::CHANNELS / 2));
+    const int pt = tid / (CHANNELS / 2), pc = 2 * (tid % (CHANNELS / 2));
     const long long two = c0 + pc;
-    float skip[2] = {0.0f, 0.0f}, bias[2] = {0.0f, 0.0f}, dd[2] = {0.0f, 0.0f}, dbias[2] = {0.0f, 0.0f};
+    f32x2 skip, bias, dd = 0, dbias = 0;
+    {
+        float x[2], y[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-        if (two + j < p.D) {
-            if (p.d && relay_in_bounds(p.d + two + j, 4)) skip[j] = p.d[two + j];
-            if (p.delta_bias && relay_in_bounds(p.delta_bias + two + j, 4)) bias[j] = p.delta_bias[two + j];
+        for (int j = 0; j < 2; ++j) {
+            const bool in = two + j < p.D;
+            x[j] = p.d && in && relay_in_bounds(p.d + two + j, 4) ? p.d[two + j] : 0.0f;
+            y[j] = p.delta_bias && in && relay_in_bounds(p.delta_bias + two + j, 4) ? p.delta_bias[two + j] : 0.0f;
         }
-    float u[2], raw[2], z[2], dy[2], wb[WEIGHTS], wc_[WEIGHTS];
-    auto fetch = [&](long long t0) {
-        const long long t = t0 + pt;
+        skip = pair(x[0], x[1]); bias = pair(y[0], y[1]);
+    }
+    for (int chunk = chunks - 1; chunk >= live_chunks; --chunk) {            // behind the sequence nothing flows back
+        const long long t0 = (long long)chunk * STEPS, row = ((t0 + pt) * p.B + i) * p.D;
+        if (t0 + pt < p.T && two < p.D) {
+            const float zero[2] = {0.0f, 0.0f};
+            store_channels<T>(p, p.du, row, two, zero);
+            store_channels<T>(p, p.ddelta, row, two, zero);
+            if (p.dz) store_channels<T>(p, p.dz, row, two, zero);
+        }
+        for (int q = tid; q < STEPS * 2 * p.N; q += THREADS) {
+            const int t = q / (2 * p.N), n = q - t * 2 * p.N;
+            float *out = p.part_bc + (((long long)group * p.T + t0 + t) * p.B + i) * 2 * p.N + n;
+            if (t0 + t < p.T && relay_in_bounds(out, 4)) *out = 0.0f;
+        }
+    }
+    for (int done = 0; done < live_chunks; ++done) {
+        const long long chunk = live_chunks - 1 - done, t0 = chunk * STEPS;
+        typename S::Stage &g = s.stage[done % STAGES];
+        // the states that the first run starts from: on their way while the rows are made fp32
+        float start[2][4];
+        if constexpr (NB == 1) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) u[j] = raw[j] = z[j] = dy[j] = 0.0f;
-        if (t < end && two < p.D) {
-            const long long row = (t * p.B + i) * p.D;
-            load_channels<T>(p, p.u, row, two, u);
-            load_channels<T>(p, p.delta, row, two, raw);
-            load_channels<T>(p, p.dy, row, two, dy);
-            if (p.z) load_channels<T>(p, p.z, row, two, z);
+            for (int j = 0; j < 2; ++j)
+                load_states(p, mine + j < p.D ? p.states : nullptr, ((chunk * p.B + i) * p.D + mine + j) * p.N, nl * 4, start[j]);
         }
-#pragma unroll
-        for (int k = 0; k < WEIGHTS; ++k) {
-            const int q = tid + k * S::THREADS, tt = q / S::NP, n = q % S::NP;
-            wb[k] = wc_[k] = 0.0f;
-            if (t0 + tt < end && n < p.N) {
-                const long long at = ((t0 + tt) * p.B + i) * p.ld_bc + n;
-                wb[k] = load_weight<T>(p.b, at);
-                wc_[k] = load_weight<T>(p.c, at);
-            }
-        }
-    };
-    const long long chunks = (p.T + STEPS - 1) / STEPS;
-    if (chunks > 0) fetch((chunks - 1) * STEPS);
-    for (long long chunk = chunks - 1; chunk >= 0; --chunk) {
-        const long long t0 = chunk * STEPS, row = ((t0 + pt) * p.B + i) * p.D;
-        const bool stored = t0 + pt < p.T && two < p.D;
-        if (t0 >= end) {                                   // behind the sequence (the whole block): nothing flows back
-            if (stored) {
-                const float zero[2] = {0.0f, 0.0f};
-                store_channels<T>(p, p.du, row, two, zero);
-                store_channels<T>(p, p.ddelta, row, two, zero);
-                if (p.dz) store_channels<T>(p, p.dz, row, two, zero);
-            }
-            for (int q = tid; q < STEPS * 2 * p.N; q += S::THREADS) {
-                const int t = q / (2 * p.N), n = q - t * 2 * p.N;
-                float *out = p.part_bc + (((long long)group * p.T + t0 + t) * p.B + i) * 2 * p.N + n;
-                if (t0 + t < p.T && relay_in_bounds(out, 4)) *out = 0.0f;
-            }
-            if (chunk > 0) fetch(t0 - STEPS);
-            continue;
-        }
-        const bool inside = t0 + pt < end;
+        if (p.tma_x || p.tma_w) tc::mbar_wait(&s.full[done % STAGES], (done / STAGES) & 1, &s.gave_up, p.err, tc::ERR_WAIT_FULL);
+        if (!p.tma_x || !p.tma_w) __syncthreads();         // everyone's plain loads
+        const int in = (int)min((long long)STEPS, end - t0);                 // steps of the chunk that are inside the sequence
+        const bool inside = pt < in;
         {
-            float2 uu, sl, gz;
-            float step[2], slope[2], e[2], gate[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                step[j] = raw[j] + bias[j];
-                slope[j] = 1.0f;
-                if (p.softplus) {
-                    const Softplus q = softplus2(pair(step[j], step[j]));
-                    float v, w;
-                    unpair(q.w, w, v);
-                    slope[j] = softplus_slope(step[j], w);
-                    unpair(q.value, step[j], v);
-                }
-                if (!inside || two + j >= p.D) step[j] = 0.0f;             // nothing decays and nothing is added
-                e[j] = dy[j];
-                gate[j] = 0.0f;
-                if (p.z) {
-                    const float q = logistic<FINE>(z[j]);
-                    e[j] *= z[j] * q;
-                    gate[j] = dy[j] * q * fmaf(z[j], 1.0f - q, 1.0f);
-                }
-                s.step[pt][pc + j] = make_float2(step[j], step[j] * u[j]);
-                s.e[pt][pc + j] = e[j];
-                dd[j] = fmaf(e[j], u[j], dd[j]);
+            float u[2], x[2], z[2], dy[2], lo, hi;
+            widen_two(&g.u[pt][pc], u);
+            widen_two(&g.delta[pt][pc], x);
+            widen_two(&g.dy[pt][pc], dy);
+            f32x2 step = add2(pair(x[0], x[1]), bias);
+            float slope[2] = {1.0f, 1.0f}, gate[2] = {0.0f, 0.0f};
+            if (p.softplus) {
+                const Softplus q = softplus2(step);
+                float w[2];
+                unpair(step, x[0], x[1]);
+                unpair(q.w, w[0], w[1]);
+                slope[0] = softplus_slope(x[0], w[0]); slope[1] = softplus_slope(x[1], w[1]);
+                step = q.value;
             }
-            uu = make_float2(u[0], u[1]); sl = make_float2(slope[0], slope[1]); gz = make_float2(gate[0], gate[1]);
-            s.u[tid] = uu; s.slope[tid] = sl; s.gate[tid] = gz;
-        }
+            if (p.z) {
+                widen_two(&g.z[pt][pc], z);
 #pragma unroll
-        for (int k = 0; k < WEIGHTS; ++k) {
-            const int q = tid + k * S::THREADS;
-            if (q < STEPS * S::NP) {
-                (&s.b[0][0])[q] = wb[k];
-                (&s.c[0][0])[q] = wc_[k];
+                for (int j = 0; j < 2; ++j) {
+                    const float q = logistic<FINE>(z[j]);
+                    gate[j] = dy[j] * q * fmaf(z[j], 1.0f - q, 1.0f);
+                    dy[j] *= z[j] * q;
+                }
+            }
+            if (!inside) {                                 // behind the end nothing decays and nothing is added
+                step = 0;
+                u[0] = u[1] = dy[0] = dy[1] = 0.0f;
+            }
+            unpair(step, lo, hi);
+            if (two >= p.D) lo = u[0] = dy[0] = 0.0f;      // channels that do not exist have no part in db and dc
+            if (two + 1 >= p.D) hi = u[1] = dy[1] = 0.0f;
+            *reinterpret_cast<float4 *>(&s.step[pt][pc]) = make_float4(lo, lo * u[0], hi, hi * u[1]);
+            *reinterpret_cast<float2 *>(&s.e[pt][pc]) = make_float2(dy[0], dy[1]);
+            dd = fma2(pair(dy[0], dy[1]), pair(u[0], u[1]), dd);
+            s.u[tid] = make_float2(u[0], u[1]); s.slope[tid] = make_float2(slope[0], slope[1]); s.gate[tid] = make_float2(gate[0], gate[1]);
+        }
+        if (p.N == S::NP) {                                // four states at a time
+            for (int e = tid; e < STEPS * S::NP / 4; e += THREADS) {
+                const int t = e / (S::NP / 4), n = e % (S::NP / 4) * 4;
+                float b[4], c[4];
+                widen_shared(p.ld_bc != p.N ? &g.bc[t * 2 * S::NP + n] : &g.bc[t * S::NP + n], b);
+                widen_shared(p.ld_bc != p.N ? &g.bc[t * 2 * S::NP + S::NP + n] : &g.bc[STEPS * S::NP + t * S::NP + n], c);
+                if (t >= in) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) b[j] = c[j] = 0.0f;
+                }
+                *reinterpret_cast<float4 *>(&s.b[t][n]) = make_float4(b[0], b[1], b[2], b[3]);
+                *reinterpret_cast<float4 *>(&s.c[t][n]) = make_float4(c[0], c[1], c[2], c[3]);
+            }
+        } else {
+            for (int e = tid; e < STEPS * S::NP; e += THREADS) {
+                const int t = e / S::NP, n = e % S::NP;
+                const bool on = t < in && n < p.N, packed = p.ld_bc != p.N;
+                s.b[t][n] = on ? to_f32(g.bc[packed ? t * 2 * p.N + n : t * p.N + n]) : 0.0f;
+                s.c[t][n] = on ? to_f32(g.bc[packed ? t * 2 * p.N + p.N + n : STEPS * p.N + t * p.N + n]) : 0.0f;
             }
         }
         __syncthreads();
+        if (done + STAGES < live_chunks) fetch(done + STAGES);               // everyone has read this chunk's rows
+        const int r0 = wt * RUN;
 #pragma unroll 1
         for (int k = 0; k < NB; ++k) {
             const int slot = NB == 1 ? 0 : k & 1;
-            if constexpr (NB > 1) { load_a(k, a1); from_slot(k, 0, G1); }
+            if constexpr (NB > 1) {
+                load_a(k);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    load_states(p, mine + j < p.D ? p.states : nullptr, ((chunk * p.B + i) * p.D + mine + j) * p.N, k * 16 + nl * 4, start[j]);
+            }
             f32x2 from[2][2];                              // the state at the start of the chunk, then of this run
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float x[4];
-                load_states(p, mine + j < p.D ? p.states : nullptr, ((chunk * p.B + i) * p.D + mine + j) * p.N, k * 16 + nl * 4, x);
-                from[j][0] = pair(x[0], x[1]); from[j][1] = pair(x[2], x[3]);
-            }
-            if (k == 0 && chunk > 0) fetch(t0 - STEPS);
+            for (int j = 0; j < 2; ++j) { from[j][0] = pair(start[j][0], start[j][1]); from[j][1] = pair(start[j][2], start[j][3]); }
             f32x2 da[RUN][2][2], h[RUN][2][2];             // decays; what is added, then the states
             {
                 f32x2 P[2][2], H[2][2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) { P[j][q] = pair(1.0f, 1.0f); H[j][q] = pair(0.0f, 0.0f); }
-#pragma unroll
                 for (int r = 0; r < RUN; ++r) {
-                    const float4 st = *reinterpret_cast<const float4 *>(&s.step[wt * RUN + r][ch]);
-                    const float4 b = *reinterpret_cast<const float4 *>(&s.b[wt * RUN + r][k * 16 + nl * 4]);
+                    const float4 st = *reinterpret_cast<const float4 *>(&s.step[r0 + r][ch]);
+                    const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const f32x2 dt = j ? pair(st.z, st.z) : pair(st.x, st.x), du = j ? pair(st.w, st.w) : pair(st.y, st.y);
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
-                            float lo, hi;
-                            unpair(mul2(dt, a1[j][q]), lo, hi);
-                            da[r][j][q] = pair(exp2_(lo), exp2_(hi));
-                            h[r][j][q] = mul2(du, q ? pair(b.z, b.w) : pair(b.x, b.y));
-                            H[j][q] = fma2(da[r][j][q], H[j][q], h[r][j][q]);
-                            P[j][q] = mul2(da[r][j][q], P[j][q]);
+                            da[r][j][q] = decay2<FINE>(mul2(dt, a[j][q]));
+                            h[r][j][q] = mul2(du, q ? b.y : b.x);
+                            H[j][q] = r ? fma2(da[r][j][q], H[j][q], h[r][j][q]) : h[r][j][q];
+                            P[j][q] = r ? mul2(da[r][j][q], P[j][q]) : da[r][j][q];
                         }
                     }
                 }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float4 v;
-                    unpair(P[j][0], v.x, v.y); unpair(P[j][1], v.z, v.w);
-                    s.decay[slot][wt][wc][j][lane] = v;
-                    unpair(H[j][0], v.x, v.y); unpair(H[j][1], v.z, v.w);
-                    s.sum[slot][wt][wc][j][lane] = v;
+                    s.decay[slot][wt][j][lane] = make_ulonglong2(P[j][0], P[j][1]);
+                    s.sum[slot][wt][j][lane] = make_ulonglong2(H[j][0], H[j][1]);
                 }
-            }
-            // what flows back through the run from a zero carry
-            {
-                f32x2 G[2][2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) G[j][0] = G[j][1] = pair(0.0f, 0.0f);
+                // what flows back through the run from a zero carry
 #pragma unroll
                 for (int r = RUN - 1; r >= 0; --r) {
-                    const float2 e = *reinterpret_cast<const float2 *>(&s.e[wt * RUN + r][ch]);
-                    const float4 c = *reinterpret_cast<const float4 *>(&s.c[wt * RUN + r][k * 16 + nl * 4]);
+                    const float2 e = *reinterpret_cast<const float2 *>(&s.e[r0 + r][ch]);
+                    const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const f32x2 ee = j ? pair(e.y, e.y) : pair(e.x, e.x);
-                        G[j][0] = mul2(da[r][j][0], fma2(ee, pair(c.x, c.y), G[j][0]));
-                        G[j][1] = mul2(da[r][j][1], fma2(ee, pair(c.z, c.w), G[j][1]));
+                        H[j][0] = mul2(da[r][j][0], r == RUN - 1 ? mul2(ee, c.x) : fma2(ee, c.x, H[j][0]));
+                        H[j][1] = mul2(da[r][j][1], r == RUN - 1 ? mul2(ee, c.y) : fma2(ee, c.y, H[j][1]));
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float4 v;
-                    unpair(G[j][0], v.x, v.y); unpair(G[j][1], v.z, v.w);
-                    s.back[slot][wt][wc][j][lane] = v;
-                }
+                for (int j = 0; j < 2; ++j) s.back[slot][wt][j][lane] = make_ulonglong2(H[j][0], H[j][1]);
             }
             __syncthreads();
+            f32x2 G[2][2];                                 // what flows back into this run
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const ulonglong2 v = s.carry[done & 1][k][j][lane];
+                G[j][0] = v.x; G[j][1] = v.y;
+            }
+#pragma unroll 2
             for (int w = 0; w < wt; ++w)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float4 pw = s.decay[slot][w][wc][j][lane], hw = s.sum[slot][w][wc][j][lane];
-                    from[j][0] = fma2(pair(pw.x, pw.y), from[j][0], pair(hw.x, hw.y));
-                    from[j][1] = fma2(pair(pw.z, pw.w), from[j][1], pair(hw.z, hw.w));
+                    const ulonglong2 d = s.decay[slot][w][j][lane], v = s.sum[slot][w][j][lane];
+                    from[j][0] = fma2(d.x, from[j][0], v.x);
+                    from[j][1] = fma2(d.y, from[j][1], v.y);
                 }
-            f32x2 G[2][2];                                 // what flows back into this run
-            for (int w = WT - 1; w >= 0; --w)
+#pragma unroll 2
+            for (int w = WT - 1; w > wt; --w)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float4 pw = s.decay[slot][w][wc][j][lane], gw = s.back[slot][w][wc][j][lane];
-                    if (w == wt) { G[j][0] = G1[j][0]; G[j][1] = G1[j][1]; }
-                    G1[j][0] = fma2(pair(pw.x, pw.y), G1[j][0], pair(gw.x, gw.y));
-                    G1[j][1] = fma2(pair(pw.z, pw.w), G1[j][1], pair(gw.z, gw.w));
+                    const ulonglong2 d = s.decay[slot][w][j][lane], v = s.back[slot][w][j][lane];
+                    G[j][0] = fma2(d.x, G[j][0], v.x);
+                    G[j][1] = fma2(d.y, G[j][1], v.y);
                 }
-            if constexpr (NB > 1) { to_slot(k, 0, G1); from_slot(k, 2, dA1); }
 #pragma unroll
             for (int r = 0; r < RUN; ++r)
 #pragma unroll
@@ -268,40 +310,43 @@ __global__ void __launch_bounds__(32 * WT * columns_of(NB), 1) selective_scan_gr
                 float y[2 * RUN], out[RUN / 2];
 #pragma unroll
                 for (int r = 0; r < RUN; ++r) {
-                    const float4 c = *reinterpret_cast<const float4 *>(&s.c[wt * RUN + r][k * 16 + nl * 4]);
+                    const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) y[2 * r + j] = sum2(fma2(pair(c.x, c.y), h[r][j][0], mul2(pair(c.z, c.w), h[r][j][1])));
+                    for (int j = 0; j < 2; ++j) y[2 * r + j] = sum2(fma2(c.x, h[r][j][0], mul2(c.y, h[r][j][1])));
                 }
                 reduce_lanes<2 * RUN, 1, 4>(y, lane, out);
 #pragma unroll
                 for (int j = 0; j < RUN / 2; ++j) {        // value 4 j + nl: step 2 j + (nl >> 1), channel nl & 1
-                    float *at = &s.plain[wt * RUN + 2 * j + (nl >> 1)][ch + (nl & 1)];
+                    float *at = &s.plain[r0 + 2 * j + (nl >> 1)][ch + (nl & 1)];
                     *at = k ? *at + out[j] : out[j];
                 }
             }
+            if constexpr (NB > 1) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) { const ulonglong2 v = s.da[k][j][tid]; dA[j][0] = v.x; dA[j][1] = v.y; }
+            }
 #pragma unroll
             for (int r = RUN - 1; r >= 0; --r) {
-                const float4 st = *reinterpret_cast<const float4 *>(&s.step[wt * RUN + r][ch]);
-                const float2 e = *reinterpret_cast<const float2 *>(&s.e[wt * RUN + r][ch]);
-                const float4 b = *reinterpret_cast<const float4 *>(&s.b[wt * RUN + r][k * 16 + nl * 4]);
-                const float4 c = *reinterpret_cast<const float4 *>(&s.c[wt * RUN + r][k * 16 + nl * 4]);
+                const float4 st = *reinterpret_cast<const float4 *>(&s.step[r0 + r][ch]);
+                const float2 e = *reinterpret_cast<const float2 *>(&s.e[r0 + r][ch]);
+                const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
+                const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
                 f32x2 db[2], dc[2];
                 float v[4];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const f32x2 ee = j ? pair(e.y, e.y) : pair(e.x, e.x), dt = j ? pair(st.z, st.z) : pair(st.x, st.x);
                     const f32x2 du = j ? pair(st.w, st.w) : pair(st.y, st.y);
-                    f32x2 along = pair(0.0f, 0.0f), kept = pair(0.0f, 0.0f);
+                    f32x2 along, kept;
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
-                        const f32x2 cc = q ? pair(c.z, c.w) : pair(c.x, c.y), bb = q ? pair(b.z, b.w) : pair(b.x, b.y);
-                        const f32x2 g = fma2(ee, cc, G[j][q]);
-                        G[j][q] = mul2(da[r][j][q], g);
+                        const f32x2 gq = fma2(ee, q ? c.y : c.x, G[j][q]), bb = q ? b.y : b.x;
+                        G[j][q] = mul2(da[r][j][q], gq);
                         const f32x2 left = mul2(G[j][q], r ? h[r ? r - 1 : 0][j][q] : from[j][q]);
-                        dA1[j][q] = fma2(left, dt, dA1[j][q]);
-                        kept = fma2(left, a1[j][q], kept);
-                        along = fma2(g, bb, along);
-                        db[q] = j ? fma2(g, du, db[q]) : mul2(g, du);
+                        dA[j][q] = fma2(left, dt, dA[j][q]);
+                        kept = q ? fma2(left, a[j][q], kept) : mul2(left, a[j][q]);
+                        along = q ? fma2(gq, bb, along) : mul2(gq, bb);
+                        db[q] = j ? fma2(gq, du, db[q]) : mul2(gq, du);
                         dc[q] = j ? fma2(ee, h[r][j][q], dc[q]) : mul2(ee, h[r][j][q]);
                     }
                     v[j] = sum2(along);
@@ -309,76 +354,94 @@ __global__ void __launch_bounds__(32 * WT * columns_of(NB), 1) selective_scan_gr
                 }
                 float one[1], w[8];
                 reduce_lanes<4, 1, 4>(v, lane, one);
-                float *at = nl < 2 ? &s.along[wt * RUN + r][ch + nl] : &s.kept[wt * RUN + r][ch + nl - 2];
+                float *at = nl < 2 ? &s.along[r0 + r][ch + nl] : &s.kept[r0 + r][ch + nl - 2];
                 *at = k ? *at + one[0] : one[0];
                 unpair(db[0], w[0], w[1]); unpair(db[1], w[2], w[3]);
                 unpair(dc[0], w[4], w[5]); unpair(dc[1], w[6], w[7]);
                 reduce_lanes<8, 4, 8>(w, lane, one);
-                s.dbc[wc][wt * RUN + r][(cl < 4 ? 0 : S::NP) + k * 16 + nl * 4 + (cl & 3)] = one[0];
+                s.dbc[r0 + r][(cl < 4 ? 0 : S::NP) + k * 16 + nl * 4 + (cl & 3)] = one[0];
             }
-            if constexpr (NB > 1) to_slot(k, 2, dA1);
-        }
-        __syncthreads();
-        if (stored) {
-            const float2 uu = s.u[tid], sl = s.slope[tid], gz = s.gate[tid];
-            float du[2], ddelta[2], dz[2];
+            if (wt == 0) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float along = s.along[pt][pc + j], uj = j ? uu.y : uu.x;
-                du[j] = fmaf(s.e[pt][pc + j], skip[j], along * s.step[pt][pc + j].x);
-                ddelta[j] = fmaf(s.kept[pt][pc + j], 0.693147181f, along * uj) * (j ? sl.y : sl.x);
-                dz[j] = 0.0f;
-                if (p.z) dz[j] = (j ? gz.y : gz.x) * fmaf(skip[j], uj, s.plain[pt][pc + j]);
-                if (!inside) du[j] = ddelta[j] = dz[j] = 0.0f;
-                dbias[j] += ddelta[j];
+                for (int j = 0; j < 2; ++j) s.carry[(done + 1) & 1][k][j][lane] = make_ulonglong2(G[j][0], G[j][1]);
             }
-            store_channels<T>(p, p.du, row, two, du);
-            store_channels<T>(p, p.ddelta, row, two, ddelta);
-            if (p.dz) store_channels<T>(p, p.dz, row, two, dz);
-        }
-        for (int q = tid; q < STEPS * 2 * p.N; q += S::THREADS) {
-            const int t = q / (2 * p.N), n = q - t * 2 * p.N, at = n < p.N ? n : S::NP + n - p.N;
-            float *out = p.part_bc + (((long long)group * p.T + t0 + t) * p.B + i) * 2 * p.N + n;
-            if (t0 + t < p.T && relay_in_bounds(out, 4)) {
-                float x = s.dbc[0][t][at];
+            if constexpr (NB > 1) {
 #pragma unroll
-                for (int w = 1; w < WC; ++w) x += s.dbc[w][t][at];
-                __stcs(out, x);
+                for (int j = 0; j < 2; ++j) s.da[k][j][tid] = make_ulonglong2(dA[j][0], dA[j][1]);
             }
         }
         __syncthreads();
+        if (t0 + pt < p.T && two < p.D) {
+            const float2 u = s.u[tid], sl = s.slope[tid], gz = s.gate[tid], e = *reinterpret_cast<const float2 *>(&s.e[pt][pc]);
+            const float4 st = *reinterpret_cast<const float4 *>(&s.step[pt][pc]);
+            const float2 al = *reinterpret_cast<const float2 *>(&s.along[pt][pc]), ke = *reinterpret_cast<const float2 *>(&s.kept[pt][pc]);
+            const f32x2 along = pair(al.x, al.y), uu = pair(u.x, u.y);
+            f32x2 du = fma2(pair(e.x, e.y), skip, mul2(along, pair(st.x, st.z)));
+            f32x2 ddelta = mul2(fma2(pair(ke.x, ke.y), pair(0.693147181f, 0.693147181f), mul2(along, uu)), pair(sl.x, sl.y));
+            if (!inside) du = ddelta = 0;
+            dbias = add2(dbias, ddelta);
+            float x[2];
+            const long long row = ((t0 + pt) * p.B + i) * p.D;
+            unpair(du, x[0], x[1]);
+            store_channels<T>(p, p.du, row, two, x);
+            unpair(ddelta, x[0], x[1]);
+            store_channels<T>(p, p.ddelta, row, two, x);
+            if (p.dz) {
+                const float2 pl = *reinterpret_cast<const float2 *>(&s.plain[pt][pc]);
+                unpair(mul2(pair(gz.x, gz.y), fma2(skip, uu, pair(pl.x, pl.y))), x[0], x[1]);
+                if (!inside) x[0] = x[1] = 0.0f;
+                store_channels<T>(p, p.dz, row, two, x);
+            }
+        }
+        if (p.N == S::NP) {
+            for (int q = tid; q < STEPS * 2 * S::NP / 4; q += THREADS) {
+                const int t = q / (S::NP / 2), n = q % (S::NP / 2) * 4;
+                float *out = p.part_bc + (((long long)group * p.T + t0 + t) * p.B + i) * (2 * S::NP) + n;
+                if (t0 + t < p.T && relay_in_bounds(out, 16)) __stcs((float4 *)out, *reinterpret_cast<const float4 *>(&s.dbc[t][n]));
+            }
+        } else {
+            for (int q = tid; q < STEPS * 2 * p.N; q += THREADS) {
+                const int t = q / (2 * p.N), n = q - t * 2 * p.N;
+                float *out = p.part_bc + (((long long)group * p.T + t0 + t) * p.B + i) * 2 * p.N + n;
+                if (t0 + t < p.T && relay_in_bounds(out, 4)) __stcs(out, s.dbc[t][n < p.N ? n : S::NP + n - p.N]);
+            }
+        }
     }
     // sums over the runs (da) and over the steps of a chunk (dd, ddelta_bias)
 #pragma unroll 1
     for (int k = 0; k < NB; ++k) {
-        if constexpr (NB > 1) { from_slot(k, 0, G1); from_slot(k, 2, dA1); }
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            float4 v;
-            unpair(dA1[j][0], v.x, v.y); unpair(dA1[j][1], v.z, v.w);
-            s.sum[0][wt][wc][j][lane] = v;
+            if constexpr (NB > 1) s.sum[0][wt][j][lane] = s.da[k][j][tid];
+            else s.sum[0][wt][j][lane] = make_ulonglong2(dA[j][0], dA[j][1]);
         }
         __syncthreads();
         if (wt != 0) continue;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             if (mine + j >= p.D) continue;
-            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f}, g[4];
+            f32x2 x = 0, y = 0;
             for (int w = 0; w < WT; ++w) {
-                const float4 v = s.sum[0][w][wc][j][lane];
-                x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w;
+                const ulonglong2 v = s.sum[0][w][j][lane];
+                x = add2(x, v.x); y = add2(y, v.y);
             }
-            store_states(p, p.part_a, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, x);
-            unpair(G1[j][0], g[0], g[1]); unpair(G1[j][1], g[2], g[3]);
-            store_states(p, p.dh0, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, g);
+            float q[4];
+            unpair(x, q[0], q[1]); unpair(y, q[2], q[3]);
+            store_states(p, p.part_a, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, q);
+            const ulonglong2 v = s.carry[live_chunks & 1][k][j][lane];
+            unpair(v.x, q[0], q[1]); unpair(v.y, q[2], q[3]);
+            store_states(p, p.dh0, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, q);
         }
     }
     __syncthreads();
-    s.step[pt][pc] = make_float2(dd[0], dbias[0]);
-    s.step[pt][pc + 1] = make_float2(dd[1], dbias[1]);
+    {
+        float x[2], y[2];
+        unpair(dd, x[0], x[1]); unpair(dbias, y[0], y[1]);
+        *reinterpret_cast<float4 *>(&s.step[pt][pc]) = make_float4(x[0], y[0], x[1], y[1]);
+    }
     __syncthreads();
-    if (tid < S::CHANNELS && c0 + tid < p.D) {
+    if (tid < CHANNELS && c0 + tid < p.D) {
         float x = 0.0f, y = 0.0f;
         for (int t = 0; t < STEPS; ++t) { x += s.step[t][tid].x; y += s.step[t][tid].y; }
         const long long at = i * p.D + c0 + tid;
@@ -407,17 +470,12 @@ __global__ void __launch_bounds__(256) join_weights_kernel(const float *part, lo
 }
 
 // ---- workspace: partial sums of db and dc, of da, dd and ddelta_bias ----------------------------------------------------
-int blocks_of_states(int64_t N) { return N <= 16 ? 1 : N <= 32 ? 2 : 4; }
-int64_t groups_of(int64_t D, int64_t N)
-{
-    const int64_t channels = 16 * columns_of(blocks_of_states(N));
-    return (D + channels - 1) / channels;
-}
+int64_t groups_of(int64_t D) { return (D + CHANNELS - 1) / CHANNELS; }
 struct Parts { size_t bc, a, d, bias, bytes; };
 Parts parts_of(const Sizes &s, int64_t N)
 {
     Parts q{};
-    q.a = align_up((size_t)groups_of(s.D, N) * s.T * s.B * 2 * N * sizeof(float), 256);
+    q.a = align_up((size_t)groups_of(s.D) * s.T * s.B * 2 * N * sizeof(float), 256);
     q.d = q.a + align_up((size_t)s.B * s.D * N * sizeof(float), 256);
     q.bias = q.d + align_up((size_t)s.B * s.D * sizeof(float), 256);
     q.bytes = q.bias + align_up((size_t)s.B * s.D * sizeof(float), 256);
@@ -425,13 +483,16 @@ Parts parts_of(const Sizes &s, int64_t N)
 }
 
 template <typename T, int NB>
-relay_status_t launch_chunks(const Args &p, cudaStream_t st)
+relay_status_t launch_chunks(Args p, cudaStream_t st)
 {
-    using S = Tile<NB>;
     const long long blocks = p.B * p.groups;
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "selective_scan_grad: %lld x %lld channels", p.B, p.D);
-    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_grad_kernel<T, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(S)));
-    RELAY_CUDA(launch_pdl(selective_scan_grad_kernel<T, NB>, dim3((unsigned)blocks), dim3(S::THREADS), sizeof(S), st, p));
+    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
+    Maps maps;
+    RELAY_TRY(make_maps(&p, &maps, sizeof(T) == 4, CHANNELS, STEPS));
+    const size_t bytes = sizeof(Tile<T, NB>) + 128;
+    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_grad_kernel<T, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    RELAY_CUDA(launch_pdl(selective_scan_grad_kernel<T, NB>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, p, maps));
     return check_launch("selective_scan_grad");
 }
 template <typename T>
@@ -521,7 +582,7 @@ extern "C" relay_status_t relay_selective_scan_grad(const relay_tensor_t *u, con
     p.dh_final = dh_final ? (const float *)dh_final->data : nullptr;
     p.du = du->data; p.ddelta = ddelta->data; p.dz = dz ? dz->data : nullptr;
     p.dh0 = dh0 ? (float *)dh0->data : nullptr;
-    p.groups = (int)groups_of(s.D, N);
+    p.groups = (int)groups_of(s.D);
     char *w = (char *)ws;
     p.part_bc = (float *)w;
     p.part_a = (float *)(w + q.a);
