@@ -1,7 +1,7 @@
 // Short causal convolution of a sequence, one filter of K taps per channel, and its gradient group:
 //   s_t = b + sum_k w[k] x_{t-K+1+k},  y_t = act(s_t)
 // HBM-bound: the forward group reads x and writes y once, the gradient reads x and dy and writes dx once; K multiply-adds an element.
-// A thread owns V consecutive channels (16 bytes of a row where rows allow it) and a span of steps; the K - 1 inputs before the
+// A thread owns V consecutive channels and a span of steps; the K - 1 inputs before the
 // current one stay in its registers, and at the start of a span they are read again (K - 1 rows in S).  The gradient walks a span
 // forwards and K - 1 steps beyond it: the partial of an input needs those of the K sums that it entered.
 #include <algorithm>
@@ -16,7 +16,7 @@ using namespace seq;
 constexpr int kMaxTaps = 8;
 constexpr int kThreads = 256;
 constexpr int kRows = 8;           // spans of a gradient block: their partial sums of dw and db are joined on the chip
-constexpr int kGradV = 4;          // most channels of a gradient thread: filter, window, slopes and sums of each stay in registers
+constexpr int kGradV = 2;          // most channels of a gradient thread: filter, window, slopes and sums of each stay in registers
 
 struct Args {
     const void *x;                 // [T][C]
@@ -39,17 +39,22 @@ __device__ __forceinline__ long long end_of(const Args &p, long long c)
     const long long n = relay_in_bounds(at, 4) ? *at : 0;
     return n < 0 ? 0 : n > p.T ? p.T : n;
 }
-// input of step t, which may lie ahead of the first one; zero behind the sequence's end
+// Input of step t, which may lie ahead of the first one; zero behind the sequence's end.  As stored: a load that is widened under its
+// condition is waited for there, and what bounds these kernels is how many loads are on their way.
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> fetch_input(const Args &p, long long t, long long c, long long end)
+{
+    const bool ahead = t < 0;
+    const T *from = ahead ? (const T *)p.before : (const T *)p.x;
+    const long long at = (ahead ? t + p.K - 1 : t) * p.C + c;
+    Raw<T, V> r{};
+    if (ahead ? from != nullptr && t >= 1 - p.K : t < end) r = load_raw<T, V>(from, at);
+    return r;
+}
 template <typename T, int V>
 __device__ __forceinline__ void load_input(const Args &p, long long t, long long c, long long end, float (&x)[V])
 {
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = 0.0f;
-    if (t >= 0) {
-        if (t < end) load<T, V>(p.x, t * p.C + c, x);
-    } else if (p.before != nullptr && t >= 1 - p.K) {
-        load<T, V>(p.before, (t + p.K - 1) * p.C + c, x);
-    }
+    widen(fetch_input<T, V>(p, t, c, end), x, T());
 }
 // the filter, right-aligned to KP taps (the first KP - K do not exist), and the bias
 template <int V, int KP>
@@ -59,7 +64,8 @@ __device__ __forceinline__ void load_filter(const Args &p, long long d, float (&
     for (int k = 0; k < KP; ++k) {
 #pragma unroll
         for (int i = 0; i < V; ++i) w[k][i] = 0.0f;
-        if (k >= KP - p.K) load_operand<V>(p.w, p.w_bf16, (k - (KP - p.K)) * p.D + d, w[k]);
+        const int first = KP < kMaxTaps ? 0 : KP - p.K;
+        if (k >= first) load_operand<V>(p.w, p.w_bf16, (k - first) * p.D + d, w[k]);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) b[i] = 0.0f;
@@ -70,13 +76,13 @@ template <typename T, int V, int KP>
 __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const Args p)
 {
     constexpr bool FINE = sizeof(T) == 4;
-    constexpr int U = V == 8 ? 4 : 8;                      // rows in flight
+    constexpr int U = 4;                                   // rows on their way
     pdl_wait();
     const long long span = blockIdx.x / p.blocks_c;
     const long long c = ((blockIdx.x - span * p.blocks_c) * kThreads + threadIdx.x) * V;
     if (c >= p.C) return;
     const long long end = end_of(p, c), t0 = span * p.S, t1 = min(t0 + p.S, p.T);
-    const int first = KP - p.K;
+    const int first = KP < kMaxTaps ? 0 : KP - p.K;        // the taps before it do not exist
     float w[KP][V], b[V], x[KP - 1 + U][V];
     load_filter<V, KP>(p, c % p.D, w, b);
     // the state for the next call: the last K - 1 inputs of the sequence
@@ -89,30 +95,39 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const Args p)
     }
 #pragma unroll
     for (int j = 0; j < KP - 1; ++j) load_input<T, V>(p, t0 - (KP - 1) + j, c, end, x[j]);
-    for (long long t = t0; t < t1; t += U) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_input<T, V>(p, t + u, c, t + u < t1 ? end : 0, x[KP - 1 + u]);
+    const T *row = (const T *)p.x + t0 * p.C + c;
+    T *to = (T *)p.y + t0 * p.C + c;
+    const int steps = (int)(t1 - t0), inside = (int)min(max(end - t0, 0ll), (long long)steps);
+    Raw<T, V> raw[U];
+    auto fetch = [&](int n) {                              // rows n .. n + U - 1 of the span
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (t + u >= t1) break;
+            raw[u] = Raw<T, V>{};
+            if (n + u < inside) raw[u] = load_raw<T, V>(row, (n + u) * p.C);
+        }
+    };
+    fetch(0);
+    for (int n = 0; n < steps; n += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) widen(raw[u], x[KP - 1 + u], T());
+        fetch(n + U);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
             float y[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = b[i];
 #pragma unroll
             for (int k = 0; k < KP; ++k)
-                if (k >= first) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) y[i] = fmaf(w[k][i], x[u + k][i], y[i]);
-                }
+                if (k >= first) muladd(w[k], x[u + k], y, y);
             if (p.silu) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] *= logistic<FINE>(y[i]);
             }
-            if (t + u >= end) {
+            if (n + u >= inside) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = 0.0f;
             }
-            store<T, V>(p.y, (t + u) * p.C + c, y);
+            if (n + u < steps) store<T, V>(to, (n + u) * p.C, y);
         }
 #pragma unroll
         for (int j = 0; j < KP - 1; ++j)
@@ -132,7 +147,7 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
     const long long c = ((blockIdx.x - part * p.blocks_c) * 32 + threadIdx.x) * V;
     const bool live = c < p.C;
     const long long end = live ? end_of(p, c) : 0, t0 = (part * kRows + threadIdx.y) * p.S, t1 = min(t0 + p.S, p.T);
-    const int first = KP - p.K;
+    const int first = KP < kMaxTaps ? 0 : KP - p.K;        // the taps before it do not exist
     float w[KP][V], b[V], x[KP][V], g[KP][V], dw[KP][V], db[V];   // x[k]: the input under tap k;  g[k]: the slope k steps back
 #pragma unroll
     for (int k = 0; k < KP; ++k)
@@ -144,60 +159,77 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
         load_filter<V, KP>(p, c % p.D, w, b);
 #pragma unroll
         for (int j = 1; j < KP; ++j) load_input<T, V>(p, t0 - KP + j, c, end, x[j]);
-#pragma unroll 2
-        for (long long t = t0; t < t1 + KP - 1; ++t) {
+        // U rows of x and dy on their way while U are worked on
+        constexpr int U = 4;
+        const long long base = t0 * p.C + c;
+        const int steps = (int)(t1 - t0), inside = (int)min(max(end - t0, 0ll), (long long)(steps + KP - 1));
+        const int after = p.dafter != nullptr ? (int)min(end - (p.K - 1) - t0, 1ll << 20) : 1 << 20;     // dafter's first step
+        const int from = t0 == 0 ? 1 - p.K : 0;            // the first step whose partial this span gives
+        Raw<T, V> rx[U], rg[U];
+        auto fetch = [&](int n) {
 #pragma unroll
-            for (int k = 0; k + 1 < KP; ++k)
+            for (int u = 0; u < U; ++u) {
+                rx[u] = Raw<T, V>{};
+                rg[u] = Raw<T, V>{};
+                if (n + u < inside) rx[u] = load_raw<T, V>(p.x, base + (n + u) * p.C);
+                if (n + u < inside) rg[u] = load_raw<T, V>(p.dy, base + (n + u) * p.C);
+            }
+        };
+        fetch(0);
+        for (int n = 0; n < steps + KP - 1; n += U) {
+            float nx[U][V], ng[U][V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) { x[k][i] = x[k + 1][i]; g[KP - 1 - k][i] = g[KP - 2 - k][i]; }
-            load_input<T, V>(p, t, c, end, x[KP - 1]);
+            for (int u = 0; u < U; ++u) { widen(rx[u], nx[u], T()); widen(rg[u], ng[u], T()); }
+            fetch(n + U);
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[0][i] = 0.0f;
-            if (t < end) {
-                load<T, V>(p.dy, t * p.C + c, g[0]);
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int k = 0; k + 1 < KP; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) { x[k][i] = x[k + 1][i]; g[KP - 1 - k][i] = g[KP - 2 - k][i]; }
+#pragma unroll
+                for (int i = 0; i < V; ++i) { x[KP - 1][i] = nx[u][i]; g[0][i] = ng[u][i]; }
                 if (p.silu) {
+                    float s[V], q[V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        float s = b[i];
+                    for (int i = 0; i < V; ++i) s[i] = b[i];
 #pragma unroll
-                        for (int k = 0; k < KP; ++k) if (k >= first) s = fmaf(w[k][i], x[k][i], s);
-                        const float q = logistic<FINE>(s);
-                        g[0][i] *= q * fmaf(s, 1.0f - q, 1.0f);
-                    }
+                    for (int k = 0; k < KP; ++k) if (k >= first) muladd(w[k], x[k], s, s);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) { q[i] = logistic<FINE>(s[i]); s[i] *= 1.0f - q[i]; }
+                    muladd(s, q, q, s);                    // the slope, q (1 + s (1 - q))
+                    mul(g[0], s, g[0]);
                 }
-                if (t < t1) {
+                if (n + u >= inside) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) g[0][i] = 0.0f;
+                }
+                if (n + u < steps) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) db[i] += g[0][i];
 #pragma unroll
                     for (int k = 0; k < KP; ++k)
-                        if (k >= first) {
-#pragma unroll
-                            for (int i = 0; i < V; ++i) dw[k][i] = fmaf(g[0][i], x[k][i], dw[k][i]);
-                        }
+                        if (k >= first) muladd(g[0], x[k], dw[k], dw[k]);
                 }
-            }
-            const long long at = t - (KP - 1);             // the step whose K sums are complete
-            if (at < (t0 == 0 ? 1 - p.K : t0)) continue;
-            float dx[V];
+                const int at = n + u - (KP - 1);           // the step whose K sums are complete
+                if (at < from || at >= steps) continue;
+                float dx[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) dx[i] = 0.0f;
-            if (at < end) {
+                for (int i = 0; i < V; ++i) dx[i] = 0.0f;
+                if (at < inside) {
 #pragma unroll
-                for (int k = 0; k < KP; ++k)
-                    if (k >= first) {
+                    for (int k = 0; k < KP; ++k)
+                        if (k >= first) muladd(w[k], g[k], dx, dx);
+                    if (at >= after) {
+                        float q[V];
+                        load<T, V>(p.dafter, (at - after) * p.C + c, q);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) dx[i] = fmaf(w[k][i], g[k][i], dx[i]);
+                        for (int i = 0; i < V; ++i) dx[i] += q[i];
                     }
-                const long long j = at - (end - (p.K - 1));
-                if (p.dafter != nullptr && j >= 0) {
-                    float q[V];
-                    load<T, V>(p.dafter, j * p.C + c, q);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) dx[i] += q[i];
                 }
+                if (at >= 0) store<T, V>(p.dx, base + at * p.C, dx);
+                else if (p.dbefore != nullptr) store<T, V>(p.dbefore, (at + p.K - 1) * p.C + c, dx);
             }
-            if (at >= 0) store<T, V>(p.dx, at * p.C + c, dx);
-            else if (p.dbefore != nullptr) store<T, V>(p.dbefore, (at + p.K - 1) * p.C + c, dx);
         }
     }
     if (p.part == nullptr) return;
@@ -266,25 +298,32 @@ relay_status_t launch_gradient(Args p, cudaStream_t st)
     RELAY_CUDA(launch_pdl(causal_conv_grad_kernel<T, V, KP>, dim3((unsigned)blocks), dim3(32, kRows), 0, st, p));
     return check_launch("causal_conv_grad");
 }
-// taps: kernels for 2, 4 and 8; fewer are right-aligned in them.  Channels of a thread: as many as divide the rows into whole
-// aligned accesses.
+// taps: kernels for 2, 3 and 4; all others are right-aligned in one for 8.  Channels of a thread: as many as divide the rows into
+// whole aligned accesses of 8 bytes (16 take so many registers that an SM has half the warps).
 template <typename T, int V>
 relay_status_t forward_taps(const Args &p, cudaStream_t st)
 {
-    if (p.K <= 2) return launch_forward<T, V, 2>(p, st);
-    return p.K <= 4 ? launch_forward<T, V, 4>(p, st) : launch_forward<T, V, 8>(p, st);
+    switch (p.K) {
+    case 2: return launch_forward<T, V, 2>(p, st);
+    case 3: return launch_forward<T, V, 3>(p, st);
+    case 4: return launch_forward<T, V, 4>(p, st);
+    default: return launch_forward<T, V, kMaxTaps>(p, st);
+    }
 }
 template <typename T, int V>
 relay_status_t gradient_taps(const Args &p, cudaStream_t st)
 {
-    if (p.K <= 2) return launch_gradient<T, V, 2>(p, st);
-    return p.K <= 4 ? launch_gradient<T, V, 4>(p, st) : launch_gradient<T, V, 8>(p, st);
+    switch (p.K) {
+    case 2: return launch_gradient<T, V, 2>(p, st);
+    case 3: return launch_gradient<T, V, 3>(p, st);
+    case 4: return launch_gradient<T, V, 4>(p, st);
+    default: return launch_gradient<T, V, kMaxTaps>(p, st);
+    }
 }
 template <typename T>
 relay_status_t forward_channels(const Args &p, cudaStream_t st)
 {
-    constexpr int V = 16 / sizeof(T);
-    if (p.D % V == 0) return forward_taps<T, V>(p, st);
+    if (p.D % 4 == 0) return forward_taps<T, 4>(p, st);
     return p.D % 2 == 0 ? forward_taps<T, 2>(p, st) : forward_taps<T, 1>(p, st);
 }
 template <typename T>

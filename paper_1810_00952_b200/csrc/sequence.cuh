@@ -96,6 +96,30 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm(
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ f32x2 neg2(f32x2 a) { return a ^ 0x8000000080000000ull; }
 __device__ __forceinline__ float sum2(f32x2 a) { float x, y; unpair(a, x, y); return x + y; }
+// r = a b + c and r = a b of V values, in pairs where V is even
+template <int V>
+__device__ __forceinline__ void muladd(const float (&a)[V], const float (&b)[V], const float (&c)[V], float (&r)[V])
+{
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) unpair(fma2(pair(a[i], a[i + 1]), pair(b[i], b[i + 1]), pair(c[i], c[i + 1])), r[i], r[i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = fmaf(a[i], b[i], c[i]);
+    }
+}
+template <int V>
+__device__ __forceinline__ void mul(const float (&a)[V], const float (&b)[V], float (&r)[V])
+{
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) unpair(mul2(pair(a[i], a[i + 1]), pair(b[i], b[i + 1])), r[i], r[i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = a[i] * b[i];
+    }
+}
+__device__ __forceinline__ float rcp_(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float exp2_(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // ---- activations ---------------------------------------------------------------------------------------------
@@ -105,7 +129,7 @@ template <bool FINE>
 __device__ __forceinline__ float logistic(float x)
 {
     if constexpr (FINE) return 1.0f / (1.0f + expf(-x));
-    else return __fdividef(1.0f, 1.0f + __expf(-x));      // 1 / inf = 0 below -88, as it should be
+    else return rcp_(1.0f + exp2_(-1.44269504f * x));     // 1 / inf = 0 far below zero, as it should be
 }
 
 // Sums of the columns of partial sums (rows,cols), rows `ld` entries apart, in a fixed order: the first n0 columns to out0, the others
