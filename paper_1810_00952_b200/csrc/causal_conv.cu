@@ -51,6 +51,11 @@ __device__ __forceinline__ Raw<T, V> fetch_input(const Args &p, long long t, lon
     if (ahead ? from != nullptr && t >= 1 - p.K : t < end) r = load_raw<T, V>(from, at);
     return r;
 }
+// rows of a span, by 32-bit offsets from its first one (the spans are cut so that these fit)
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> load_row(const T *first, unsigned off) { return load_raw<T, V>((const char *)first + off, 0); }
+template <typename T, int V>
+__device__ __forceinline__ void store_row(T *first, unsigned off, const float (&x)[V]) { store<T, V>((char *)first + off, 0, x); }
 template <typename T, int V>
 __device__ __forceinline__ void load_input(const Args &p, long long t, long long c, long long end, float (&x)[V])
 {
@@ -98,12 +103,13 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const Args p)
     const T *row = (const T *)p.x + t0 * p.C + c;
     T *to = (T *)p.y + t0 * p.C + c;
     const int steps = (int)(t1 - t0), inside = (int)min(max(end - t0, 0ll), (long long)steps);
+    const unsigned bytes = (unsigned)(p.C * sizeof(T));    // of a row
     Raw<T, V> raw[U];
     auto fetch = [&](int n) {                              // rows n .. n + U - 1 of the span
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             raw[u] = Raw<T, V>{};
-            if (n + u < inside) raw[u] = load_raw<T, V>(row, (n + u) * p.C);
+            if (n + u < inside) raw[u] = load_row<T, V>(row, (unsigned)(n + u) * bytes);
         }
     };
     fetch(0);
@@ -127,7 +133,7 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const Args p)
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = 0.0f;
             }
-            if (n + u < steps) store<T, V>(to, (n + u) * p.C, y);
+            if (n + u < steps) store_row<T, V>(to, (unsigned)(n + u) * bytes, y);
         }
 #pragma unroll
         for (int j = 0; j < KP - 1; ++j)
@@ -161,7 +167,9 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
         for (int j = 1; j < KP; ++j) load_input<T, V>(p, t0 - KP + j, c, end, x[j]);
         // U rows of x and dy on their way while U are worked on
         constexpr int U = 4;
-        const long long base = t0 * p.C + c;
+        const T *px = (const T *)p.x + t0 * p.C + c, *pg = (const T *)p.dy + t0 * p.C + c;
+        T *to = (T *)p.dx + t0 * p.C + c;
+        const unsigned bytes = (unsigned)(p.C * sizeof(T));                  // of a row
         const int steps = (int)(t1 - t0), inside = (int)min(max(end - t0, 0ll), (long long)(steps + KP - 1));
         const int after = p.dafter != nullptr ? (int)min(end - (p.K - 1) - t0, 1ll << 20) : 1 << 20;     // dafter's first step
         const int from = t0 == 0 ? 1 - p.K : 0;            // the first step whose partial this span gives
@@ -171,8 +179,8 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
             for (int u = 0; u < U; ++u) {
                 rx[u] = Raw<T, V>{};
                 rg[u] = Raw<T, V>{};
-                if (n + u < inside) rx[u] = load_raw<T, V>(p.x, base + (n + u) * p.C);
-                if (n + u < inside) rg[u] = load_raw<T, V>(p.dy, base + (n + u) * p.C);
+                if (n + u < inside) rx[u] = load_row<T, V>(px, (unsigned)(n + u) * bytes);
+                if (n + u < inside) rg[u] = load_row<T, V>(pg, (unsigned)(n + u) * bytes);
             }
         };
         fetch(0);
@@ -227,7 +235,7 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
                         for (int i = 0; i < V; ++i) dx[i] += q[i];
                     }
                 }
-                if (at >= 0) store<T, V>(p.dx, base + at * p.C, dx);
+                if (at >= 0) store_row<T, V>(to, (unsigned)at * bytes, dx);
                 else if (p.dbefore != nullptr) store<T, V>(p.dbefore, (at + p.K - 1) * p.C + c, dx);
             }
         }
@@ -258,18 +266,21 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
 // ---- launches ------------------------------------------------------------------------------------------------
 constexpr long long kSms = 148;
 
-// Steps of a span: the longest that still give every SM its threads, so that as few rows as possible are read twice.
-int forward_span(long long T, long long C, int V)
+// Steps of a span: the longest that still give every SM its threads, so that as few rows as possible are read twice; and no longer than
+// 32-bit offsets reach (S + 8 rows of 4 bytes a channel at most).
+int span_of(long long C, long long enough, long long per_span, long long T, int rows)
 {
     int S = 64;
-    while (S > 8 && (C / V) * ((T + S - 1) / S) < kSms * 1024) S /= 2;
+    while (S > 8 && per_span * ((T + (long long)S * rows - 1) / ((long long)S * rows)) < enough) S /= 2;
+    while (S > 1 && (S + 8) * C >= 1ll << 30) S /= 2;
     return S;
 }
-int gradient_span(long long T, long long C, int V)
+int forward_span(long long T, long long C, int V) { return span_of(C, kSms * 1024, C / V, T, 1); }
+int gradient_span(long long T, long long C, int V) { return span_of(C, kSms * 4, (C / V + 31) / 32, T, kRows); }
+relay_status_t check_offsets(const Args &p)
 {
-    int S = 64;
-    while (S > 8 && ((C / V + 31) / 32) * ((T + (long long)S * kRows - 1) / ((long long)S * kRows)) < kSms * 4) S /= 2;
-    return S;
+    if ((p.S + 8) * p.C >= 1ll << 30) return fail(RELAY_ERR_UNSUPPORTED, "causal_conv: rows of %lld channels", p.C);
+    return RELAY_OK;
 }
 int channels_of_gradient(long long D) { return D % kGradV == 0 ? kGradV : 1; }
 long long gradient_parts(long long T, long long C, long long D)
@@ -282,6 +293,7 @@ template <typename T, int V, int KP>
 relay_status_t launch_forward(Args p, cudaStream_t st)
 {
     p.S = forward_span(p.T, p.C, V);
+    RELAY_TRY(check_offsets(p));
     p.blocks_c = (p.C / V + kThreads - 1) / kThreads;
     const long long blocks = p.blocks_c * std::max<long long>(1, (p.T + p.S - 1) / p.S);
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "causal_conv: %lld steps of %lld channels", p.T, p.C);
@@ -292,6 +304,7 @@ template <typename T, int V, int KP>
 relay_status_t launch_gradient(Args p, cudaStream_t st)
 {
     p.S = gradient_span(p.T, p.C, V);
+    RELAY_TRY(check_offsets(p));
     p.blocks_c = (p.C / V + 31) / 32;
     const long long blocks = p.blocks_c * gradient_parts(p.T, p.C, p.D);
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "causal_conv_grad: %lld steps of %lld channels", p.T, p.C);

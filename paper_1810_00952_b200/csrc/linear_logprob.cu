@@ -21,12 +21,13 @@ using head::Piece;
 constexpr long long kPieceElements = 1ll << 27;            // scores (or copied weights) of a piece, at most
 
 // ---- small kernels -----------------------------------------------------------------------------------------------
-// Joins the partial statistics of a row: eight groups of them, each in its order.
-__global__ void __launch_bounds__(256) join_stats_kernel(const float2 *part, long long ld, long long parts, const float *at, const void *tokens,
-                                                         int tokens_i64, long long rows, long long V, float inv_temperature, float *logp,
-                                                         float *lse)
+// Joins the partial statistics of a row: kJoin groups of them, each in its order.
+constexpr int kJoin = 32;
+__global__ void __launch_bounds__(32 * kJoin) join_stats_kernel(const float2 *part, long long ld, long long parts, const float *at, const void *tokens,
+                                                                int tokens_i64, long long rows, long long V, float inv_temperature, float *logp,
+                                                                float *lse)
 {
-    __shared__ float2 joint[8][32];
+    __shared__ float2 joint[kJoin][32];
     pdl_wait();
     const long long row = (long long)blockIdx.x * 32 + threadIdx.x;
     float m = -INFINITY, s = 0.0f;
@@ -35,18 +36,26 @@ __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *part, lon
         s = s * exp2f(m - off) + q.y * exp2f(q.x - off);
         m = top;
     };
-    if (row < rows) {
-#pragma unroll 4
-        for (long long j = threadIdx.y; j < parts; j += 8) {
-            const float2 *from = part + j * ld + row;
-            if (relay_in_bounds(from, 8)) add(__ldcs(from));
+    constexpr int U = 8;                                   // on their way at once
+    for (long long j = threadIdx.y; j < parts; j += kJoin * U) {
+        float2 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float2 *from = part + (j + u * kJoin) * ld + row;
+            q[u] = make_float2(-INFINITY, 0.0f);
+            if (row < rows && j + u * kJoin < parts && relay_in_bounds(from, 8)) q[u] = __ldcs(from);
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(q[u]);
     }
     joint[threadIdx.y][threadIdx.x] = make_float2(m, s);
-    __syncthreads();
+    for (int n = kJoin / 2; n > 0; n /= 2) {
+        __syncthreads();
+        if (threadIdx.y >= n) continue;
+        add(joint[threadIdx.y + n][threadIdx.x]);
+        joint[threadIdx.y][threadIdx.x] = make_float2(m, s);
+    }
     if (threadIdx.y != 0 || row >= rows) return;
-#pragma unroll
-    for (int g = 1; g < 8; ++g) add(joint[g][threadIdx.x]);
     const float l = m == -INFINITY && s == 0.0f ? -INFINITY : fmaf(m, 0.693147181f, logf(s));
     float lp = 0.0f;
     if (head::token_in_piece(tokens, tokens_i64, row, V, 0, V) >= 0 && relay_in_bounds(at + row, 4))
@@ -55,38 +64,80 @@ __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *part, lon
     if (relay_in_bounds(lse + row, 4)) lse[row] = l;
 }
 
+// 16 bytes from an address of any 2-byte alignment: the two aligned pieces that hold them, shifted
+__device__ __forceinline__ uint4 load_shifted(const char *p)
+{
+    const unsigned skew = (unsigned)((uintptr_t)p & 15);
+    const uint4 *q = (const uint4 *)(p - skew);
+    if (skew == 0) return relay_in_bounds(q, 16) ? __ldg(q) : make_uint4(0, 0, 0, 0);
+    if (!relay_in_bounds(p, 16)) return make_uint4(0, 0, 0, 0);
+    const uint4 a = __ldg(q), b = __ldg(q + 1);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t v[5];
+    const unsigned words = skew >> 2, bits = (skew & 3) * 8;
+#pragma unroll
+    for (int j = 0; j < 5; ++j) v[j] = words == 0 ? w[j] : words == 1 ? w[j + 1 < 8 ? j + 1 : 7] : words == 2 ? w[j + 2 < 8 ? j + 2 : 7] : w[j + 3 < 8 ? j + 3 : 7];
+    return make_uint4(__funnelshift_r(v[0], v[1], bits), __funnelshift_r(v[1], v[2], bits), __funnelshift_r(v[2], v[3], bits),
+                      __funnelshift_r(v[3], v[4], bits));
+}
 // to (to_rows, to_cols) <- from (rows, cols), zero beyond; rows whose token names no class are zero too where tokens are given: whatever x
-// holds there (NaN too) takes no part in dw
+// holds there (NaN too) takes no part in dw.  A thread has the elements that share 16 aligned bytes of the result: one access each way
+// unless the row's end or what must not be read lies in between.
 template <typename T>
 __global__ void __launch_bounds__(256) copy_padded_kernel(const T *from, long long ld_from, long long rows, long long cols, T *to, long long ld_to,
                                                           long long to_rows, long long to_cols, const void *tokens, int tokens_i64, long long V)
 {
+    constexpr int E = 16 / sizeof(T);
     pdl_wait();
     for (long long r = blockIdx.y; r < to_rows; r += gridDim.y) {
         const bool live = r < rows && (tokens == nullptr || head::token_in_piece(tokens, tokens_i64, r, V, 0, V) >= 0);
-        for (long long c = (long long)blockIdx.x * 256 + threadIdx.x; c < to_cols; c += (long long)gridDim.x * 256) {
-            const T *p = from + r * ld_from + c;
-            T *q = to + r * ld_to + c;
-            const T x = live && c < cols && relay_in_bounds(p, sizeof(T)) ? *p : T(0.0f);
-            if (relay_in_bounds(q, sizeof(T))) *q = x;
+        const T *src = from + r * ld_from;
+        T *dst = to + r * ld_to;
+        const int skew = (int)(((uintptr_t)dst & 15) / sizeof(T));
+        // the last piece that may be read whole: an aligned 16-byte piece behind the tensor's end may not be there
+        const long long safe = r + 1 < rows ? cols : cols - E;
+        for (long long g = (long long)blockIdx.x * 256 + threadIdx.x; g * E < skew + to_cols; g += (long long)gridDim.x * 256) {
+            const long long c = g * E - skew;
+            if (c >= 0 && c + E <= to_cols && (!live || c + E <= safe || c >= cols)) {
+                const uint4 v = live && c < cols ? load_shifted((const char *)(src + c)) : make_uint4(0, 0, 0, 0);
+                if (relay_in_bounds(dst + c, 16)) *(uint4 *)(dst + c) = v;
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (c + j >= 0 && c + j < to_cols) {
+                    const T x = live && c + j < cols && relay_in_bounds(src + c + j, sizeof(T)) ? src[c + j] : T(0.0f);
+                    if (relay_in_bounds(dst + c + j, sizeof(T))) dst[c + j] = x;
+                }
         }
     }
 }
-// out (rows, cols) <- a + b, both fp32 (b may be null), rounded once
+// out (rows, cols) <- a + b, both fp32 with rows of `ld` values, whole 16-byte pieces (b may be null), rounded once
 template <typename T>
 __global__ void __launch_bounds__(256) add_kernel(const float *a, const float *b, long long ld, T *out, long long ld_out, long long rows,
                                                   long long cols)
 {
     pdl_wait();
+    const bool whole = ld % 4 == 0 && ld_out % 4 == 0;
     for (long long r = blockIdx.y; r < rows; r += gridDim.y)
-        for (long long c = (long long)blockIdx.x * 256 + threadIdx.x; c < cols; c += (long long)gridDim.x * 256) {
+        for (long long c = ((long long)blockIdx.x * 256 + threadIdx.x) * 4; c < cols; c += (long long)gridDim.x * 1024) {
             const long long at = r * ld + c;
-            if (!relay_in_bounds(a + at, 4)) continue;
-            const float x = a[at] + (b != nullptr && relay_in_bounds(b + at, 4) ? b[at] : 0.0f);
             T *q = out + r * ld_out + c;
-            if (!relay_in_bounds(q, sizeof(T))) continue;
-            if constexpr (sizeof(T) == 2) *q = __float2bfloat16_rn(x);
-            else *q = x;
+            float x[4] = {0.0f, 0.0f, 0.0f, 0.0f}, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (whole && c + 4 <= cols) {
+                seq::load<float, 4>(a, at, x);
+                if (b != nullptr) seq::load<float, 4>(b, at, y);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] += y[j];
+                seq::store<T, 4>(q, 0, x);
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (c + j >= cols || !relay_in_bounds(a + at + j, 4)) continue;
+                const float one[1] = {a[at + j] + (b != nullptr && relay_in_bounds(b + at + j, 4) ? b[at + j] : 0.0f)};
+                seq::store<T, 1>(q, j, one);
+            }
         }
 }
 
@@ -141,7 +192,7 @@ __global__ void __launch_bounds__(256) slopes_kernel(float *z, long long ld, con
     }
 }
 
-dim3 grid_of(long long rows, long long cols)
+dim3 grid_of(long long rows, long long cols)               // cols: threads along a row
 {
     return dim3((unsigned)std::min<long long>(std::max<long long>(1, (cols + 255) / 256), 64), (unsigned)std::min<long long>(std::max<long long>(1, rows), 16384));
 }
@@ -149,14 +200,14 @@ template <typename T>
 relay_status_t copy_padded(const void *from, long long ld_from, long long rows, long long cols, void *to, long long ld_to, long long to_rows,
                            long long to_cols, const Piece *masked, cudaStream_t st)
 {
-    RELAY_CUDA(launch_pdl(copy_padded_kernel<T>, grid_of(to_rows, to_cols), dim3(256), 0, st, (const T *)from, ld_from, rows, cols, (T *)to, ld_to,
+    RELAY_CUDA(launch_pdl(copy_padded_kernel<T>, grid_of(to_rows, (to_cols * sizeof(T) + 31) / 16), dim3(256), 0, st, (const T *)from, ld_from, rows, cols, (T *)to, ld_to,
                           to_rows, to_cols, masked ? masked->tokens : nullptr, masked ? masked->tokens_i64 : 0, masked ? masked->V : 0));
     return check_launch("linear_logprob");
 }
 template <typename T>
 relay_status_t add(const float *a, const float *b, long long ld, void *out, long long ld_out, long long rows, long long cols, cudaStream_t st)
 {
-    RELAY_CUDA(launch_pdl(add_kernel<T>, grid_of(rows, cols), dim3(256), 0, st, a, b, ld, (T *)out, ld_out, rows, cols));
+    RELAY_CUDA(launch_pdl(add_kernel<T>, grid_of(rows, (cols + 3) / 4), dim3(256), 0, st, a, b, ld, (T *)out, ld_out, rows, cols));
     return check_launch("linear_logprob");
 }
 
@@ -275,7 +326,7 @@ relay_status_t run_forward(Piece p, const Sizes &s, const void *w, bool bf16, fl
             parts += 1;
         }
     }
-    RELAY_CUDA(launch_pdl(join_stats_kernel, dim3((unsigned)((s.rows + 31) / 32)), dim3(32, 8), 0, st, (const float2 *)part, (long long)s.rows, parts,
+    RELAY_CUDA(launch_pdl(join_stats_kernel, dim3((unsigned)((s.rows + 31) / 32)), dim3(32, kJoin), 0, st, (const float2 *)part, (long long)s.rows, parts,
                           (const float *)at, p.tokens, p.tokens_i64, (long long)s.rows, (long long)s.V, p.inv_temperature, logp, lse));
     return check_launch("linear_logprob");
 }

@@ -73,58 +73,76 @@ struct StatsEpilogue {
     __device__ __forceinline__ void finish() {}
 };
 
+// The partials of 64 columns a warp: -slope 2^(z log2(e) / temperature - lse log2(e)), the slope's size taken into the exponent, its sign and
+// the rows without a part put in where two values are already one register.  Tokens and the vocabulary's end, which few groups of 32 columns
+// meet, are seen to under a condition that the whole warp shares.
 struct SlopeEpilogue {
     using Params = HeadParams;
     int token;
-    float off, slope, lse;                 // -lse log2(e), dlogp / temperature
-    bool nothing;                          // no token, or no class that can occur: no partials
+    float off, slope, lse;                 // log2 |slope| - lse log2(e), dlogp / temperature
+    uint32_t keep, sign;                   // of two bf16 values: all bits or none (no token, or no class that can occur); their signs
     __device__ __forceinline__ void prepare(const Params &p, int lane, int row0, int, int)
     {
         const long long row = row0 + lane;
         token = -1;
-        nothing = true;
-        slope = off = lse = 0.0f;
+        slope = lse = 0.0f;
+        off = -INFINITY;
+        keep = sign = 0;
         if (row >= p.rows) return;
         lse = p.lse[row];
+        if (lse == -INFINITY || head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, 0, p.V) < 0) return;
         token = head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, p.first, p.classes);
-        nothing = lse == -INFINITY || head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, 0, p.V) < 0;
-        if (nothing) return;
         slope = p.dlogp[row] * p.inv_temperature;
-        off = -lse * 1.44269504f;
+        off = fmaf(-lse, 1.44269504f, log2f(fabsf(slope)));
+        keep = 0xffffffffu;
+        sign = slope > 0.0f ? 0x80008000u : 0u;
     }
     __device__ __forceinline__ void drain(const Params &p, const CUtensorMap *tm_c, uint32_t taddr, uint8_t *stage, int lane, int row0, int n0,
                                           int width, int slot)
     {
         const int c0 = slot * 64;
         if (c0 >= width) return;
-#pragma unroll 1
+        uint32_t r[2][32];
+        tc::tmem_ld_32x32(taddr + c0, r[0]);
+        tc::tmem_ld_32x32(taddr + c0 + 32, r[1]);
+        tc::tmem_ld_wait();
+        const int sw = (lane >> 1) & 3;
+#pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int n = n0 + c0 + 32 * half;
             if (n >= p.N) break;                           // warp-uniform; p.N: columns of the stored piece
-            uint32_t r[32];
-            tc::tmem_ld_32x32(taddr + c0 + 32 * half, r);
-            tc::tmem_ld_wait();
-            const int hit = nothing ? -1 : token - n;
-            float v[32], own = 0.0f;
-            if (hit >= 0 && hit < 32) {                    // 1 - p of a class that is nearly certain keeps its precision
+            const int hit = token - n;
+            const bool mine = hit >= 0 && hit < 32;
+            float own = 0.0f;
+            if (__any_sync(0xffffffffu, mine)) {           // 1 - p of a class that is nearly certain keeps its precision
 #pragma unroll
-                for (int j = 0; j < 32; ++j) if (j == hit) own = __uint_as_float(r[j]);
+                for (int j = 0; j < 32; ++j) if (j == hit) own = __uint_as_float(r[half][j]);
                 own = -slope * expm1f(fmaf(own, p.inv_temperature, -lse));
             }
+            uint32_t v[16];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                v[j] = -slope * ex2(fmaf(__uint_as_float(r[j]), p.scale, off));
-                if (j == hit) v[j] = own;
-                if (nothing || n + j >= p.classes) v[j] = 0.0f;
+            for (int j = 0; j < 16; ++j)
+                v[j] = (pack2(ex2(fmaf(__uint_as_float(r[half][2 * j]), p.scale, off)), ex2(fmaf(__uint_as_float(r[half][2 * j + 1]), p.scale, off))) ^ sign) & keep;
+            if (__any_sync(0xffffffffu, mine)) {
+                const uint32_t bits = pack2(own, own);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (hit == 2 * j) v[j] = (v[j] & 0xffff0000u) | (bits & 0xffffu);
+                    if (hit == 2 * j + 1) v[j] = (v[j] & 0xffffu) | (bits & 0xffff0000u);
+                }
             }
-            const int sw = (lane >> 1) & 3;
+            if (n + 32 > p.classes) {                      // warp-uniform: columns that do not exist
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (n + 2 * j >= p.classes) v[j] = 0;
+                    else if (n + 2 * j + 1 >= p.classes) v[j] &= 0xffffu;
+                }
+            }
             if (tc::elect_one()) tc::tma_store_wait_read<0>();
             __syncwarp();
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-                *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ sw) << 4)) =
-                    make_uint4(pack2(v[8 * c], v[8 * c + 1]), pack2(v[8 * c + 2], v[8 * c + 3]), pack2(v[8 * c + 4], v[8 * c + 5]),
-                               pack2(v[8 * c + 6], v[8 * c + 7]));
+                *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ sw) << 4)) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
             tc::fence_proxy_async();
             __syncwarp();
             if (tc::elect_one()) {
