@@ -1,5 +1,6 @@
 // Selective scan: h = exp(delta a) h + delta u b per channel and state, y = sum_n c h + d u, with an optional gate silu(z).
 #include <algorithm>
+#include <type_traits>
 
 #include "selective_scan.cuh"
 
@@ -80,36 +81,41 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
 }
 
 // ---- chunks -----------------------------------------------------------------------------------------------------------
-// A block: WC warps of eight channels side by side, WT rows of them; four lanes a channel, each with four neighbouring states of every
-// sixteen.  A chunk's rows are fetched a chunk ahead by TMA.  Three phases: steps and weights are made fp32, four channels a thread, each
-// step and step times u twice over, as the scan's paired instructions take them; the scan itself; and skip, gate and rounding of the
-// results, whose four partial sums a channel the scan leaves side by side.  Several blocks on an SM are in different phases.
-// WT = 1: a warp takes its channels through the whole chunk.  WT > 1: each row of warps has a run of RUN steps.
-constexpr int RUN = 8, STAGES = 2;
+// A block: two warps of eight channels each; four lanes a channel, with four neighbouring states of every sixteen each.  A chunk's rows are
+// fetched a chunk ahead by TMA.  Three phases: steps and weights are made fp32, four channels a thread; the scan itself; and skip, gate and
+// rounding of the results, whose four parts a channel the scan leaves side by side.  Several blocks on an SM are in different phases.
+//
+// Where there are too few channels for that, the blocks of a cluster take a part of the sequence each.  Every block first takes its part from
+// a zero state, for the state that it leaves and the sum of its steps alone; then the blocks read each other's (shared memory of the cluster),
+// join those before their own, exp(a sum of steps) being the part's decay, and take their part again from the state that it starts with.
+constexpr int STAGES = 2, STEPS = 32, WARPS = 2, THREADS = 32 * WARPS, CHANNELS = 8 * WARPS;
 
-template <typename T, int WT, int WC, int NB, int TD>
+template <typename T, int NB>
 struct Tile {
-    static constexpr int THREADS = 32 * WT * WC, CHANNELS = 8 * TD * WC, STEPS = RUN * WT < 32 ? 32 : RUN * WT, NP = 16 * NB;
+    static constexpr int NP = 16 * NB;
     struct Stage { alignas(128) T u[STEPS][CHANNELS]; alignas(128) T delta[STEPS][CHANNELS]; alignas(128) T z[STEPS][CHANNELS]; alignas(128) T bc[STEPS * 2 * NP]; };
     Stage stage[STAGES];
     alignas(16) float2 step[STEPS][CHANNELS];              // delta, delta u
     alignas(16) float b[STEPS][NP], c[STEPS][NP];
     alignas(16) float y[STEPS][4][CHANNELS];               // the four lanes' parts of sum_n c h
-    float4 decay[WT == 1 ? 1 : 2][WT][WC][WT == 1 ? 1 : 32], sum[WT == 1 ? 1 : 2][WT][WC][WT == 1 ? 1 : 32];
+    ulonglong2 left[NB][THREADS];                          // for the cluster: the state from zero, the sum of steps
+    float sum[THREADS];
     uint64_t full[STAGES];
     int gave_up;
 };
 
-template <typename T, int WT, int WC, int NB, int TD>
-__global__ void __launch_bounds__(32 * WT * WC) selective_scan_kernel(const Args p, const __grid_constant__ Maps maps)
+template <typename T, int NB, bool SPLIT>
+__global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, const __grid_constant__ Maps maps, const int parts)
 {
-    using S = Tile<T, WT, WC, NB, TD>;
+    using S = Tile<T, NB>;
     constexpr bool FINE = sizeof(T) == 4;
     extern __shared__ uint8_t shared_raw[];
     S &s = *reinterpret_cast<S *>(((uintptr_t)shared_raw + 127) & ~(uintptr_t)127);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wt = warp / WC, wc = warp % WC, nl = lane & 3, cl = lane >> 2;
-    const long long i = blockIdx.x / p.groups;
-    const long long c0 = (blockIdx.x - i * p.groups) * S::CHANNELS;
+    const int tid = threadIdx.x, lane = tid & 31, wc = tid >> 5, nl = lane & 3, cl = lane >> 2;
+    const long long block = SPLIT ? blockIdx.x / parts : blockIdx.x;
+    const int part = SPLIT ? (int)(blockIdx.x - block * parts) : 0;        // rank in the cluster
+    const long long i = block / p.groups;
+    const long long c0 = (block - i * p.groups) * CHANNELS;
     if (tid == 0) {
         for (int q = 0; q < STAGES; ++q) tc::mbar_init(&s.full[q], 1);
         s.gave_up = 0;
@@ -118,124 +124,130 @@ __global__ void __launch_bounds__(32 * WT * WC) selective_scan_kernel(const Args
     __syncthreads();
     pdl_wait();
     const long long end = end_of(p, i);
-    const int live_chunks = (int)((end + S::STEPS - 1) / S::STEPS);
-    // rows of chunk k into its stage, by TMA (one thread) or by everyone's plain loads
-    auto fetch = [&](int k) {
-        typename S::Stage &g = s.stage[k % STAGES];
-        const long long t0 = (long long)k * S::STEPS;
+    const int all = (int)((p.T + STEPS - 1) / STEPS), each = SPLIT ? (all + parts - 1) / parts : all;
+    const int first = min(all, part * each), last = min(all, first + each);                  // this block's chunks
+    const int live = max(0, min(last, (int)((end + STEPS - 1) / STEPS)) - first);             // those of them inside the sequence
+    // rows of the k-th live chunk into the stage of the q-th fetch, by TMA (one thread) or by everyone's plain loads
+    auto fetch = [&](int q, int k, bool with_z) {
+        typename S::Stage &g = s.stage[q % STAGES];
+        const long long t0 = (long long)(first + k) * STEPS;
         if (tid == 0 && (p.tma_x || p.tma_w)) {
-            const uint32_t x = p.tma_x ? (p.z ? 3u : 2u) * (uint32_t)sizeof(g.u) : 0u, w = p.tma_w ? (uint32_t)(S::STEPS * 2 * p.N * sizeof(T)) : 0u;
-            tc::mbar_expect_tx(&s.full[k % STAGES], x + w);
+            uint64_t *full = &s.full[q % STAGES];
+            const uint32_t x = p.tma_x ? (with_z ? 3u : 2u) * (uint32_t)sizeof(g.u) : 0u, w = p.tma_w ? (uint32_t)(STEPS * 2 * p.N * sizeof(T)) : 0u;
+            tc::mbar_expect_tx(full, x + w);
             const int col = (int)(i * p.D + c0), row = (int)t0;
             if (p.tma_x) {
-                tc::tma_load_2d(g.u, &maps.u, &s.full[k % STAGES], col, row);
-                tc::tma_load_2d(g.delta, &maps.delta, &s.full[k % STAGES], col, row);
-                if (p.z) tc::tma_load_2d(g.z, &maps.z, &s.full[k % STAGES], col, row);
+                tc::tma_load_2d(g.u, &maps.u, full, col, row);
+                tc::tma_load_2d(g.delta, &maps.delta, full, col, row);
+                if (with_z) tc::tma_load_2d(g.z, &maps.z, full, col, row);
             }
             if (p.tma_w) {
-                tc::tma_load_2d(g.bc, &maps.b, &s.full[k % STAGES], (int)(i * p.ld_bc), row);
-                if (p.ld_bc == p.N) tc::tma_load_2d(g.bc + S::STEPS * p.N, &maps.c, &s.full[k % STAGES], (int)(i * p.ld_bc), row);
+                tc::tma_load_2d(g.bc, &maps.b, full, (int)(i * p.ld_bc), row);
+                if (p.ld_bc == p.N) tc::tma_load_2d(g.bc + STEPS * p.N, &maps.c, full, (int)(i * p.ld_bc), row);
             }
         }
         if (!p.tma_x) {
 #pragma unroll 4
-            for (int e = tid; e < S::STEPS * S::CHANNELS; e += S::THREADS) {
-                const int t = e / S::CHANNELS, c = e % S::CHANNELS;
+            for (int e = tid; e < STEPS * CHANNELS; e += THREADS) {
+                const int t = e / CHANNELS, c = e % CHANNELS;
                 const long long at = ((t0 + t) * p.B + i) * p.D + c0 + c;
                 if (t0 + t < end && c0 + c < p.D) {
                     g.u[t][c] = load_raw_one<T>(p.u, at);
                     g.delta[t][c] = load_raw_one<T>(p.delta, at);
-                    if (p.z) g.z[t][c] = load_raw_one<T>(p.z, at);
+                    if (with_z) g.z[t][c] = load_raw_one<T>(p.z, at);
                 }
             }
         }
         if (!p.tma_w) {
             const bool packed = p.ld_bc != p.N;
 #pragma unroll 4
-            for (int e = tid; e < S::STEPS * p.N; e += S::THREADS) {
+            for (int e = tid; e < STEPS * p.N; e += THREADS) {
                 const int t = e / p.N, n = e - t * p.N;
                 const long long at = ((t0 + t) * p.B + i) * p.ld_bc + n;
                 if (t0 + t < end) {
                     g.bc[packed ? t * 2 * p.N + n : e] = load_raw_one<T>(p.b, at);
-                    g.bc[packed ? t * 2 * p.N + p.N + n : S::STEPS * p.N + e] = load_raw_one<T>(p.c, at);
+                    g.bc[packed ? t * 2 * p.N + p.N + n : STEPS * p.N + e] = load_raw_one<T>(p.c, at);
                 }
             }
         }
     };
-    for (int k = 0; k < STAGES && k < live_chunks; ++k) fetch(k);
-    // this thread's states: of channels mine .. mine + TD - 1
-    const int ch = (wc * 8 + cl) * TD;
+    int fetched = 0, used = 0;                             // fetches so far, and chunks taken from them
+    // this thread's states: of channel mine
+    const int ch = wc * 8 + cl;
     const long long mine = c0 + ch;
-    f32x2 a[TD][NB][2], h[TD][NB][2];                      // a log2(e); the state
+    f32x2 a[NB][2], h[NB][2];                              // a log2(e); the state
 #pragma unroll
-    for (int d = 0; d < TD; ++d)
+    for (int k = 0; k < NB; ++k) {
+        float x[4];
+        load_states(p, mine < p.D ? p.a : nullptr, mine * p.N, k * 16 + nl * 4, x);
+        a[k][0] = pair(x[0] * kLog2e, x[1] * kLog2e);
+        a[k][1] = pair(x[2] * kLog2e, x[3] * kLog2e);
+    }
+    auto from_start = [&] {
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
             float x[4];
-            load_states(p, mine + d < p.D ? p.a : nullptr, (mine + d) * p.N, k * 16 + nl * 4, x);
-            a[d][k][0] = pair(x[0] * kLog2e, x[1] * kLog2e);
-            a[d][k][1] = pair(x[2] * kLog2e, x[3] * kLog2e);
-            load_states(p, mine + d < p.D ? p.h0 : nullptr, (i * p.D + mine + d) * p.N, k * 16 + nl * 4, x);
-            h[d][k][0] = pair(x[0], x[1]);
-            h[d][k][1] = pair(x[2], x[3]);
+            load_states(p, mine < p.D ? p.h0 : nullptr, (i * p.D + mine) * p.N, k * 16 + nl * 4, x);
+            h[k][0] = pair(x[0], x[1]);
+            h[k][1] = pair(x[2], x[3]);
         }
-    auto write = [&](float *to, long long first, int d, int k, const f32x2 (&v)[2]) {
-        float g[4];
-        unpair(v[0], g[0], g[1]); unpair(v[1], g[2], g[3]);
-        if (mine + d < p.D) store_states(p, to, (first + mine + d) * p.N, k * 16 + nl * 4, g);
     };
-    auto save = [&](long long t, int d, int k, const f32x2 (&v)[2]) {
-        if (p.states && t < p.T && t % kSpan == 0) write(p.states, (t / kSpan * p.B + i) * p.D, d, k, v);
+    auto write = [&](float *to, long long row, int k) {
+        float g[4];
+        unpair(h[k][0], g[0], g[1]); unpair(h[k][1], g[2], g[3]);
+        if (mine < p.D) store_states(p, to, (row + mine) * p.N, k * 16 + nl * 4, g);
     };
     // four channels that this thread turns into steps, and whose results it finishes: always the same ones
-    constexpr int FOURS = S::CHANNELS / 4, PASSES = (S::STEPS * FOURS + S::THREADS - 1) / S::THREADS;
-    static_assert(S::THREADS % FOURS == 0, "a thread's channels are the same in every row");
-    const int pc = 4 * (tid % FOURS);
-    f32x2 skip[2], bias[2];
-    {
-        float x[4], y[4];
+    constexpr int G = 4, UNITS = CHANNELS / G, PASSES = STEPS * UNITS / THREADS;
+    static_assert(THREADS % UNITS == 0 && PASSES * THREADS == STEPS * UNITS, "a thread's channels are the same in every row");
+    const int pc = G * (tid % UNITS);
+    f32x2 skip[G / 2], bias[G / 2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool in = c0 + pc + j < p.D;
-            x[j] = p.d && in && relay_in_bounds(p.d + c0 + pc + j, 4) ? p.d[c0 + pc + j] : 0.0f;
-            y[j] = p.delta_bias && in && relay_in_bounds(p.delta_bias + c0 + pc + j, 4) ? p.delta_bias[c0 + pc + j] : 0.0f;
+    for (int j = 0; j < G; j += 2) {
+        float x[2], y[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const long long d = c0 + pc + j + q;
+            x[q] = p.d && d < p.D && relay_in_bounds(p.d + d, 4) ? p.d[d] : 0.0f;
+            y[q] = p.delta_bias && d < p.D && relay_in_bounds(p.delta_bias + d, 4) ? p.delta_bias[d] : 0.0f;
         }
-        skip[0] = pair(x[0], x[1]); skip[1] = pair(x[2], x[3]);
-        bias[0] = pair(y[0], y[1]); bias[1] = pair(y[2], y[3]);
+        skip[j / 2] = pair(x[0], x[1]);
+        bias[j / 2] = pair(y[0], y[1]);
     }
-    for (int chunk = 0; chunk < live_chunks; ++chunk) {
-        typename S::Stage &g = s.stage[chunk % STAGES];
-        const long long t0 = (long long)chunk * S::STEPS;
-        if (p.tma_x || p.tma_w) tc::mbar_wait(&s.full[chunk % STAGES], (chunk / STAGES) & 1, &s.gave_up, p.err, tc::ERR_WAIT_FULL);
+    // waits for a chunk's rows; steps and weights in fp32
+    auto prepare = [&](const typename S::Stage &g, int in) {
+        if (p.tma_x || p.tma_w) tc::mbar_wait(&s.full[used % STAGES], (used / STAGES) & 1, &s.gave_up, p.err, tc::ERR_WAIT_FULL);
         if (!p.tma_x || !p.tma_w) __syncthreads();         // everyone's plain loads
-        const int in = (int)min((long long)S::STEPS, end - t0);              // steps of the chunk that are inside the sequence
 #pragma unroll
         for (int k = 0; k < PASSES; ++k) {
-            const int t = tid / FOURS + k * (S::THREADS / FOURS);
-            if (t >= S::STEPS) break;
-            float u[4], x[4];
+            const int t = tid / UNITS + k * (THREADS / UNITS);
+            float u[G], x[G];
             widen_shared(&g.u[t][pc], u);
             widen_shared(&g.delta[t][pc], x);
-            f32x2 step[2] = {add2(pair(x[0], x[1]), bias[0]), add2(pair(x[2], x[3]), bias[1])};
-            if (p.softplus) { step[0] = softplus2(step[0]).value; step[1] = softplus2(step[1]).value; }
+            f32x2 step[G / 2];
+#pragma unroll
+            for (int j = 0; j < G / 2; ++j) step[j] = add2(pair(x[2 * j], x[2 * j + 1]), bias[j]);
+            if (p.softplus) {
+#pragma unroll
+                for (int j = 0; j < G / 2; ++j) step[j] = softplus2(step[j]).value;
+            }
             if (t >= in) {                                 // behind the end nothing decays and nothing is added
-                step[0] = step[1] = 0;
-                u[0] = u[1] = u[2] = u[3] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < G; ++j) { step[j / 2] = 0; u[j] = 0.0f; }
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float lo, hi, ulo, uhi;
+            for (int j = 0; j < G / 2; ++j) {
+                float lo, hi;
                 unpair(step[j], lo, hi);
-                unpair(mul2(step[j], pair(u[2 * j], u[2 * j + 1])), ulo, uhi);
-                *reinterpret_cast<float4 *>(&s.step[t][pc + 2 * j]) = make_float4(lo, ulo, hi, uhi);
+                *reinterpret_cast<float4 *>(&s.step[t][pc + 2 * j]) = make_float4(lo, lo * u[2 * j], hi, hi * u[2 * j + 1]);
             }
         }
         if (p.N == S::NP) {                                // four states at a time
-            for (int e = tid; e < S::STEPS * S::NP / 4; e += S::THREADS) {
+            for (int e = tid; e < STEPS * S::NP / 4; e += THREADS) {
                 const int t = e / (S::NP / 4), n = e % (S::NP / 4) * 4;
                 float b[4], c[4];
                 widen_shared(p.ld_bc != p.N ? &g.bc[t * 2 * S::NP + n] : &g.bc[t * S::NP + n], b);
-                widen_shared(p.ld_bc != p.N ? &g.bc[t * 2 * S::NP + S::NP + n] : &g.bc[S::STEPS * S::NP + t * S::NP + n], c);
+                widen_shared(p.ld_bc != p.N ? &g.bc[t * 2 * S::NP + S::NP + n] : &g.bc[STEPS * S::NP + t * S::NP + n], c);
                 if (t >= in) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) b[j] = c[j] = 0.0f;
@@ -244,122 +256,112 @@ __global__ void __launch_bounds__(32 * WT * WC) selective_scan_kernel(const Args
                 *reinterpret_cast<float4 *>(&s.c[t][n]) = make_float4(c[0], c[1], c[2], c[3]);
             }
         } else {
-            for (int e = tid; e < S::STEPS * S::NP; e += S::THREADS) {
+            for (int e = tid; e < STEPS * S::NP; e += THREADS) {
                 const int t = e / S::NP, n = e % S::NP;
                 const bool on = t < in && n < p.N, packed = p.ld_bc != p.N;
                 s.b[t][n] = on ? to_f32(g.bc[packed ? t * 2 * p.N + n : t * p.N + n]) : 0.0f;
-                s.c[t][n] = on ? to_f32(g.bc[packed ? t * 2 * p.N + p.N + n : S::STEPS * p.N + t * p.N + n]) : 0.0f;
+                s.c[t][n] = on ? to_f32(g.bc[packed ? t * 2 * p.N + p.N + n : STEPS * p.N + t * p.N + n]) : 0.0f;
             }
         }
+        ++used;
         __syncthreads();
-        if constexpr (WT == 1) {
-#pragma unroll
-            for (int d = 0; d < TD; ++d)
-#pragma unroll
-                for (int k = 0; k < NB; ++k) save(t0, d, k, h[d][k]);
-            // a few steps at a time: first their decays and what they add, all independent, then the chain
-            constexpr int AT_ONCE = NB == 1 ? 8 / TD : 1;
+    };
+    // A few steps at a time: first their decays and what they add, all independent, then the chain.  RESULTS: leaves the parts of sum_n c h.
+    float sum = 0.0f;
+    auto chain = [&](auto results) {
+        constexpr bool RESULTS = decltype(results)::value;
+        constexpr int AT_ONCE = NB == 1 ? 8 : 2;
 #pragma unroll 2
-            for (int r0 = 0; r0 < S::STEPS; r0 += AT_ONCE) {
-                f32x2 da[AT_ONCE][TD][NB][2], x[AT_ONCE][TD][NB][2];
+        for (int r0 = 0; r0 < STEPS; r0 += AT_ONCE) {
+            f32x2 da[AT_ONCE][NB][2], x[AT_ONCE][NB][2];
 #pragma unroll
-                for (int r = 0; r < AT_ONCE; ++r) {
-                    float2 st[TD];
-                    if constexpr (TD == 1) st[0] = s.step[r0 + r][ch];
-                    else {
+            for (int r = 0; r < AT_ONCE; ++r) {
+                const float2 st = s.step[r0 + r][ch];
+                const f32x2 dd = pair(st.x, st.x), du = pair(st.y, st.y);
+                if (!RESULTS) sum += st.x;
 #pragma unroll
-                        for (int d = 0; d < TD; d += 2) *reinterpret_cast<float4 *>(&st[d]) = *reinterpret_cast<const float4 *>(&s.step[r0 + r][ch + d]);
-                    }
-#pragma unroll
-                    for (int k = 0; k < NB; ++k) {
-                        const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
-#pragma unroll
-                        for (int d = 0; d < TD; ++d) {
-                            const f32x2 dd = pair(st[d].x, st[d].x), du = pair(st[d].y, st[d].y);
-                            da[r][d][k][0] = decay2<FINE>(mul2(dd, a[d][k][0]));
-                            da[r][d][k][1] = decay2<FINE>(mul2(dd, a[d][k][1]));
-                            x[r][d][k][0] = mul2(du, b.x);
-                            x[r][d][k][1] = mul2(du, b.y);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < AT_ONCE; ++r) {
-                    float sum[TD];
-#pragma unroll
-                    for (int d = 0; d < TD; ++d) {
-                        f32x2 y = 0;
-#pragma unroll
-                        for (int k = 0; k < NB; ++k) {
-                            const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
-                            h[d][k][0] = fma2(da[r][d][k][0], h[d][k][0], x[r][d][k][0]);
-                            h[d][k][1] = fma2(da[r][d][k][1], h[d][k][1], x[r][d][k][1]);
-                            y = k ? fma2(c.x, h[d][k][0], y) : mul2(c.x, h[d][k][0]);
-                            y = fma2(c.y, h[d][k][1], y);
-                        }
-                        sum[d] = sum2(y);
-                    }
-                    if constexpr (TD == 1) s.y[r0 + r][nl][ch] = sum[0];
-                    else if constexpr (TD == 2) *reinterpret_cast<float2 *>(&s.y[r0 + r][nl][ch]) = make_float2(sum[0], sum[1]);
-                    else *reinterpret_cast<float4 *>(&s.y[r0 + r][nl][ch]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                for (int k = 0; k < NB; ++k) {
+                    const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
+                    da[r][k][0] = decay2<FINE>(mul2(dd, a[k][0]));
+                    da[r][k][1] = decay2<FINE>(mul2(dd, a[k][1]));
+                    x[r][k][0] = mul2(du, b.x);
+                    x[r][k][1] = mul2(du, b.y);
                 }
             }
-        } else {
-            const int r0 = wt * RUN;                       // this warp's run
-            float y[RUN];
+#pragma unroll
+            for (int r = 0; r < AT_ONCE; ++r) {
+                f32x2 y = 0;
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    h[k][0] = fma2(da[r][k][0], h[k][0], x[r][k][0]);
+                    h[k][1] = fma2(da[r][k][1], h[k][1], x[r][k][1]);
+                    if (!RESULTS) continue;
+                    const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
+                    y = k ? fma2(c.x, h[k][0], y) : mul2(c.x, h[k][0]);
+                    y = fma2(c.y, h[k][1], y);
+                }
+                if (RESULTS) s.y[r0 + r][nl][ch] = sum2(y);
+            }
+        }
+    };
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int k = 0; k < NB; ++k) h[k][0] = h[k][1] = 0;
+        if (part < parts - 1) {                            // nobody joins the last part
+            for (int k = 0; k < STAGES && k < live; ++k) fetch(fetched++, k, false);
+            for (int chunk = 0; chunk < live; ++chunk) {
+                prepare(s.stage[used % STAGES], (int)min((long long)STEPS, end - (long long)(first + chunk) * STEPS));
+                if (chunk + STAGES < live) fetch(fetched++, chunk + STAGES, false);           // its rows have been read
+                chain(std::false_type());
+                __syncthreads();                           // steps and weights have been read
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NB; ++k) s.left[k][tid] = make_ulonglong2(h[k][0], h[k][1]);
+        s.sum[tid] = sum;
+    }
+    // the rows that the second pass begins with are on their way while the blocks meet
+    for (int k = 0; k < STAGES && k < live; ++k) fetch(fetched++, k, p.z != nullptr);
+    from_start();
+    if constexpr (SPLIT) {
+        tc::cluster_sync();
+        for (int r = 0; r < part; ++r) {
+            const uint32_t at = tc::mapa(tc::smem_u32(&s.sum[tid]), (uint32_t)r);
+            float total;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(total) : "r"(at));
 #pragma unroll
             for (int k = 0; k < NB; ++k) {
-                f32x2 da[RUN][2], x[RUN][2], P[2], H[2];                   // decays; what is added, then the states
-#pragma unroll
-                for (int r = 0; r < RUN; ++r) {
-                    const float2 st = s.step[r0 + r][ch];
-                    const f32x2 dd = pair(st.x, st.x), du = pair(st.y, st.y);
-                    const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        da[r][q] = decay2<FINE>(mul2(dd, a[0][k][q]));
-                        x[r][q] = mul2(du, q ? b.y : b.x);
-                        H[q] = r ? fma2(da[r][q], H[q], x[r][q]) : x[r][q];
-                        P[q] = r ? mul2(da[r][q], P[q]) : da[r][q];
-                    }
-                }
-                const int slot = k & 1;
-                *reinterpret_cast<ulonglong2 *>(&s.decay[slot][wt][wc][lane]) = make_ulonglong2(P[0], P[1]);
-                *reinterpret_cast<ulonglong2 *>(&s.sum[slot][wt][wc][lane]) = make_ulonglong2(H[0], H[1]);
-                __syncthreads();
-                f32x2 from[2];                             // the state at the start of this run
-#pragma unroll
-                for (int w = 0; w < WT; ++w) {
-                    const ulonglong2 pw = *reinterpret_cast<const ulonglong2 *>(&s.decay[slot][w][wc][lane]);
-                    const ulonglong2 hw = *reinterpret_cast<const ulonglong2 *>(&s.sum[slot][w][wc][lane]);
-                    if (w == wt) { from[0] = h[0][k][0]; from[1] = h[0][k][1]; }
-                    h[0][k][0] = fma2(pw.x, h[0][k][0], hw.x);
-                    h[0][k][1] = fma2(pw.y, h[0][k][1], hw.y);
-                }
-                save(t0 + r0, 0, k, from);
-#pragma unroll
-                for (int r = 0; r < RUN; ++r) {
-                    const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
-                    from[0] = fma2(da[r][0], from[0], x[r][0]);
-                    from[1] = fma2(da[r][1], from[1], x[r][1]);
-                    const float v = sum2(fma2(c.y, from[1], mul2(c.x, from[0])));
-                    y[r] = k ? y[r] + v : v;
-                }
+                const uint32_t from = tc::mapa(tc::smem_u32(&s.left[k][tid]), (uint32_t)r);
+                unsigned long long x, y;
+                asm volatile("ld.shared::cluster.v2.u64 {%0, %1}, [%2];" : "=l"(x), "=l"(y) : "r"(from));
+                h[k][0] = fma2(decay2<FINE>(mul2(pair(total, total), a[k][0])), h[k][0], x);
+                h[k][1] = fma2(decay2<FINE>(mul2(pair(total, total), a[k][1])), h[k][1], y);
             }
-#pragma unroll
-            for (int r = 0; r < RUN; ++r) s.y[r0 + r][nl][ch] = y[r];
         }
+        tc::cluster_sync();                                // every block has read what it needs of the others
+    }
+    for (int chunk = 0; chunk < live; ++chunk) {
+        typename S::Stage &g = s.stage[used % STAGES];
+        const long long t0 = (long long)(first + chunk) * STEPS;
+        const int in = (int)min((long long)STEPS, end - t0);                 // steps of the chunk that are inside the sequence
+        prepare(g, in);
+        if (p.states) {
+#pragma unroll
+            for (int k = 0; k < NB; ++k) write(p.states, ((first + chunk) * p.B + i) * p.D, k);
+        }
+        chain(std::true_type());
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < PASSES; ++k) {
-            const int t = tid / FOURS + k * (S::THREADS / FOURS);
-            if (t >= S::STEPS || t0 + t >= p.T) break;
-            f32x2 out[2] = {0, 0};
-            float q[4];
+            const int t = tid / UNITS + k * (THREADS / UNITS);
+            if (t0 + t >= p.T) break;
+            f32x2 out[G / 2];
+            float q[G];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&s.y[t][j][pc]);
-                out[0] = add2(out[0], v.x); out[1] = add2(out[1], v.y);
+                out[0] = j ? add2(out[0], v.x) : v.x;
+                out[1] = j ? add2(out[1], v.y) : v.y;
             }
             widen_shared(&g.u[t][pc], q);
             if (p.d) { out[0] = fma2(skip[0], pair(q[0], q[1]), out[0]); out[1] = fma2(skip[1], pair(q[2], q[3]), out[1]); }
@@ -370,27 +372,28 @@ __global__ void __launch_bounds__(32 * WT * WC) selective_scan_kernel(const Args
             }
             unpair(out[0], q[0], q[1]); unpair(out[1], q[2], q[3]);
             if (t >= in) q[0] = q[1] = q[2] = q[3] = 0.0f;
-            store_four<T>(p, p.y, ((t0 + t) * p.B + i) * p.D, c0 + pc, q);
+            store_some<T>(p, p.y, ((t0 + t) * p.B + i) * p.D, c0 + pc, q);
         }
         __syncthreads();                                   // the stage is free
-        if (chunk + STAGES < live_chunks) fetch(chunk + STAGES);
+        if (chunk + STAGES < live) fetch(fetched++, chunk + STAGES, p.z != nullptr);
     }
     // behind the sequence
-    const long long tail = (long long)live_chunks * S::STEPS;
-    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (long long t = tail + tid / FOURS; t < p.T; t += S::THREADS / FOURS) store_four<T>(p, p.y, (t * p.B + i) * p.D, c0 + pc, zero);
-    if (wt != 0) return;
+    const float zero[G] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (long long t = (long long)(first + live) * STEPS + tid / UNITS; t < min(p.T, (long long)last * STEPS); t += THREADS / UNITS)
+        store_some<T>(p, p.y, (t * p.B + i) * p.D, c0 + pc, zero);
 #pragma unroll
-    for (int d = 0; d < TD; ++d)
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-            for (long long t = (tail + kSpan - 1) / kSpan * kSpan; t < p.T; t += kSpan) save(t, d, k, h[d][k]);
-            if (p.h_final) write(p.h_final, i * p.D, d, k, h[d][k]);
-        }
+    for (int k = 0; k < NB; ++k) {
+        if (p.states)
+            for (int q = first + live; q < last; ++q) write(p.states, (q * p.B + i) * p.D, k);
+        if (p.h_final && part == parts - 1) write(p.h_final, i * p.D, k);
+    }
 }
+static_assert(STEPS == kSpan, "a chunk starts where a state is saved");
 
 // ---- launches ------------------------------------------------------------------------------------------------------
-constexpr long long kFewSteps = 4;
+// Up to here step by step: 64 x 2048 channels 30 us for 8 steps against 43 by chunks, 51 against 43 for 16; 4 x 2048 channels 15 against 17
+// and 16 against 16.
+constexpr long long kFewSteps = 10, kSms = 148;
 
 template <typename T, int NB>
 relay_status_t launch_steps(const Args &p, cudaStream_t st)
@@ -400,28 +403,40 @@ relay_status_t launch_steps(const Args &p, cudaStream_t st)
     RELAY_CUDA(launch_pdl(selective_scan_steps_kernel<T, NB>, dim3((unsigned)blocks), dim3(kStepThreads), 0, st, p));
     return check_launch("selective_scan");
 }
-template <typename T, int WT, int WC, int NB, int TD>
-relay_status_t launch_chunks(Args p, cudaStream_t st)
+template <typename T, int NB, bool SPLIT>
+relay_status_t launch_chunks(Args p, int parts, cudaStream_t st)
 {
-    using S = Tile<T, WT, WC, NB, TD>;
-    p.groups = (int)((p.D + S::CHANNELS - 1) / S::CHANNELS);
-    const long long blocks = p.B * p.groups;
+    using S = Tile<T, NB>;
+    p.groups = (int)((p.D + CHANNELS - 1) / CHANNELS);
+    const long long blocks = p.B * p.groups * parts;
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "selective_scan: %lld x %lld channels", p.B, p.D);
+    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
     Maps maps;
-    RELAY_TRY(make_maps(&p, &maps, sizeof(T) == 4, S::CHANNELS, S::STEPS));
+    RELAY_TRY(make_maps(&p, &maps, sizeof(T) == 4, CHANNELS, STEPS));
     const size_t bytes = sizeof(S) + 128;
-    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_kernel<T, WT, WC, NB, TD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    RELAY_CUDA(launch_pdl(selective_scan_kernel<T, WT, WC, NB, TD>, dim3((unsigned)blocks), dim3(S::THREADS), bytes, st, p, maps));
+    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_kernel<T, NB, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if constexpr (SPLIT)
+        RELAY_CUDA(launch_pdl_cluster(selective_scan_kernel<T, NB, SPLIT>, dim3((unsigned)blocks), dim3(THREADS), dim3(parts), bytes, st, p, maps, parts));
+    else
+        RELAY_CUDA(launch_pdl(selective_scan_kernel<T, NB, SPLIT>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, p, maps, parts));
     return check_launch("selective_scan");
 }
-// Rows of warps share the channels where there are too few of them to give every SM eight warps.
+// Blocks that share a sequence: as many as give every SM eight warps, with four chunks each at least.  What the second pass costs them is half as
+// much again: 2048 x 8 x 2048 x 16 (2048 warps) 322 us alone and 463 shared by two, 4096 x 4 569 and 519, 8192 x 2 764, 880 (two), 530
+// (four) and 521, 16384 x 1 1290, 1260 (two), 857 (four) and 529 (eight).
+int parts_of(const Args &p)
+{
+    const long long warps = p.B * ((p.D + 7) / 8), chunks = (p.T + STEPS - 1) / STEPS;
+    int parts = 1;
+    while (parts < 8 && warps * parts < 8 * kSms && chunks >= 8 * parts) parts *= 2;
+    return parts;
+}
 template <typename T, int NB>
 relay_status_t launch_form(const Args &p, cudaStream_t st)
 {
     if (p.T <= kFewSteps) return launch_steps<T, NB>(p, st);
-    if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
-    if (p.B * p.D < 148 * 64) return launch_chunks<T, NB == 1 ? 8 : 4, 1, NB, 1>(p, st);
-    return launch_chunks<T, 1, 2, NB, 1>(p, st);
+    const int parts = parts_of(p);
+    return parts > 1 ? launch_chunks<T, NB, true>(p, parts, st) : launch_chunks<T, NB, false>(p, 1, st);
 }
 template <typename T>
 relay_status_t launch_states(const Args &p, cudaStream_t st)

@@ -77,35 +77,16 @@ __device__ __forceinline__ float softplus_slope(float x, float w)
     return x >= 0.0f ? 1.0f - small : small;
 }
 
-// two neighbouring channels c, c + 1 of a row that starts at `row`; those from D on are zero
-template <typename T>
-__device__ __forceinline__ void load_channels(const Args &p, const void *base, long long row, long long c, float (&x)[2])
+// two or four neighbouring channels
+template <typename T, int G>
+__device__ __forceinline__ void store_some(const Args &p, void *base, long long row, long long c, const float (&x)[G])
 {
-    if (p.pairs) { load<T, 2>(base, row + c, x); return; }
-    float q[1];
-    load<T, 1>(base, row + c, q);
-    x[0] = q[0];
-    x[1] = 0.0f;
-    if (c + 1 < p.D) { load<T, 1>(base, row + c + 1, q); x[1] = q[0]; }
-}
-template <typename T>
-__device__ __forceinline__ void store_channels(const Args &p, void *base, long long row, long long c, const float (&x)[2])
-{
-    if (p.pairs) { store<T, 2>(base, row + c, x); return; }
-    const float lo[1] = {x[0]}, hi[1] = {x[1]};
-    store<T, 1>(base, row + c, lo);
-    if (c + 1 < p.D) store<T, 1>(base, row + c + 1, hi);
-}
-// four neighbouring channels
-template <typename T>
-__device__ __forceinline__ void store_four(const Args &p, void *base, long long row, long long c, const float (&x)[4])
-{
-    if (p.four) {
-        if (c < p.D) store<T, 4>(base, row + c, x);
+    if (G == 2 ? p.pairs : p.four) {
+        if (c < p.D) store<T, G>(base, row + c, x);
         return;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < G; ++j) {
         const float q[1] = {x[j]};
         if (c + j < p.D) store<T, 1>(base, row + c + j, q);
     }
@@ -117,11 +98,13 @@ __device__ __forceinline__ T load_raw_one(const void *base, long long at)
     const T *p = (const T *)base + at;
     return relay_in_bounds(p, sizeof(T)) ? *p : T(0.0f);
 }
-// four neighbouring values in shared memory, as fp32
+// two or four neighbouring values in shared memory, as fp32
 __device__ __forceinline__ void widen_shared(const __nv_bfloat16 *p, float (&x)[4]) { widen(*reinterpret_cast<const uint2 *>(p), x, __nv_bfloat16()); }
 __device__ __forceinline__ void widen_shared(const float *p, float (&x)[4]) { unpack(*reinterpret_cast<const uint4 *>(p), x); }
-__device__ __forceinline__ void widen_two(const __nv_bfloat16 *p, float (&x)[2]) { widen(*reinterpret_cast<const uint32_t *>(p), x, __nv_bfloat16()); }
-__device__ __forceinline__ void widen_two(const float *p, float (&x)[2]) { widen(*reinterpret_cast<const uint2 *>(p), x, float()); }
+__device__ __forceinline__ void widen_shared(const __nv_bfloat16 *p, float (&x)[2]) { widen(*reinterpret_cast<const uint32_t *>(p), x, __nv_bfloat16()); }
+__device__ __forceinline__ void widen_shared(const float *p, float (&x)[2]) { widen(*reinterpret_cast<const uint2 *>(p), x, float()); }
+__device__ __forceinline__ void shared_values(const float *p, float (&x)[2]) { widen_shared(p, x); }
+__device__ __forceinline__ void shared_values(const float *p, float (&x)[4]) { widen_shared(p, x); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 

@@ -142,9 +142,9 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
         const long long t0 = (long long)chunk * STEPS, row = ((t0 + pt) * p.B + i) * p.D;
         if (t0 + pt < p.T && two < p.D) {
             const float zero[2] = {0.0f, 0.0f};
-            store_channels<T>(p, p.du, row, two, zero);
-            store_channels<T>(p, p.ddelta, row, two, zero);
-            if (p.dz) store_channels<T>(p, p.dz, row, two, zero);
+            store_some<T>(p, p.du, row, two, zero);
+            store_some<T>(p, p.ddelta, row, two, zero);
+            if (p.dz) store_some<T>(p, p.dz, row, two, zero);
         }
         for (int q = tid; q < STEPS * 2 * p.N; q += THREADS) {
             const int t = q / (2 * p.N), n = q - t * 2 * p.N;
@@ -168,9 +168,9 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
         const bool inside = pt < in;
         {
             float u[2], x[2], z[2], dy[2], lo, hi;
-            widen_two(&g.u[pt][pc], u);
-            widen_two(&g.delta[pt][pc], x);
-            widen_two(&g.dy[pt][pc], dy);
+            widen_shared(&g.u[pt][pc], u);
+            widen_shared(&g.delta[pt][pc], x);
+            widen_shared(&g.dy[pt][pc], dy);
             f32x2 step = add2(pair(x[0], x[1]), bias);
             float slope[2] = {1.0f, 1.0f}, gate[2] = {0.0f, 0.0f};
             if (p.softplus) {
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
                 step = q.value;
             }
             if (p.z) {
-                widen_two(&g.z[pt][pc], z);
+                widen_shared(&g.z[pt][pc], z);
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const float q = logistic<FINE>(z[j]);
@@ -383,14 +383,14 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
             float x[2];
             const long long row = ((t0 + pt) * p.B + i) * p.D;
             unpair(du, x[0], x[1]);
-            store_channels<T>(p, p.du, row, two, x);
+            store_some<T>(p, p.du, row, two, x);
             unpair(ddelta, x[0], x[1]);
-            store_channels<T>(p, p.ddelta, row, two, x);
+            store_some<T>(p, p.ddelta, row, two, x);
             if (p.dz) {
                 const float2 pl = *reinterpret_cast<const float2 *>(&s.plain[pt][pc]);
                 unpair(mul2(pair(gz.x, gz.y), fma2(skip, uu, pair(pl.x, pl.y))), x[0], x[1]);
                 if (!inside) x[0] = x[1] = 0.0f;
-                store_channels<T>(p, p.dz, row, two, x);
+                store_some<T>(p, p.dz, row, two, x);
             }
         }
         if (p.N == S::NP) {
