@@ -97,9 +97,12 @@ struct Tile {
     Stage stage[STAGES];
     alignas(16) float2 step[STEPS][CHANNELS];              // delta, delta u
     alignas(16) float b[STEPS][NP], c[STEPS][NP];
-    alignas(16) float y[STEPS][4][CHANNELS];               // the four lanes' parts of sum_n c h
-    ulonglong2 left[NB][THREADS];                          // for the cluster: the state from zero, the sum of steps
-    float sum[THREADS];
+    // The four lanes' parts of sum_n c h, channel ch of lane l at ch ^ 8 (l >> 1): no two lanes of a warp in one bank.  Between the passes of a
+    // shared sequence: the state from zero and the sum of steps of every lane, for the cluster.
+    union {
+        alignas(16) float y[STEPS][4][CHANNELS];
+        struct { ulonglong2 left[NB][THREADS]; float sum[THREADS]; };
+    };
     uint64_t full[STAGES];
     int gave_up;
 };
@@ -300,7 +303,7 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
                     y = k ? fma2(c.x, h[k][0], y) : mul2(c.x, h[k][0]);
                     y = fma2(c.y, h[k][1], y);
                 }
-                if (RESULTS) s.y[r0 + r][nl][ch] = sum2(y);
+                if (RESULTS) s.y[r0 + r][nl][ch ^ ((nl >> 1) << 3)] = sum2(y);
             }
         }
     };
@@ -359,7 +362,7 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
             float q[G];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&s.y[t][j][pc]);
+                const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&s.y[t][j][pc ^ ((j >> 1) << 3)]);
                 out[0] = j ? add2(out[0], v.x) : v.x;
                 out[1] = j ? add2(out[1], v.y) : v.y;
             }
