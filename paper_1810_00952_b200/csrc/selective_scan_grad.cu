@@ -10,7 +10,7 @@ using namespace scan;
 
 // A block: sixteen channels of a batch element, eight warps; a lane has two neighbouring channels and four neighbouring states of every sixteen,
 // and each warp a run of RUN steps of the chunk, which is the span whose starting states the forward call saved.  The runs' products and sums
-// meet in shared memory in both directions at once.  Chunks are taken from the last to the first; rows are fetched a chunk ahead by TMA.
+// meet in shared memory, in both directions at once.  Chunks are taken from the last to the first; rows are fetched a chunk ahead by TMA.
 constexpr int RUN = 4, WT = kSpan / RUN, STEPS = kSpan, CHANNELS = 16, THREADS = 32 * WT, STAGES = 2;
 
 template <typename T, int NB>
@@ -21,8 +21,10 @@ struct Tile {
     alignas(16) float2 step[STEPS][CHANNELS];              // delta, delta u
     alignas(16) float e[STEPS][CHANNELS];                  // dy silu(z)
     alignas(16) float b[STEPS][NP], c[STEPS][NP];
+    // Of every run: its decay, the state it leaves from zero, what flows back through it from zero.  Joined in place, a thread each of the
+    // 256 chains of states: the state a run starts from, and what flows back into it.
     ulonglong2 decay[SLOTS][WT][2][32], sum[SLOTS][WT][2][32], back[SLOTS][WT][2][32];
-    ulonglong2 carry[2][NB][2][32];                        // what flows back into the chunk
+    float carry[NB == 1 ? 1 : NB][NB == 1 ? 1 : THREADS];  // more than sixteen states: what flows back into the chunk
     alignas(16) float along[STEPS][CHANNELS], kept[STEPS][CHANNELS], plain[STEPS][CHANNELS];   // sum_n g b, sum_n a G h[t-1], sum_n c h
     alignas(16) float dbc[STEPS][2 * NP];
     float2 u[THREADS], slope[THREADS], gate[THREADS];      // what a thread needs again at the end of a chunk
@@ -112,15 +114,28 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
     };
 #pragma unroll
     for (int j = 0; j < 2; ++j) dA[j][0] = dA[j][1] = 0;
+    // this thread's chain in the joins: channel and first state of every sixteen
+    const int chain = (tid >> 2 & 31);                     // the lane that holds it
+    const long long chain_d = c0 + (chain >> 2) * 2 + (tid >> 7);
+    const int chain_n = (chain & 3) * 4 + (tid & 3);
+    auto chain_load = [&](const float *base, long long row, int k) {
+        const int n = k * 16 + chain_n;
+        const float *at = base + (row + chain_d) * p.N + n;
+        return base != nullptr && chain_d < p.D && n < p.N && relay_in_bounds(at, 4) ? __ldcs(at) : 0.0f;
+    };
+    auto chain_store = [&](float *base, long long row, int k, float x) {
+        const int n = k * 16 + chain_n;
+        float *at = base + (row + chain_d) * p.N + n;
+        if (base != nullptr && chain_d < p.D && n < p.N && relay_in_bounds(at, 4)) __stcs(at, x);
+    };
+    float carry = 0.0f;
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
+        carry = chain_load(p.dh_final, i * p.D, k);
+        if constexpr (NB > 1) {
+            s.carry[k][tid] = carry;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if constexpr (NB > 1) s.da[k][j][tid] = make_ulonglong2(0, 0);
-            if (wt != 0) continue;
-            float x[4];
-            load_states(p, mine + j < p.D ? p.dh_final : nullptr, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, x);
-            s.carry[0][k][j][lane] = make_ulonglong2(pair(x[0], x[1]), pair(x[2], x[3]));
+            for (int j = 0; j < 2; ++j) s.da[k][j][tid] = make_ulonglong2(0, 0);
         }
     }
     if constexpr (NB == 1) load_a(0);
@@ -155,13 +170,9 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
     for (int done = 0; done < live_chunks; ++done) {
         const long long chunk = live_chunks - 1 - done, t0 = chunk * STEPS;
         typename S::Stage &g = s.stage[done % STAGES];
-        // the states that the first run starts from: on their way while the rows are made fp32
-        float start[2][4];
-        if constexpr (NB == 1) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                load_states(p, mine + j < p.D ? p.states : nullptr, ((chunk * p.B + i) * p.D + mine + j) * p.N, nl * 4, start[j]);
-        }
+        // the state that the first run starts from: on its way while the rows are made fp32
+        float start = 0.0f;
+        if constexpr (NB == 1) start = chain_load(p.states, (chunk * p.B + i) * p.D, 0);
         if (p.tma_x || p.tma_w) tc::mbar_wait(&s.full[done % STAGES], (done / STAGES) & 1, &s.gave_up, p.err, tc::ERR_WAIT_FULL);
         if (!p.tma_x || !p.tma_w) __syncthreads();         // everyone's plain loads
         const int in = (int)min((long long)STEPS, end - t0);                 // steps of the chunk that are inside the sequence
@@ -231,13 +242,9 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
             const int slot = NB == 1 ? 0 : k & 1;
             if constexpr (NB > 1) {
                 load_a(k);
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    load_states(p, mine + j < p.D ? p.states : nullptr, ((chunk * p.B + i) * p.D + mine + j) * p.N, k * 16 + nl * 4, start[j]);
+                start = chain_load(p.states, (chunk * p.B + i) * p.D, k);
+                carry = s.carry[k][tid];
             }
-            f32x2 from[2][2];                              // the state at the start of the chunk, then of this run
-#pragma unroll
-            for (int j = 0; j < 2; ++j) { from[j][0] = pair(start[j][0], start[j][1]); from[j][1] = pair(start[j][2], start[j][3]); }
             f32x2 da[RUN][2][2], h[RUN][2][2];             // decays; what is added, then the states
             {
                 f32x2 P[2][2], H[2][2];
@@ -278,28 +285,31 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
                 for (int j = 0; j < 2; ++j) s.back[slot][wt][j][lane] = make_ulonglong2(H[j][0], H[j][1]);
             }
             __syncthreads();
-            f32x2 G[2][2];                                 // what flows back into this run
+            {
+                float *P = reinterpret_cast<float *>(&s.decay[slot][0][0][0]) + tid, *H = reinterpret_cast<float *>(&s.sum[slot][0][0][0]) + tid;
+                float *R = reinterpret_cast<float *>(&s.back[slot][0][0][0]) + tid, d[WT], x[WT], y[WT];
+#pragma unroll
+                for (int w = 0; w < WT; ++w) { d[w] = P[w * THREADS]; x[w] = H[w * THREADS]; y[w] = R[w * THREADS]; }
+#pragma unroll
+                for (int w = 0; w < WT; ++w) {
+                    H[w * THREADS] = start;
+                    start = fmaf(d[w], start, x[w]);
+                }
+#pragma unroll
+                for (int w = WT - 1; w >= 0; --w) {
+                    R[w * THREADS] = carry;
+                    carry = fmaf(d[w], carry, y[w]);
+                }
+                if constexpr (NB > 1) s.carry[k][tid] = carry;
+            }
+            __syncthreads();
+            f32x2 from[2][2], G[2][2];                     // the state at the start of this run, what flows back into it
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const ulonglong2 v = s.carry[done & 1][k][j][lane];
-                G[j][0] = v.x; G[j][1] = v.y;
+                const ulonglong2 x = s.sum[slot][wt][j][lane], y = s.back[slot][wt][j][lane];
+                from[j][0] = x.x; from[j][1] = x.y;
+                G[j][0] = y.x; G[j][1] = y.y;
             }
-#pragma unroll 2
-            for (int w = 0; w < wt; ++w)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const ulonglong2 d = s.decay[slot][w][j][lane], v = s.sum[slot][w][j][lane];
-                    from[j][0] = fma2(d.x, from[j][0], v.x);
-                    from[j][1] = fma2(d.y, from[j][1], v.y);
-                }
-#pragma unroll 2
-            for (int w = WT - 1; w > wt; --w)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const ulonglong2 d = s.decay[slot][w][j][lane], v = s.back[slot][w][j][lane];
-                    G[j][0] = fma2(d.x, G[j][0], v.x);
-                    G[j][1] = fma2(d.y, G[j][1], v.y);
-                }
 #pragma unroll
             for (int r = 0; r < RUN; ++r)
 #pragma unroll
@@ -361,10 +371,6 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
                 reduce_lanes<8, 4, 8>(w, lane, one);
                 s.dbc[r0 + r][(cl < 4 ? 0 : S::NP) + k * 16 + nl * 4 + (cl & 3)] = one[0];
             }
-            if (wt == 0) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) s.carry[(done + 1) & 1][k][j][lane] = make_ulonglong2(G[j][0], G[j][1]);
-            }
             if constexpr (NB > 1) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) s.da[k][j][tid] = make_ulonglong2(dA[j][0], dA[j][1]);
@@ -417,22 +423,12 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
             else s.sum[0][wt][j][lane] = make_ulonglong2(dA[j][0], dA[j][1]);
         }
         __syncthreads();
-        if (wt != 0) continue;
+        float x = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if (mine + j >= p.D) continue;
-            f32x2 x = 0, y = 0;
-            for (int w = 0; w < WT; ++w) {
-                const ulonglong2 v = s.sum[0][w][j][lane];
-                x = add2(x, v.x); y = add2(y, v.y);
-            }
-            float q[4];
-            unpair(x, q[0], q[1]); unpair(y, q[2], q[3]);
-            store_states(p, p.part_a, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, q);
-            const ulonglong2 v = s.carry[live_chunks & 1][k][j][lane];
-            unpair(v.x, q[0], q[1]); unpair(v.y, q[2], q[3]);
-            store_states(p, p.dh0, (i * p.D + mine + j) * p.N, k * 16 + nl * 4, q);
-        }
+        for (int w = 0; w < WT; ++w) x += reinterpret_cast<const float *>(&s.sum[0][0][0][0])[w * THREADS + tid];
+        chain_store(p.part_a, i * p.D, k, x);
+        if constexpr (NB > 1) carry = s.carry[k][tid];
+        chain_store(p.dh0, i * p.D, k, carry);
     }
     __syncthreads();
     {
