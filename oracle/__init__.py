@@ -23,7 +23,7 @@ _LIB = os.path.join(_HERE, "_relay_oracle.so")
 
 # dtype / activation / opcode / reduction codes (the oracle's own copy of the tables)
 F32, BF16, I32, I64, BOOL, F64 = 0, 1, 2, 3, 4, 5
-ACT_NONE, ACT_RELU, ACT_TANH, ACT_SIGMOID = 0, 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_TANH, ACT_SIGMOID, ACT_SILU = 0, 1, 2, 3, 4
 RED_NONE, RED_SUM, RED_MAX, RED_MEAN, RED_ARGMAX = 0, 1, 2, 3, 4
 
 

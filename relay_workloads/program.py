@@ -23,7 +23,7 @@ F32, BF16, I32, I64, BOOL = 0, 1, 2, 3, 4
 # reduction codes of the C-ABI
 RED_NONE, RED_SUM, RED_MAX, RED_MEAN, RED_ARGMAX = range(5)
 
-ACT_NONE, ACT_RELU, ACT_TANH, ACT_SIGMOID = range(4)
+ACT_NONE, ACT_RELU, ACT_TANH, ACT_SIGMOID, ACT_SILU = range(5)
 
 
 class Program:

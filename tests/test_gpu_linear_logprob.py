@@ -92,11 +92,35 @@ def test_parity(shape, dt, tied):
     check(make(N, K, V, dt, seed=N + V, tied=tied, i64=N % 2 == 0), 1.0 if N % 2 else 0.7)
 
 
+def check64(t, logp, lse, dx, dw, temperature=1.0):
+    """The same comparisons with torch's 64-bit products, for sizes that take NumPy minutes."""
+    x, w, dlogp, tokens = (t[k].to(DEV) for k in ("x", "w", "dlogp", "tokens"))
+    x, w, dlogp, tokens = x.double(), (w.T if t["tied"] else w).double(), dlogp.double(), tokens.long()
+    V = w.shape[1]
+    real = (tokens >= 0) & (tokens < V)
+    z = (x @ w) / temperature
+    want = torch.logsumexp(z, 1)
+    assert float((lse.double() - want).abs().max()) <= 2e-5 * (1 + float(want.abs().max()))
+    rows, at = torch.arange(len(x), device=DEV), tokens.clamp(0, V - 1)
+    wl = torch.where(real, z[rows, at] - want, 0.0)
+    assert float((logp.double() - wl).abs().max()) <= 2e-5 * (1 + float(want.abs().max()) + float(wl.abs().max()))
+    slope = torch.where(real, dlogp, 0.0) / temperature
+    dz = -slope[:, None] * torch.exp(z - want[:, None])
+    size = dz.abs()
+    size[rows, at] += slope.abs()
+    dz[rows, at] += slope
+    flip = (lambda v: v.T) if t["tied"] else (lambda v: v)
+    within(dx, to_np(dz @ w.T), to_np(size @ w.T.abs()), "dx")
+    within(dw, to_np(flip(x.T @ dz)), to_np(flip(x.T.abs() @ size)), "dw")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("tied,K", [(False, 256), (True, 264), (False, 2112), (True, 2112)])
 def test_many_tiles(tied, K):
     """More row blocks and columns than pairs of SMs; contractions on both sides of the length from which units are wider."""
-    check(make(700, K, 9000, BF16, seed=K, tied=tied))
+    t = make(700, K, 9000, BF16, seed=K, tied=tied)
+    logp, lse = forward(t, 1.0)
+    check64(t, logp, lse, *gradient(t, 1.0, lse))
 
 
 @pytest.mark.gpu
@@ -200,19 +224,7 @@ def test_pieces_of_the_vocabulary_join():
         need = B.relay_workspace_bytes_linear_logprob_grad(x, w, tied)
         assert need < N * V * (2 if dt == BF16 else 4)     # less than the scores
         B.relay_linear_logprob_grad(x, w, tied, tokens, 1.0, lse, dlogp, dx.t, dw.t, workspace(need, DEV).fill_(0xFF))
-        x64, w64 = x.double(), (w.T if tied else w).double()
-        z = x64 @ w64
-        want = torch.logsumexp(z, 1)
-        assert float((lse.double() - want).abs().max()) <= 2e-5 * float(want.abs().max())
-        rows = torch.arange(N, device=DEV)
-        dz = -dlogp.double()[:, None] * torch.exp(z - want[:, None])
-        dz[rows, tokens.long()] += dlogp.double()
-        flip = (lambda v: v.T) if tied else (lambda v: v)
-        size = dz.abs()
-        size[rows, tokens.long()] = dlogp.double().abs() * (1 + torch.exp(z[rows, tokens.long()] - want))
-        within(dx.check(), to_np(dz @ w64.T), to_np(size @ w64.T.abs()), "dx")
-        within(dw.check(), to_np(flip(x64.T @ dz)), to_np(flip(x64.T.abs() @ size)), "dw")
-        del z, dz
+        check64(dict(x=x, w=w, tokens=tokens, dlogp=dlogp, tied=tied), logp, lse, dx.check(), dw.check())
     B.relay_poll_status()
 
 
