@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
 #pragma unroll
                 for (int j = 0; j < 4; j += 2) {
                     float decay[2];
-                    unpair(decay2<FINE>(pair(step * (a[k][j] * kLog2e), step * (a[k][j + 1] * kLog2e))), decay[0], decay[1]);
+                    unpair(decay2(pair(step * (a[k][j] * kLog2e), step * (a[k][j + 1] * kLog2e))), decay[0], decay[1]);
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         const int n = k * 16 + nl * 4 + j + q;
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
     const int all = (int)((p.T + STEPS - 1) / STEPS), each = SPLIT ? (all + parts - 1) / parts : all;
     const int first = min(all, part * each), last = min(all, first + each);                  // this block's chunks
     const int live = max(0, min(last, (int)((end + STEPS - 1) / STEPS)) - first);             // those of them inside the sequence
-    // rows of the k-th live chunk into the stage of the q-th fetch, by TMA (one thread) or by everyone's plain loads
+    // rows of the k-th live chunk into the stage of the q-th fetch, by TMA (one thread) or by everyone's own copies
     auto fetch = [&](int q, int k, bool with_z) {
         typename S::Stage &g = s.stage[q % STAGES];
         const long long t0 = (long long)(first + k) * STEPS;
@@ -149,30 +149,20 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
                 if (p.ld_bc == p.N) tc::tma_load_2d(g.bc + STEPS * p.N, &maps.c, full, (int)(i * p.ld_bc), row);
             }
         }
+        const int rows = (int)min((long long)STEPS, end - t0);
         if (!p.tma_x) {
-#pragma unroll 4
-            for (int e = tid; e < STEPS * CHANNELS; e += THREADS) {
-                const int t = e / CHANNELS, c = e % CHANNELS;
-                const long long at = ((t0 + t) * p.B + i) * p.D + c0 + c;
-                if (t0 + t < end && c0 + c < p.D) {
-                    g.u[t][c] = load_raw_one<T>(p.u, at);
-                    g.delta[t][c] = load_raw_one<T>(p.delta, at);
-                    if (with_z) g.z[t][c] = load_raw_one<T>(p.z, at);
-                }
-            }
+            const int width = (int)min((long long)CHANNELS, p.D - c0);
+            const long long at = (t0 * p.B + i) * p.D + c0;
+            copy_rows<T>(&g.u[0][0], CHANNELS, (const T *)p.u + at, p.B * p.D, rows, width, tid, THREADS);
+            copy_rows<T>(&g.delta[0][0], CHANNELS, (const T *)p.delta + at, p.B * p.D, rows, width, tid, THREADS);
+            if (with_z) copy_rows<T>(&g.z[0][0], CHANNELS, (const T *)p.z + at, p.B * p.D, rows, width, tid, THREADS);
         }
         if (!p.tma_w) {
-            const bool packed = p.ld_bc != p.N;
-#pragma unroll 4
-            for (int e = tid; e < STEPS * p.N; e += THREADS) {
-                const int t = e / p.N, n = e - t * p.N;
-                const long long at = ((t0 + t) * p.B + i) * p.ld_bc + n;
-                if (t0 + t < end) {
-                    g.bc[packed ? t * 2 * p.N + n : e] = load_raw_one<T>(p.b, at);
-                    g.bc[packed ? t * 2 * p.N + p.N + n : STEPS * p.N + e] = load_raw_one<T>(p.c, at);
-                }
-            }
+            const long long at = (t0 * p.B + i) * p.ld_bc;
+            copy_rows<T>(g.bc, p.ld_bc, (const T *)p.b + at, p.B * p.ld_bc, rows, p.ld_bc, tid, THREADS);
+            if (p.ld_bc == p.N) copy_rows<T>(g.bc + STEPS * p.N, p.N, (const T *)p.c + at, p.B * p.ld_bc, rows, p.N, tid, THREADS);
         }
+        copies_end();
     };
     int fetched = 0, used = 0;                             // fetches so far, and chunks taken from them
     // this thread's states: of channel mine
@@ -220,7 +210,7 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
     // waits for a chunk's rows; steps and weights in fp32
     auto prepare = [&](const typename S::Stage &g, int in) {
         if (p.tma_x || p.tma_w) tc::mbar_wait(&s.full[used % STAGES], (used / STAGES) & 1, &s.gave_up, p.err, tc::ERR_WAIT_FULL);
-        if (!p.tma_x || !p.tma_w) __syncthreads();         // everyone's plain loads
+        if (!p.tma_x || !p.tma_w) { copies_done(fetched - used - 1); __syncthreads(); }      // everyone's own copies
 #pragma unroll
         for (int k = 0; k < PASSES; ++k) {
             const int t = tid / UNITS + k * (THREADS / UNITS);
@@ -285,8 +275,8 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
 #pragma unroll
                 for (int k = 0; k < NB; ++k) {
                     const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
-                    da[r][k][0] = decay2<FINE>(mul2(dd, a[k][0]));
-                    da[r][k][1] = decay2<FINE>(mul2(dd, a[k][1]));
+                    da[r][k][0] = decay2(mul2(dd, a[k][0]));
+                    da[r][k][1] = decay2(mul2(dd, a[k][1]));
                     x[r][k][0] = mul2(du, b.x);
                     x[r][k][1] = mul2(du, b.y);
                 }
@@ -337,8 +327,8 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
                 const uint32_t from = tc::mapa(tc::smem_u32(&s.left[k][tid]), (uint32_t)r);
                 unsigned long long x, y;
                 asm volatile("ld.shared::cluster.v2.u64 {%0, %1}, [%2];" : "=l"(x), "=l"(y) : "r"(from));
-                h[k][0] = fma2(decay2<FINE>(mul2(pair(total, total), a[k][0])), h[k][0], x);
-                h[k][1] = fma2(decay2<FINE>(mul2(pair(total, total), a[k][1])), h[k][1], y);
+                h[k][0] = fma2(decay2(mul2(pair(total, total), a[k][0])), h[k][0], x);
+                h[k][1] = fma2(decay2(mul2(pair(total, total), a[k][1])), h[k][1], y);
             }
         }
         tc::cluster_sync();                                // every block has read what it needs of the others

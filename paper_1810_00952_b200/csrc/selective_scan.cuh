@@ -108,34 +108,54 @@ __device__ __forceinline__ void shared_values(const float *p, float (&x)[4]) { w
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 
-// 2^x of two exponents.  With bf16 data the hardware's exponential serves: a few units of 2^-24 off, 2e-8 low on average.  A state adds
-// that up over the steps in which it forgets, so fp32 data takes a polynomial whose only error beyond 2e-9 is its last rounding: x = n + f with
-// n the nearest whole number (the low bits of a sum with 1.5 * 2^23), 2^f on |f| <= 1/2 by its Chebyshev expansion up to f^6, n added to
-// the exponent's bits.  Exponents below -126 give zero, above 126 infinity comes a little early.
-template <bool FINE>
+// 2^x of two exponents.  The hardware's exponential is 2e-8 low on average, and a state adds that up over the steps in which it forgets: a
+// thousand of them where |x| is 1/1000.  So up to 1/16 (a memory of 23 steps) the value comes from 2^x = 1 + z + z^2 / 2 + z^3 / 6 + z^4 / 24, z = x log 2,
+// whose only error beyond 2e-9 is its last rounding.
 __device__ __forceinline__ f32x2 decay2(f32x2 x)
 {
-    float lo, hi;
-    if constexpr (!FINE) {
-        unpair(x, lo, hi);
-        return pair(exp2_(lo), exp2_(hi));
-    } else {
-        float a, b, c, d;
-        unpair(x, lo, hi);
-        a = fminf(fmaxf(lo, -126.0f), 127.0f); b = fminf(fmaxf(hi, -126.0f), 127.0f);
-        const f32x2 y = pair(a, b), t = add2(y, pair(12582912.0f, 12582912.0f)), f = add2(y, neg2(add2(t, pair(-12582912.0f, -12582912.0f))));
-        constexpr float of[7] = {1.0f, 6.931471825e-01f, 2.402265072e-01f, 5.550327152e-02f, 9.618025273e-03f, 1.340043265e-03f, 1.546973217e-04f};
-        f32x2 r = pair(of[6], of[6]);
-#pragma unroll
-        for (int k = 5; k >= 0; --k) r = fma2(r, f, pair(of[k], of[k]));
-        unpair(t, c, d);
-        unpair(r, a, b);
-        a = __int_as_float(__float_as_int(a) + (__float_as_int(c) << 23));
-        b = __int_as_float(__float_as_int(b) + (__float_as_int(d) << 23));
-        // far below zero nothing is left; NaN stays NaN
-        a = lo < -126.0f ? 0.0f : lo != lo ? lo : a;
-        b = hi < -126.0f ? 0.0f : hi != hi ? hi : b;
-        return pair(a, b);
+    f32x2 q = fma2(x, pair(9.61812911e-3f, 9.61812911e-3f), pair(5.55041087e-2f, 5.55041087e-2f));
+    q = fma2(q, x, pair(0.240226507f, 0.240226507f));
+    q = fma2(q, x, pair(0.693147181f, 0.693147181f));
+    q = fma2(q, x, pair(1.0f, 1.0f));
+    float a, b, c, d;
+    unpair(x, a, b);
+    unpair(q, c, d);
+    return pair(fabsf(a) <= 0.0625f ? c : exp2_(a), fabsf(b) <= 0.0625f ? d : exp2_(b));
+}
+
+// ---- rows that TMA cannot fetch ------------------------------------------------------------------------------------------
+// A copy of four bytes to shared memory that nothing waits for until copies_done.
+__device__ __forceinline__ void copy_four(void *to, const void *from)
+{
+    if (relay_in_bounds(from, 4)) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(tc::smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// all but the last `younger` (0 or 1) groups of this thread's copies have arrived
+__device__ __forceinline__ void copies_done(int younger)
+{
+    if (younger > 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+// `rows` rows of `width` values from `from`, `ld` values apart, to rows of `to_ld` values; four bytes at a time where both sides' rows are
+// whole four bytes, else one by one (bf16 rows of odd length)
+template <typename T>
+__device__ __forceinline__ void copy_rows(T *to, int to_ld, const T *from, long long ld, int rows, int width, int tid, int threads)
+{
+    constexpr int E = 4 / sizeof(T);
+    if (sizeof(T) == 4 || (ld % 2 == 0 && width % 2 == 0 && ((uintptr_t)from & 3) == 0)) {
+        const int per = width / E;
+        for (int e = tid; e < rows * per; e += threads) {
+            const int t = e / per, c = (e - t * per) * E;
+            copy_four(to + t * to_ld + c, from + t * ld + c);
+        }
+        return;
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll 4
+        for (int e = tid; e < rows * width; e += threads) {
+            const int t = e / width, c = e - t * width;
+            to[t * to_ld + c] = load_raw_one<T>(from, t * ld + c);
+        }
     }
 }
 

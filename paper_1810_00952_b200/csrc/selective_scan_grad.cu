@@ -73,31 +73,21 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
                 if (p.ld_bc == p.N) tc::tma_load_2d(g.bc + STEPS * p.N, &maps.c, full, (int)(i * p.ld_bc), row);
             }
         }
+        const int rows = (int)min((long long)STEPS, end - t0);
         if (!p.tma_x) {
-#pragma unroll
-            for (int e = tid; e < STEPS * CHANNELS; e += THREADS) {
-                const int t = e / CHANNELS, c = e % CHANNELS;
-                const long long at = ((t0 + t) * p.B + i) * p.D + c0 + c;
-                if (t0 + t < end && c0 + c < p.D) {
-                    g.u[t][c] = load_raw_one<T>(p.u, at);
-                    g.delta[t][c] = load_raw_one<T>(p.delta, at);
-                    g.dy[t][c] = load_raw_one<T>(p.dy, at);
-                    if (p.z) g.z[t][c] = load_raw_one<T>(p.z, at);
-                }
-            }
+            const int width = (int)min((long long)CHANNELS, p.D - c0);
+            const long long at = (t0 * p.B + i) * p.D + c0;
+            copy_rows<T>(&g.u[0][0], CHANNELS, (const T *)p.u + at, p.B * p.D, rows, width, tid, THREADS);
+            copy_rows<T>(&g.delta[0][0], CHANNELS, (const T *)p.delta + at, p.B * p.D, rows, width, tid, THREADS);
+            copy_rows<T>(&g.dy[0][0], CHANNELS, (const T *)p.dy + at, p.B * p.D, rows, width, tid, THREADS);
+            if (p.z) copy_rows<T>(&g.z[0][0], CHANNELS, (const T *)p.z + at, p.B * p.D, rows, width, tid, THREADS);
         }
         if (!p.tma_w) {
-            const bool packed = p.ld_bc != p.N;
-#pragma unroll 2
-            for (int e = tid; e < STEPS * p.N; e += THREADS) {
-                const int t = e / p.N, n = e - t * p.N;
-                const long long at = ((t0 + t) * p.B + i) * p.ld_bc + n;
-                if (t0 + t < end) {
-                    g.bc[packed ? t * 2 * p.N + n : e] = load_raw_one<T>(p.b, at);
-                    g.bc[packed ? t * 2 * p.N + p.N + n : STEPS * p.N + e] = load_raw_one<T>(p.c, at);
-                }
-            }
+            const long long at = (t0 * p.B + i) * p.ld_bc;
+            copy_rows<T>(g.bc, p.ld_bc, (const T *)p.b + at, p.B * p.ld_bc, rows, p.ld_bc, tid, THREADS);
+            if (p.ld_bc == p.N) copy_rows<T>(g.bc + STEPS * p.N, p.N, (const T *)p.c + at, p.B * p.ld_bc, rows, p.N, tid, THREADS);
         }
+        copies_end();
     };
     for (int q = 0; q < STAGES && q < live_chunks; ++q) fetch(q);
     const int ch = cl * 2;                                 // this lane's channels: ch, ch + 1 of the block
@@ -174,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
         float start = 0.0f;
         if constexpr (NB == 1) start = chain_load(p.states, (chunk * p.B + i) * p.D, 0);
         if (p.tma_x || p.tma_w) tc::mbar_wait(&s.full[done % STAGES], (done / STAGES) & 1, &s.gave_up, p.err, tc::ERR_WAIT_FULL);
-        if (!p.tma_x || !p.tma_w) __syncthreads();         // everyone's plain loads
+        if (!p.tma_x || !p.tma_w) { copies_done(min(live_chunks - done, STAGES) - 1); __syncthreads(); }   // everyone's own copies
         const int in = (int)min((long long)STEPS, end - t0);                 // steps of the chunk that are inside the sequence
         const bool inside = pt < in;
         {
@@ -257,7 +247,7 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
                         const f32x2 dt = j ? pair(st.z, st.z) : pair(st.x, st.x), du = j ? pair(st.w, st.w) : pair(st.y, st.y);
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
-                            da[r][j][q] = decay2<FINE>(mul2(dt, a[j][q]));
+                            da[r][j][q] = decay2(mul2(dt, a[j][q]));
                             h[r][j][q] = mul2(du, q ? b.y : b.x);
                             H[j][q] = r ? fma2(da[r][j][q], H[j][q], h[r][j][q]) : h[r][j][q];
                             P[j][q] = r ? mul2(da[r][j][q], P[j][q]) : da[r][j][q];
