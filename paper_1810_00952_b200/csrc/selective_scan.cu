@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
     auto chain = [&](auto results) {
         constexpr bool RESULTS = decltype(results)::value;
         constexpr int AT_ONCE = NB == 1 ? 8 : 2;
-#pragma unroll 2
+#pragma unroll (NB == 1 ? 4 : 2)
         for (int r0 = 0; r0 < STEPS; r0 += AT_ONCE) {
             f32x2 da[AT_ONCE][NB][2], x[AT_ONCE][NB][2];
 #pragma unroll
