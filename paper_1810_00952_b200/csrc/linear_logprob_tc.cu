@@ -172,8 +172,8 @@ relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, 
     if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
     p.tokens = q.tokens; p.tokens_i64 = q.tokens_i64;
     p.rows = q.rows; p.V = q.V; p.first = q.first; p.classes = q.classes;
-    p.inv_temperature = q.inv_temperature;
-    p.scale = (float)(1.4426950408889634 * (double)q.inv_temperature);
+    p.inv_temperature = head::score_scale(q.inv_temperature, q.K);
+    p.scale = (float)(1.4426950408889634 * (double)p.inv_temperature);
     const int n_tiles = p.tiles_m * p.tiles_n, pairs = std::min(n_tiles, sms / 2);
     static thread_local UnitTable tb;
     tb.n = 0;
