@@ -1,9 +1,8 @@
 // Pieces shared by the selective scan (selective_scan.cu) and its gradient (selective_scan_grad.cu).
 //
-// Both cut a sequence into chunks and a chunk into runs of a few steps, one run per warp of a row of warps.  A lane holds four
-// neighbouring states of a channel, four lanes a block of sixteen.  Every warp sums its run up from a zero state, once, keeping the decays
-// exp(delta a) in registers (the exponentials are what the forward call is bounded by); the runs' products and sums meet in shared memory,
-// every warp joins those before its own, and the run is summed again from the state that it really starts with.
+// Per step, channel and state: an exponential, and a multiply-add each for its argument, for what is added, for the state and for the
+// result.  With N = 16 the special-function pipe (16 lanes an SM) is what bounds the forward call before memory does: 2048 x 8 x 2048 x 16 are 537 M
+// exponentials and 134 M of steps and gates, 150 us, beside 41 us of bytes.
 #pragma once
 #include "sequence.cuh"
 #include "tc_common.cuh"

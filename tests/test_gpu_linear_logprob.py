@@ -273,3 +273,24 @@ def test_refusals_leave_outputs_untouched(monkeypatch):
     assert B.relay_launch_count() == n0
     assert all(bool((t == 5).all()) for t in (logp, lse, dx, dw))
     assert B.relay_workspace_bytes_linear_logprob(x, w, 1) == 0 and B.relay_workspace_bytes_linear_logprob_grad(x, z(15, 40), 0) == 0
+
+
+@pytest.mark.gpu
+def test_more_rows_than_one_slab_of_statistics():
+    """2^28 bytes of statistics are 33,280 rows of 64,100 classes (1,004 statistics of 8 bytes a row, whole tiles of 256 rows): the rows behind them come in a second slab."""
+    N, K, V = 34000, 64, 64100
+    g = torch.Generator(device=DEV).manual_seed(8)
+    x, w = torch.randn(N, K, generator=g, device=DEV).to(BF16), (0.2 * torch.randn(V, K, generator=g, device=DEV)).to(BF16)
+    tokens = torch.randint(0, V, (N,), generator=g, device=DEV)
+    logp, lse = Guarded((N,), F32, DEV), Guarded((N,), F32, DEV)
+    need = B.relay_workspace_bytes_linear_logprob(x, w, True)
+    assert need < 3 << 27
+    B.relay_linear_logprob(x, w, True, tokens, 1.0, logp.t, lse.t, workspace(need, DEV).fill_(0xFF))
+    logp, lse = logp.check(), lse.check()
+    for rows in (slice(0, 300), slice(33000, N)):
+        z = x[rows].double() @ w.double().T
+        want = torch.logsumexp(z, 1)
+        assert float((lse[rows].double() - want).abs().max()) <= 2e-5 * (1 + float(want.abs().max()))
+        at = z.gather(1, tokens[rows, None])[:, 0] - want
+        assert float((logp[rows].double() - at).abs().max()) <= 2e-5 * (1 + 2 * float(want.abs().max()) + float(at.abs().max()))
+    B.relay_poll_status()
