@@ -388,9 +388,17 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
 static_assert(STEPS == kSpan, "a chunk starts where a state is saved");
 
 // ---- launches ------------------------------------------------------------------------------------------------------
-// Up to here step by step: 64 x 2048 channels 30 us for 8 steps against 43 by chunks, 51 against 43 for 16; 4 x 2048 channels 15 against 17
-// and 16 against 16.
-constexpr long long kFewSteps = 10, kSms = 148;
+// Up to few_steps() step by step, longer ones by chunks, whose time grows with the number of chunks alone.  bf16, 64 x 2048 channels, us step by step and
+// by chunks: N = 16, 8 steps 40 and 43, 10 steps 49 and 44; N = 32, 10 steps 73 and 80, 12 steps 86 and 80; N = 64, 16 steps 150 and 158, 20 steps 182 and 161.
+// Few channels wait for each step's rows in turn: 4 x 2048, N = 16, 4 steps 8.4 and 8.7, 8 steps 13.6 and 8.7; 10 x 2048, 5 steps 10.5 and 11.8, 8 steps
+// 15.1 and 11.8; 16 x 2048, 8 steps 15.4 and 14.8.
+constexpr long long kSms = 148;
+
+template <int NB>
+long long few_steps(const Args &p)
+{
+    return p.B * p.D < 32768 ? 4 : NB == 1 ? 8 : NB == 2 ? 12 : 16;
+}
 
 template <typename T, int NB>
 relay_status_t launch_steps(const Args &p, cudaStream_t st)
@@ -418,20 +426,22 @@ relay_status_t launch_chunks(Args p, int parts, cudaStream_t st)
         RELAY_CUDA(launch_pdl(selective_scan_kernel<T, NB, SPLIT>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, p, maps, parts));
     return check_launch("selective_scan");
 }
-// Blocks that share a sequence: as many as give every SM eight warps, with four chunks each at least.  What the second pass costs them is half as
-// much again: 2048 x 8 x 2048 x 16 (2048 warps) 322 us alone and 463 shared by two, 4096 x 4 569 and 519, 8192 x 2 764, 880 (two), 530
-// (four) and 521, 16384 x 1 1290, 1260 (two), 857 (four) and 529 (eight).
+// Blocks that share a sequence.  A second pass costs them three quarters as much again, so it pays where one pass leaves most of the chip empty, and
+// later with more states, whose blocks hold more of it.  us alone, by four and by eight; bf16, N = 16: 2048 steps of 2048 warps 345, 575, 610; 4096
+// of 1024 505, 598, 587; 4096 of 640 447, 496, 397; 8192 of 512 768, 603, 602; 16384 of 256 1490, 851, 603; 256 of 512 28, 25, 30; 256 of 256 27, 21, 17;
+// 256 of 128 27, 16, 14; 128 of 256 16, 13.  f32: 2048 of 640 258, 242, 244; 256 of 512 31, 39, 38; 256 of 256 29, 21, 26.  N = 64: 2048 of 512 538,
+// 554, 572; 2048 of 256 472, 280, 289; 256 of 256 63, 43, 55.
 int parts_of(const Args &p)
 {
     const long long warps = p.B * ((p.D + 7) / 8), chunks = (p.T + STEPS - 1) / STEPS;
-    int parts = 1;
-    while (parts < 8 && warps * parts < 8 * kSms && chunks >= 8 * parts) parts *= 2;
-    return parts;
+    if (warps > (p.N <= 16 ? 5 : 3) * kSms) return 1;
+    if (chunks >= (warps <= kSms ? 8 : 16)) return 8;
+    return warps <= 2 * kSms && chunks >= 4 ? 4 : 1;
 }
 template <typename T, int NB>
 relay_status_t launch_form(const Args &p, cudaStream_t st)
 {
-    if (p.T <= kFewSteps) return launch_steps<T, NB>(p, st);
+    if (p.T <= few_steps<NB>(p)) return launch_steps<T, NB>(p, st);
     const int parts = parts_of(p);
     return parts > 1 ? launch_chunks<T, NB, true>(p, parts, st) : launch_chunks<T, NB, false>(p, 1, st);
 }
