@@ -51,17 +51,20 @@ __device__ __forceinline__ long long end_of(const Args &p, long long i)
 
 // softplus(x) = max(x, 0) + log(1 + w), w = exp(-|x|) <= 1, of two values, and its slope, the logistic function.  log(1 + w) = w q(w), q
 // the expansion of log(1 + w) / w in Chebyshev polynomials on [0,1] up to the ninth (5e-9 off): steps are small numbers, and a relative
-// error in one moves a whole state.  w = 2^t with what the rounding of t = -|x| log2(e) left put back.
+// error in one moves a whole state.  w = 2^t with what the rounding of t = -|x| log2(e) left put back; from 128 on w is zero, and x may be infinite
+// (a step of -inf is one of no length) or so large that t would be.
 struct Softplus { f32x2 value, w; };
+__device__ __forceinline__ float down_to_128(float x) { float y; asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(-fabsf(x)), "f"(-128.0f)); return y; }
 __device__ __forceinline__ Softplus softplus2(f32x2 x)
 {
     constexpr float of[10] = {1.0f, -4.999990463e-01f, 3.333000541e-01f, -2.495455891e-01f, 1.967811733e-01f, -1.531186253e-01f, 1.061426476e-01f,
                               -5.706420168e-02f, 1.990716159e-02f, -3.256378463e-03f};
-    const f32x2 m = x | 0x8000000080000000ull;                             // -|x|
+    float a, b;
+    unpair(x, a, b);
+    const f32x2 m = pair(down_to_128(a), down_to_128(b));                  // -|x|
     const f32x2 t = mul2(m, pair(kLog2e, kLog2e));
     f32x2 left = fma2(m, pair(kLog2e, kLog2e), neg2(t));
     left = fma2(m, pair(1.925963033e-8f, 1.925963033e-8f), left);          // log2(e) beyond fp32
-    float a, b;
     unpair(t, a, b);
     const f32x2 p = pair(exp2_(a), exp2_(b)), w = fma2(p, mul2(left, pair(0.693147181f, 0.693147181f)), p);
     f32x2 r = pair(of[9], of[9]);
@@ -102,8 +105,6 @@ __device__ __forceinline__ void widen_shared(const __nv_bfloat16 *p, float (&x)[
 __device__ __forceinline__ void widen_shared(const float *p, float (&x)[4]) { unpack(*reinterpret_cast<const uint4 *>(p), x); }
 __device__ __forceinline__ void widen_shared(const __nv_bfloat16 *p, float (&x)[2]) { widen(*reinterpret_cast<const uint32_t *>(p), x, __nv_bfloat16()); }
 __device__ __forceinline__ void widen_shared(const float *p, float (&x)[2]) { widen(*reinterpret_cast<const uint2 *>(p), x, float()); }
-__device__ __forceinline__ void shared_values(const float *p, float (&x)[2]) { widen_shared(p, x); }
-__device__ __forceinline__ void shared_values(const float *p, float (&x)[4]) { widen_shared(p, x); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 

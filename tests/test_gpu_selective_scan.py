@@ -224,6 +224,18 @@ def test_steep_decays_and_long_steps(dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("T", [3, 80, 300])
+def test_steps_of_no_length(T, dt):
+    """delta of -inf or of the type's lowest value: softplus is zero there, the state stays, and no partial passes through."""
+    t = make(T, 2, 20, 16, dt, seed=12)
+    t["delta"][::2, :, :10] = float("-inf")
+    t["delta"][1::3, :, 5:] = torch.finfo(dt).min
+    t["delta"][T - 1, 0] = float("-inf")
+    check(t)
+
+
+@pytest.mark.gpu
 def test_nan_stays_in_its_channel_and_behind_its_step():
     for T in (4, 80):
         t = make(T, 2, 20, 16, F32, seed=10)
