@@ -226,10 +226,12 @@ int64_t piece_of(int64_t V, int64_t other)
 }
 bool rows_fit(const Sizes &s, bool trans_w) { return (trans_w ? s.K : s.V) % 8 == 0; }                // rows of w are whole 16 bytes
 
-// The forward call takes as many rows at a time as have a quarter of a gigabyte of partial statistics, whole tiles of 256.
+// The forward call takes as many rows at a time as have a quarter of a gigabyte of partial statistics, whole tiles of 256; in fp32 as many as
+// have a whole piece of scores.
 int64_t slab_of(const Sizes &s, bool bf16)
 {
-    const int64_t per_row = (bf16 ? head::parts_of(s.V) : 1) * (int64_t)sizeof(float2);
+    if (!bf16) return std::min<int64_t>(s.rows, kPieceElements / 256);
+    const int64_t per_row = head::parts_of(s.V) * (int64_t)sizeof(float2);
     return std::min<int64_t>(s.rows, std::max<int64_t>(256, (1ll << 28) / per_row / 256 * 256));
 }
 

@@ -294,3 +294,24 @@ def test_more_rows_than_one_slab_of_statistics():
         at = z.gather(1, tokens[rows, None])[:, 0] - want
         assert float((logp[rows].double() - at).abs().max()) <= 2e-5 * (1 + 2 * float(want.abs().max()) + float(at.abs().max()))
     B.relay_poll_status()
+
+
+@pytest.mark.gpu
+def test_more_rows_than_one_slab_of_scores():
+    """f32: 2^27 scores are 524,288 rows of 256 classes, the smallest piece; the rows behind them come in a second slab."""
+    N, K, V = 525000, 8, 300
+    g = torch.Generator(device=DEV).manual_seed(9)
+    x, w = torch.randn(N, K, generator=g, device=DEV), torch.randn(K, V, generator=g, device=DEV)
+    tokens = torch.randint(0, V, (N,), generator=g, device=DEV)
+    logp, lse = Guarded((N,), F32, DEV), Guarded((N,), F32, DEV)
+    need = B.relay_workspace_bytes_linear_logprob(x, w, False)
+    assert need < 5 << 27                                   # 2^27 scores of 4 bytes and a little
+    B.relay_linear_logprob(x, w, False, tokens, 1.0, logp.t, lse.t, workspace(need, DEV).fill_(0xFF))
+    logp, lse = logp.check(), lse.check()
+    for rows in (slice(0, 300), slice(524000, N)):
+        z = x[rows].double() @ w.double()
+        want = torch.logsumexp(z, 1)
+        assert float((lse[rows].double() - want).abs().max()) <= 2e-5 * (1 + float(want.abs().max()))
+        at = z.gather(1, tokens[rows, None])[:, 0] - want
+        assert float((logp[rows].double() - at).abs().max()) <= 2e-5 * (1 + 2 * float(want.abs().max()) + float(at.abs().max()))
+    B.relay_poll_status()
