@@ -481,6 +481,6 @@ extern "C" relay_status_t relay_causal_conv_grad(const relay_tensor_t *x, const 
     if (s.B > 0)
         RELAY_TRY(x->dtype == RELAY_F32 ? gradient_channels<float>(p, st) : gradient_channels<__nv_bfloat16>(p, st));
     const long long rows = s.B > 0 ? gradient_parts(s.T, p.C, p.D) * s.B : 0;
-    return seq::launch_column_sums((const float *)ws, rows, (K + 1) * s.D, (K + 1) * s.D, dw ? (float *)dw->data : nullptr, K * s.D,
-                                   db ? (float *)db->data : nullptr, st);
+    return seq::launch_column_sums((const float *)ws, rows, {{dw ? (float *)dw->data : nullptr, db ? (float *)db->data : nullptr, nullptr}, {K * s.D, s.D, 0}},
+                                   st);
 }

@@ -30,7 +30,7 @@ struct Args {
     void *du, *ddelta, *dz;                // [T][B][D]; dz or null
     float *dh0;                            // [B][D][N] or null
     float *part_bc;                        // [groups][T * B][2N]: each group of channels' sums of db and dc
-    float *part_a, *part_d, *part_bias;    // [B][D][N], [B][D], [B][D]; the last two or null
+    float *part_a;                         // [B][D N | D | D]: each batch element's sums of da, dd and ddelta_bias
     long long T, B, D;
     int N, ld_bc, softplus, groups;
     int pairs;                             // two neighbouring channels are one aligned access
@@ -142,10 +142,13 @@ __device__ __forceinline__ void copy_rows(T *to, int to_ld, const T *from, long 
 {
     constexpr int E = 4 / sizeof(T);
     if (sizeof(T) == 4 || (ld % 2 == 0 && width % 2 == 0 && ((uintptr_t)from & 3) == 0)) {
-        const int per = width / E;
-        for (int e = tid; e < rows * per; e += threads) {
-            const int t = e / per, c = (e - t * per) * E;
-            copy_four(to + t * to_ld + c, from + t * ld + c);
+        const int per = width / E, down = threads / per, along = threads - down * per;
+        int t = tid / per, c = tid - t * per;
+        while (t < rows) {
+            copy_four(to + t * to_ld + c * E, from + t * ld + c * E);
+            t += down;
+            c += along;
+            if (c >= per) { c -= per; ++t; }
         }
         return;
     }

@@ -403,10 +403,15 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
                 if (t0 + t < p.T && relay_in_bounds(out, 16)) __stcs((float4 *)out, *reinterpret_cast<const float4 *>(&s.dbc[t][n]));
             }
         } else {
-            for (int q = tid; q < STEPS * 2 * p.N; q += THREADS) {
-                const int t = q / (2 * p.N), n = q - t * 2 * p.N;
-                float *out = p.part_bc + (((long long)group * p.T + t0 + t) * p.B + i) * 2 * p.N + n;
-                if (t0 + t < p.T && relay_in_bounds(out, 4)) __stcs(out, s.dbc[t][n < p.N ? n : S::NP + n - p.N]);
+            const int N = p.N, down = THREADS / (2 * N), along = THREADS - down * 2 * N, rows = (int)min((long long)STEPS, p.T - t0);
+            const long long step = p.B * 2 * N;
+            float *first = p.part_bc + (((long long)group * p.T + t0) * p.B + i) * 2 * N;
+            for (int t = tid / (2 * N), n = tid - t * 2 * N; t < rows;) {
+                float *out = first + t * step + n;
+                if (relay_in_bounds(out, 4)) __stcs(out, s.dbc[t][n < N ? n : S::NP + n - N]);
+                t += down;
+                n += along;
+                if (n >= 2 * N) { n -= 2 * N; ++t; }
             }
         }
     }
@@ -423,7 +428,7 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
         float x = 0.0f;
 #pragma unroll
         for (int w = 0; w < WT; ++w) x += reinterpret_cast<const float *>(&s.sum[0][0][0][0])[w * THREADS + tid];
-        chain_store(p.part_a, i * p.D, k, x);
+        chain_store(p.part_a + i * 2 * p.D, i * p.D, k, x);
         if constexpr (NB > 1) carry = s.carry[k][tid];
         chain_store(p.dh0, i * p.D, k, carry);
     }
@@ -437,9 +442,9 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
     if (tid < CHANNELS && c0 + tid < p.D) {
         float x = 0.0f, y = 0.0f;
         for (int t = 0; t < STEPS; ++t) { x += s.step[t][tid].x; y += s.step[t][tid].y; }
-        const long long at = i * p.D + c0 + tid;
-        if (p.part_d && relay_in_bounds(p.part_d + at, 4)) p.part_d[at] = x;
-        if (p.part_bias && relay_in_bounds(p.part_bias + at, 4)) p.part_bias[at] = y;
+        float *at = p.part_a + i * p.D * (p.N + 2) + p.D * p.N + c0 + tid;
+        if (relay_in_bounds(at, 4)) *at = x;
+        if (relay_in_bounds(at + p.D, 4)) at[p.D] = y;
     }
 }
 
@@ -464,14 +469,12 @@ __global__ void __launch_bounds__(256) join_weights_kernel(const float *part, lo
 
 // ---- workspace: partial sums of db and dc, of da, dd and ddelta_bias ----------------------------------------------------
 int64_t groups_of(int64_t D) { return (D + CHANNELS - 1) / CHANNELS; }
-struct Parts { size_t bc, a, d, bias, bytes; };
+struct Parts { size_t a, bytes; };                         // the first are at the start
 Parts parts_of(const Sizes &s, int64_t N)
 {
     Parts q{};
     q.a = align_up((size_t)groups_of(s.D) * s.T * s.B * 2 * N * sizeof(float), 256);
-    q.d = q.a + align_up((size_t)s.B * s.D * N * sizeof(float), 256);
-    q.bias = q.d + align_up((size_t)s.B * s.D * sizeof(float), 256);
-    q.bytes = q.bias + align_up((size_t)s.B * s.D * sizeof(float), 256);
+    q.bytes = q.a + align_up((size_t)s.B * s.D * (N + 2) * sizeof(float), 256);
     return q;
 }
 
@@ -579,12 +582,8 @@ extern "C" relay_status_t relay_selective_scan_grad(const relay_tensor_t *u, con
     char *w = (char *)ws;
     p.part_bc = (float *)w;
     p.part_a = (float *)(w + q.a);
-    p.part_d = dd ? (float *)(w + q.d) : nullptr;
-    p.part_bias = ddelta_bias ? (float *)(w + q.bias) : nullptr;
     void *dcp = dc ? dc->data : nullptr;
     RELAY_TRY(t == RELAY_F32 ? launch_gradient<float>(p, db->data, dcp, st) : launch_gradient<__nv_bfloat16>(p, db->data, dcp, st));
-    RELAY_TRY(seq::launch_column_sums(p.part_a, s.B, s.D * N, s.D * N, (float *)da->data, s.D * N, nullptr, st));
-    if (dd) RELAY_TRY(seq::launch_column_sums(p.part_d, s.B, s.D, s.D, (float *)dd->data, s.D, nullptr, st));
-    if (ddelta_bias) RELAY_TRY(seq::launch_column_sums(p.part_bias, s.B, s.D, s.D, (float *)ddelta_bias->data, s.D, nullptr, st));
-    return RELAY_OK;
+    return seq::launch_column_sums(p.part_a, s.B, {{(float *)da->data, dd ? (float *)dd->data : nullptr, ddelta_bias ? (float *)ddelta_bias->data : nullptr},
+                                                   {s.D * N, s.D, s.D}}, st);
 }

@@ -7,8 +7,7 @@ namespace {
 
 constexpr int kGroups = 8;          // rows are dealt to this many threads per column
 
-__global__ void __launch_bounds__(32 * kGroups) column_sums_kernel(const float *in, long long rows, long long cols, long long ld, float *out0,
-                                                                   long long n0, float *out1)
+__global__ void __launch_bounds__(32 * kGroups) column_sums_kernel(const float *in, long long rows, long long cols, const ColumnSums to)
 {
     __shared__ float part[kGroups][32];
     pdl_wait();
@@ -17,7 +16,7 @@ __global__ void __launch_bounds__(32 * kGroups) column_sums_kernel(const float *
     if (c < cols) {
 #pragma unroll 4
         for (long long r = threadIdx.y; r < rows; r += kGroups) {
-            const float *p = in + r * ld + c;
+            const float *p = in + r * cols + c;
             if (relay_in_bounds(p, 4)) sum += __ldcs(p);
         }
     }
@@ -26,21 +25,26 @@ __global__ void __launch_bounds__(32 * kGroups) column_sums_kernel(const float *
     if (threadIdx.y != 0 || c >= cols) return;
 #pragma unroll
     for (int g = 1; g < kGroups; ++g) sum += part[g][threadIdx.x];
-    float *out = c < n0 ? out0 : out1;
-    if (out == nullptr) return;
-    out += c < n0 ? c : c - n0;
-    if (relay_in_bounds(out, 4)) *out = sum;
+    long long first = 0;
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        float *out = to.out[k] + (c - first);
+        if (c >= first && c < first + to.n[k] && to.out[k] != nullptr && relay_in_bounds(out, 4)) *out = sum;
+        first += to.n[k];
+    }
 }
 
 }  // namespace
 
-relay_status_t launch_column_sums(const float *in, long long rows, long long cols, long long ld, float *out0, long long n0, float *out1,
-                                  cudaStream_t st)
+relay_status_t launch_column_sums(const float *in, long long rows, const ColumnSums &to, cudaStream_t st)
 {
-    if (cols == 0 || (out0 == nullptr && out1 == nullptr)) return RELAY_OK;
+    long long cols = 0;
+    bool wanted = false;
+    for (int k = 0; k < kSums; ++k) { cols += to.n[k]; wanted |= to.n[k] > 0 && to.out[k] != nullptr; }
+    if (!wanted) return RELAY_OK;
     const long long blocks = (cols + 31) / 32;
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "%lld columns", cols);
-    RELAY_CUDA(launch_pdl(column_sums_kernel, dim3((unsigned)blocks), dim3(32, kGroups), 0, st, in, rows, cols, ld, out0, n0, out1));
+    RELAY_CUDA(launch_pdl(column_sums_kernel, dim3((unsigned)blocks), dim3(32, kGroups), 0, st, in, rows, cols, to));
     return check_launch("column_sums");
 }
 

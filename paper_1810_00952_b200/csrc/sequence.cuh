@@ -132,10 +132,11 @@ __device__ __forceinline__ float logistic(float x)
     else return rcp_(1.0f + exp2_(-1.44269504f * x));     // 1 / inf = 0 far below zero, as it should be
 }
 
-// Sums of the columns of partial sums (rows,cols), rows `ld` entries apart, in a fixed order: the first n0 columns to out0, the others
-// to out1 (either may be null: not wanted).
-relay_status_t launch_column_sums(const float *in, long long rows, long long cols, long long ld, float *out0, long long n0, float *out1,
-                                  cudaStream_t st);
+// Sums of the columns of partial sums (rows,cols) in a fixed order: the first n[0] columns to out[0], the next n[1] to out[1] and so on, cols
+// in all (an out may be null: not wanted).
+constexpr int kSums = 3;
+struct ColumnSums { float *out[kSums]; long long n[kSums]; };
+relay_status_t launch_column_sums(const float *in, long long rows, const ColumnSums &to, cudaStream_t st);
 
 // ---- checks ----------------------------------------------------------------------------------------------------
 // an optional tensor of one of two base types and the given extents
