@@ -1,13 +1,15 @@
 // Short causal convolution of a sequence, one filter of K taps per channel, and its gradient group:
 //   s_t = b + sum_k w[k] x_{t-K+1+k},  y_t = act(s_t)
 // The forward group reads x and writes y once, the gradient reads x and dy and writes dx once; K multiply-adds an element, and two
-// instructions of the special-function pipe an element for the activation.  Measured, bf16, K = 4, silu: 8192 x 2 x 4096 57 us (4.7 TB/s of 6.56 copied;
-// 57 % of issue slots, 48 % of the special-function pipe, 31 % of the warps there are: registers hold the window, the filter and the rows on their
-// way), gradient of 2048 x 8 x 2048 72 us with its column sums (2.8 TB/s; 62 % of issue slots: window, slopes and sums shift every step).
+// instructions of the special-function pipe an element for the activation.  Measured, K = 4, silu: 8192 x 2 x 4096 54 us in bf16 (5.0 TB/s of 6.56
+// copied) and 107 in fp32, gradient of 2048 x 8 x 2048 with its column sums 71 us (2.8 TB/s) and 98.  Counters before the rows inside a span had code
+// without conditions (57, 169, 73, 106 us): 57 and 62 % of issue slots, 48 and 25 % of the special-function pipe, 31 and 23 % of the warps there are:
+// registers hold the window, the filter, the slopes and the rows on their way.
 // A thread owns V consecutive channels and a span of steps; the K - 1 inputs before the current one stay in its registers, and at the
 // start of a span they are read again (K - 1 rows in S).  The gradient walks a span forwards and K - 1 steps beyond it: the partial of an
 // input needs those of the K sums that it entered.
 #include <algorithm>
+#include <type_traits>
 
 #include "sequence.cuh"
 
@@ -108,18 +110,14 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const Args p)
     const int steps = (int)(t1 - t0), inside = (int)min(max(end - t0, 0ll), (long long)steps);
     const unsigned bytes = (unsigned)(p.C * sizeof(T));    // of a row
     Raw<T, V> raw[U];
-    auto fetch = [&](int n) {                              // rows n .. n + U - 1 of the span
+    auto fetch = [&](int n, auto whole) {                  // rows n .. n + U - 1 of the span; whole: all inside the sequence
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            raw[u] = Raw<T, V>{};
-            if (n + u < inside) raw[u] = load_row<T, V>(row, (unsigned)(n + u) * bytes);
+            if constexpr (!whole) raw[u] = Raw<T, V>{};
+            if (whole || n + u < inside) raw[u] = load_row<T, V>(row, (unsigned)(n + u) * bytes);
         }
     };
-    fetch(0);
-    for (int n = 0; n < steps; n += U) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) widen(raw[u], x[KP - 1 + u], T());
-        fetch(n + U);
+    auto results = [&](int n, auto whole) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float y[V];
@@ -132,12 +130,23 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const Args p)
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] *= logistic<FINE>(y[i]);
             }
-            if (n + u >= inside) {
+            if (!whole && n + u >= inside) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = 0.0f;
             }
-            if (n + u < steps) store_row<T, V>(to, (unsigned)(n + u) * bytes, y);
+            if (whole || n + u < steps) store_row<T, V>(to, (unsigned)(n + u) * bytes, y);
         }
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    fetch(0, No());
+    for (int n = 0; n < steps; n += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) widen(raw[u], x[KP - 1 + u], T());
+        if (n + 2 * U <= inside) fetch(n + U, Yes());
+        else fetch(n + U, No());
+        if (n + U <= inside) results(n, Yes());
+        else results(n, No());
 #pragma unroll
         for (int j = 0; j < KP - 1; ++j)
 #pragma unroll
@@ -177,21 +186,16 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
         const int after = p.dafter != nullptr ? (int)min(end - (p.K - 1) - t0, 1ll << 20) : 1 << 20;     // dafter's first step
         const int from = t0 == 0 ? 1 - p.K : 0;            // the first step whose partial this span gives
         Raw<T, V> rx[U], rg[U];
-        auto fetch = [&](int n) {
+        auto fetch = [&](int n, auto whole) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                rx[u] = Raw<T, V>{};
-                rg[u] = Raw<T, V>{};
-                if (n + u < inside) rx[u] = load_row<T, V>(px, (unsigned)(n + u) * bytes);
-                if (n + u < inside) rg[u] = load_row<T, V>(pg, (unsigned)(n + u) * bytes);
+                if constexpr (!whole) rx[u] = rg[u] = Raw<T, V>{};
+                if (whole || n + u < inside) rx[u] = load_row<T, V>(px, (unsigned)(n + u) * bytes);
+                if (whole || n + u < inside) rg[u] = load_row<T, V>(pg, (unsigned)(n + u) * bytes);
             }
         };
-        fetch(0);
-        for (int n = 0; n < steps + KP - 1; n += U) {
-            float nx[U][V], ng[U][V];
-#pragma unroll
-            for (int u = 0; u < U; ++u) { widen(rx[u], nx[u], T()); widen(rg[u], ng[u], T()); }
-            fetch(n + U);
+        float nx[U][V], ng[U][V];
+        auto work = [&](int n, auto whole) {               // whole: no step here is at an end of the span or of the sequence
 #pragma unroll
             for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -211,11 +215,11 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
                     muladd(s, q, q, s);                    // the slope, q (1 + s (1 - q))
                     mul(g[0], s, g[0]);
                 }
-                if (n + u >= inside) {
+                if (!whole && n + u >= inside) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) g[0][i] = 0.0f;
                 }
-                if (n + u < steps) {
+                if (whole || n + u < steps) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) db[i] += g[0][i];
 #pragma unroll
@@ -223,24 +227,36 @@ __global__ void __launch_bounds__(32 * kRows) causal_conv_grad_kernel(const Args
                         if (k >= first) muladd(g[0], x[k], dw[k], dw[k]);
                 }
                 const int at = n + u - (KP - 1);           // the step whose K sums are complete
-                if (at < from || at >= steps) continue;
+                if (!whole && (at < from || at >= steps)) continue;
                 float dx[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) dx[i] = 0.0f;
-                if (at < inside) {
+                if (whole || at < inside) {
 #pragma unroll
                     for (int k = 0; k < KP; ++k)
                         if (k >= first) muladd(w[k], g[k], dx, dx);
-                    if (at >= after) {
+                    if (!whole && at >= after) {
                         float q[V];
                         load<T, V>(p.dafter, (at - after) * p.C + c, q);
 #pragma unroll
                         for (int i = 0; i < V; ++i) dx[i] += q[i];
                     }
                 }
-                if (at >= 0) store_row<T, V>(to, (unsigned)at * bytes, dx);
+                if (whole || at >= 0) store_row<T, V>(to, (unsigned)at * bytes, dx);
                 else if (p.dbefore != nullptr) store<T, V>(p.dbefore, (at + p.K - 1) * p.C + c, dx);
             }
+        };
+        using Yes = std::true_type;
+        using No = std::false_type;
+        const int whole_to = min(min(inside, steps), after + KP - 1);        // steps from KP - 1 up to here
+        fetch(0, No());
+        for (int n = 0; n < steps + KP - 1; n += U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) { widen(rx[u], nx[u], T()); widen(rg[u], ng[u], T()); }
+            if (n + 2 * U <= inside) fetch(n + U, Yes());
+            else fetch(n + U, No());
+            if (n >= KP - 1 && n + U <= whole_to) work(n, Yes());
+            else work(n, No());
         }
     }
     if (p.part == nullptr) return;
