@@ -509,7 +509,8 @@ relay_status_t relay_causal_conv_grad(const relay_tensor_t *x, const relay_tenso
  *   delta_bias:(D) f32 or NULL;  h0:(B,D,N) f32 or NULL (zero);  lengths:(B) i32 or NULL
  *   -> y:(T,B,D) t;  h_final:(B,D,N) f32 or NULL: the state after each sequence's last step;
  *      states:(ceil(T / RELAY_SCAN_SPAN),B,D,N) f32 or NULL: the state before every RELAY_SCAN_SPAN-th step, for the gradient.
- * Arithmetic and states in f32.  With softplus a delta' of -inf (or the type's lowest value) is a step of no length: the state stays as it is.
+ * Arithmetic and states in f32.  With softplus a delta' of -inf (or the type's lowest value) is a step of no length: the state stays as it is,
+ * whatever a is, and no partial passes to delta.  a = -inf counts as the type's lowest value: any other step leaves nothing of a state.
  * T = 1 is the step of a decoder.  No workspace.  T = 0 gives h_final = h0.
  * Long sequences are summed in spans that are joined: where exp(delta' a) over a span overflows (a > 0), a state can become infinite
  * or NaN where a step-by-step sum would not. */

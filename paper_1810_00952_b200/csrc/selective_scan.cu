@@ -35,6 +35,8 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
     for (int k = 0; k < NB; ++k) {
         load_states(p, live ? p.h0 : nullptr, at * p.N, k * 16 + nl * 4, h[k]);
         load_states(p, live ? p.a : nullptr, d * p.N, k * 16 + nl * 4, a[k]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[k][j] = exponent_of(a[k][j]);
     }
     const float skip = p.d && live && relay_in_bounds(p.d + d, 4) ? p.d[d] : 0.0f;
     const float bias = p.delta_bias && live && relay_in_bounds(p.delta_bias + d, 4) ? p.delta_bias[d] : 0.0f;
@@ -55,7 +57,7 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
 #pragma unroll
                 for (int j = 0; j < 4; j += 2) {
                     float decay[2];
-                    unpair(decay2(pair(step * (a[k][j] * kLog2e), step * (a[k][j + 1] * kLog2e))), decay[0], decay[1]);
+                    unpair(decay2(pair(step * a[k][j], step * a[k][j + 1])), decay[0], decay[1]);
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         const int n = k * 16 + nl * 4 + j + q;
@@ -177,8 +179,8 @@ __global__ void __launch_bounds__(THREADS) selective_scan_kernel(const Args p, c
     for (int k = 0; k < NB; ++k) {
         float x[4];
         load_states(p, mine < p.D ? p.a : nullptr, mine * p.N, k * 16 + nl * 4, x);
-        a[k][0] = pair(x[0] * kLog2e, x[1] * kLog2e);
-        a[k][1] = pair(x[2] * kLog2e, x[3] * kLog2e);
+        a[k][0] = pair(exponent_of(x[0]), exponent_of(x[1]));
+        a[k][1] = pair(exponent_of(x[2]), exponent_of(x[3]));
     }
     auto from_start = [&] {
 #pragma unroll

@@ -4,6 +4,8 @@
 // result.  With N = 16 the special-function pipe (16 lanes an SM) is what bounds the forward call before memory does: 2048 x 8 x 2048 x 16 are 537 M
 // exponentials and 134 M of steps and gates, 150 us, beside 41 us of bytes.
 #pragma once
+#include <cfloat>
+
 #include "sequence.cuh"
 #include "tc_common.cuh"
 
@@ -120,6 +122,16 @@ __device__ __forceinline__ f32x2 decay2(f32x2 x)
     unpair(x, a, b);
     unpair(q, c, d);
     return pair(fabsf(a) <= 0.03125f ? c : exp2_(a), fabsf(b) <= 0.03125f ? d : exp2_(b));
+}
+
+// a log2(e), what a step multiplies for its exponent: finite, so that a step of no length (those behind a sequence's end are such) has the decay 1
+// even where a, or this product, is beyond fp32: 0 inf would be NaN.  Any step that is not as small as 1e-36 leaves nothing then, as it should.
+__device__ __forceinline__ float exponent_of(float a)
+{
+    float x;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(a * kLog2e), "f"(-FLT_MAX));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(x), "f"(FLT_MAX));
+    return x;
 }
 
 // ---- rows that TMA cannot fetch ------------------------------------------------------------------------------------------

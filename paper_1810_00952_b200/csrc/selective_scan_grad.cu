@@ -105,8 +105,8 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
         for (int j = 0; j < 2; ++j) {
             float x[4];
             load_states(p, mine + j < p.D ? p.a : nullptr, (mine + j) * p.N, k * 16 + nl * 4, x);
-            a[j][0] = pair(x[0] * kLog2e, x[1] * kLog2e);
-            a[j][1] = pair(x[2] * kLog2e, x[3] * kLog2e);
+            a[j][0] = pair(exponent_of(x[0]), exponent_of(x[1]));
+            a[j][1] = pair(exponent_of(x[2]), exponent_of(x[3]));
         }
     };
 #pragma unroll
@@ -382,8 +382,10 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
             f32x2 du = fma2(pair(e.x, e.y), skip, mul2(along, pair(st.x, st.z)));
             f32x2 ddelta = mul2(fma2(pair(ke.x, ke.y), pair(0.693147181f, 0.693147181f), mul2(along, uu)), pair(sl.x, sl.y));
             if (!inside) du = ddelta = 0;
-            dbias = add2(dbias, ddelta);
             float x[2];
+            unpair(ddelta, x[0], x[1]);                    // a step of no length passes nothing, also where a state times a is beyond fp32
+            ddelta = pair(sl.x == 0.0f ? 0.0f : x[0], sl.y == 0.0f ? 0.0f : x[1]);
+            dbias = add2(dbias, ddelta);
             const long long row = ((t0 + pt) * p.B + i) * p.D;
             unpair(du, x[0], x[1]);
             store_some<T>(p, p.du, row, two, x);
