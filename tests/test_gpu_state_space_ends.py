@@ -7,7 +7,7 @@ import torch
 from oracle import state_space as S
 from paper_1810_00952_b200 import binding as B
 
-from parity import to_np
+from parity import to_np, workspace
 
 import test_gpu_selective_scan as G
 
@@ -65,3 +65,60 @@ def test_steps_of_no_length_keep_a_state_whatever_its_decay(T, dt):
     t["delta"][::2, :, :10] = -INF
     t["delta"][T - 1, 0] = -INF
     check(t)
+
+
+def _forward_y(t):
+    """As G.forward, where results may be infinite or NaN."""
+    T, Bn, D = t["u"].shape
+    N = t["a"].shape[1]
+    y, h, s = (torch.zeros(k, dtype=v, device=DEV) for k, v in (((T, Bn, D), t["u"].dtype), ((Bn, D, N), F32), ((-(-T // B.SCAN_SPAN), Bn, D, N), F32)))
+    B.relay_selective_scan(*G.inputs(t), G.on(t["h0"]), G.on(t["lengths"]), t["softplus"], y, h, s)
+    torch.cuda.synchronize()
+    return y, h, s
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("N", [17, 24, 32, 33, 64])
+@pytest.mark.parametrize("T", [130, 300])
+def test_shared_sequences_of_more_than_sixteen_states(T, N, dt):
+    """Four blocks a sequence (130 steps) and eight (300), the last ones without a chunk, and sequences that end in an early block's part."""
+    check(G.make(T, 2, 19, N, dt, seed=N + T, packed=True))
+    t = G.make(T, 6, 20, N, dt, seed=N, ragged=True)
+    t["lengths"][5] = 40
+    check(t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N", [16, 33])
+def test_shared_sequences_keep_nan_in_its_channel_and_can_be_captured(N):
+    T = 300
+    t = G.make(T, 2, 20, N, F32, seed=10)
+    clean, _, states = G.forward(t)
+    grads = G.gradient(t, states)
+    ins, h0, dy, dh = G.inputs(t), G.on(t["h0"]), G.on(t["dy"]), G.on(t["dh_final"])
+    y, h, s = torch.empty_like(clean), torch.empty(2, 20, N, device=DEV), torch.empty_like(states)
+    o = {k: torch.empty_like(v) for k, v in grads.items()}
+    ws = workspace(B.relay_workspace_bytes_selective_scan_grad(ins[0], ins[2]), DEV)
+
+    def run():
+        B.relay_selective_scan(*ins, h0, None, True, y, h, s)
+        B.relay_selective_scan_grad(*ins, None, True, s, dy, dh, *o.values(), ws)
+
+    run()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        run()
+    for _ in range(2):
+        for v in (y, h, s, *o.values()):
+            v.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        B.relay_poll_status()
+        assert torch.equal(y, clean) and torch.equal(s, states) and all(torch.equal(o[k], grads[k]) for k in o)
+    t["u"][T // 2, 1, 3] = float("nan")
+    bad = torch.zeros(T, 2, 20, dtype=torch.bool)
+    bad[T // 2:, 1, 3] = True
+    y = _forward_y(t)[0].cpu()
+    assert torch.equal(y[~bad], clean.cpu()[~bad]) and bool(torch.isnan(y[bad]).all())
