@@ -550,9 +550,11 @@ relay_status_t relay_selective_scan_grad(const relay_tensor_t *u, const relay_te
  *   lse[i] = log sum_j exp(z[i,j]);   logp[i] = z[i,tokens[i]] - lse[i]
  *   x:(..,K) t in {f32, bf16}, rank 1..6, the leading axes are the rows;  w:(K,V) t, or (V,K);  tokens:(..) i32 or i64;  temperature > 0
  *   -> logp, lse:(..) f32.
- * bf16 operands are multiplied as they are and summed in f32; f32 runs in true fp32.  A token outside [0,V) names no class: its logp
- * is 0.  With bf16 operands scores of -inf are classes that cannot occur, and a row of nothing else has lse = -inf, logp = -inf; a row with
- * a NaN or +inf score has NaN results.  With f32 operands an infinite score is NaN (the contraction's sums are compensated).  V = 0 is RELAY_ERR_SHAPE; V < 2^31 - 512.
+ * bf16 operands are multiplied as they are and summed in f32, 1024 at a time on the tensor cores, whose sums drop what lies below their
+ * last bit (less than 2^-23 of the sum so far for every 16 products; sums that fp32 holds are exact), and these with one rounding each; f32
+ * runs in true fp32.  A token outside [0,V) names no class: its logp is 0.  With bf16 operands scores of -inf are classes that cannot
+ * occur, and a row of nothing else has lse = -inf, logp = -inf; a row with a NaN or +inf score has NaN results.  With f32 operands an
+ * infinite score is NaN (the contraction's sums are compensated).  V = 0 is RELAY_ERR_SHAPE; V < 2^31 - 512.
  * `ws` must hold relay_workspace_bytes_linear_logprob() bytes. */
 size_t relay_workspace_bytes_linear_logprob(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w);
 relay_status_t relay_linear_logprob(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, const relay_tensor_t *tokens,

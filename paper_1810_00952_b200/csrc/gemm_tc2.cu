@@ -98,6 +98,7 @@ __device__ __forceinline__ void drain_groups(const Params &p, const CUtensorMap 
 template <bool TRANSC>
 struct StoreEpilogue {
     using Params = gemm_tc::Params;
+    static constexpr int kDepth = 0;
     float bias_r[8];
     __device__ __forceinline__ void prepare(const Params &p, int lane, int, int n0, int width) { load_bias(p, lane, n0, width, bias_r); }
     __device__ __forceinline__ void drain(const Params &p, const CUtensorMap *tm_c, uint32_t taddr, uint8_t *stage, int lane, int row0, int n0,

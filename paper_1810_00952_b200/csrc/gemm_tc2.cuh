@@ -122,6 +122,9 @@ __device__ __forceinline__ Unit unit_of(const Params &p, const UnitTable &tb, in
 //   prepare(p, lane, row0, n0, width)          before the wait for the accumulator, so that its loads overlap the main loop
 //   drain(p, tm_c, taddr, stage, lane, row0, n0, width, slot)   of the columns that fall to the warp's slot (0..3)
 //   finish()                                    before the block leaves
+//   kDepth                                      0, or the k-blocks after which an accumulator is handed over although the contraction goes on:
+//   collect(taddr, width, slot, first)          then takes (first) or adds up its columns, and drain() has them from there.  Units of class 1 and
+//                                               2 only: wider ones have more columns than a warp has registers for
 // Epi::Params is gemm_tc::Params or derived from it.
 template <bool A_MN, bool B_MN, typename Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
@@ -246,39 +249,44 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
                     s = 0; phase = 0; stage_off = 0;
                 }
                 const bool both = c >= 3;                 // the unit owns both accumulator halves (t_local is even: such units come first)
-                const int buf = t_local & 1;
-                const uint32_t par = ((t_local >> 1) & 1) ^ 1;
-                // every lane waits; the votes reconverge the warp (the lanes leave a wait at different times)
-                if (!__all_sync(0xffffffffu, tc::mbar_wait(&tmem_empty[buf], par, abort_flag, p.err, tc::ERR_WAIT_TMEM_EMPTY))) break;
-                if (both && !__all_sync(0xffffffffu, tc::mbar_wait(&tmem_empty[1], par, abort_flag, p.err, tc::ERR_WAIT_TMEM_EMPTY))) break;
-                tc::tc_fence_after_sync();
-                const uint32_t d0 = tmem_base + buf * BN, d1 = tmem_base + BN;
-                const uint32_t idesc0 = c == 1 ? idesc_128 : idesc_256, idesc1 = c == 3 ? idesc_128 : idesc_256;
-                for (int kb = 0; kb < p.k_blocks; ++kb) {
-                    ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[s], phase, abort_flag, p.err, tc::ERR_WAIT_FULL));
+                int kb = 0;
+                do {                                      // once per accumulator: all of the contraction, or kDepth k-blocks of it
+                    const int kb0 = kb, kb1 = Epi::kDepth > 0 ? min(kb + Epi::kDepth, p.k_blocks) : p.k_blocks;
+                    const int buf = t_local & 1;
+                    const uint32_t par = ((t_local >> 1) & 1) ^ 1;
+                    // every lane waits; the votes reconverge the warp (the lanes leave a wait at different times)
+                    ok = __all_sync(0xffffffffu, tc::mbar_wait(&tmem_empty[buf], par, abort_flag, p.err, tc::ERR_WAIT_TMEM_EMPTY));
+                    if (ok && both) ok = __all_sync(0xffffffffu, tc::mbar_wait(&tmem_empty[1], par, abort_flag, p.err, tc::ERR_WAIT_TMEM_EMPTY));
                     if (!ok) break;
                     tc::tc_fence_after_sync();
-                    const uint64_t da = desc_a0 + stage_off, db = desc_b0 + stage_off;
-                    const uint32_t acc = kb != 0;
-                    if (both) {
+                    const uint32_t d0 = tmem_base + buf * BN, d1 = tmem_base + BN;
+                    const uint32_t idesc0 = c == 1 ? idesc_128 : idesc_256, idesc1 = c == 3 ? idesc_128 : idesc_256;
+                    for (; kb < kb1; ++kb) {
+                        ok = __all_sync(0xffffffffu, tc::mbar_wait(&full[s], phase, abort_flag, p.err, tc::ERR_WAIT_FULL));
+                        if (!ok) break;
+                        tc::tc_fence_after_sync();
+                        const uint64_t da = desc_a0 + stage_off, db = desc_b0 + stage_off;
+                        const uint32_t acc = kb != kb0;
+                        if (both) {
 #pragma unroll
-                        for (int kk = 0; kk < BK / 16; ++kk) {
-                            tc::mma_bf16_pair_elect(d0, da + ((kk * a_step) >> 4), db + ((kk * b_step) >> 4), idesc0, acc | (kk != 0));
-                            tc::mma_bf16_pair_elect(d1, da + ((kk * a_step) >> 4), db + b1_off + ((kk * b_step) >> 4), idesc1, acc | (kk != 0));
+                            for (int kk = 0; kk < BK / 16; ++kk) {
+                                tc::mma_bf16_pair_elect(d0, da + ((kk * a_step) >> 4), db + ((kk * b_step) >> 4), idesc0, acc | (kk != 0));
+                                tc::mma_bf16_pair_elect(d1, da + ((kk * a_step) >> 4), db + b1_off + ((kk * b_step) >> 4), idesc1, acc | (kk != 0));
+                            }
+                        } else {
+#pragma unroll
+                            for (int kk = 0; kk < BK / 16; ++kk)
+                                tc::mma_bf16_pair_elect(d0, da + ((kk * a_step) >> 4), db + ((kk * b_step) >> 4), idesc0, acc | (kk != 0));
                         }
-                    } else {
-#pragma unroll
-                        for (int kk = 0; kk < BK / 16; ++kk)
-                            tc::mma_bf16_pair_elect(d0, da + ((kk * a_step) >> 4), db + ((kk * b_step) >> 4), idesc0, acc | (kk != 0));
+                        tc::mma_commit_pair_elect(&empty[s]);
+                        stage_off += (uint32_t)st_bytes >> 4;
+                        if (++s == n_st) { s = 0; phase ^= 1; stage_off = 0; }
                     }
-                    tc::mma_commit_pair_elect(&empty[s]);
-                    stage_off += (uint32_t)st_bytes >> 4;
-                    if (++s == n_st) { s = 0; phase ^= 1; stage_off = 0; }
-                }
-                if (!ok) break;
-                tc::mma_commit_pair_elect(&tmem_full[buf]);
-                if (both) tc::mma_commit_pair_elect(&tmem_full[1]);
-                t_local += both ? 2 : 1;
+                    if (!ok) break;
+                    tc::mma_commit_pair_elect(&tmem_full[buf]);
+                    if (both) tc::mma_commit_pair_elect(&tmem_full[1]);
+                    t_local += both ? 2 : 1;
+                } while (Epi::kDepth > 0 && kb < p.k_blocks);
             }
         }
     } else {
@@ -292,22 +300,31 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
         for (int u = pair; u < n_units && ok_all; u += n_pairs) {
             const Unit w = unit_of(p, tb, u);
             const int items = w.width > BN ? 2 : 1;       // accumulator halves of this unit, in the order the issuer fills them
-            for (int item = 0; item < items; ++item, ++t_local) {
-                const int buf = t_local & 1;
+            for (int item = 0; item < items; ++item) {
                 const int n0 = w.n0 + item * BN, width = item == 0 ? min(w.width, BN) : w.width - BN;
                 const int m0 = w.tile_m * 256 + (int)rank * 128;
                 const int row0 = m0 + quarter * 32;
                 epi.prepare(p, lane, row0, n0, width);
-                int ok = 1;
-                if (lane == 0) ok = tc::mbar_wait(&tmem_full[buf], (t_local >> 1) & 1, abort_flag, p.err, tc::ERR_WAIT_TMEM_FULL) ? 1 : 0;
-                ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (!ok) { ok_all = false; break; }
-                tc::tc_fence_after_sync();
-                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * BN;
-                if (row0 < p.M) epi.drain(p, &tm_c, taddr, my_stage, lane, row0, n0, width, slot);
-                tc::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive_cluster(tc::mapa(tc::smem_u32(&tmem_empty[buf]), 0));
+                int left = p.k_blocks;                    // of the contraction
+                do {
+                    const int buf = t_local & 1;
+                    int ok = 1;
+                    if (lane == 0) ok = tc::mbar_wait(&tmem_full[buf], (t_local >> 1) & 1, abort_flag, p.err, tc::ERR_WAIT_TMEM_FULL) ? 1 : 0;
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                    if (!ok) { ok_all = false; break; }
+                    tc::tc_fence_after_sync();
+                    const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * BN;
+                    if (row0 < p.M) {
+                        if constexpr (Epi::kDepth > 0) epi.collect(taddr, width, slot, left == p.k_blocks);
+                        if (Epi::kDepth == 0 || left <= Epi::kDepth) epi.drain(p, &tm_c, taddr, my_stage, lane, row0, n0, width, slot);
+                    }
+                    tc::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) tc::mbar_arrive_cluster(tc::mapa(tc::smem_u32(&tmem_empty[buf]), 0));
+                    ++t_local;
+                    left -= Epi::kDepth;
+                } while (Epi::kDepth > 0 && left > 0);
+                if (!ok_all) break;
             }
         }
         __syncwarp();

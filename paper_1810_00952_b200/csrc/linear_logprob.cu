@@ -340,7 +340,7 @@ relay_status_t run_forward(Piece p, const Sizes &s, const void *w, bool bf16, fl
     }
     RELAY_CUDA(launch_pdl(join_stats_kernel, dim3((unsigned)((s.rows + 31) / 32)), dim3(32, kJoin), 0, st, (const float2 *)part, (long long)s.rows, parts,
                           (const float *)at, p.tokens, p.tokens_i64, (long long)s.rows, (long long)s.V,
-                          bf16 ? head::score_scale(p.inv_temperature, s.K) : p.inv_temperature, logp, lse));
+                          p.inv_temperature, logp, lse));
     return check_launch("linear_logprob");
 }
 

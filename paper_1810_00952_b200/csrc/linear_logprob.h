@@ -20,11 +20,12 @@ struct Piece {
 constexpr int kPartColumns = 64;           // columns that one partial sum covers
 inline long long parts_of(long long classes) { return (classes + 255) / 256 * (256 / kPartColumns); }      // that a piece writes, or may write
 
-// The tensor cores add the products of sixteen k at a time to an fp32 accumulator and drop what lies below its last bit: towards zero, so that a
-// score comes out small by 2^-26 of itself for every such addition, on average (measured on normal operands: 4.9e-8, 8.6e-7 and 3.8e-6 of a score
-// at K = 64, 1024 and 4096, 4 % within this rule; what is left after it is half as large and of either sign).  Every score is small alike, so a
-// softmax's normaliser would carry the whole of it: 1.3e-6 of lse at K = 4096, 4e-7 with this factor in the scale.
-inline float score_scale(float inv_temperature, long long K) { return (float)((double)inv_temperature * (1.0 + (double)K / 16.0 * 1.4901161e-8)); }
+// The tensor cores add the products of sixteen k at a time to an fp32 accumulator and drop what lies below its last bit, towards zero: a score whose
+// terms are of all sizes comes out small by 2^-26 of itself for every such addition, on average (measured on normal operands: 4.9e-8, 8.6e-7 and
+// 3.8e-6 of a score at K = 64, 1024 and 4096), one whose sums are exact not at all.  So an accumulator takes 1024 k at most; the epilogue adds
+// those of a longer contraction up with one rounding each, on units of 256 columns (4096 x 2048 x 131072 with its gradient 6.8 ms; in one accumulator
+// on units of up to 512 columns 7.0).
+constexpr int kDepth = 1024;
 
 // part[j][row] = (m, s): over the 64 columns from 64 j on, m = max z log2(e) / temperature and s = sum 2^(z log2(e) / temperature - m);
 // at[row] = the token's score where the token is in this piece.  `ld` entries from one j to the next.

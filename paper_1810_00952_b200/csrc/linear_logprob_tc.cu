@@ -30,9 +30,41 @@ struct HeadParams : gemm_tc::Params {
     const float *lse, *dlogp;              // slopes
 };
 
-// Each warp takes 64 neighbouring columns of its 32 rows: of a 128-column accumulator only the first two of the four slots have some.
-struct StatsEpilogue {
+// The scores that a warp has of an accumulator: 64 neighbouring columns of its 32 rows, so that of a 128-column accumulator only the first two of
+// the four slots have some.  DEPTH = 0: read as they are.  Else they are summed up over accumulators of DEPTH k-blocks each.
+template <int DEPTH>
+struct Scores {
+    static constexpr int kDepth = DEPTH;
+    uint32_t r[2][32];
+    __device__ __forceinline__ void read(uint32_t taddr)
+    {
+        tc::tmem_ld_32x32(taddr, r[0]);
+        tc::tmem_ld_32x32(taddr + 32, r[1]);
+        tc::tmem_ld_wait();
+    }
+    __device__ __forceinline__ void collect(uint32_t taddr, int width, int slot, bool first)
+    {
+        const int c0 = slot * 64;
+        if (c0 >= width) return;
+        if (first) { read(taddr + c0); return; }
+#pragma unroll
+        for (int k = 0; k < 64; k += 8) {                  // few columns at a time: the sums leave no registers for more
+            uint32_t q[8];
+            tc::tmem_ld_32x8(taddr + c0 + k, q);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t &to = r[k >> 5][(k & 31) + j];
+                to = __float_as_uint(__uint_as_float(to) + __uint_as_float(q[j]));
+            }
+        }
+    }
+};
+
+template <int DEPTH>
+struct StatsEpilogue : Scores<DEPTH> {
     using Params = HeadParams;
+    using Scores<DEPTH>::r;
     int token;
     __device__ __forceinline__ void prepare(const Params &p, int lane, int row0, int, int)
     {
@@ -44,10 +76,7 @@ struct StatsEpilogue {
     {
         const int c0 = slot * head::kPartColumns;
         if (c0 >= width) return;
-        uint32_t r[2][32];
-        tc::tmem_ld_32x32(taddr + c0, r[0]);
-        tc::tmem_ld_32x32(taddr + c0 + 32, r[1]);
-        tc::tmem_ld_wait();
+        if (DEPTH == 0) this->read(taddr + c0);
         const int n = n0 + c0;
         if (n + 64 > p.classes) {                          // warp-uniform: columns that do not exist
 #pragma unroll
@@ -77,8 +106,10 @@ struct StatsEpilogue {
 // The partials of 64 columns a warp: -slope 2^(z log2(e) / temperature - lse log2(e)), the slope's size taken into the exponent, its sign and
 // the rows without a part put in where two values are already one register.  Tokens and the vocabulary's end, which few groups of 32 columns
 // meet, are seen to under a condition that the whole warp shares.
-struct SlopeEpilogue {
+template <int DEPTH>
+struct SlopeEpilogue : Scores<DEPTH> {
     using Params = HeadParams;
+    using Scores<DEPTH>::r;
     int token;
     float off, slope, lse;                 // log2 |slope| - lse log2(e), dlogp / temperature
     uint32_t keep, sign;                   // of two bf16 values: all bits or none (no token, or no class that can occur); their signs
@@ -103,10 +134,7 @@ struct SlopeEpilogue {
     {
         const int c0 = slot * 64;
         if (c0 >= width) return;
-        uint32_t r[2][32];
-        tc::tmem_ld_32x32(taddr + c0, r[0]);
-        tc::tmem_ld_32x32(taddr + c0 + 32, r[1]);
-        tc::tmem_ld_wait();
+        if (DEPTH == 0) this->read(taddr + c0);
         const int sw = (lane >> 1) & 3;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -155,7 +183,7 @@ struct SlopeEpilogue {
     __device__ __forceinline__ void finish() { if (tc::elect_one()) tc::tma_store_wait_all<0>(); }
 };
 
-template <typename Epi>
+template <template <int> class Epi>
 relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, void *c, int64_t ldc, cudaStream_t st)
 {
     int dev = 0, sms = 148;
@@ -173,27 +201,29 @@ relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, 
     if (!p.err) return fail(RELAY_ERR_CUDA, "no device error word");
     p.tokens = q.tokens; p.tokens_i64 = q.tokens_i64;
     p.rows = q.rows; p.V = q.V; p.first = q.first; p.classes = q.classes;
-    p.inv_temperature = head::score_scale(q.inv_temperature, q.K);
+    p.inv_temperature = q.inv_temperature;
     p.scale = (float)(1.4426950408889634 * (double)p.inv_temperature);
     if ((long long)p.tiles_m * p.tiles_n > 1 << 30) return fail(RELAY_ERR_UNSUPPORTED, "linear_logprob: %lld x %lld scores at a time", (long long)M, (long long)N);
     const int n_tiles = p.tiles_m * p.tiles_n, pairs = std::min(n_tiles, sms / 2);
     static thread_local UnitTable tb;
     tb.n = 0;
     p.tail_split = 1;
-    if (!plan_units(p.tiles_m, (int)((N + 127) / 128), pairs, p.k_blocks, &tb)) {
+    // no wide units: a contraction long enough to gain by them is cut
+    constexpr int kCut = head::kDepth / BK;
+    static_assert(kCut < kWideMinKBlocks, "units of class 3 and 4 have no epilogue here");
+    if (!plan_units(p.tiles_m, (int)((N + 127) / 128), pairs, std::min(p.k_blocks, kCut), &tb)) {
         tb.n = 0;
-        const int wide_rounds = p.k_blocks >= kWideMinKBlocks ? std::min(n_tiles / (2 * pairs), (p.tiles_m * (p.tiles_n / 2)) / pairs) : 0;
-        p.wide_units = wide_rounds * pairs;
-        const int narrow = n_tiles - 2 * p.wide_units, rem = narrow % pairs;
+        const int rem = n_tiles % pairs;
         p.tail_split = (rem > 0 && 2 * rem <= pairs) ? 2 : 1;
-        p.full_tiles = p.tail_split == 2 ? narrow - rem : narrow;
+        p.full_tiles = p.tail_split == 2 ? n_tiles - rem : n_tiles;
     }
     auto go = [&](auto kernel) -> relay_status_t {
         RELAY_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES));
         RELAY_CUDA(launch_pdl(kernel, dim3(2 * pairs), dim3(NUM_THREADS), SMEM_BYTES, st, tm_a, tm_b, tm_c, p, tb));
         return check_launch("linear_logprob");
     };
-    return q.trans_w ? go(gemm_tc2_kernel<false, false, Epi>) : go(gemm_tc2_kernel<false, true, Epi>);
+    if (p.k_blocks <= kCut) return q.trans_w ? go(gemm_tc2_kernel<false, false, Epi<0>>) : go(gemm_tc2_kernel<false, true, Epi<0>>);
+    return q.trans_w ? go(gemm_tc2_kernel<false, false, Epi<kCut>>) : go(gemm_tc2_kernel<false, true, Epi<kCut>>);
 }
 
 }  // namespace

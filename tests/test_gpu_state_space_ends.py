@@ -9,6 +9,7 @@ from paper_1810_00952_b200 import binding as B
 
 from parity import to_np, workspace
 
+import test_gpu_linear_logprob as H
 import test_gpu_selective_scan as G
 
 DEV = "cuda:0"
@@ -122,3 +123,53 @@ def test_shared_sequences_keep_nan_in_its_channel_and_can_be_captured(N):
     bad[T // 2:, 1, 3] = True
     y = _forward_y(t)[0].cpu()
     assert torch.equal(y[~bad], clean.cpu()[~bad]) and bool(torch.isnan(y[bad]).all())
+
+
+# ---- log-probabilities from the head's operands ----------------------------------------------------------------
+def _log_terms(t, temperature):
+    """Scores, lse and logp in 64 bits by torch."""
+    x, w = t["x"].to(DEV).double(), (t["w"].T if t["tied"] else t["w"]).to(DEV).double()
+    z = (x @ w) / temperature
+    lse = torch.logsumexp(z, 1)
+    return z, lse, z.gather(1, t["tokens"].to(DEV).long()[:, None])[:, 0] - lse
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tied", [False, True])
+@pytest.mark.parametrize("K", [1024, 4096, 65536])
+def test_sums_that_fp32_holds_exactly_are_exact(K, tied):
+    """One entry in a row of x, as in a table's row or a padded width, and weights in eighths: every score is an fp32 number and no sum rounds.  What
+    is left, in units of 2^-24: of a score, the roundings of 1 / temperature, of log2(e) / temperature, of the maximum, of log(2), of its product
+    and of the last sum, one each; of the sum of exponentials, made by an instruction good to 2^-22, 4 and as much again for its additions and log."""
+    N, V = 65, 200
+    r = np.random.default_rng(K)
+    x, w = np.zeros((N, K)), r.integers(-16, 17, (K, V)) / 8
+    x[np.arange(N), r.integers(0, K, N)] = r.integers(8, 32, N)
+    t = dict(x=torch.from_numpy(x).to(BF16), w=torch.from_numpy(w.T.copy() if tied else w).to(BF16), tokens=torch.from_numpy(r.integers(0, V, N)).to(torch.int32),
+             tied=tied)
+    for temperature in (1.0, 0.75):
+        logp, lse = H.forward(t, temperature)
+        z, ws, wl = _log_terms(t, temperature)
+        bound = (6 * z.abs().amax(1) + 16) * 2.0 ** -24
+        assert bool(((lse.double() - ws).abs() <= bound).all()), float(((lse.double() - ws).abs() / bound).max())
+        assert bool(((logp.double() - wl).abs() <= 2 * bound).all()), float(((logp.double() - wl).abs() / bound).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tied", [False, True])
+@pytest.mark.parametrize("K", [512, 1024, 1032, 4096, 16384])
+def test_long_contractions_lose_no_more_than_one_of_a_thousand_terms(K, tied):
+    """Terms of one sign.  The tensor cores drop, at each addition of sixteen products, less than a unit in the last place (2^-23) of the sum so far,
+    half of the final one on average: of 64 such additions, 64 x 2^-24 of the score.  Longer contractions are cut into pieces of 1024 whose sums
+    are added with one rounding each.  The roundings behind the scores as above."""
+    N, V = 40, 300
+    r = np.random.default_rng(K)
+    x, w = np.abs(r.normal(size=(N, K))), np.abs(r.normal(size=(K, V))) * 20 / (0.64 * K)
+    t = dict(x=torch.from_numpy(x).to(BF16), w=torch.from_numpy(w.T.copy() if tied else w).to(BF16), tokens=torch.from_numpy(r.integers(0, V, N)).to(torch.int32),
+             tied=tied, dlogp=torch.from_numpy(r.normal(size=N)).float())
+    logp, lse = H.forward(t, 1.0)
+    z, ws, wl = _log_terms(t, 1.0)
+    bound = ((min(K, 1024) / 16 + K / 1024 + 6) * z.abs().amax(1) + 16) * 2.0 ** -24
+    worst = float(((lse.double() - ws).abs() / bound).max())
+    assert worst <= 1.0, worst
+    H.check64(t, logp, lse, *H.gradient(t, 1.0, lse))
