@@ -565,7 +565,8 @@ relay_status_t relay_linear_logprob(const relay_tensor_t *x, const relay_tensor_
  *   dz[i,j] = dlogp[i] (1[j = tokens[i]] - exp(z[i,j] - lse[i])) / temperature
  *   dx[i,k] = sum_j dz[i,j] w[k,j];   dw[k,j] = sum_i x[i,k] dz[i,j]      dx, dw: types and shapes of x and w; one of them may be NULL
  * The scores are computed again, a piece of the vocabulary at a time; with bf16 operands dz is rounded to bf16, the operand type of
- * the two products, whose sums are f32.  A row whose token names no class has no part in either; a row with lse = -inf neither.
+ * the two products, whose sums are f32.  A row whose token names no class has no part in either, whatever x holds there; a row with lse = -inf
+ * neither.  dx is NaN where the zero partial of an impossible class meets its infinite weight (column k of every row with a part, w[k,j] infinite).
  * `ws` must hold relay_workspace_bytes_linear_logprob_grad() bytes. */
 size_t relay_workspace_bytes_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w);
 relay_status_t relay_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, const relay_tensor_t *tokens,

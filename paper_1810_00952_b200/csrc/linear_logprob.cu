@@ -83,17 +83,30 @@ __device__ __forceinline__ uint4 load_shifted(const char *p)
     return make_uint4(__funnelshift_r(v[0], v[1], bits), __funnelshift_r(v[1], v[2], bits), __funnelshift_r(v[2], v[3], bits),
                       __funnelshift_r(v[3], v[4], bits));
 }
-// to (to_rows, to_cols) <- from (rows, cols), zero beyond; rows whose token names no class are zero too where tokens are given: whatever x
-// holds there (NaN too) takes no part in dw.  A thread has the elements that share 16 aligned bytes of the result: one access each way
+// Which rows have a part in a gradient: those whose token names a class and which have a class that can occur.
+struct Rows {
+    const void *tokens;                    // null: all of them
+    int i64;
+    long long V;
+    const float *lse;
+    __device__ __forceinline__ bool part(long long row) const
+    {
+        if (tokens == nullptr) return true;
+        if (head::token_in_piece(tokens, i64, row, V, 0, V) < 0 || !relay_in_bounds(lse + row, 4)) return false;
+        return lse[row] != -INFINITY;
+    }
+};
+// to (to_rows, to_cols) <- from (rows, cols), zero beyond; rows without a part are zero too: whatever x holds there (infinities and NaN too) takes
+// no part in dw.  A thread has the elements that share 16 aligned bytes of the result: one access each way
 // unless the row's end or what must not be read lies in between.
 template <typename T>
 __global__ void __launch_bounds__(256) copy_padded_kernel(const T *from, long long ld_from, long long rows, long long cols, T *to, long long ld_to,
-                                                          long long to_rows, long long to_cols, const void *tokens, int tokens_i64, long long V)
+                                                          long long to_rows, long long to_cols, const Rows some)
 {
     constexpr int E = 16 / sizeof(T);
     pdl_wait();
     for (long long r = blockIdx.y; r < to_rows; r += gridDim.y) {
-        const bool live = r < rows && (tokens == nullptr || head::token_in_piece(tokens, tokens_i64, r, V, 0, V) >= 0);
+        const bool live = r < rows && some.part(r);
         const T *src = from + r * ld_from;
         T *dst = to + r * ld_to;
         const int skew = (int)(((uintptr_t)dst & 15) / sizeof(T));
@@ -115,21 +128,23 @@ __global__ void __launch_bounds__(256) copy_padded_kernel(const T *from, long lo
         }
     }
 }
-// out (rows, cols) <- a + b, both fp32 with rows of `ld` values, whole 16-byte pieces (b may be null), rounded once
+// out (rows, cols) <- a + b, both fp32 with rows of `ld` values, whole 16-byte pieces (b may be null), rounded once; rows without a part are zero
+// (their sums are, unless a weight is infinite)
 template <typename T>
 __global__ void __launch_bounds__(256) add_kernel(const float *a, const float *b, long long ld, T *out, long long ld_out, long long rows,
-                                                  long long cols)
+                                                  long long cols, const Rows some)
 {
     pdl_wait();
     const bool whole = ld % 4 == 0 && ld_out % 4 == 0;
-    for (long long r = blockIdx.y; r < rows; r += gridDim.y)
+    for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
+        const bool part = some.part(r);
         for (long long c = ((long long)blockIdx.x * 256 + threadIdx.x) * 4; c < cols; c += (long long)gridDim.x * 1024) {
             const long long at = r * ld + c;
             T *q = out + r * ld_out + c;
             float x[4] = {0.0f, 0.0f, 0.0f, 0.0f}, y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             if (whole && c + 4 <= cols) {
-                seq::load<float, 4>(a, at, x);
-                if (b != nullptr) seq::load<float, 4>(b, at, y);
+                if (part) seq::load<float, 4>(a, at, x);
+                if (part && b != nullptr) seq::load<float, 4>(b, at, y);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] += y[j];
                 seq::store<T, 4>(q, 0, x);
@@ -138,10 +153,21 @@ __global__ void __launch_bounds__(256) add_kernel(const float *a, const float *b
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (c + j >= cols || !relay_in_bounds(a + at + j, 4)) continue;
-                const float one[1] = {a[at + j] + (b != nullptr && relay_in_bounds(b + at + j, 4) ? b[at + j] : 0.0f)};
+                const float one[1] = {part ? a[at + j] + (b != nullptr && relay_in_bounds(b + at + j, 4) ? b[at + j] : 0.0f) : 0.0f};
                 seq::store<T, 1>(q, j, one);
             }
         }
+    }
+}
+// f32, whose products write dx themselves: zeros in the rows without a part
+__global__ void __launch_bounds__(256) clear_rows_kernel(float *dx, long long rows, long long cols, const Rows some)
+{
+    pdl_wait();
+    for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
+        if (some.part(r)) continue;
+        for (long long c = (long long)blockIdx.x * 256 + threadIdx.x; c < cols; c += (long long)gridDim.x * 256)
+            if (relay_in_bounds(dx + r * cols + c, 4)) dx[r * cols + c] = 0.0f;
+    }
 }
 
 // f32: statistics of a piece of scores in memory, one block a row (base 2, as the other path's)
@@ -201,16 +227,17 @@ dim3 grid_of(long long rows, long long cols)               // cols: threads alon
 }
 template <typename T>
 relay_status_t copy_padded(const void *from, long long ld_from, long long rows, long long cols, void *to, long long ld_to, long long to_rows,
-                           long long to_cols, const Piece *masked, cudaStream_t st)
+                           long long to_cols, const Rows &some, cudaStream_t st)
 {
     RELAY_CUDA(launch_pdl(copy_padded_kernel<T>, grid_of(to_rows, (to_cols * sizeof(T) + 31) / 16), dim3(256), 0, st, (const T *)from, ld_from, rows, cols, (T *)to, ld_to,
-                          to_rows, to_cols, masked ? masked->tokens : nullptr, masked ? masked->tokens_i64 : 0, masked ? masked->V : 0));
+                          to_rows, to_cols, some));
     return check_launch("linear_logprob");
 }
 template <typename T>
-relay_status_t add(const float *a, const float *b, long long ld, void *out, long long ld_out, long long rows, long long cols, cudaStream_t st)
+relay_status_t add(const float *a, const float *b, long long ld, void *out, long long ld_out, long long rows, long long cols, const Rows &some,
+                   cudaStream_t st)
 {
-    RELAY_CUDA(launch_pdl(add_kernel<T>, grid_of(rows, (cols + 3) / 4), dim3(256), 0, st, a, b, ld, (T *)out, ld_out, rows, cols));
+    RELAY_CUDA(launch_pdl(add_kernel<T>, grid_of(rows, (cols + 3) / 4), dim3(256), 0, st, a, b, ld, (T *)out, ld_out, rows, cols, some));
     return check_launch("linear_logprob");
 }
 
@@ -303,7 +330,7 @@ relay_status_t weights_of(Piece *p, const Sizes &s, const char *w, const Layout 
     if (!copy) return RELAY_OK;
     const int64_t rows = p->trans_w ? p->classes : s.K, cols = p->trans_w ? s.K : p->classes;
     const int64_t to_rows = p->trans_w ? padded(p->classes) : q.K, to_cols = p->trans_w ? q.K : padded(p->classes);
-    RELAY_TRY(copy_padded<__nv_bfloat16>(p->w, p->ldw, rows, cols, ws + q.w, to_cols, to_rows, to_cols, nullptr, st));
+    RELAY_TRY(copy_padded<__nv_bfloat16>(p->w, p->ldw, rows, cols, ws + q.w, to_cols, to_rows, to_cols, Rows{}, st));
     p->w = ws + q.w;
     p->ldw = to_cols;
     return RELAY_OK;
@@ -318,7 +345,7 @@ relay_status_t run_forward(Piece p, const Sizes &s, const void *w, bool bf16, fl
     const long long per_piece = bf16 ? head::parts_of(q.piece) : 1;
     long long parts = 0;
     if (q.copy_x) {
-        RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, ws + q.x, q.K, s.rows, q.K, nullptr, st));
+        RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, ws + q.x, q.K, s.rows, q.K, Rows{}, st));
         p.x = ws + q.x;
         p.ldx = q.K;
     }
@@ -349,7 +376,8 @@ relay_status_t run_gradient_f32(Piece p, const Sizes &s, const float *w, const f
 {
     const Layout q = gradient_layout(s, p.trans_w, false);
     float *x = (float *)(ws + q.x), *z = (float *)(ws + q.z), *more = (float *)(ws + q.dx_more);
-    RELAY_TRY(copy_padded<float>(p.x, s.K, s.rows, s.K, x, s.K, s.rows, s.K, &p, st));
+    const Rows some{p.tokens, p.tokens_i64, p.V, lse};
+    RELAY_TRY(copy_padded<float>(p.x, s.K, s.rows, s.K, x, s.K, s.rows, s.K, some, st));
     for (p.first = 0; p.first < s.V; p.first += q.piece) {
         p.classes = std::min<int64_t>(q.piece, s.V - p.first);
         const int64_t at = p.trans_w ? p.first * s.K : p.first, w_k = p.trans_w ? 1 : s.V, w_v = p.trans_w ? s.K : 1;
@@ -359,13 +387,15 @@ relay_status_t run_gradient_f32(Piece p, const Sizes &s, const float *w, const f
         if (dx) {
             float *to = p.first == 0 ? dx : more;
             RELAY_TRY(launch_gemm(product(s.rows, s.K, p.classes, z, q.piece, 1, w + at, w_v, w_k, to, s.K, RELAY_F32, RELAY_F32), st));
-            if (to == more) RELAY_TRY(add<float>(dx, more, s.K, dx, s.K, s.rows, s.K, st));
+            if (to == more) RELAY_TRY(add<float>(dx, more, s.K, dx, s.K, s.rows, s.K, Rows{}, st));
         }
         if (!dw) continue;
         if (p.trans_w) RELAY_TRY(launch_gemm(product(p.classes, s.K, s.rows, z, 1, q.piece, x, s.K, 1, dw + at, s.K, RELAY_F32, RELAY_F32), st));
         else RELAY_TRY(launch_gemm(product(s.K, p.classes, s.rows, x, 1, s.K, z, q.piece, 1, dw + at, s.V, RELAY_F32, RELAY_F32), st));
     }
-    return RELAY_OK;
+    if (!dx) return RELAY_OK;
+    RELAY_CUDA(launch_pdl(clear_rows_kernel, grid_of(s.rows, s.K), dim3(256), 0, st, dx, (long long)s.rows, (long long)s.K, some));
+    return check_launch("linear_logprob_grad");
 }
 
 relay_status_t run_gradient_bf16(Piece p, const Sizes &s, const void *w, const float *lse, const float *dlogp, __nv_bfloat16 *dx, __nv_bfloat16 *dw,
@@ -374,7 +404,8 @@ relay_status_t run_gradient_bf16(Piece p, const Sizes &s, const void *w, const f
     const Layout q = gradient_layout(s, p.trans_w, true);
     void *x = ws + q.x, *z = ws + q.z;
     float *sum = (float *)(ws + q.dx), *more = (float *)(ws + q.dx_more);
-    RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, x, q.K, q.N, q.K, &p, st));
+    const Rows some{p.tokens, p.tokens_i64, p.V, lse};
+    RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, x, q.K, q.N, q.K, some, st));
     p.x = x;
     p.ldx = q.K;
     for (p.first = 0; p.first < s.V; p.first += q.piece) {
@@ -389,8 +420,8 @@ relay_status_t run_gradient_bf16(Piece p, const Sizes &s, const void *w, const f
             RELAY_TRY(launch_gemm(product(q.N, q.K, C, z, C, 1, p.w, w_v, w_k, to, q.K, RELAY_BF16, RELAY_F32), st));
             const bool last = p.first + q.piece >= s.V;
             const float *b = to == more ? more : nullptr;
-            if (last) RELAY_TRY(add<__nv_bfloat16>(sum, b, q.K, dx, s.K, s.rows, s.K, st));
-            else if (b) RELAY_TRY(add<float>(sum, b, q.K, sum, q.K, q.N, q.K, st));
+            if (last) RELAY_TRY(add<__nv_bfloat16>(sum, b, q.K, dx, s.K, s.rows, s.K, some, st));
+            else if (b) RELAY_TRY(add<float>(sum, b, q.K, sum, q.K, q.N, q.K, Rows{}, st));
         }
         if (!dw) continue;
         void *to = copy ? (void *)(ws + q.dw) : (void *)(dw + at);
@@ -399,7 +430,7 @@ relay_status_t run_gradient_bf16(Piece p, const Sizes &s, const void *w, const f
         else RELAY_TRY(launch_gemm(product(q.K, C, q.N, x, 1, q.K, z, C, 1, to, ld, RELAY_BF16, RELAY_BF16), st));
         if (copy) {
             const int64_t rows = p.trans_w ? p.classes : s.K, cols = p.trans_w ? s.K : p.classes;
-            RELAY_TRY(copy_padded<__nv_bfloat16>(to, ld, rows, cols, dw + at, p.trans_w ? s.K : s.V, rows, cols, nullptr, st));
+            RELAY_TRY(copy_padded<__nv_bfloat16>(to, ld, rows, cols, dw + at, p.trans_w ? s.K : s.V, rows, cols, Rows{}, st));
         }
     }
     return RELAY_OK;

@@ -173,3 +173,81 @@ def test_long_contractions_lose_no_more_than_one_of_a_thousand_terms(K, tied):
     worst = float(((lse.double() - ws).abs() / bound).max())
     assert worst <= 1.0, worst
     H.check64(t, logp, lse, *H.gradient(t, 1.0, lse))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tied", [False, True])
+def test_rows_without_a_class_that_can_occur_have_no_part_in_the_gradient(tied):
+    """lse = -inf, from x and from w: no partial passes, although the operands hold infinities."""
+    N, K, V = 70, 24, 300
+    t = H.make(N, K, V, BF16, seed=6, tied=tied, padded=False)
+    flip = (lambda v: v.T) if tied else (lambda v: v)
+    flip(t["w"])[0] = flip(t["w"])[0].abs() + 0.25
+    _, clean = H.forward(t, 1.0)
+    t["tokens"][::7] = -1
+    none = torch.zeros(N, dtype=torch.bool)
+    none[1::7] = True
+    t["tokens"][none] = -1                                 # the same rows, without a token in place of without a class
+    want = H.gradient(t, 1.0, clean)
+    t["tokens"][none] = 5
+    t["x"][none, 0] = -INF
+    logp, lse = H.forward(t, 1.0)
+    assert bool(torch.isneginf(lse.cpu()[none]).all()) and bool(torch.isneginf(logp.cpu()[none]).all()) and torch.equal(lse.cpu()[~none], clean.cpu()[~none])
+    dx, dw = H.gradient(t, 1.0, lse)
+    assert torch.equal(dx, want[0]) and torch.equal(dw, want[1]) and not bool(dx.cpu()[none].any())
+    # every class impossible, by w: no row has a part
+    t["x"][:, 0] = t["x"][:, 0].abs().clamp(0.5, 4.0)
+    flip(t["w"])[0] = -INF
+    _, lse = H.forward(t, 1.0)
+    assert bool(torch.isneginf(lse).all())
+    dx, dw = H.gradient(t, 1.0, lse)
+    assert not bool(dx.any()) and not bool(dw.any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_rows_without_a_part_have_zero_partials_beside_infinite_weights(dt):
+    t = H.make(70, 24, 300, dt, seed=6, padded=False)
+    t["tokens"][::3] = -1
+    t["w"][0, 100:] = -INF
+    lse = torch.full((70,), 3.0, device=DEV)
+    lse[1::3] = -INF
+    gx, gw = torch.full((70, 24), 3.0, dtype=dt, device=DEV), torch.zeros(24, 300, dtype=dt, device=DEV)
+    x, w = t["x"].to(DEV), t["w"].to(DEV)
+    ws = workspace(B.relay_workspace_bytes_linear_logprob_grad(x, w, False), DEV)
+    B.relay_linear_logprob_grad(x, w, False, t["tokens"].to(DEV), 1.0, lse, t["dlogp"].to(DEV), gx, gw, ws)
+    assert not bool(gx[::3].any()) and not bool(gx[1::3].any())
+
+
+@pytest.mark.gpu
+def test_impossible_classes_in_the_gradient():
+    """Weights of -inf beside finite ones: the partials of the scores are zero there, so that dw is what it is without these classes; dx is NaN where
+    zero meets the infinite weight, and right in the other columns."""
+    N, K, V = 64, 24, 200
+    t = H.make(N, K, V, BF16, seed=8, padded=False)
+    t["x"][:, 0] = t["x"][:, 0].abs().clamp(0.5, 4.0)
+    t["tokens"] %= 150
+    some = dict(t, w=t["w"][:, :150].contiguous())
+    logp, lse = H.forward(some, 1.0)
+    dx, dw = H.gradient(some, 1.0, lse)
+    t["w"][0, 150:] = -INF
+    l2, s2 = H.forward(t, 1.0)
+    assert float((s2 - lse).abs().max()) <= 1e-5
+    x, w = t["x"].to(DEV), t["w"].to(DEV)
+    gx, gw = torch.empty_like(x), torch.empty_like(w)
+    ws = workspace(B.relay_workspace_bytes_linear_logprob_grad(x, w, False), DEV)
+    B.relay_linear_logprob_grad(x, w, False, t["tokens"].to(DEV), 1.0, lse, t["dlogp"].to(DEV), gx, gw, ws)
+    assert torch.equal(gw[:, :150], dw) and not bool(gw[:, 150:].any())
+    assert bool(torch.isnan(gx[:, 0]).all()) and torch.equal(gx[:, 1:], dx[:, 1:])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_calls_repeat_bit_for_bit(dt):
+    """Sums in a fixed order: the same call gives the same bits, over several pieces and with products that are split."""
+    t = H.make(1500, 520, 5003, dt, seed=9, tied=dt == BF16)
+    first = H.forward(t, 1.0)
+    grads = H.gradient(t, 1.0, first[1])
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(H.forward(t, 1.0), first))
+        assert all(torch.equal(a, b) for a, b in zip(H.gradient(t, 1.0, first[1]), grads))
