@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kStepThreads) selective_scan_steps_kernel(cons
         if (live && nl == 0) {
             float out[1] = {0.0f};
             if (t < end) {
-                out[0] = fmaf(skip, u, y);
+                out[0] = p.d ? fmaf(skip, u, y) : y;       // no term, not one of zero: u may be infinite
                 if (p.z) {
                     const float z = load_weight<T>(p.z, row + d);
                     out[0] *= z * logistic<FINE>(z);

@@ -379,7 +379,8 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
             const float4 st = *reinterpret_cast<const float4 *>(&s.step[pt][pc]);
             const float2 al = *reinterpret_cast<const float2 *>(&s.along[pt][pc]), ke = *reinterpret_cast<const float2 *>(&s.kept[pt][pc]);
             const f32x2 along = pair(al.x, al.y), uu = pair(u.x, u.y);
-            f32x2 du = fma2(pair(e.x, e.y), skip, mul2(along, pair(st.x, st.z)));
+            f32x2 du = mul2(along, pair(st.x, st.z));
+            if (p.d) du = fma2(pair(e.x, e.y), skip, du);
             f32x2 ddelta = mul2(fma2(pair(ke.x, ke.y), pair(0.693147181f, 0.693147181f), mul2(along, uu)), pair(sl.x, sl.y));
             if (!inside) du = ddelta = 0;
             float x[2];
@@ -393,7 +394,9 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
             store_some<T>(p, p.ddelta, row, two, x);
             if (p.dz) {
                 const float2 pl = *reinterpret_cast<const float2 *>(&s.plain[pt][pc]);
-                unpair(mul2(pair(gz.x, gz.y), fma2(skip, uu, pair(pl.x, pl.y))), x[0], x[1]);
+                f32x2 plain = pair(pl.x, pl.y);
+                if (p.d) plain = fma2(skip, uu, plain);
+                unpair(mul2(pair(gz.x, gz.y), plain), x[0], x[1]);
                 if (!inside) x[0] = x[1] = 0.0f;
                 store_some<T>(p, p.dz, row, two, x);
             }

@@ -68,6 +68,28 @@ def test_steps_of_no_length_keep_a_state_whatever_its_decay(T, dt):
     check(t)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 40, 130])
+def test_without_a_skip_infinite_inputs_make_infinities(T):
+    """A missing d is no term, not one of zero: 0 inf would be NaN."""
+    t = G.make(T, 2, 20, 16, F32, seed=5, d=False, gated=True)
+    for k in ("b", "c", "dy", "z"):
+        t[k] = t[k].abs() + 0.1
+    t["a"] /= 16
+    t["u"][1, 0, 3] = INF
+    y = _forward_y(t)[0]
+    want, _ = S.selective_scan(*G.reference(t))
+    assert np.isposinf(want[1:, 0, 3]).all() and np.array_equal(np.isposinf(to_np(y)), np.isposinf(want)) and not bool(torch.isnan(y).any())
+    t["u"][1, 0, 3] = 1.0
+    t["dy"][T - 1, 1, 7] = INF
+    g = _gradient_raw(t, _forward_y(t)[2], {"du": (T, 2, 20)})
+    assert bool(torch.isposinf(g["du"][:, 1, 7]).all())
+    t["dy"][T - 1, 1, 7] = 1.0
+    t["u"][1, 0, 3] = INF
+    g = _gradient_raw(t, _forward_y(t)[2], {"dz": (T, 2, 20)})
+    assert bool(torch.isposinf(g["dz"][1:, 0, 3]).all())
+
+
 def _forward_y(t):
     """As G.forward, where results may be infinite or NaN."""
     T, Bn, D = t["u"].shape
@@ -76,6 +98,19 @@ def _forward_y(t):
     B.relay_selective_scan(*G.inputs(t), G.on(t["h0"]), G.on(t["lengths"]), t["softplus"], y, h, s)
     torch.cuda.synchronize()
     return y, h, s
+
+
+def _gradient_raw(t, states, keep=None):
+    T, Bn, D = t["u"].shape
+    N, dt = t["a"].shape[1], t["u"].dtype
+    shapes = dict(du=(T, Bn, D), ddelta=(T, Bn, D), da=(D, N), db=(T, Bn, N), dc=(T, Bn, N), dd=(D,), dz=(T, Bn, D), ddelta_bias=(D,), dh0=(Bn, D, N))
+    gone = {"d" + k for k in ("d", "z", "delta_bias") if t[k] is None}
+    o = {k: None if k in gone else torch.full(s, 3.0, dtype=dt if k in ("du", "ddelta", "db", "dc", "dz") else F32, device=DEV) for k, s in shapes.items()}
+    ins = G.inputs(t)
+    ws = workspace(B.relay_workspace_bytes_selective_scan_grad(ins[0], ins[2]), DEV).fill_(0xFF)
+    B.relay_selective_scan_grad(*ins, G.on(t["lengths"]), t["softplus"], states, G.on(G.spoil(t, t["dy"])), G.on(t["dh_final"]), *o.values(), ws)
+    torch.cuda.synchronize()
+    return o
 
 
 @pytest.mark.gpu
