@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(32 * kRows, KP * V > 4 ? 2 : 3) causal_conv_gr
         T *to = (T *)p.dx + t0 * p.C + c;
         const unsigned bytes = (unsigned)(p.C * sizeof(T));                  // of a row
         const int steps = (int)(t1 - t0), inside = (int)min(max(end - t0, 0ll), (long long)(steps + KP - 1));
+        const int summed = min(inside, steps);             // steps that this span's dw and db are made of
         const int after = p.dafter != nullptr ? (int)min(end - (p.K - 1) - t0, 1ll << 20) : 1 << 20;     // dafter's first step
         const int from = t0 == 0 ? 1 - p.K : 0;            // the first step whose partial this span gives
         Raw<T, V> rx[U], rg[U];
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(32 * kRows, KP * V > 4 ? 2 : 3) causal_conv_gr
 #pragma unroll
                     for (int i = 0; i < V; ++i) g[0][i] = 0.0f;
                 }
-                if (whole || n + u < steps) {
+                if (whole || n + u < summed) {             // not behind the end: a zero slope times an infinite input is NaN
 #pragma unroll
                     for (int i = 0; i < V; ++i) db[i] += g[0][i];
 #pragma unroll
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(32 * kRows, KP * V > 4 ? 2 : 3) causal_conv_gr
         };
         using Yes = std::true_type;
         using No = std::false_type;
-        const int whole_to = min(min(inside, steps), after + KP - 1);        // steps from KP - 1 up to here
+        const int whole_to = min(summed, after + KP - 1);        // steps from KP - 1 up to here
         fetch(0, No());
         for (int n = 0; n < steps + KP - 1; n += U) {
 #pragma unroll

@@ -9,12 +9,20 @@ from paper_1810_00952_b200 import binding as B
 
 from parity import to_np, workspace
 
+import test_gpu_causal_conv as C
 import test_gpu_linear_logprob as H
 import test_gpu_selective_scan as G
 
 DEV = "cuda:0"
 F32, BF16 = torch.float32, torch.bfloat16
 LOWEST, INF = torch.finfo(torch.float32).min, float("inf")
+
+
+def finite_where(got, want, what, rel=1e-4):
+    """Finite, and close, where the definition is."""
+    g, on = to_np(got), np.isfinite(want)
+    assert on.any() and np.isfinite(g[on]).all(), (what, int((~np.isfinite(g[on])).sum()))
+    assert np.abs(g[on] - want[on]).max() <= rel * np.abs(want[on]).max(), what
 
 
 # ---- selective scan ----------------------------------------------------------------------------------------
@@ -158,6 +166,28 @@ def test_shared_sequences_keep_nan_in_its_channel_and_can_be_captured(N):
     bad[T // 2:, 1, 3] = True
     y = _forward_y(t)[0].cpu()
     assert torch.equal(y[~bad], clean.cpu()[~bad]) and bool(torch.isnan(y[bad]).all())
+
+
+# ---- convolution -------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [8, 9])
+@pytest.mark.parametrize("K", [2, 4, 6])
+def test_infinite_inputs_do_not_reach_the_filters_partials_from_behind_the_end(K, D):
+    """dw[k] sums over the steps of the sequence alone: an infinite last input enters only under the last tap, and the inputs ahead of a sequence of
+    no steps not at all."""
+    t = C.make(40, 4, D, K, F32, F32, seed=K, ragged=False)
+    t["lengths"] = torch.tensor([40, 21, 0, 33], dtype=torch.int32)
+    t["x"][20, 1, 3] = t["x"][39, 0, 2] = INF
+    t["before"][K - 2, 2, 5] = INF
+    with np.errstate(invalid="ignore"):
+        want = S.causal_conv_grad(to_np(t["x"]), to_np(t["w"]), to_np(t["b"]), to_np(t["before"]), t["lengths"].tolist(), False, to_np(t["dy"]), to_np(t["dafter"]))
+    assert np.isfinite(want[1][:, 5]).all() and np.isfinite(want[1][:K - 1, 3]).all() and not np.isfinite(want[1][K - 1, 3])
+    x, w = C.on(C.spoil(t, t["x"])), C.on(t["w"])
+    dx, dw, db, dbefore = (torch.zeros(v, device=DEV) for v in ((40, 4, D), (K, D), (D,), (K - 1, 4, D)))
+    ws = workspace(B.relay_workspace_bytes_causal_conv_grad(x, w), DEV).fill_(0xFF)
+    B.relay_causal_conv_grad(x, w, C.on(t["b"]), C.on(t["before"]), C.on(t["lengths"]), B.ACT_NONE, C.on(C.spoil(t, t["dy"])), C.on(t["dafter"]), dx, dw, db, dbefore, ws)
+    for got, v, what in ((dx, want[0], "dx"), (dw, want[1], "dw"), (db, want[2], "db"), (dbefore, want[3], "dbefore")):
+        finite_where(got, v, what)
 
 
 # ---- log-probabilities from the head's operands ----------------------------------------------------------------
