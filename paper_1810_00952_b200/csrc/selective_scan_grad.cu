@@ -7,6 +7,7 @@
 // slots, 57 % of shared memory's cycles, 16 warps an SM (128 registers).  Taken out one at a time, reductions between lanes cost 85 us, the
 // joins 170, and what follows the scan 190, of which 72 are bytes.
 #include <algorithm>
+#include <type_traits>
 
 #include "selective_scan.cuh"
 
@@ -40,7 +41,8 @@ struct Tile {
     int gave_up;
 };
 
-template <typename T, int NB>
+// ENDS: a sequence may end inside a chunk (without: 1548 us for 2048 x 8 x 2048 x 16 with the forward call, 1568 with)
+template <typename T, int NB, bool ENDS>
 __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_kernel(const Args p, const __grid_constant__ Maps maps)
 {
     using S = Tile<T, NB>;
@@ -332,42 +334,50 @@ __global__ void __launch_bounds__(THREADS, NB == 1 ? 2 : 1) selective_scan_grad_
 #pragma unroll
                 for (int j = 0; j < 2; ++j) { const ulonglong2 v = s.da[k][j][tid]; dA[j][0] = v.x; dA[j][1] = v.y; }
             }
+            auto backwards = [&](auto whole) {             // whole: all steps of the chunk are inside the sequence
 #pragma unroll
-            for (int r = RUN - 1; r >= 0; --r) {
-                const float4 st = *reinterpret_cast<const float4 *>(&s.step[r0 + r][ch]);
-                const float2 e = *reinterpret_cast<const float2 *>(&s.e[r0 + r][ch]);
-                const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
-                const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
-                f32x2 db[2], dc[2];
-                float v[4];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const f32x2 ee = j ? pair(e.y, e.y) : pair(e.x, e.x), dt = j ? pair(st.z, st.z) : pair(st.x, st.x);
-                    const f32x2 du = j ? pair(st.w, st.w) : pair(st.y, st.y);
-                    f32x2 along, kept;
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const f32x2 gq = fma2(ee, q ? c.y : c.x, G[j][q]), bb = q ? b.y : b.x;
-                        G[j][q] = mul2(da[r][j][q], gq);
-                        const f32x2 left = mul2(G[j][q], r ? h[r ? r - 1 : 0][j][q] : from[j][q]);
-                        dA[j][q] = fma2(left, dt, dA[j][q]);
-                        kept = q ? fma2(left, a[j][q], kept) : mul2(left, a[j][q]);
-                        along = q ? fma2(gq, bb, along) : mul2(gq, bb);
-                        db[q] = j ? fma2(gq, du, db[q]) : mul2(gq, du);
-                        dc[q] = j ? fma2(ee, h[r][j][q], dc[q]) : mul2(ee, h[r][j][q]);
+                for (int r = RUN - 1; r >= 0; --r) {
+                    if (!whole && r0 + r >= in) {          // behind the end: a zero partial of an infinite state would be NaN
+                        s.dbc[r0 + r][(cl < 4 ? 0 : S::NP) + k * 16 + nl * 4 + (cl & 3)] = 0.0f;
+                        continue;
                     }
-                    v[j] = sum2(along);
-                    v[2 + j] = sum2(kept);
+                    const float4 st = *reinterpret_cast<const float4 *>(&s.step[r0 + r][ch]);
+                    const float2 e = *reinterpret_cast<const float2 *>(&s.e[r0 + r][ch]);
+                    const ulonglong2 b = *reinterpret_cast<const ulonglong2 *>(&s.b[r0 + r][k * 16 + nl * 4]);
+                    const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(&s.c[r0 + r][k * 16 + nl * 4]);
+                    f32x2 db[2], dc[2];
+                    float v[4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const f32x2 ee = j ? pair(e.y, e.y) : pair(e.x, e.x), dt = j ? pair(st.z, st.z) : pair(st.x, st.x);
+                        const f32x2 du = j ? pair(st.w, st.w) : pair(st.y, st.y);
+                        f32x2 along, kept;
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const f32x2 gq = fma2(ee, q ? c.y : c.x, G[j][q]), bb = q ? b.y : b.x;
+                            G[j][q] = mul2(da[r][j][q], gq);
+                            const f32x2 left = mul2(G[j][q], r ? h[r ? r - 1 : 0][j][q] : from[j][q]);
+                            dA[j][q] = fma2(left, dt, dA[j][q]);
+                            kept = q ? fma2(left, a[j][q], kept) : mul2(left, a[j][q]);
+                            along = q ? fma2(gq, bb, along) : mul2(gq, bb);
+                            db[q] = j ? fma2(gq, du, db[q]) : mul2(gq, du);
+                            dc[q] = j ? fma2(ee, h[r][j][q], dc[q]) : mul2(ee, h[r][j][q]);
+                        }
+                        v[j] = sum2(along);
+                        v[2 + j] = sum2(kept);
+                    }
+                    float one[1], w[8];
+                    reduce_lanes<4, 1, 4>(v, lane, one);
+                    float *at = nl < 2 ? &s.along[r0 + r][ch + nl] : &s.kept[r0 + r][ch + nl - 2];
+                    *at = k ? *at + one[0] : one[0];
+                    unpair(db[0], w[0], w[1]); unpair(db[1], w[2], w[3]);
+                    unpair(dc[0], w[4], w[5]); unpair(dc[1], w[6], w[7]);
+                    reduce_lanes<8, 4, 8>(w, lane, one);
+                    s.dbc[r0 + r][(cl < 4 ? 0 : S::NP) + k * 16 + nl * 4 + (cl & 3)] = one[0];
                 }
-                float one[1], w[8];
-                reduce_lanes<4, 1, 4>(v, lane, one);
-                float *at = nl < 2 ? &s.along[r0 + r][ch + nl] : &s.kept[r0 + r][ch + nl - 2];
-                *at = k ? *at + one[0] : one[0];
-                unpair(db[0], w[0], w[1]); unpair(db[1], w[2], w[3]);
-                unpair(dc[0], w[4], w[5]); unpair(dc[1], w[6], w[7]);
-                reduce_lanes<8, 4, 8>(w, lane, one);
-                s.dbc[r0 + r][(cl < 4 ? 0 : S::NP) + k * 16 + nl * 4 + (cl & 3)] = one[0];
-            }
+            };
+            if (!ENDS || in == STEPS) backwards(std::true_type());
+            else if constexpr (ENDS) backwards(std::false_type());
             if constexpr (NB > 1) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) s.da[k][j][tid] = make_ulonglong2(dA[j][0], dA[j][1]);
@@ -483,7 +493,7 @@ Parts parts_of(const Sizes &s, int64_t N)
     return q;
 }
 
-template <typename T, int NB>
+template <typename T, int NB, bool ENDS>
 relay_status_t launch_chunks(Args p, cudaStream_t st)
 {
     const long long blocks = p.B * p.groups;
@@ -492,16 +502,21 @@ relay_status_t launch_chunks(Args p, cudaStream_t st)
     Maps maps;
     RELAY_TRY(make_maps(&p, &maps, sizeof(T) == 4, CHANNELS, STEPS));
     const size_t bytes = sizeof(Tile<T, NB>) + 128;
-    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_grad_kernel<T, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-    RELAY_CUDA(launch_pdl(selective_scan_grad_kernel<T, NB>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, p, maps));
+    RELAY_CUDA(cudaFuncSetAttribute(selective_scan_grad_kernel<T, NB, ENDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    RELAY_CUDA(launch_pdl(selective_scan_grad_kernel<T, NB, ENDS>, dim3((unsigned)blocks), dim3(THREADS), bytes, st, p, maps));
     return check_launch("selective_scan_grad");
+}
+template <typename T, int NB>
+relay_status_t launch_ends(const Args &p, cudaStream_t st)
+{
+    return p.lengths == nullptr && p.T % STEPS == 0 ? launch_chunks<T, NB, false>(p, st) : launch_chunks<T, NB, true>(p, st);
 }
 template <typename T>
 relay_status_t launch_gradient(const Args &p, void *db, void *dc, cudaStream_t st)
 {
-    if (p.N <= 16) RELAY_TRY((launch_chunks<T, 1>(p, st)));
-    else if (p.N <= 32) RELAY_TRY((launch_chunks<T, 2>(p, st)));
-    else RELAY_TRY((launch_chunks<T, 4>(p, st)));
+    if (p.N <= 16) RELAY_TRY((launch_ends<T, 1>(p, st)));
+    else if (p.N <= 32) RELAY_TRY((launch_ends<T, 2>(p, st)));
+    else RELAY_TRY((launch_ends<T, 4>(p, st)));
     const long long rows = p.T * p.B, blocks = (rows * 2 * p.N + 255) / 256;
     if (blocks == 0) return RELAY_OK;
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "selective_scan_grad: %lld steps", rows);

@@ -122,6 +122,26 @@ def _gradient_raw(t, states, keep=None):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("N", [16, 10, 40])
+@pytest.mark.parametrize("T", [33, 130])
+def test_an_infinite_last_input_does_not_reach_behind_the_end(T, N):
+    """The last input of a sequence is infinite: it makes infinities of what it enters, but the steps behind the end have no partials, and the
+    partials of the decays, which it does not enter, are finite."""
+    t = G.make(T, 6, 20, N, F32, seed=41, ragged=True, gated=False)
+    t["lengths"][5] = T - 7
+    t["u"][T - 8, 5, 3] = t["u"][T - 1, 0, 4] = t["u"][0, 2, 5] = INF
+    y, h, s = _forward_y(t)
+    with np.errstate(invalid="ignore"):
+        want = S.selective_scan_grad(*G.reference(t), to_np(t["dy"]), to_np(t["dh_final"]))
+    g = _gradient_raw(t, s)
+    for i, end in enumerate(S._ends(t["lengths"].tolist(), T, 6)):
+        for k in ("du", "ddelta", "db", "dc"):
+            assert not bool(g[k][end:, i].any()), (k, i)
+    for k in ("du", "ddelta", "da", "db", "dc", "dh0"):
+        finite_where(g[k], want[k], k)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dt", [BF16, F32])
 @pytest.mark.parametrize("N", [17, 24, 32, 33, 64])
 @pytest.mark.parametrize("T", [130, 300])
