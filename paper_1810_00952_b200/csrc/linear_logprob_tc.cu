@@ -91,13 +91,14 @@ struct StatsEpilogue : Scores<DEPTH> {
 #pragma unroll
         for (int j = 0; j < 64; ++j) s[j & 3] += ex2(fmaf(__uint_as_float(r[j >> 5][j & 31]), p.scale, off));
         const long long row = row0 + lane;
-        if (row < p.rows) p.part[(long long)(n / head::kPartColumns) * p.ld + row] = make_float2(m, (s[0] + s[1]) + (s[2] + s[3]));
+        const long long to = (long long)(n / head::kPartColumns) * p.ld + row;
+        if (row < p.rows && relay_in_bounds(p.part + to, 8)) p.part[to] = make_float2(m, (s[0] + s[1]) + (s[2] + s[3]));
         const int hit = token - n;
         if (hit >= 0 && hit < 64) {
             float z = 0.0f;
 #pragma unroll
             for (int j = 0; j < 64; ++j) if (j == hit) z = __uint_as_float(r[j >> 5][j & 31]);
-            p.at[row] = z;
+            if (relay_in_bounds(p.at + row, 4)) p.at[row] = z;
         }
     }
     __device__ __forceinline__ void finish() {}
@@ -121,10 +122,10 @@ struct SlopeEpilogue : Scores<DEPTH> {
         off = -INFINITY;
         keep = sign = 0;
         if (row >= p.rows) return;
-        lse = p.lse[row];
+        if (relay_in_bounds(p.lse + row, 4)) lse = p.lse[row];
         if (lse == -INFINITY || head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, 0, p.V) < 0) return;
         token = head::token_in_piece(p.tokens, p.tokens_i64, row, p.V, p.first, p.classes);
-        slope = p.dlogp[row] * p.inv_temperature;
+        if (relay_in_bounds(p.dlogp + row, 4)) slope = p.dlogp[row] * p.inv_temperature;
         off = fmaf(-lse, 1.44269504f, log2f(fabsf(slope)));
         keep = 0xffffffffu;
         sign = slope > 0.0f ? 0x80008000u : 0u;
@@ -217,6 +218,11 @@ relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, 
         p.tail_split = (rem > 0 && 2 * rem <= pairs) ? 2 : 1;
         p.full_tiles = p.tail_split == 2 ? n_tiles - rem : n_tiles;
     }
+    BoundsReg reg;
+    reg.add(q.tokens, (size_t)q.rows * (q.tokens_i64 ? 8 : 4));
+    if (p.part) reg.add(p.part, ((size_t)(head::parts_of(q.classes) - 1) * p.ld + q.rows) * sizeof(float2));
+    for (const float *t : {(const float *)p.at, p.lse, p.dlogp}) reg.add(t, (size_t)q.rows * 4);
+    RELAY_TRY(reg.commit(st));
     auto go = [&](auto kernel) -> relay_status_t {
         RELAY_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES));
         RELAY_CUDA(launch_pdl(kernel, dim3(2 * pairs), dim3(NUM_THREADS), SMEM_BYTES, st, tm_a, tm_b, tm_c, p, tb));

@@ -44,6 +44,10 @@ relay_status_t launch_column_sums(const float *in, long long rows, const ColumnS
     if (!wanted) return RELAY_OK;
     const long long blocks = (cols + 31) / 32;
     if (blocks > 0x7fffffffLL) return fail(RELAY_ERR_UNSUPPORTED, "%lld columns", cols);
+    BoundsReg reg;
+    reg.add(in, (size_t)rows * cols * 4);
+    for (int k = 0; k < kSums; ++k) reg.add(to.out[k], (size_t)to.n[k] * 4);
+    RELAY_TRY(reg.commit(st));
     RELAY_CUDA(launch_pdl(column_sums_kernel, dim3((unsigned)blocks), dim3(32, kGroups), 0, st, in, rows, cols, to));
     return check_launch("column_sums");
 }

@@ -12,6 +12,7 @@ from parity import to_np, workspace
 import test_gpu_causal_conv as C
 import test_gpu_linear_logprob as H
 import test_gpu_selective_scan as G
+from test_gpu_bounds_check import child
 
 DEV = "cuda:0"
 F32, BF16 = torch.float32, torch.bfloat16
@@ -329,10 +330,16 @@ def test_impossible_classes_in_the_gradient():
 @pytest.mark.gpu
 @pytest.mark.parametrize("dt", [BF16, F32])
 def test_calls_repeat_bit_for_bit(dt):
-    """Sums in a fixed order: the same call gives the same bits, over several pieces and with products that are split."""
+    """Sums in a fixed order: the same call gives the same bits, with products that are split too."""
     t = H.make(1500, 520, 5003, dt, seed=9, tied=dt == BF16)
     first = H.forward(t, 1.0)
     grads = H.gradient(t, 1.0, first[1])
     for _ in range(3):
         assert all(torch.equal(a, b) for a, b in zip(H.forward(t, 1.0), first))
         assert all(torch.equal(a, b) for a, b in zip(H.gradient(t, 1.0, first[1]), grads))
+
+
+@pytest.mark.gpu
+def test_these_forms_pass_with_bounds_checks():
+    r = child(["tests/test_gpu_state_space_ends.py", "-k", "not captured and not bounds_checks and not fp32_holds"])
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
