@@ -30,7 +30,6 @@
 // the end, which every thread reaches unconditionally.
 #pragma once
 #include <algorithm>
-#include <vector>
 
 #include "gemm.h"
 #include "gemm_tc_common.cuh"
@@ -344,35 +343,34 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
 // ceil(chunks / pairs) chunks; rounds over the pairs take it widest class first (4, 4, ..., then the rest), since a
 // 64-deep k-step of class c costs max(256 c MMA cycles, (16 + 8 c) KB / 48 B per cycle).  A unit never crosses a
 // row block, so what is left at the end of a row becomes a narrower unit.  Returns false when the list would not fit.
+// Allocates nothing: an exception must not leave a C entry point.
 inline bool plan_units(int tiles_m, int cpr, int pairs, int k_blocks, UnitTable *tb)
 {
     const int max_c = k_blocks >= kWideMinKBlocks ? 4 : 2;
     const long long total = (long long)tiles_m * cpr;
     if (tiles_m > 0xFFF || cpr > 0xFFF || total > 4LL * MAX_UNITS) return false;
-    long long share = (total + pairs - 1) / pairs;
-    std::vector<int> rounds;
-    while (share > 0) {
-        const int c = (int)std::min<long long>(max_c, share);
-        rounds.push_back(c);
-        share -= c;
-    }
-    std::vector<uint32_t> units;
-    size_t r = 0;
-    int quota = pairs;
-    for (int m = 0; m < tiles_m; ++m) {
-        int at = 0;
-        while (at < cpr) {
-            const int want = r < rounds.size() ? rounds[r] : std::min(2, max_c);
-            const int c = std::min(want, cpr - at);
-            units.push_back((uint32_t)m | ((uint32_t)at << 12) | ((uint32_t)c << 24));
-            at += c;
-            if (--quota == 0) { quota = pairs; ++r; }
+    const long long share = (total + pairs - 1) / pairs;
+    auto walk = [&](auto &&unit) {                         // units in the order of their row blocks
+        long long left = share;                            // of a pair's chunks, in the round that is dealt
+        int quota = pairs;
+        for (int m = 0; m < tiles_m; ++m) {
+            int at = 0;
+            while (at < cpr) {
+                const int want = left > 0 ? (int)std::min<long long>(max_c, left) : std::min(2, max_c);
+                const int c = std::min(want, cpr - at);
+                unit((uint32_t)m | ((uint32_t)at << 12) | ((uint32_t)c << 24), c);
+                at += c;
+                if (--quota == 0) { quota = pairs; left -= max_c; }
+            }
         }
-    }
-    if (units.size() > (size_t)MAX_UNITS) return false;
-    std::stable_sort(units.begin(), units.end(), [](uint32_t a, uint32_t b) { return (a >> 24) > (b >> 24); });
-    tb->n = (int)units.size();
-    std::copy(units.begin(), units.end(), tb->e);
+    };
+    int of_class[4] = {0, 0, 0, 0}, n = 0;           // of_class[c - 1]: units of class c, then how many are wider
+    walk([&](uint32_t, int c) { ++of_class[c - 1]; ++n; });
+    if (n > MAX_UNITS) return false;
+    int first = 0;
+    for (int c = 4; c > 0; --c) { const int k = of_class[c - 1]; of_class[c - 1] = first; first += k; }
+    walk([&](uint32_t e, int c) { tb->e[of_class[c - 1]++] = e; });
+    tb->n = n;
     return true;
 }
 
