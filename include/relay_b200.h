@@ -533,7 +533,8 @@ relay_status_t relay_selective_scan(const relay_tensor_t *u, const relay_tensor_
  *   du, ddelta, db, dc, dz: types and shapes of u, delta, b, c, z (db:(T,B,2N) with dc = NULL where c is NULL; dz NULL where z is NULL);
  *   da:(D,N) f32;  dd, ddelta_bias:(D) f32 or NULL (NULL where d or delta_bias is NULL);  dh0:(B,D,N) f32 or NULL.
  * The states between those saved are computed again.  Sums in f32 and in a fixed order.
- * `ws` must hold relay_workspace_bytes_selective_scan_grad() bytes. */
+ * `ws` must hold relay_workspace_bytes_selective_scan_grad() bytes: 2N floats for every step, batch element and 16 channels (N / 4 times a
+ * bf16 u, for its part), and B D (N + 2) floats.  A long batch is best handed over in pieces of the batch. */
 size_t relay_workspace_bytes_selective_scan_grad(const relay_tensor_t *u, const relay_tensor_t *a);
 relay_status_t relay_selective_scan_grad(const relay_tensor_t *u, const relay_tensor_t *delta, const relay_tensor_t *a, const relay_tensor_t *b,
                                          const relay_tensor_t *c, const relay_tensor_t *d, const relay_tensor_t *z,
@@ -567,7 +568,8 @@ relay_status_t relay_linear_logprob(const relay_tensor_t *x, const relay_tensor_
  * The scores are computed again, a piece of the vocabulary at a time; with bf16 operands dz is rounded to bf16, the operand type of
  * the two products, whose sums are f32.  A row whose token names no class has no part in either, whatever x holds there; a row with lse = -inf
  * neither.  dx is NaN where the zero partial of an impossible class meets its infinite weight (column k of every row with a part, w[k,j] infinite).
- * `ws` must hold relay_workspace_bytes_linear_logprob_grad() bytes. */
+ * `ws` must hold relay_workspace_bytes_linear_logprob_grad() bytes: a piece of at most 2^27 partials, a copy of x, and with bf16 operands dx
+ * in f32, twice where there is more than one piece, and a piece of w and dw where their rows are copied. */
 size_t relay_workspace_bytes_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w);
 relay_status_t relay_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w, const relay_tensor_t *tokens,
                                          float temperature, const relay_tensor_t *lse, const relay_tensor_t *dlogp, const relay_tensor_t *dx,

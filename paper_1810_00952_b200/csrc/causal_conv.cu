@@ -2,7 +2,7 @@
 //   s_t = b + sum_k w[k] x_{t-K+1+k},  y_t = act(s_t)
 // The forward group reads x and writes y once, the gradient reads x and dy and writes dx once; K multiply-adds an element, and two
 // instructions of the special-function pipe an element for the activation.  Measured, K = 4, silu: 8192 x 2 x 4096 54 us in bf16 (5.0 TB/s of 6.56
-// copied) and 107 in fp32, gradient of 2048 x 8 x 2048 with its column sums 71 us (2.8 TB/s) and 98.  Counters before the rows inside a span had code
+// copied) and 107 in fp32, gradient of 2048 x 8 x 2048 with its column sums 72 us (2.8 TB/s) and 97.  Counters before the rows inside a span had code
 // without conditions (57, 169, 73, 106 us): 57 and 62 % of issue slots, 48 and 25 % of the special-function pipe, 31 and 23 % of the warps there are:
 // registers hold the window, the filter, the slopes and the rows on their way.
 // A thread owns V consecutive channels and a span of steps; the K - 1 inputs before the current one stay in its registers, and at the

@@ -7,8 +7,9 @@
 // (odd vocabularies, odd widths) are copied to padded rows first, and dw of such a piece back.
 // f32: the same pieces through the fp32 contraction, with the scores of a piece in the workspace.
 //
-// Measured, bf16: 8192 x 1024 x 32768 354 us (1.55 PFLOP/s in the product) and 1.50 ms with the gradient in a short series, 418 us and 1.79 ms in a long
-// one (power); 4096 x 2048 x 131072 tied 6.1 and 6.9 ms; 509 x 1024 x 50021, rows of odd length, 106 us, 47 of them the copy of w.
+// Measured, bf16: 8192 x 1024 x 32768 360 us (1.53 PFLOP/s) and 1.53 ms with the gradient in a short series, 424 us and 1.82 ms in a long one (power);
+// 4096 x 2048 x 131072 tied with the gradient 6.2 to 6.4 and 6.8 ms; 509 x 1024 x 50021, rows of odd length, 102 to 107 us, 47 of them the copy of w.
+// f32: 2048 x 1024 x 32768 5.0 ms, with the gradient 20.1.
 #include <algorithm>
 #include <cfloat>
 

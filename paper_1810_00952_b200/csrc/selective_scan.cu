@@ -1,8 +1,8 @@
 // Selective scan: h = exp(delta a) h + delta u b per channel and state, y = sum_n c h + d u, with an optional gate silu(z).
 //
-// Measured, bf16, N = 16, gate and softplus: 2048 x 8 x 2048 345 us, 16384 x 1 x 2048 605 us (two passes), one step of 64 x 2048 12 us (mostly the
-// call).  Counters of the first (T = 512): 49 % of issue slots, 40 % of the special-function pipe, two thirds of shared memory's cycles, with
-// 14 warps an SM, all there are: waits of fixed length are what is left.
+// Measured, bf16, N = 16, gate and softplus: 2048 x 8 x 2048 344 us, 16384 x 1 x 2048 608 us (two passes), one step of 64 x 2048 12 us (9.5 in a
+// captured graph: 65 % of issue slots).  Counters of the first (T = 512): 53 % of issue slots, 40 % of the special-function pipe, two thirds of
+// shared memory's cycles, with 14 warps an SM, all there are: waits of fixed length are what is left.
 #include <algorithm>
 #include <type_traits>
 

@@ -4,7 +4,7 @@
 // really starts with, and what flows back.  Sums over states end in four lanes, sums over channels in eight and then over the groups of
 // sixteen channels, through the workspace in a fixed order.
 // Measured, bf16, 2048 x 8 x 2048 x 16, gated: 1.13 ms, 47 us for the sums over groups, 1.55 ms with the forward call.  Counters (T = 512): 53 % of issue
-// slots, 57 % of shared memory's cycles, 16 warps an SM (128 registers).  Taken out one at a time, reductions between lanes cost 85 us, the
+// slots, 56 % of shared memory's cycles, 16 warps an SM (128 registers).  Taken out one at a time, reductions between lanes cost 85 us, the
 // joins 170, and what follows the scan 190, of which 72 are bytes.
 #include <algorithm>
 #include <type_traits>
