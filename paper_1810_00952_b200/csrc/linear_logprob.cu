@@ -266,6 +266,7 @@ int64_t slab_of(const Sizes &s, bool bf16)
 struct Layout {
     int64_t piece, pieces;                 // classes of a piece
     int64_t N, K, C;                       // padded rows, width and classes of a piece (bf16)
+    int parts;                             // of the partials of the scores (bf16)
     bool copy_x, copy_w;
     size_t part, at, x, w, z, dx, dx_more, dw, bytes;
 };
@@ -288,11 +289,19 @@ Layout forward_layout(const Sizes &s, bool trans_w, bool bf16)
     q.bytes = at;
     return q;
 }
+// The partials of the scores are operands of the products and so rounded to bf16.  A row's error is mostly that of its token's own partial, a factor
+// that all of its part in dx and dw has in common, and over few rows such errors do not average out: dx and dw are 1.9 times as far from 64 bits as
+// the rounding of the results alone leaves them with one row, 1.66 with nine, 1.5 with 128 or 300, 1.44 from 500 rows on, at the worst of six seeds.  So up
+// to 512 rows, whose products wait for their other operand anyway, the partials come in two bf16 numbers, one below the other in a contraction
+// twice as long (1.00).  1024 x 32768: 1 row 220 -> 232 us, 128 rows 222 -> 242, 512 rows 255 -> 291; 2048 x 131072 tied: 64 rows 0.98 -> 1.04 ms, 512
+// rows 1.18 -> 1.49; at 8192 rows they would cost half as much again.
+constexpr int64_t kTwoPartRows = 512;
 Layout gradient_layout(const Sizes &s, bool trans_w, bool bf16)
 {
     Layout q{};
-    q.N = bf16 ? padded(s.rows) : s.rows; q.K = bf16 ? padded(s.K) : s.K;
-    q.piece = piece_of(s.V, std::max(q.N, q.K));
+    q.parts = bf16 && s.rows <= kTwoPartRows ? 2 : 1;
+    q.N = !bf16 ? s.rows : q.parts == 2 ? std::max<int64_t>(64, (s.rows + 31) / 32 * 32) : padded(s.rows); q.K = bf16 ? padded(s.K) : s.K;
+    q.piece = piece_of(s.V, std::max(q.N * q.parts, q.K));
     q.pieces = (s.V + q.piece - 1) / q.piece;
     q.C = bf16 ? padded(q.piece) : q.piece;
     q.copy_x = true;                                       // masked
@@ -300,10 +309,11 @@ Layout gradient_layout(const Sizes &s, bool trans_w, bool bf16)
     q.copy_w = bf16 && (!rows_fit(s, trans_w) || padded(last) != last || q.K != s.K);                     // some piece is copied
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
-    q.x = take((size_t)q.N * q.K * (bf16 ? 2 : 4));
-    q.z = take((size_t)q.N * q.C * (bf16 ? 2 : 4));
-    q.dx = take(bf16 ? (size_t)q.N * q.K * 4 : 0);
-    q.dx_more = take(q.pieces > 1 ? (size_t)q.N * q.K * 4 : 0);
+    const size_t rows = (size_t)q.N * q.parts;
+    q.x = take(rows * q.K * (bf16 ? 2 : 4));
+    q.z = take(rows * q.C * (bf16 ? 2 : 4));
+    q.dx = take(bf16 ? rows * q.K * 4 : 0);
+    q.dx_more = take(q.pieces > 1 ? rows * q.K * 4 : 0);
     q.w = take(q.copy_w ? (size_t)q.K * q.C * 2 : 0);
     q.dw = take(q.copy_w ? (size_t)q.K * q.C * 2 : 0);
     q.bytes = at;
@@ -406,7 +416,10 @@ relay_status_t run_gradient_bf16(Piece p, const Sizes &s, const void *w, const f
     void *x = ws + q.x, *z = ws + q.z;
     float *sum = (float *)(ws + q.dx), *more = (float *)(ws + q.dx_more);
     const Rows some{p.tokens, p.tokens_i64, p.V, lse};
-    RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, x, q.K, q.N, q.K, some, st));
+    for (int part = q.parts - 1; part >= 0; --part)
+        RELAY_TRY(copy_padded<__nv_bfloat16>(p.x, s.K, s.rows, s.K, (char *)x + part * q.N * q.K * 2, q.K, q.N, q.K, some, st));
+    const int64_t N = q.N * q.parts;                       // rows of the products
+    float *low = q.parts == 2 ? sum + q.N * q.K : nullptr;
     p.x = x;
     p.ldx = q.K;
     for (p.first = 0; p.first < s.V; p.first += q.piece) {
@@ -414,21 +427,24 @@ relay_status_t run_gradient_bf16(Piece p, const Sizes &s, const void *w, const f
         const int64_t C = padded(p.classes), at = p.trans_w ? p.first * s.K : p.first;
         const bool copy = !rows_fit(s, p.trans_w) || C != p.classes || q.K != s.K;
         RELAY_TRY(weights_of(&p, s, (const char *)w, q, ws, copy, st));
-        RELAY_TRY(head::launch_slopes(p, lse, dlogp, z, C, q.N, C, st));
+        RELAY_TRY(head::launch_slopes(p, lse, dlogp, z, C, q.N, C, q.parts, st));
         const int64_t w_k = p.trans_w ? 1 : p.ldw, w_v = p.trans_w ? p.ldw : 1;
         if (dx) {
             float *to = p.first == 0 ? sum : more;
-            RELAY_TRY(launch_gemm(product(q.N, q.K, C, z, C, 1, p.w, w_v, w_k, to, q.K, RELAY_BF16, RELAY_F32), st));
+            RELAY_TRY(launch_gemm(product(N, q.K, C, z, C, 1, p.w, w_v, w_k, to, q.K, RELAY_BF16, RELAY_F32), st));
             const bool last = p.first + q.piece >= s.V;
             const float *b = to == more ? more : nullptr;
-            if (last) RELAY_TRY(add<__nv_bfloat16>(sum, b, q.K, dx, s.K, s.rows, s.K, some, st));
-            else if (b) RELAY_TRY(add<float>(sum, b, q.K, sum, q.K, q.N, q.K, Rows{}, st));
+            if (b && (low || !last)) {
+                RELAY_TRY(add<float>(sum, b, q.K, sum, q.K, N, q.K, Rows{}, st));
+                b = nullptr;
+            }
+            if (last) RELAY_TRY(add<__nv_bfloat16>(sum, low ? low : b, q.K, dx, s.K, s.rows, s.K, some, st));
         }
         if (!dw) continue;
         void *to = copy ? (void *)(ws + q.dw) : (void *)(dw + at);
         const int64_t ld = copy ? (p.trans_w ? q.K : C) : p.ldw;
-        if (p.trans_w) RELAY_TRY(launch_gemm(product(C, q.K, q.N, z, 1, C, x, q.K, 1, to, ld, RELAY_BF16, RELAY_BF16), st));
-        else RELAY_TRY(launch_gemm(product(q.K, C, q.N, x, 1, q.K, z, C, 1, to, ld, RELAY_BF16, RELAY_BF16), st));
+        if (p.trans_w) RELAY_TRY(launch_gemm(product(C, q.K, N, z, 1, C, x, q.K, 1, to, ld, RELAY_BF16, RELAY_BF16), st));
+        else RELAY_TRY(launch_gemm(product(q.K, C, N, x, 1, q.K, z, C, 1, to, ld, RELAY_BF16, RELAY_BF16), st));
         if (copy) {
             const int64_t rows = p.trans_w ? p.classes : s.K, cols = p.trans_w ? s.K : p.classes;
             RELAY_TRY(copy_padded<__nv_bfloat16>(to, ld, rows, cols, dw + at, p.trans_w ? s.K : s.V, rows, cols, Rows{}, st));

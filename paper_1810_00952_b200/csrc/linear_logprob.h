@@ -30,9 +30,10 @@ constexpr int kDepth = 1024;
 // part[j][row] = (m, s): over the 64 columns from 64 j on, m = max z log2(e) / temperature and s = sum 2^(z log2(e) / temperature - m);
 // at[row] = the token's score where the token is in this piece.  `ld` entries from one j to the next.
 relay_status_t launch_stats(const Piece &p, float2 *part, long long ld, float *at, cudaStream_t st);
-// dz[row][class] (bf16, ld entries a row; `padded_rows` x `padded_classes`, zero outside the piece)
+// dz[row][class] (bf16, ld entries a row; `padded_rows` x `padded_classes`, zero outside the piece).  In two parts (padded_rows a multiple of 32):
+// the values rounded to bf16, and `padded_rows` rows further what that leaves, rounded to bf16 too.
 relay_status_t launch_slopes(const Piece &p, const float *lse, const float *dlogp, void *dz, long long ld, long long padded_rows,
-                             long long padded_classes, cudaStream_t st);
+                             long long padded_classes, int parts, cudaStream_t st);
 
 __device__ __forceinline__ int token_in_piece(const void *tokens, int i64, long long row, long long V, long long first, long long classes)
 {

@@ -16,6 +16,13 @@ namespace {
 
 using namespace gemm_tc2;
 
+// what rounding 2^(x scale + off) to bf16 leaves; the exponential is made again (32 kept ones would spill)
+__device__ __forceinline__ float low_part(float x, float scale, float off)
+{
+    float y;
+    asm volatile("fma.rn.f32 %0, %1, %2, %3;\n\tex2.approx.ftz.f32 %0, %0;" : "=&f"(y) : "f"(x), "f"(scale), "f"(off));
+    return y - __bfloat162float(__float2bfloat16_rn(y));
+}
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 struct HeadParams : gemm_tc::Params {
@@ -28,6 +35,7 @@ struct HeadParams : gemm_tc::Params {
     long long ld;
     float *at;
     const float *lse, *dlogp;              // slopes
+    int low_rows;                          // of two parts: rows from the first to the second
 };
 
 // The scores that a warp has of an accumulator: 64 neighbouring columns of its 32 rows, so that of a 128-column accumulator only the first two of
@@ -106,8 +114,8 @@ struct StatsEpilogue : Scores<DEPTH> {
 
 // The partials of 64 columns a warp: -slope 2^(z log2(e) / temperature - lse log2(e)), the slope's size taken into the exponent, its sign and
 // the rows without a part put in where two values are already one register.  Tokens and the vocabulary's end, which few groups of 32 columns
-// meet, are seen to under a condition that the whole warp shares.
-template <int DEPTH>
+// meet, are seen to under a condition that the whole warp shares.  PARTS = 2: what the rounding to bf16 leaves is stored as well.
+template <int DEPTH, int PARTS>
 struct SlopeEpilogue : Scores<DEPTH> {
     using Params = HeadParams;
     using Scores<DEPTH>::r;
@@ -130,62 +138,83 @@ struct SlopeEpilogue : Scores<DEPTH> {
         keep = 0xffffffffu;
         sign = slope > 0.0f ? 0x80008000u : 0u;
     }
+    // the token's own partial, where the token is among 32 columns from n on: 1 - p of a class that is nearly certain keeps its precision
+    __device__ __forceinline__ float own_partial(const Params &p, const uint32_t (&z)[32], int n)
+    {
+        const int hit = token - n;
+        float own = 0.0f;
+        if (__any_sync(0xffffffffu, hit >= 0 && hit < 32)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) if (j == hit) own = __uint_as_float(z[j]);
+            own = -slope * expm1f(fmaf(own, p.inv_temperature, -lse));
+        }
+        return own;
+    }
+    // those 32 columns; LOW: of the second part
+    template <bool LOW>
+    __device__ __forceinline__ void store(const Params &p, const CUtensorMap *tm_c, const uint32_t (&z)[32], float own, uint8_t *stage, int lane, int row0,
+                                          int n)
+    {
+        const int sw = (lane >> 1) & 3;
+        const int hit = token - n;
+        if (LOW) own -= __bfloat162float(__float2bfloat16_rn(own));
+        uint32_t v[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float a = __uint_as_float(z[2 * j]), b = __uint_as_float(z[2 * j + 1]);
+            v[j] = LOW ? pack2(low_part(a, p.scale, off), low_part(b, p.scale, off)) : pack2(ex2(fmaf(a, p.scale, off)), ex2(fmaf(b, p.scale, off)));
+            v[j] = (v[j] ^ sign) & keep;
+        }
+        if (__any_sync(0xffffffffu, hit >= 0 && hit < 32)) {
+            const uint32_t bits = pack2(own, own);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (hit == 2 * j) v[j] = (v[j] & 0xffff0000u) | (bits & 0xffffu);
+                if (hit == 2 * j + 1) v[j] = (v[j] & 0xffffu) | (bits & 0xffff0000u);
+            }
+        }
+        if (n + 32 > p.classes) {                          // warp-uniform: columns that do not exist
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (n + 2 * j >= p.classes) v[j] = 0;
+                else if (n + 2 * j + 1 >= p.classes) v[j] &= 0xffffu;
+            }
+        }
+        if (tc::elect_one()) tc::tma_store_wait_read<0>();
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ sw) << 4)) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+        tc::fence_proxy_async();
+        __syncwarp();
+        if (tc::elect_one()) {
+            tc::tma_store_2d(tm_c, stage, n, LOW ? row0 + p.low_rows : row0);
+            tc::tma_store_commit();
+        }
+    }
     __device__ __forceinline__ void drain(const Params &p, const CUtensorMap *tm_c, uint32_t taddr, uint8_t *stage, int lane, int row0, int n0,
                                           int width, int slot)
     {
         const int c0 = slot * 64;
         if (c0 >= width) return;
         if (DEPTH == 0) this->read(taddr + c0);
-        const int sw = (lane >> 1) & 3;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int n = n0 + c0 + 32 * half;
             if (n >= p.N) break;                           // warp-uniform; p.N: columns of the stored piece
-            const int hit = token - n;
-            const bool mine = hit >= 0 && hit < 32;
-            float own = 0.0f;
-            if (__any_sync(0xffffffffu, mine)) {           // 1 - p of a class that is nearly certain keeps its precision
-#pragma unroll
-                for (int j = 0; j < 32; ++j) if (j == hit) own = __uint_as_float(r[half][j]);
-                own = -slope * expm1f(fmaf(own, p.inv_temperature, -lse));
-            }
-            uint32_t v[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                v[j] = (pack2(ex2(fmaf(__uint_as_float(r[half][2 * j]), p.scale, off)), ex2(fmaf(__uint_as_float(r[half][2 * j + 1]), p.scale, off))) ^ sign) & keep;
-            if (__any_sync(0xffffffffu, mine)) {
-                const uint32_t bits = pack2(own, own);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (hit == 2 * j) v[j] = (v[j] & 0xffff0000u) | (bits & 0xffffu);
-                    if (hit == 2 * j + 1) v[j] = (v[j] & 0xffffu) | (bits & 0xffff0000u);
-                }
-            }
-            if (n + 32 > p.classes) {                      // warp-uniform: columns that do not exist
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (n + 2 * j >= p.classes) v[j] = 0;
-                    else if (n + 2 * j + 1 >= p.classes) v[j] &= 0xffffu;
-                }
-            }
-            if (tc::elect_one()) tc::tma_store_wait_read<0>();
-            __syncwarp();
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ sw) << 4)) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-            tc::fence_proxy_async();
-            __syncwarp();
-            if (tc::elect_one()) {
-                tc::tma_store_2d(tm_c, stage, n, row0);
-                tc::tma_store_commit();
-            }
+            const float own = own_partial(p, r[half], n);
+            store<false>(p, tm_c, r[half], own, stage, lane, row0, n);
+            if (PARTS == 2) store<true>(p, tm_c, r[half], own, stage, lane, row0, n);
         }
     }
     __device__ __forceinline__ void finish() { if (tc::elect_one()) tc::tma_store_wait_all<0>(); }
 };
 
+template <int DEPTH> using Slopes = SlopeEpilogue<DEPTH, 1>;
+template <int DEPTH> using SlopesInTwo = SlopeEpilogue<DEPTH, 2>;
+
 template <template <int> class Epi>
-relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, void *c, int64_t ldc, cudaStream_t st)
+relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, void *c, int64_t ldc, int64_t c_rows, cudaStream_t st)
 {
     int dev = 0, sms = 148;
     RELAY_CUDA(cudaGetDevice(&dev));
@@ -195,7 +224,7 @@ relay_status_t launch(const head::Piece &q, HeadParams p, int64_t M, int64_t N, 
     if (q.trans_w) RELAY_TRY(make_tmap_2d_bf16(&tm_b, q.w, q.K, q.classes, q.ldw, BK, 64));
     else RELAY_TRY(make_tmap_2d_bf16(&tm_b, q.w, q.classes, q.K, q.ldw, 64, BK));
     tm_c = tm_a;                                           // statistics are not stored by tile
-    if (c) RELAY_TRY(make_tmap_2d_sw64(&tm_c, false, c, N, M, ldc, 32));
+    if (c) RELAY_TRY(make_tmap_2d_sw64(&tm_c, false, c, N, c_rows, ldc, 32));
     p.M = (int)M; p.N = (int)N; p.K = (int)q.K;
     p.tiles_m = (int)((M + 255) / 256); p.tiles_n = (int)((N + BN - 1) / BN); p.k_blocks = (int)((q.K + BK - 1) / BK);
     p.err = device_error_word();
@@ -240,14 +269,16 @@ relay_status_t launch_stats(const Piece &q, float2 *part, long long ld, float *a
 {
     HeadParams p{};
     p.part = part; p.ld = ld; p.at = at;
-    return launch<StatsEpilogue>(q, p, q.rows, q.classes, nullptr, 0, st);
+    return launch<StatsEpilogue>(q, p, q.rows, q.classes, nullptr, 0, 0, st);
 }
 relay_status_t launch_slopes(const Piece &q, const float *lse, const float *dlogp, void *dz, long long ld, long long padded_rows,
-                             long long padded_classes, cudaStream_t st)
+                             long long padded_classes, int parts, cudaStream_t st)
 {
     HeadParams p{};
     p.lse = lse; p.dlogp = dlogp;
-    return launch<SlopeEpilogue>(q, p, padded_rows, padded_classes, dz, ld, st);
+    p.low_rows = (int)padded_rows;
+    if (parts == 2) return launch<SlopesInTwo>(q, p, padded_rows, padded_classes, dz, ld, 2 * padded_rows, st);
+    return launch<Slopes>(q, p, padded_rows, padded_classes, dz, ld, padded_rows, st);
 }
 
 }  // namespace head
