@@ -565,9 +565,11 @@ relay_status_t relay_linear_logprob(const relay_tensor_t *x, const relay_tensor_
 /* Gradient group of the above, given the forward call's lse:(..) f32 and dlogp:(..) f32:
  *   dz[i,j] = dlogp[i] (1[j = tokens[i]] - exp(z[i,j] - lse[i])) / temperature
  *   dx[i,k] = sum_j dz[i,j] w[k,j];   dw[k,j] = sum_i x[i,k] dz[i,j]      dx, dw: types and shapes of x and w; one of them may be NULL
- * The scores are computed again, a piece of the vocabulary at a time; with bf16 operands dz is rounded to bf16, the operand type of
- * the two products, whose sums are f32; up to 512 rows to the sum of two bf16 numbers.  A row whose token names no class has no part in either, whatever x holds there; a row with lse = -inf
- * neither.  dx is NaN where the zero partial of an impossible class meets its infinite weight (column k of every row with a part, w[k,j] infinite).
+ * The scores are computed again, a piece of the vocabulary at a time.  With bf16 operands dz is rounded to bf16, the operand type of the two
+ * products, whose sums are f32; up to 512 rows to the sum of two bf16 numbers.  With more, equal dlogp share their rounding (up to 2^-8 of
+ * the tokens' part; a power of two has none, so a mean's factor is best applied to the results).  A row whose token names no class has no
+ * part in either, whatever x holds there; a row with lse = -inf neither.  dx is NaN where the zero partial of an impossible class meets its
+ * infinite weight (column k of every row with a part, w[k,j] infinite).
  * `ws` must hold relay_workspace_bytes_linear_logprob_grad() bytes: a piece of at most 2^27 partials, a copy of x, and with bf16 operands dx
  * in f32, twice where there is more than one piece, and a piece of w and dw where their rows are copied. */
 size_t relay_workspace_bytes_linear_logprob_grad(const relay_tensor_t *x, const relay_tensor_t *w, int32_t trans_w);

@@ -293,7 +293,8 @@ Layout forward_layout(const Sizes &s, bool trans_w, bool bf16)
 // that all of its part in dx and dw has in common, and over few rows such errors do not average out: dx and dw are 1.9 times as far from 64 bits as
 // the rounding of the results alone leaves them with one row, 1.66 with nine, 1.5 with 128 or 300, 1.44 from 500 rows on, at the worst of six seeds.  So up
 // to 512 rows, whose products wait for their other operand anyway, the partials come in two bf16 numbers, one below the other in a contraction
-// twice as long (1.00).  1024 x 32768: 1 row 220 -> 232 us, 128 rows 222 -> 242, 512 rows 255 -> 291; 2048 x 131072 tied: 64 rows 0.98 -> 1.04 ms, 512
+// twice as long (1.00).  (The slopes on dx's fp32 sums and on x instead: 1.15 in dx, but 1.53 in dw, and the products of x with a slope near a power
+// of two round alike.)  1024 x 32768: 1 row 220 -> 232 us, 128 rows 222 -> 242, 512 rows 255 -> 291; 2048 x 131072 tied: 64 rows 0.98 -> 1.04 ms, 512
 // rows 1.18 -> 1.49; at 8192 rows they would cost half as much again.
 constexpr int64_t kTwoPartRows = 512;
 Layout gradient_layout(const Sizes &s, bool trans_w, bool bf16)
